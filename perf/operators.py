@@ -185,8 +185,8 @@ def _codes(x):
     g[:, :cols] = x
     g = g.view(rows, -1, GROUP)
     bits = g.abs().amax(2).view(torch.int32)
-    s = (((bits + 0x10000) >> 23) - 6).clamp(min=1)
-    q = torch.round(g / (s << 23).view(torch.float32).unsqueeze(2))
+    s = (((bits + 0x10000) >> 23) - 6).clamp(min=1, max=248)  # 2^121 the largest: 128 of it would overflow
+    q = torch.round(g / (s << 23).view(torch.float32).unsqueeze(2)).clamp(-127, 127)
     return q.view(rows, -1), s
 
 
@@ -462,9 +462,9 @@ def _nearest64(a):
     e = torch.floor(torch.log2(top.clamp(min=2.0 ** -149))) - 6
     e = torch.where(top >= torch.exp2(e) * 128, e + 1, e)  # the logarithm may have rounded across a power of two
     e = torch.where(top < torch.exp2(e) * 64, e - 1, e)
-    e = torch.where(top >= torch.exp2(e) * 127.5, e + 1, e).clamp(min=-126)
+    e = torch.where(top >= torch.exp2(e) * 127.5, e + 1, e).clamp(min=-126, max=121)
     unit = torch.exp2(e)
-    return (torch.round(pad / unit) * unit).reshape(rows, -1)[:, :cols]
+    return (torch.round(pad / unit).clamp(-127, 127) * unit).reshape(rows, -1)[:, :cols]
 
 
 def _act64(x, act):
