@@ -44,7 +44,7 @@ typedef enum shampoo_status {
   SHAMPOO_ENOMEM = -4        /* workspace too small, or a library allocation failed */
 } shampoo_status;
 
-/* Element type of the gradient views G. */
+/* Element type of the gradient views G (and of logits and activations). */
 typedef enum shampoo_dtype {
   SHAMPOO_F32 = 0,
   SHAMPOO_BF16 = 1 /* raw bfloat16 bit patterns; up-cast exactly to fp32 on load */
@@ -428,6 +428,134 @@ shampoo_status shampoo_embedding_graft(void* handle, const int32_t* rows, const 
                                        int64_t ldw, float eta0, int use_shampoo, float* norms, void* stream);
 
 /*
+ * From the loss to the gradient.  The calls below compute what a training
+ * step has in hand before shampoo_update_stats: the loss at the output layer
+ * and its gradient, 8-bit checkpoints of activations, and the weight gradient
+ * G that the calls above take.  They use no handle scratch: two calls of one
+ * handle may overlap on different streams if their buffers differ.
+ */
+
+/*
+ * Log probabilities of given tokens.  z = row r of the logits (rows x vocab,
+ * row stride ld >= vocab, element type dtype, SHAMPOO_F32 or SHAMPOO_BF16):
+ *   lse[r]     = log sum_j exp(z_j)
+ *   logp[r]    = z_t - lse[r], t = targets[r]; 0 when t is outside [0, vocab)
+ *                (a token without loss)
+ *   entropy[r] = -sum_j p_j log p_j,  p_j = exp(z_j - lse[r])
+ *   top_ids, top_logp (rows x k, contiguous): the k largest logits in
+ *                descending order, equal ones by ascending index, and
+ *                z_j - lse[r]; -1 and -inf past the last entry above -inf
+ * Sums are kept in fp32.  An entry of -inf is not allowed: it has probability
+ * 0 and is never an alternative.  A row of -inf only has lse = -inf, logp =
+ * -inf (0 without a target), entropy 0 and no alternatives; a row holding a
+ * NaN or +inf has lse, entropy, top_logp and (with a target) logp NaN, and
+ * top_ids -1.  logp and targets may both be NULL, entropy may be NULL, and
+ * top_ids and top_logp are NULL when k == 0.
+ * `workspace` is device memory of at least
+ * shampoo_token_logprobs_workspace_bytes(rows, vocab, k) bytes (0 when the
+ * call needs none), used exclusively by this call until the stream reaches
+ * its end.  rows == 0 does nothing.
+ * Errors: EINVAL (NULL pointers, rows outside [0, 2^31), vocab outside
+ * [1, 2^30], ld < vocab, k outside [0, SHAMPOO_MAX_TOP], dtype), ENOMEM
+ * (workspace too small).
+ */
+#define SHAMPOO_MAX_TOP 64
+size_t shampoo_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int k);
+shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
+                                      int64_t ld, const int32_t* targets, float* logp, float* lse, float* entropy,
+                                      int k, int32_t* top_ids, float* top_logp, void* workspace, size_t ws_bytes,
+                                      void* stream);
+
+/*
+ * The gradient of shampoo_token_logprobs with respect to the logits.  Given
+ * the gradients of its outputs (g_logp, g_lse, g_entropy: rows; g_top: rows x
+ * k; each may be NULL for zero),
+ *   dz_j = p_j (g_lse - g_logp - sum_i g_top_i - g_entropy (log p_j + H))
+ *          + [j = t] g_logp + sum_i [j = top_ids_i] g_top_i,
+ * with p_j = exp(z_j - lse[r]) and H = entropy[r] (needed with g_entropy).  A
+ * target outside [0, vocab) has no g_logp, an alternative outside it no g_top.
+ * Rows with lse = -inf have gradient 0.  dlogits has the logits' element type
+ * (rounded once, to nearest even) and row stride ld_d >= vocab; it may be the
+ * logits themselves (same pointer, ld_d == ld).  Deterministic.
+ * Errors: EINVAL (NULL logits, lse or dlogits; targets NULL with g_logp,
+ * entropy NULL with g_entropy, top_ids NULL with g_top; sizes and dtype as
+ * above; dlogits == logits with ld_d != ld).
+ */
+shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
+                                           int64_t ld, const int32_t* targets, const float* lse,
+                                           const float* entropy, int k, const int32_t* top_ids,
+                                           const float* g_logp, const float* g_lse, const float* g_entropy,
+                                           const float* g_top, void* dlogits, int64_t ld_d, void* stream);
+
+/*
+ * Activation checkpoints in 8 bits.  A checkpoint holds a rows x cols tensor
+ * as signed 8-bit codes with one power-of-two scale for every 32 columns of a
+ * row (the last group of a row may be shorter):
+ *   x^ = q 2^e,  |q| <= 127,  e the smallest exponent in [-126, 121] for which
+ *   the group's largest |x| 2^-e rounds to at most 127,  q = x 2^-e rounded to
+ *   nearest even
+ * (|x - x^| <= 2^(e-1), at most 1/127 of the group's largest |x|; values from
+ * 127.5 2^121 on, which would round to 2^128, are held as 127 2^121).  x^ is
+ * exact in bfloat16.  A group that holds an infinity or NaN is NaN throughout.
+ * Layout, one buffer of shampoo_act_checkpoint_bytes(rows, cols) bytes aligned
+ * to 16: with ldq = cols rounded up to 32, rows x ldq codes (0 in the
+ * columns at and past cols); then, at the next multiple of 256 bytes, rows x
+ * (ldq / 32) bytes s = e + 127 (255 and codes 0 for a NaN group).
+ * Sizes: rows in [0, 2^31), cols in [1, 2^20]; row strides >= cols.
+ * rows == 0 does nothing (the weight gradient then is beta G).
+ */
+enum {
+  SHAMPOO_ACT_NONE = 0,      /* y = x */
+  SHAMPOO_ACT_RELU = 1,      /* y = max(x, 0); slope 0 at 0 */
+  SHAMPOO_ACT_GELU = 2,      /* y = x (1 + erf(x / sqrt 2)) / 2 */
+  SHAMPOO_ACT_GELU_TANH = 3, /* y = x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+  SHAMPOO_ACT_SILU = 4       /* y = x / (1 + exp(-x)) */
+};
+size_t shampoo_act_checkpoint_bytes(int64_t rows, int64_t cols);
+
+/*
+ * One pass over X (rows x cols, row stride ld_x, dtype): Y = act(X) (same
+ * type, row stride ld_y; NULL: not wanted), the checkpoint of X (ckpt_x) and
+ * the checkpoint of Y as stored (ckpt_y); each may be NULL, not all three.
+ * Y may be X itself (ld_y == ld_x).
+ * Errors: EINVAL (NULL X, no output, sizes, strides, dtype, act, a checkpoint
+ * not aligned to 16 bytes).
+ */
+shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                                  int act, void* Y, int64_t ld_y, void* ckpt_x, void* ckpt_y, void* stream);
+
+/* X = the values x^ of a checkpoint (dtype; exact).  Errors: as above. */
+shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, int64_t cols, void* X, int dtype,
+                                  int64_t ld_x, void* stream);
+
+/*
+ * Activation gradient dX = dY o act'(x^) from the checkpoint of the
+ * activation's input.  dY and dX: dtype, row strides ld_dy and ld_dx; dX may
+ * be dY itself (ld_dx == ld_dy).  Errors: as above.
+ */
+shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, int act, const void* dY,
+                                int dtype, int64_t ld_dy, void* dX, int64_t ld_dx, void* stream);
+
+/*
+ * Weight gradient of a linear layer Y = X W from the checkpoint of its input:
+ *   G = beta G + X^^T dY     (cols x out, row stride ld_g; G is not read when
+ *                             beta == 0)
+ * dY: rows x out, row stride ld_dy, dtype; G: g_dtype (either type; rounded
+ * once at the end).  Products of x^ with bfloat16 gradients are exact and
+ * summed in fp32; fp32 gradients are split exactly into three bfloat16 terms.
+ * Long sums over few output tiles are cut into parts that are added in a fixed
+ * order (deterministic).  `workspace`: at least
+ * shampoo_act_weight_grad_workspace_bytes(rows, cols, out) bytes of device
+ * memory (0: none needed), as for shampoo_token_logprobs.
+ * Sizes: out in [1, 2^20].  Errors: as above, EINVAL for a non-finite beta or
+ * G the same buffer as dY or the checkpoint, ENOMEM (workspace too small).
+ */
+size_t shampoo_act_weight_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t out);
+shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, const void* dY,
+                                       int dtype, int64_t out, int64_t ld_dy, void* G, int g_dtype, int64_t ld_g,
+                                       float beta, void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Measurement support.  While enabled, every launch of the timed kernel
  * classes below is bracketed by HIP events on its stream.
  * shampoo_timing_read synchronizes those events, returns the summed duration
@@ -442,7 +570,10 @@ enum {
   SHAMPOO_KCLASS_ROOT_AUX = 5,   /* root prologue/epilogue/state kernels */
   SHAMPOO_KCLASS_EMB = 6,        /* embedding row compaction (sort, runs, segment sums) */
   SHAMPOO_KCLASS_NEWTON_WARM = 7, /* full products of warm-started roots (fp32 or fp64) */
-  SHAMPOO_KCLASS_COUNT = 8
+  SHAMPOO_KCLASS_LOGPROBS = 8,   /* token log probabilities and their gradient */
+  SHAMPOO_KCLASS_ACT = 9,        /* activation checkpoints: encode, decode, activation gradient */
+  SHAMPOO_KCLASS_WGRAD = 10,     /* weight gradients from checkpoints */
+  SHAMPOO_KCLASS_COUNT = 11
 };
 shampoo_status shampoo_timing_enable(void* handle, int enable);
 shampoo_status shampoo_timing_read(void* handle, int kclass, double* total_ms, int64_t* launches);

@@ -28,8 +28,11 @@ ROOT_CONVERGED, ROOT_STAGNATED, ROOT_MAXITER, ROOT_DIVERGED, ROOT_NOT_PD = 0, 1,
 PRECISION_FP32, PRECISION_AUTO, PRECISION_FP64 = 0, 1, 2
 SCALING_FROBENIUS, SCALING_POWER4 = 0, 1
 (KCLASS_NEWTON_F32, KCLASS_NEWTON_F64, KCLASS_STATS, KCLASS_PRECOND, KCLASS_GRAFT, KCLASS_ROOT_AUX, KCLASS_EMB,
- KCLASS_NEWTON_WARM) = range(8)
-KCLASS_NAMES = ["newton_f32", "newton_f64", "stats", "precond", "graft", "root_aux", "emb", "newton_warm"]
+ KCLASS_NEWTON_WARM, KCLASS_LOGPROBS, KCLASS_ACT, KCLASS_WGRAD) = range(11)
+KCLASS_NAMES = ["newton_f32", "newton_f64", "stats", "precond", "graft", "root_aux", "emb", "newton_warm", "logprobs",
+                "act", "wgrad"]
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+MAX_TOP = 64
 
 
 class shampoo_block(C.Structure):
@@ -81,6 +84,16 @@ _sig = {
     "shampoo_embedding_stats": (_i, [_vp, _vp, _vp, _i, _i, _vp, _f, _vp, _sz, _vp]),
     "shampoo_embedding_precondition": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp]),
     "shampoo_embedding_graft": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _i64, _i64, _f, _i, _vp, _vp]),
+    "shampoo_token_logprobs_workspace_bytes": (_sz, [_i64, _i64, _i]),
+    "shampoo_token_logprobs": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "shampoo_token_logprobs_grad": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp,
+                                         _vp, _i64, _vp]),
+    "shampoo_act_checkpoint_bytes": (_sz, [_i64, _i64]),
+    "shampoo_act_encode": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _i, _vp, _i64, _vp, _vp, _vp]),
+    "shampoo_act_decode": (_i, [_vp, _vp, _i64, _i64, _vp, _i, _i64, _vp]),
+    "shampoo_act_grad": (_i, [_vp, _vp, _i64, _i64, _i, _vp, _i, _i64, _vp, _i64, _vp]),
+    "shampoo_act_weight_grad_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "shampoo_act_weight_grad": (_i, [_vp, _vp, _i64, _i64, _vp, _i, _i64, _i64, _vp, _i, _i64, _f, _vp, _sz, _vp]),
     "shampoo_timing_enable": (_i, [_vp, _i]),
     "shampoo_timing_read": (_i, [_vp, _i, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
 }
@@ -674,6 +687,200 @@ def shampoo_graft_lamb(handle, blocks, eta0, beta1=0.0, use_shampoo=True, norms=
     arr, nb, dt = _block_args(handle, blocks, norms)
     _check(handle, _lib.shampoo_graft_lamb(handle, arr, nb, dt, float(eta0), float(beta1), int(bool(use_shampoo)),
                                            _ptr(norms), _stream(stream)))
+
+
+# ------------------------------------------------------------------ from the loss to the gradient
+def _check_matrix(t, what, shape=None, dtype=None):
+    """(rows, cols, row stride, dtype code) of an fp32 or bf16 matrix whose columns are adjacent."""
+    torch = _torch()
+    dt = t.dtype
+    _need(t.dim() == 2, f"{what}: {t.dim()} dimensions, expected 2")
+    _need(dt is torch.float32 or dt is torch.bfloat16, f"{what}: dtype {dt}, expected float32 or bfloat16")
+    _need(dtype is None or dt is dtype, f"{what}: dtype {dt}, expected {dtype}")
+    m, n = t.shape
+    _need(shape is None or (m, n) == shape, f"{what}: shape {(m, n)}, expected {shape}")
+    ld, sc = t.stride()
+    _need(n <= 1 or sc == 1, f"{what}: columns must be adjacent (stride(1) == 1)")
+    # one row, or none, uses no stride; rows that overlap (an expanded view)
+    # are no layout the library takes
+    if m <= 1:
+        ld = n
+    _need(ld >= n, f"{what}: row stride {ld} < {n} columns")
+    return m, n, ld, SHAMPOO_F32 if dt is torch.float32 else SHAMPOO_BF16
+
+
+def _check_rows(t, rows, what, kind="float32"):
+    """A contiguous vector of `rows` elements, or None."""
+    if t is None:
+        return
+    (_int32 if kind == "int32" else _fp32)(t, what)
+    _need(tuple(t.shape) == (rows,), f"{what}: shape {tuple(t.shape)}, expected ({rows},)")
+    _contig(t, what)
+
+
+def _check_top(t, rows, k, what, kind="float32"):
+    (_int32 if kind == "int32" else _fp32)(t, what)
+    _need(tuple(t.shape) == (rows, k), f"{what}: shape {tuple(t.shape)}, expected ({rows}, {k})")
+    _contig(t, what)
+
+
+def _check_bytes(t, nbytes, what):
+    """A contiguous uint8 buffer of at least nbytes (None where none are needed)."""
+    if t is None:
+        _need(nbytes == 0, f"{what}: {nbytes} bytes needed, got None")
+        return
+    _need(_is_dtype(t, "uint8"), f"{what}: dtype {t.dtype}, expected uint8")
+    _contig(t, what)
+    _min_numel(t, nbytes, what)
+
+
+def _overlap(a, b):
+    """Whether the memory ranges of two tensors meet."""
+    if a is None or b is None or a.numel() == 0 or b.numel() == 0:
+        return False
+
+    def span(t):
+        size = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1
+        return t.data_ptr(), t.data_ptr() + size * t.element_size()
+    a0, a1 = span(a)
+    b0, b1 = span(b)
+    return a0 < b1 and b0 < a1
+
+
+def _in_place(out, src, what):
+    """out is src itself (same view) or shares no memory with it."""
+    _need(not _overlap(out, src) or (out.data_ptr() == src.data_ptr() and
+                                     (out.shape[0] <= 1 or out.stride(0) == src.stride(0))),
+          f"{what} overlap without being the same view")
+
+
+def shampoo_token_logprobs_workspace_bytes(rows, vocab, k=0):
+    return int(_lib.shampoo_token_logprobs_workspace_bytes(int(rows), int(vocab), int(k)))
+
+
+def shampoo_token_logprobs(handle, logits, targets, logp, lse, entropy=None, top_ids=None, top_logp=None,
+                           workspace=None, stream=None):
+    """logits: rows x vocab, fp32 or bf16 (row-major view); targets int32 [rows]
+    and logp fp32 [rows] (both or neither); lse, entropy: fp32 [rows]; top_ids
+    int32 and top_logp fp32, rows x k, for the k largest alternatives."""
+    rows, vocab, ld, dt = _check_matrix(logits, "logits")
+    _need((targets is None) == (logp is None), "targets and logp go together")
+    _need((top_ids is None) == (top_logp is None), "top_ids and top_logp go together")
+    _check_rows(targets, rows, "targets", "int32")
+    _check_rows(logp, rows, "logp")
+    _need(lse is not None, "lse is required")
+    _check_rows(lse, rows, "lse")
+    _check_rows(entropy, rows, "entropy")
+    k = 0
+    if top_ids is not None:
+        _need(top_ids.dim() == 2, f"top_ids: {top_ids.dim()} dimensions, expected 2")
+        k = int(top_ids.shape[1])
+        _check_top(top_ids, rows, k, "top_ids", "int32")
+        _check_top(top_logp, rows, k, "top_logp")
+    _check_bytes(workspace, _lib.shampoo_token_logprobs_workspace_bytes(rows, vocab, k), "workspace")
+    _devices(handle, (("logits", logits), ("targets", targets), ("logp", logp), ("lse", lse), ("entropy", entropy),
+                      ("top_ids", top_ids), ("top_logp", top_logp), ("workspace", workspace)))
+    _check(handle, _lib.shampoo_token_logprobs(handle, _ptr(logits), dt, rows, vocab, ld, _ptr(targets), _ptr(logp),
+                                               _ptr(lse), _ptr(entropy), k, _ptr(top_ids), _ptr(top_logp),
+                                               _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def shampoo_token_logprobs_grad(handle, logits, targets, lse, dlogits, g_logp=None, g_lse=None, entropy=None,
+                                g_entropy=None, top_ids=None, g_top=None, stream=None):
+    """dlogits (logits' shape and type; may be logits) from the gradients of
+    shampoo_token_logprobs' outputs: g_logp (with targets), g_lse, g_entropy
+    (with entropy): fp32 [rows]; g_top (with top_ids): fp32 rows x k."""
+    rows, vocab, ld, dt = _check_matrix(logits, "logits")
+    _, _, ld_d, _ = _check_matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
+    _in_place(dlogits, logits, "dlogits and logits")
+    _need(g_logp is None or targets is not None, "g_logp needs targets")
+    _need(g_entropy is None or entropy is not None, "g_entropy needs entropy")
+    _need(g_top is None or top_ids is not None, "g_top needs top_ids")
+    _need(lse is not None, "lse is required")
+    _check_rows(targets, rows, "targets", "int32")
+    for what, t in (("lse", lse), ("g_logp", g_logp), ("g_lse", g_lse), ("entropy", entropy),
+                    ("g_entropy", g_entropy)):
+        _check_rows(t, rows, what)
+    k = 0
+    if top_ids is not None:
+        _need(top_ids.dim() == 2, f"top_ids: {top_ids.dim()} dimensions, expected 2")
+        k = int(top_ids.shape[1])
+        _check_top(top_ids, rows, k, "top_ids", "int32")
+        if g_top is not None:
+            _check_top(g_top, rows, k, "g_top")
+    _devices(handle, (("logits", logits), ("dlogits", dlogits), ("targets", targets), ("lse", lse),
+                      ("g_logp", g_logp), ("g_lse", g_lse), ("entropy", entropy), ("g_entropy", g_entropy),
+                      ("top_ids", top_ids), ("g_top", g_top)))
+    _check(handle, _lib.shampoo_token_logprobs_grad(handle, _ptr(logits), dt, rows, vocab, ld, _ptr(targets),
+                                                    _ptr(lse), _ptr(entropy), k, _ptr(top_ids), _ptr(g_logp),
+                                                    _ptr(g_lse), _ptr(g_entropy), _ptr(g_top), _ptr(dlogits), ld_d,
+                                                    _stream(stream)))
+
+
+def shampoo_act_checkpoint_bytes(rows, cols):
+    return int(_lib.shampoo_act_checkpoint_bytes(int(rows), int(cols)))
+
+
+def _check_ckpt(t, rows, cols, what):
+    if t is not None:
+        _check_bytes(t, _lib.shampoo_act_checkpoint_bytes(rows, cols), what)
+
+
+def shampoo_act_encode(handle, X, ckpt_x=None, act=ACT_NONE, Y=None, ckpt_y=None, stream=None):
+    """X: rows x cols, fp32 or bf16 (row-major view); Y = act(X): X's shape and
+    type (may be X), or None; ckpt_x, ckpt_y: uint8 tensors of
+    shampoo_act_checkpoint_bytes(rows, cols), or None."""
+    rows, cols, ld, dt = _check_matrix(X, "X")
+    ld_y = 0
+    if Y is not None:
+        _, _, ld_y, _ = _check_matrix(Y, "Y", (rows, cols), X.dtype)
+        _in_place(Y, X, "Y and X")
+    _check_ckpt(ckpt_x, rows, cols, "ckpt_x")
+    _check_ckpt(ckpt_y, rows, cols, "ckpt_y")
+    _devices(handle, (("X", X), ("Y", Y), ("ckpt_x", ckpt_x), ("ckpt_y", ckpt_y)))
+    _check(handle, _lib.shampoo_act_encode(handle, _ptr(X), dt, rows, cols, ld, int(act), _ptr(Y), ld_y,
+                                           _ptr(ckpt_x), _ptr(ckpt_y), _stream(stream)))
+
+
+def shampoo_act_decode(handle, ckpt, X, stream=None):
+    """X: rows x cols, fp32 or bf16: the values that the checkpoint holds."""
+    rows, cols, ld, dt = _check_matrix(X, "X")
+    _need(ckpt is not None, "ckpt is required")
+    _check_ckpt(ckpt, rows, cols, "ckpt")
+    _devices(handle, (("ckpt", ckpt), ("X", X)))
+    _check(handle, _lib.shampoo_act_decode(handle, _ptr(ckpt), rows, cols, _ptr(X), dt, ld, _stream(stream)))
+
+
+def shampoo_act_grad(handle, ckpt, act, dY, dX, stream=None):
+    """dX = dY o act'(x^), x^ the checkpoint's values; dX: dY's shape and type (may be dY)."""
+    rows, cols, ld_dy, dt = _check_matrix(dY, "dY")
+    _, _, ld_dx, _ = _check_matrix(dX, "dX", (rows, cols), dY.dtype)
+    _in_place(dX, dY, "dX and dY")
+    _need(ckpt is not None, "ckpt is required")
+    _check_ckpt(ckpt, rows, cols, "ckpt")
+    _devices(handle, (("ckpt", ckpt), ("dY", dY), ("dX", dX)))
+    _check(handle, _lib.shampoo_act_grad(handle, _ptr(ckpt), rows, cols, int(act), _ptr(dY), dt, ld_dy, _ptr(dX),
+                                         ld_dx, _stream(stream)))
+
+
+def shampoo_act_weight_grad_workspace_bytes(rows, cols, out):
+    return int(_lib.shampoo_act_weight_grad_workspace_bytes(int(rows), int(cols), int(out)))
+
+
+def shampoo_act_weight_grad(handle, ckpt, dY, G, beta=0.0, workspace=None, stream=None):
+    """G (cols x out) = beta G + X^^T dY, X^ the rows x cols values of the
+    checkpoint, dY rows x out; dY and G fp32 or bf16, each its own."""
+    cols, out, ld_g, g_dt = _check_matrix(G, "G")
+    rows, _, ld_dy, dt = _check_matrix(dY, "dY")
+    _need(int(dY.shape[1]) == out, f"dY: {int(dY.shape[1])} columns, G has {out}")
+    _need(ckpt is not None, "ckpt is required")
+    _check_ckpt(ckpt, rows, cols, "ckpt")
+    _need(not _overlap(G, dY), "G and dY overlap")
+    _check_bytes(workspace, _lib.shampoo_act_weight_grad_workspace_bytes(rows, cols, out), "workspace")
+    _devices(handle, (("ckpt", ckpt), ("dY", dY), ("G", G), ("workspace", workspace)))
+    _check(handle, _lib.shampoo_act_weight_grad(handle, _ptr(ckpt), rows, cols, _ptr(dY), dt, out, ld_dy, _ptr(G),
+                                                g_dt, ld_g, float(beta), _ptr(workspace), _nbytes(workspace),
+                                                _stream(stream)))
 
 
 def shampoo_timing_enable(handle, enable=True):

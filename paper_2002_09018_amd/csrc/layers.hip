@@ -1,0 +1,262 @@
+// Host side of the calls from the loss to the gradient: argument checking and
+// launches of logprobs.hpp, act_checkpoint.hpp and weight_grad.hpp.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+
+#include "act_checkpoint.hpp"
+#include "handle.hpp"
+#include "logprobs.hpp"
+#include "shampoo.h"
+#include "weight_grad.hpp"
+
+using namespace shp;
+
+namespace {
+
+constexpr int64_t kMaxTokens = INT32_MAX;   // rows of logits and activations
+constexpr int64_t kMaxVocab = 1 << 30;
+constexpr int64_t kMaxCols = 1 << 20;       // columns of activations and output gradients
+
+inline int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// An entry point's body: no exception passes the C boundary.
+template <typename F>
+shampoo_status entry(void* handle, F&& f) {
+  Handle* h = static_cast<Handle*>(handle);
+  if (!h) return SHAMPOO_EINVAL;
+  h->err.clear();
+  try {
+    return f(h);
+  } catch (const std::bad_alloc&) {
+    return SHAMPOO_ENOMEM;
+  } catch (...) {
+    return SHAMPOO_EHIP;
+  }
+}
+
+shampoo_status check_dtype(Handle* h, int dtype, const char* what) {
+  if (dtype != SHAMPOO_F32 && dtype != SHAMPOO_BF16) return fail(h, SHAMPOO_EINVAL, "%s: bad dtype %d", what, dtype);
+  return SHAMPOO_OK;
+}
+
+shampoo_status check_logits(Handle* h, int dtype, int64_t rows, int64_t vocab, int64_t ld, int k) {
+  STATUS_TRY(check_dtype(h, dtype, "logits"));
+  if (rows < 0 || rows >= kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31 - 1)", (long long)rows);
+  if (vocab < 1 || vocab > kMaxVocab) return fail(h, SHAMPOO_EINVAL, "vocab = %lld outside [1, 2^30]", (long long)vocab);
+  if (ld < vocab) return fail(h, SHAMPOO_EINVAL, "ld %lld < vocab %lld", (long long)ld, (long long)vocab);
+  if (k < 0 || k > SHAMPOO_MAX_TOP) return fail(h, SHAMPOO_EINVAL, "k = %d outside [0, %d]", k, SHAMPOO_MAX_TOP);
+  return SHAMPOO_OK;
+}
+
+shampoo_status check_act(Handle* h, int dtype, int64_t rows, int64_t cols, int act) {
+  STATUS_TRY(check_dtype(h, dtype, "activations"));
+  if (rows < 0 || rows >= kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31 - 1)", (long long)rows);
+  if (cols < 1 || cols > kMaxCols) return fail(h, SHAMPOO_EINVAL, "cols = %lld outside [1, 2^20]", (long long)cols);
+  if (act < SHAMPOO_ACT_NONE || act > SHAMPOO_ACT_SILU) return fail(h, SHAMPOO_EINVAL, "bad activation %d", act);
+  return SHAMPOO_OK;
+}
+
+// Workgroups of an elementwise launch over n items, one per thread and turn: a
+// launch holds fewer than 2^32 threads, so larger ones take turns.
+unsigned act_grid(int64_t n) { return (unsigned)std::min<int64_t>(cdiv64(n, kThreads), 1 << 20); }
+
+bool ckpt_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Calls f with the activation as a compile-time constant.
+template <typename F>
+void with_act(int act, F&& f) {
+  switch (act) {
+    case SHAMPOO_ACT_RELU: f(std::integral_constant<int, SHAMPOO_ACT_RELU>()); break;
+    case SHAMPOO_ACT_GELU: f(std::integral_constant<int, SHAMPOO_ACT_GELU>()); break;
+    case SHAMPOO_ACT_GELU_TANH: f(std::integral_constant<int, SHAMPOO_ACT_GELU_TANH>()); break;
+    case SHAMPOO_ACT_SILU: f(std::integral_constant<int, SHAMPOO_ACT_SILU>()); break;
+    default: f(std::integral_constant<int, SHAMPOO_ACT_NONE>()); break;
+  }
+}
+
+// Calls f with a null pointer of the element type.
+template <typename F>
+void with_type(int dtype, F&& f) {
+  if (dtype == SHAMPOO_F32) f((float*)nullptr);
+  else f((uint16_t*)nullptr);
+}
+
+}  // namespace
+
+extern "C" {
+
+// ---------------------------------------------------------------- loss
+size_t shampoo_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int k) {
+  return 0;
+}
+
+shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
+                                      int64_t ld, const int32_t* targets, float* logp, float* lse, float* entropy,
+                                      int k, int32_t* top_ids, float* top_logp, void* workspace, size_t ws_bytes,
+                                      void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_logits(h, dtype, rows, vocab, ld, k));
+    if (rows == 0) return SHAMPOO_OK;
+    if (!logits || !lse || !logp != !targets || (k > 0 && (!top_ids || !top_logp)))
+      return fail(h, SHAMPOO_EINVAL, "logits or lse, one of targets and logp, or top_ids or top_logp is NULL");
+    const size_t need = shampoo_token_logprobs_workspace_bytes(rows, vocab, k);
+    if (need && (!workspace || ws_bytes < need))
+      return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        hipLaunchKernelGGL(logprobs_kernel<S>, dim3((unsigned)rows), dim3(kThreads), 0, s, (const S*)logits, ld,
+                           (int)vocab, targets, logp, lse, entropy, k, top_ids, top_logp);
+      });
+    });
+  });
+}
+
+shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
+                                           int64_t ld, const int32_t* targets, const float* lse,
+                                           const float* entropy, int k, const int32_t* top_ids,
+                                           const float* g_logp, const float* g_lse, const float* g_entropy,
+                                           const float* g_top, void* dlogits, int64_t ld_d, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_logits(h, dtype, rows, vocab, ld, k));
+    if (ld_d < vocab) return fail(h, SHAMPOO_EINVAL, "ld_d %lld < vocab %lld", (long long)ld_d, (long long)vocab);
+    if (rows == 0) return SHAMPOO_OK;
+    if (!logits || !lse || !dlogits) return fail(h, SHAMPOO_EINVAL, "logits, lse or dlogits is NULL");
+    if ((g_logp && !targets) || (g_entropy && !entropy) || (g_top && k > 0 && !top_ids))
+      return fail(h, SHAMPOO_EINVAL, "g_logp without targets, g_entropy without entropy, or g_top without top_ids");
+    if (dlogits == logits && ld_d != ld) return fail(h, SHAMPOO_EINVAL, "in place, ld_d %lld must be ld %lld", (long long)ld_d, (long long)ld);
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        hipLaunchKernelGGL(logprobs_grad_kernel<S>, dim3((unsigned)rows), dim3(kThreads), 0, s, (const S*)logits, ld,
+                           (int)vocab, targets, lse, entropy, g_top ? k : 0, top_ids, g_logp, g_lse, g_entropy, g_top,
+                           (S*)dlogits, ld_d);
+      });
+    });
+  });
+}
+
+// ---------------------------------------------------------------- activations
+size_t shampoo_act_checkpoint_bytes(int64_t rows, int64_t cols) {
+  if (rows < 0 || rows >= kMaxTokens || cols < 1 || cols > kMaxCols) return 0;
+  return (size_t)act_ckpt(rows, cols).bytes;
+}
+
+shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                                  int act, void* Y, int64_t ld_y, void* ckpt_x, void* ckpt_y, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_act(h, dtype, rows, cols, act));
+    if (ld_x < cols) return fail(h, SHAMPOO_EINVAL, "ld_x %lld < cols %lld", (long long)ld_x, (long long)cols);
+    if (Y && ld_y < cols) return fail(h, SHAMPOO_EINVAL, "ld_y %lld < cols %lld", (long long)ld_y, (long long)cols);
+    if (rows == 0) return SHAMPOO_OK;
+    if (!X || (!Y && !ckpt_x && !ckpt_y)) return fail(h, SHAMPOO_EINVAL, "X is NULL, or no output is asked for");
+    if (Y == X && ld_y != ld_x) return fail(h, SHAMPOO_EINVAL, "in place, ld_y %lld must be ld_x %lld", (long long)ld_y, (long long)ld_x);
+    if (!ckpt_aligned(ckpt_x) || !ckpt_aligned(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int64_t n = rows * (act_ckpt(rows, cols).ldq / kActGroup);
+    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        with_act(act, [&](auto a) {
+          hipLaunchKernelGGL((act_encode_kernel<S, decltype(a)::value>), dim3(act_grid(n)),
+                             dim3(kThreads), 0, s, (const S*)X, ld_x, rows, cols, (S*)Y, ld_y, (char*)ckpt_x,
+                             (char*)ckpt_y);
+        });
+      });
+    });
+  });
+}
+
+shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, int64_t cols, void* X, int dtype,
+                                  int64_t ld_x, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_act(h, dtype, rows, cols, SHAMPOO_ACT_NONE));
+    if (ld_x < cols) return fail(h, SHAMPOO_EINVAL, "ld_x %lld < cols %lld", (long long)ld_x, (long long)cols);
+    if (rows == 0) return SHAMPOO_OK;
+    if (!ckpt || !X) return fail(h, SHAMPOO_EINVAL, "ckpt or X is NULL");
+    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        hipLaunchKernelGGL(act_decode_kernel<S>, dim3(act_grid(rows * cols)), dim3(kThreads), 0, s,
+                           (const char*)ckpt, rows, cols, (S*)X, ld_x);
+      });
+    });
+  });
+}
+
+shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, int act, const void* dY,
+                                int dtype, int64_t ld_dy, void* dX, int64_t ld_dx, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_act(h, dtype, rows, cols, act));
+    if (ld_dy < cols || ld_dx < cols)
+      return fail(h, SHAMPOO_EINVAL, "ld_dy %lld or ld_dx %lld < cols %lld", (long long)ld_dy, (long long)ld_dx, (long long)cols);
+    if (rows == 0) return SHAMPOO_OK;
+    if (!ckpt || !dY || !dX) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or dX is NULL");
+    if (dX == dY && ld_dx != ld_dy) return fail(h, SHAMPOO_EINVAL, "in place, ld_dx %lld must be ld_dy %lld", (long long)ld_dx, (long long)ld_dy);
+    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        with_act(act, [&](auto a) {
+          hipLaunchKernelGGL((act_grad_kernel<S, decltype(a)::value>), dim3(act_grid(rows * cols)),
+                             dim3(kThreads), 0, s, (const char*)ckpt, rows, cols, (const S*)dY, ld_dy, (S*)dX, ld_dx);
+        });
+      });
+    });
+  });
+}
+
+// ---------------------------------------------------------------- weight gradient
+size_t shampoo_act_weight_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t out) {
+  return 0;
+}
+
+shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, const void* dY,
+                                       int dtype, int64_t out, int64_t ld_dy, void* G, int g_dtype, int64_t ld_g,
+                                       float beta, void* workspace, size_t ws_bytes, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_act(h, dtype, rows, cols, SHAMPOO_ACT_NONE));
+    STATUS_TRY(check_dtype(h, g_dtype, "G"));
+    if (out < 1 || out > kMaxCols) return fail(h, SHAMPOO_EINVAL, "out = %lld outside [1, 2^20]", (long long)out);
+    if (ld_dy < out || ld_g < out)
+      return fail(h, SHAMPOO_EINVAL, "ld_dy %lld or ld_g %lld < out %lld", (long long)ld_dy, (long long)ld_g, (long long)out);
+    if (!isfinite(beta)) return fail(h, SHAMPOO_EINVAL, "beta is not finite");
+    if (!G || (rows > 0 && (!ckpt || !dY))) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or G is NULL");
+    if (G == dY || G == ckpt) return fail(h, SHAMPOO_EINVAL, "G must not be dY or the checkpoint");
+    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    const size_t need = shampoo_act_weight_grad_workspace_bytes(rows, cols, out);
+    if (need && (!workspace || ws_bytes < need))
+      return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    const int64_t tiles = cdiv64(cols, 16) * cdiv64(out, 16);
+    if (tiles > INT32_MAX) return fail(h, SHAMPOO_EUNSUPPORTED, "G of %lld x %lld", (long long)cols, (long long)out);
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        with_type(g_dtype, [&](auto* gtype) {
+          using SG = std::remove_pointer_t<decltype(gtype)>;
+          hipLaunchKernelGGL((weight_grad_kernel<S, SG>), dim3((unsigned)tiles), dim3(256), 0, s, (const char*)ckpt,
+                             rows, cols, (const S*)dY, out, ld_dy, (SG*)G, ld_g, beta);
+        });
+      });
+    });
+  });
+}
+
+}  // extern "C"

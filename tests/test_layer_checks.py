@@ -1,0 +1,146 @@
+"""Refusals of the calls from the loss to the gradient: the binding's layout
+checks (CPU tensors, nothing reaches a device) and the workspace and size
+queries."""
+import pytest
+import torch
+
+from paper_2002_09018_amd import binding as B
+
+BF16 = torch.bfloat16
+
+
+def _raises(fn, match):
+    with pytest.raises(ValueError, match=match):
+        fn()
+
+
+def _i32(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def test_sizes():
+    assert B.shampoo_act_checkpoint_bytes(0, 5) == 0
+    assert B.shampoo_act_checkpoint_bytes(1, 0) == 0 and B.shampoo_act_checkpoint_bytes(-1, 5) == 0
+    assert B.shampoo_act_checkpoint_bytes(1, (1 << 20) + 1) == 0
+    assert B.shampoo_act_checkpoint_bytes(1, 1) == 512          # 32 codes, 1 scale byte, both rounded up to 256
+    assert B.shampoo_act_checkpoint_bytes(7, 100) == 1024 + 256  # 7 x 128 codes, 7 x 4 scale bytes
+    assert B.shampoo_act_checkpoint_bytes(70000, 65536) == 70000 * 65536 + 70000 * 2048  # past 2^32
+    assert B.shampoo_token_logprobs_workspace_bytes(-1, 10, 0) == 0
+    assert B.shampoo_token_logprobs_workspace_bytes(1, 0, 0) == 0
+    assert B.shampoo_token_logprobs_workspace_bytes(1, 10, B.MAX_TOP + 1) == 0
+    assert B.shampoo_act_weight_grad_workspace_bytes(-1, 8, 8) == 0
+    assert B.shampoo_act_weight_grad_workspace_bytes(8, 0, 8) == 0
+
+
+def test_logprobs_checks():
+    n, v, k = 4, 10, 3
+
+    def call(**o):
+        a = dict(logits=torch.zeros(n, v), targets=_i32(n), logp=torch.zeros(n), lse=torch.zeros(n),
+                 entropy=torch.zeros(n), top_ids=_i32(n, k), top_logp=torch.zeros(n, k),
+                 workspace=torch.zeros(1 << 20, dtype=torch.uint8))
+        a.update(o)
+        return lambda: B.shampoo_token_logprobs(None, **a)
+    _raises(call(), "expected a GPU tensor")
+    _raises(call(logits=torch.zeros(n, v, dtype=BF16)), "expected a GPU tensor")
+    _raises(call(logits=torch.zeros(n, v + 3)[:, :v]), "expected a GPU tensor")
+    _raises(call(logits=torch.zeros(n, v, dtype=torch.float16)), "float32 or bfloat16")
+    _raises(call(logits=torch.zeros(n * v)), "dimensions")
+    _raises(call(logits=torch.zeros(n, 2 * v)[:, ::2]), "adjacent")
+    _raises(call(logits=torch.zeros(1, v).expand(n, v)), "row stride")
+    _raises(call(targets=None), "go together")
+    _raises(call(logp=None), "go together")
+    _raises(call(top_logp=None), "go together")
+    _raises(call(targets=torch.zeros(n, dtype=torch.int64)), "int32")
+    _raises(call(targets=_i32(n + 1)), "expected")
+    _raises(call(lse=None), "required")
+    _raises(call(lse=torch.zeros(n, dtype=torch.float64)), "float32")
+    _raises(call(lse=torch.zeros(2 * n)[::2]), "contiguous")
+    _raises(call(entropy=torch.zeros(n - 1)), "expected")
+    _raises(call(top_ids=_i32(n, k).long()), "int32")
+    _raises(call(top_logp=torch.zeros(n, k + 1)), "expected")
+    _raises(call(top_ids=_i32(n, 2 * k)[:, ::2]), "contiguous")
+    _raises(call(workspace=torch.zeros(8)), "uint8")
+
+
+def test_logprobs_grad_checks():
+    n, v, k = 4, 10, 3
+
+    def call(**o):
+        a = dict(logits=torch.zeros(n, v), targets=_i32(n), lse=torch.zeros(n), dlogits=torch.zeros(n, v),
+                 g_logp=torch.zeros(n), g_lse=torch.zeros(n), entropy=torch.zeros(n), g_entropy=torch.zeros(n),
+                 top_ids=_i32(n, k), g_top=torch.zeros(n, k))
+        a.update(o)
+        return lambda: B.shampoo_token_logprobs_grad(None, **a)
+    z = torch.zeros(n, v)
+    _raises(call(), "expected a GPU tensor")
+    _raises(call(logits=z, dlogits=z), "expected a GPU tensor")          # in place
+    _raises(call(dlogits=torch.zeros(n, v, dtype=BF16)), "dtype")
+    _raises(call(dlogits=torch.zeros(n, v + 1)), "expected")
+    big = torch.zeros(n * v + 1)
+    _raises(call(logits=big[:n * v].view(n, v), dlogits=big[1:].view(n, v)), "overlap")
+    wide = torch.zeros(n, 2 * v)
+    _raises(call(logits=wide[:, :v], dlogits=wide.view(-1)[:n * v].view(n, v)), "overlap")
+    _raises(call(targets=None), "needs targets")
+    _raises(call(entropy=None), "needs entropy")
+    _raises(call(top_ids=None), "needs top_ids")
+    _raises(call(lse=None), "required")
+    _raises(call(g_logp=torch.zeros(n, 1)), "expected")
+    _raises(call(g_top=torch.zeros(n, k - 1)), "expected")
+    _raises(call(g_entropy=torch.zeros(n, dtype=BF16)), "float32")
+
+
+def _ckpt(rows, cols, less=0):
+    return torch.zeros(B.shampoo_act_checkpoint_bytes(rows, cols) - less, dtype=torch.uint8)
+
+
+def test_act_checks():
+    n, c = 5, 70
+    x, q = torch.zeros(n, c), _ckpt(n, c)
+
+    def enc(**o):
+        a = dict(X=x, ckpt_x=q, act=B.ACT_GELU, Y=torch.zeros(n, c), ckpt_y=_ckpt(n, c))
+        a.update(o)
+        return lambda: B.shampoo_act_encode(None, **a)
+    _raises(enc(), "expected a GPU tensor")
+    _raises(enc(Y=x), "expected a GPU tensor")
+    _raises(enc(X=x.half()), "float32 or bfloat16")
+    _raises(enc(Y=torch.zeros(n, c, dtype=BF16)), "dtype")
+    _raises(enc(Y=torch.zeros(n, c + 1)), "expected")
+    _raises(enc(ckpt_x=_ckpt(n, c, 1)), "at least")
+    _raises(enc(ckpt_y=_ckpt(n, c).view(torch.int8)), "uint8")
+    _raises(enc(ckpt_y=torch.zeros(4096, dtype=torch.uint8)[::2]), "contiguous")
+    _raises(lambda: B.shampoo_act_decode(None, q, x), "expected a GPU tensor")
+    _raises(lambda: B.shampoo_act_decode(None, None, x), "required")
+    _raises(lambda: B.shampoo_act_decode(None, _ckpt(n, c, 1), x), "at least")
+    _raises(lambda: B.shampoo_act_decode(None, q, x.t()), "adjacent")
+    _raises(lambda: B.shampoo_act_grad(None, q, B.ACT_SILU, x, x), "expected a GPU tensor")
+    _raises(lambda: B.shampoo_act_grad(None, q, B.ACT_SILU, x, x.bfloat16()), "dtype")
+    _raises(lambda: B.shampoo_act_grad(None, _ckpt(n, c, 1), B.ACT_SILU, x, x), "at least")
+
+
+def test_weight_grad_checks():
+    n, c, o = 5, 70, 9
+    q, dy, G = _ckpt(n, c), torch.zeros(n, o), torch.zeros(c, o)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+
+    def call(ckpt=q, dY=dy, G=G, workspace=ws, **kw):
+        return lambda: B.shampoo_act_weight_grad(None, ckpt, dY, G, workspace=workspace, **kw)
+    _raises(call(), "expected a GPU tensor")
+    _raises(call(dY=dy.bfloat16()), "expected a GPU tensor")
+    _raises(call(dY=torch.zeros(n, o + 1)), "columns")
+    _raises(call(dY=torch.zeros(n + 1, o)), "at least")
+    _raises(call(ckpt=None), "required")
+    _raises(call(G=G.half()), "float32 or bfloat16")
+    _raises(call(G=torch.zeros(o, c).t()), "adjacent")
+    buf = torch.zeros(n * o + c * o - 1)
+    _raises(call(dY=buf[:n * o].view(n, o), G=buf[n * o - 1:].view(c, o)), "overlap")
+
+
+def test_null_handle_is_refused():
+    lib = B._lib
+    assert lib.shampoo_token_logprobs(None, None, 0, 1, 1, 1, None, None, None, None, 0, None, None, None, 0,
+                                      None) == B.SHAMPOO_EINVAL
+    assert lib.shampoo_act_decode(None, None, 1, 1, None, 0, 1, None) == B.SHAMPOO_EINVAL
+    assert lib.shampoo_act_weight_grad(None, None, 1, 1, None, 0, 1, 1, None, 0, 1, 0.0, None, 0,
+                                       None) == B.SHAMPOO_EINVAL
