@@ -65,7 +65,7 @@ shampoo_status check_act(Handle* h, int dtype, int64_t rows, int64_t cols, int a
 // launch holds fewer than 2^32 threads, so larger ones take turns.
 unsigned act_grid(int64_t n) { return (unsigned)std::min<int64_t>(cdiv64(n, kThreads), 1 << 20); }
 
-bool ckpt_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // Calls f with the activation as a compile-time constant.
 template <typename F>
@@ -84,6 +84,47 @@ template <typename F>
 void with_type(int dtype, F&& f) {
   if (dtype == SHAMPOO_F32) f((float*)nullptr);
   else f((uint16_t*)nullptr);
+}
+
+// How a weight gradient is cut: the tile, and the splits of the token axis.
+struct WgradPlan {
+  int tile = 256, splits = 1;
+  int64_t per_split = 0, tiles_m = 0, tiles_n = 0;
+  size_t ws = 0;
+};
+
+WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
+  WgradPlan p;
+  const int64_t bk = dtype == SHAMPOO_BF16 ? 64 : 32;
+  const int64_t t256 = cdiv64(cols, 256) * cdiv64(out, 256);
+  p.tile = t256 >= 64 ? 256 : 128;
+  p.tiles_m = cdiv64(cols, p.tile);
+  p.tiles_n = cdiv64(out, p.tile);
+  const int64_t tiles = p.tiles_m * p.tiles_n, slots = p.tile == 256 ? 256 : 512;
+  const int64_t stages = std::max<int64_t>(1, cdiv64(rows, bk));
+  p.splits = (int)std::min(std::max<int64_t>(1, slots / tiles), cdiv64(stages, 4));
+  p.per_split = cdiv64(stages, p.splits) * bk;
+  p.splits = (int)std::max<int64_t>(1, cdiv64(rows, p.per_split));
+  if (p.splits > 1) p.ws = (size_t)(p.splits * tiles) * p.tile * p.tile * sizeof(float);
+  return p;
+}
+
+template <typename S, typename SG, int T, int WM, int WN>
+shampoo_status wgrad_launch(Handle* h, const WgradArgs& q, hipStream_t s) {
+  using L = WgradTile<S, T, WM, WN>;
+  auto k = weight_grad_kernel<S, SG, T, WM, WN>;
+  // more LDS than a launch may take by default
+  HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, L::kLdsB));
+  const int64_t tiles = (int64_t)q.tiles_m * q.tiles_n;
+  STATUS_TRY(launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
+    hipLaunchKernelGGL(k, dim3((unsigned)(tiles * q.splits)), dim3(L::kThr), L::kLdsB, s, q);
+  }));
+  if (q.splits == 1) return SHAMPOO_OK;
+  const int64_t pieces = tiles * (T / 32) * (T / 32) * 4;
+  return launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
+    hipLaunchKernelGGL((weight_grad_sum_kernel<SG, T, WM, WN>), dim3((unsigned)cdiv64(pieces, kThreads / 64)),
+                       dim3(kThreads), 0, s, q);
+  });
 }
 
 }  // namespace
@@ -160,7 +201,7 @@ shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_
     if (rows == 0) return SHAMPOO_OK;
     if (!X || (!Y && !ckpt_x && !ckpt_y)) return fail(h, SHAMPOO_EINVAL, "X is NULL, or no output is asked for");
     if (Y == X && ld_y != ld_x) return fail(h, SHAMPOO_EINVAL, "in place, ld_y %lld must be ld_x %lld", (long long)ld_y, (long long)ld_x);
-    if (!ckpt_aligned(ckpt_x) || !ckpt_aligned(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    if (!aligned16(ckpt_x) || !aligned16(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t n = rows * (act_ckpt(rows, cols).ldq / kActGroup);
@@ -184,7 +225,7 @@ shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, 
     if (ld_x < cols) return fail(h, SHAMPOO_EINVAL, "ld_x %lld < cols %lld", (long long)ld_x, (long long)cols);
     if (rows == 0) return SHAMPOO_OK;
     if (!ckpt || !X) return fail(h, SHAMPOO_EINVAL, "ckpt or X is NULL");
-    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
@@ -206,7 +247,7 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
     if (rows == 0) return SHAMPOO_OK;
     if (!ckpt || !dY || !dX) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or dX is NULL");
     if (dX == dY && ld_dx != ld_dy) return fail(h, SHAMPOO_EINVAL, "in place, ld_dx %lld must be ld_dy %lld", (long long)ld_dx, (long long)ld_dy);
-    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
@@ -223,7 +264,10 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
 
 // ---------------------------------------------------------------- weight gradient
 size_t shampoo_act_weight_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t out) {
-  return 0;
+  if (rows < 0 || rows >= kMaxTokens || cols < 1 || cols > kMaxCols || out < 1 || out > kMaxCols) return 0;
+  size_t need = 0;
+  for (int dtype : {SHAMPOO_F32, SHAMPOO_BF16}) need = std::max(need, wgrad_plan(rows, cols, out, dtype).ws);
+  return need;
 }
 
 shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, const void* dY,
@@ -238,24 +282,50 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
     if (!isfinite(beta)) return fail(h, SHAMPOO_EINVAL, "beta is not finite");
     if (!G || (rows > 0 && (!ckpt || !dY))) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or G is NULL");
     if (G == dY || G == ckpt) return fail(h, SHAMPOO_EINVAL, "G must not be dY or the checkpoint");
-    if (!ckpt_aligned(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    if (!aligned16(ckpt) || !aligned16(workspace))
+      return fail(h, SHAMPOO_EINVAL, "checkpoint or workspace not aligned to 16 bytes");
     const size_t need = shampoo_act_weight_grad_workspace_bytes(rows, cols, out);
     if (need && (!workspace || ws_bytes < need))
       return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
-    const int64_t tiles = cdiv64(cols, 16) * cdiv64(out, 16);
-    if (tiles > INT32_MAX) return fail(h, SHAMPOO_EUNSUPPORTED, "G of %lld x %lld", (long long)cols, (long long)out);
+    const WgradPlan p = wgrad_plan(rows, cols, out, dtype);
+    if (p.tiles_m * p.tiles_n * p.splits > INT32_MAX / 512)
+      return fail(h, SHAMPOO_EUNSUPPORTED, "G of %lld x %lld", (long long)cols, (long long)out);
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
-      with_type(dtype, [&](auto* type) {
-        using S = std::remove_pointer_t<decltype(type)>;
-        with_type(g_dtype, [&](auto* gtype) {
-          using SG = std::remove_pointer_t<decltype(gtype)>;
-          hipLaunchKernelGGL((weight_grad_kernel<S, SG>), dim3((unsigned)tiles), dim3(256), 0, s, (const char*)ckpt,
-                             rows, cols, (const S*)dY, out, ld_dy, (SG*)G, ld_g, beta);
-        });
+    const ActCkpt c = act_ckpt(rows, cols);
+    WgradArgs q{};
+    q.codes = static_cast<const char*>(ckpt);
+    q.scales = static_cast<const uint8_t*>(ckpt) + c.scales;
+    q.ldq = c.ldq;
+    q.dY = dY;
+    q.ld_dy = ld_dy;
+    q.rows = rows;
+    q.cols = (int)cols;
+    q.out = (int)out;
+    q.G = G;
+    q.ld_g = ld_g;
+    q.beta = beta;
+    q.part = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+    q.splits = p.splits;
+    q.per_split = p.per_split;
+    q.tiles_m = (int)p.tiles_m;
+    q.tiles_n = (int)p.tiles_n;
+    shampoo_status st = SHAMPOO_OK;
+    with_type(dtype, [&](auto* type) {
+      using S = std::remove_pointer_t<decltype(type)>;
+      with_type(g_dtype, [&](auto* gtype) {
+        using SG = std::remove_pointer_t<decltype(gtype)>;
+        if (rows == 0)
+          st = launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
+            hipLaunchKernelGGL(weight_grad_scale_kernel<SG>, dim3(act_grid(cols * out)), dim3(kThreads), 0, s, q);
+          });
+        else if (p.tile == 256)
+          st = wgrad_launch<S, SG, 256, 128, 64>(h, q, s);
+        else
+          st = wgrad_launch<S, SG, 128, 64, 64>(h, q, s);
       });
     });
+    return st;
   });
 }
 

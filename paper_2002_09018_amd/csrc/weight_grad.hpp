@@ -1,36 +1,371 @@
-// Weight gradient G = beta G + X^^T dY from an 8-bit activation checkpoint.
+// Weight gradient G = beta G + X^^T dY from an 8-bit activation checkpoint, on
+// the bf16 matrix cores (v_mfma_f32_32x32x16_bf16).
+//
+// A code times its power of two has at most 7 significant bits, so x^ is exact
+// in bf16, and so is a bf16 gradient: their products are exact, and one
+// instruction per 16 tokens forms them.  An fp32 gradient is cut into three
+// bf16 terms, y = p0 + p1 + p2 (truncated: 8 bits each, every difference exact;
+// p0 keeps the sign of an infinity and never rounds up to one), which takes
+// three.  (Below 2^-109 the last term reaches bf16's subnormals: it is held to
+// 2^-134 then.)
+//
+// Both operands lie token by token, and the contraction runs over tokens.  A
+// stage of kBk tokens of both is copied into LDS as it lies,
+//   [operand][term][token][column],
+// and the fragments, 8 tokens of one column for each lane, are read with the
+// transposing read (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 columns and
+// receive 4 tokens of one column each).  A row of 16 columns is 32 bytes; the
+// 32-byte pieces of a row are stored at piece ^ swz(token), which puts the four
+// tokens of such a read, and its neighbour's, on different banks.
+//
+// While stage s is multiplied, the registers loaded during stage s - 1 are
+// written as stage s + 1 (codes converted on the way) and the loads of stage
+// s + 2 are issued; one barrier per stage, before the last 16 tokens of it, so
+// that the first fragments of the next stage are read while those are
+// multiplied.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "act_checkpoint.hpp"
+#include "split_mfma.hpp"
 #include "tile_mfma.hpp"
 
 namespace shp {
 
-// One workgroup per 16 x 16 tile of G: 16 tokens at a time through LDS, fp32.
-template <typename S, typename SG>
-__global__ __launch_bounds__(256) void weight_grad_kernel(const char* __restrict__ ckpt, int64_t rows, int64_t cols,
-                                                         const S* __restrict__ dY, int64_t out, int64_t ld_dy,
-                                                         SG* __restrict__ G, int64_t ld_g, float beta) {
-  __shared__ float a[16][17], b[16][17];
-  const ActCkpt c = act_ckpt(rows, cols);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t tiles_n = (out + 15) / 16;
-  const int64_t m0 = blockIdx.x / tiles_n * 16, n0 = blockIdx.x % tiles_n * 16;
-  float acc = 0.f;
-  for (int64_t k0 = 0; k0 < rows; k0 += 16) {
-    const int64_t r = k0 + ty;
-    a[ty][tx] = r < rows && m0 + tx < cols ? act_load(ckpt, c, r, m0 + tx) : 0.f;
-    b[ty][tx] = r < rows && n0 + tx < out ? cvt<float, S>(dY[r * ld_dy + n0 + tx]) : 0.f;
-    __syncthreads();
-    for (int k = 0; k < 16; ++k) acc += a[k][ty] * b[k][tx];
-    __syncthreads();
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float wg_acc __attribute__((ext_vector_type(16)));
+
+struct WgradArgs {
+  const char* codes;     // rows x ldq
+  const uint8_t* scales; // rows x ldq / 32
+  int64_t ldq;
+  const void* dY;        // rows x out
+  int64_t ld_dy;
+  int64_t rows;
+  int cols, out;
+  void* G;
+  int64_t ld_g;
+  float beta;
+  float* part;           // partial tiles of a split launch, or NULL
+  int splits;
+  int64_t per_split;     // tokens of one split, a multiple of the stage
+  int tiles_m, tiles_n;
+};
+
+// T x T tiles of G; waves of WM x WN.
+template <typename S, int T, int WM, int WN>
+struct WgradTile {
+  static constexpr int kTerms = sizeof(S) == 2 ? 1 : 3;
+  static constexpr int kBk = sizeof(S) == 2 ? 64 : 32;  // tokens of a stage
+  static constexpr int kWavesN = T / WN;
+  static constexpr int kThr = (T / WM) * (T / WN) * 64;
+  static constexpr int kRowB = 2 * T;  // bytes of one token of one operand
+  static constexpr int kPlaneB = kBk * kRowB;
+  static constexpr int kStageB = (1 + kTerms) * kPlaneB;
+  static constexpr int kLdsB = 2 * kStageB;
+  static constexpr int kBm = WM / 32, kBn = WN / 32;
+  static constexpr int kUa = kBk * (T / 16) / kThr;  // 16-code units of a thread
+  static constexpr int kUb = kBk * (T / 8) / kThr;   // 8-column units of a thread
+  static constexpr int kSteps = kBk / 16;
+};
+
+__device__ __forceinline__ int wg_swz(int token) { return (token & 3) ^ ((token & 1) << 2); }
+
+// The bf16 of two values that are exact in it (or NaN), x in the low half.
+__device__ __forceinline__ uint32_t wg_pack(float x, float y) {
+  return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+
+template <typename S, int T, int WM, int WN>
+struct WgradLoader {
+  using L = WgradTile<S, T, WM, WN>;
+  static constexpr int kTa = L::kThr / (T / 16), kTb = L::kThr / (T / 8);  // tokens between a thread's units
+  const char* pa;
+  const uint8_t* ps;
+  const S* pb;
+  int nb;  // columns of the thread's units inside G
+  u32x4 a[L::kUa];
+  uint32_t sc[L::kUa];
+  uint32_t b[L::kUb][sizeof(S) == 2 ? 4 : 8];
+
+  // A thread's units lie in the same columns: 16 codes, 8 gradient columns.
+  static __device__ __forceinline__ void unit_a(int tid, int u, int& token, int& piece) {
+    token = tid / (T / 16) + u * kTa;
+    piece = tid % (T / 16);
   }
-  if (m0 + ty < cols && n0 + tx < out) {
-    SG* g = G + (m0 + ty) * ld_g + n0 + tx;
-    *g = from_f32<SG>(beta == 0.f ? acc : beta * cvt<float, SG>(*g) + acc);
+  static __device__ __forceinline__ void unit_b(int tid, int u, int& token, int& c8) {
+    token = tid / (T / 8) + u * kTb;
+    c8 = tid % (T / 8);
+  }
+
+  __device__ __forceinline__ void init(const WgradArgs& q, int64_t k0, int m0, int n0, int tid) {
+    int token, piece;
+    unit_a(tid, 0, token, piece);
+    // columns past the codes only feed rows of G that are not stored: any codes do
+    int64_t m = m0 + piece * 16;
+    if (m >= q.ldq) m = 0;
+    pa = q.codes + (k0 + token) * q.ldq + m;
+    ps = q.scales + (k0 + token) * (q.ldq / kActGroup) + m / kActGroup;
+    unit_b(tid, 0, token, piece);
+    const int n = n0 + piece * 8;
+    nb = min(8, max(0, q.out - n));
+    pb = static_cast<const S*>(q.dY) + (k0 + token) * q.ld_dy + n;
+  }
+
+  // Stage of tokens k0..; tokens at or past k_end are zeros.
+  __device__ __forceinline__ void load(const WgradArgs& q, int64_t k0, int64_t k_end, int tid) {
+    const int64_t left = k_end - k0;
+    const bool full = left >= L::kBk;
+#pragma unroll
+    for (int u = 0; u < L::kUa; ++u) {
+      int token, piece;
+      unit_a(tid, u, token, piece);
+      if (full || token < left) {
+        a[u] = gload<u32x4>(pa + u * kTa * q.ldq);
+        sc[u] = gload<uint8_t>(ps + u * kTa * (q.ldq / kActGroup));
+      } else {
+        a[u] = u32x4{0, 0, 0, 0};
+        sc[u] = 0;
+      }
+    }
+    pa += L::kBk * q.ldq;
+    ps += L::kBk * (q.ldq / kActGroup);
+#pragma unroll
+    for (int u = 0; u < L::kUb; ++u) {
+      int token, c8;
+      unit_b(tid, u, token, c8);
+      const int have = full || token < left ? nb : 0;
+      const S* p = pb + u * kTb * q.ld_dy;
+      if (have == 8) {
+        const u32x4u v = *(const __attribute__((address_space(1))) u32x4u*)(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[u][i] = v[i];
+        if constexpr (sizeof(S) == 4) {
+          const u32x4u w = *(const __attribute__((address_space(1))) u32x4u*)(p + 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) b[u][4 + i] = w[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (sizeof(S) == 4) {
+            b[u][i] = i < have ? gload<uint32_t>(p + i) : 0u;
+          } else {
+            const uint32_t v = i < have ? (uint32_t)gload<uint16_t>(p + i) : 0u;
+            b[u][i / 2] = i & 1 ? b[u][i / 2] | v << 16 : v;
+          }
+        }
+      }
+    }
+    pb += L::kBk * q.ld_dy;
+  }
+
+  __device__ __forceinline__ void store(char* stage, int tid) {
+#pragma unroll
+    for (int u = 0; u < L::kUa; ++u) {
+      int token, piece;
+      unit_a(tid, u, token, piece);
+      const float s = act_scale(sc[u]);
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t x = a[u][i / 2] >> (16 * (i & 1));
+        w[i] = wg_pack((float)(int8_t)(x & 0xff) * s, (float)(int8_t)((x >> 8) & 0xff) * s);
+      }
+      u32x4* d = reinterpret_cast<u32x4*>(stage + token * L::kRowB + (piece ^ wg_swz(token)) * 32);
+      d[0] = u32x4{w[0], w[1], w[2], w[3]};
+      d[1] = u32x4{w[4], w[5], w[6], w[7]};
+    }
+    char* sb = stage + L::kPlaneB;
+#pragma unroll
+    for (int u = 0; u < L::kUb; ++u) {
+      int token, c8;
+      unit_b(tid, u, token, c8);
+      char* d = sb + token * L::kRowB + ((c8 >> 1) ^ wg_swz(token)) * 32 + (c8 & 1) * 16;
+      if constexpr (sizeof(S) == 2) {
+        *reinterpret_cast<u32x4*>(d) = u32x4{b[u][0], b[u][1], b[u][2], b[u][3]};
+      } else {
+        uint32_t p[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x[3][2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // a NaN is made quiet, so that its upper half is one too
+            const float y = __builtin_canonicalizef(__uint_as_float(b[u][2 * i + h]));
+            x[0][h] = y;
+            // infinities and NaN are the first term alone
+            const float r = finite_f32(y) ? y - __uint_as_float(__float_as_uint(y) & 0xffff0000u) : 0.f;
+            x[1][h] = r;
+            x[2][h] = r - __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+          }
+#pragma unroll
+          for (int t = 0; t < 3; ++t) p[t][i] = wg_pack(x[t][0], x[t][1]);
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          *reinterpret_cast<u32x4*>(d + t * L::kPlaneB) = u32x4{p[t][0], p[t][1], p[t][2], p[t][3]};
+      }
+    }
+  }
+};
+
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+// The 8 tokens of a lane: two transposing reads, 4 rows apart.
+__device__ __forceinline__ bf16x8 wg_frag(const char* p, int row_b) {
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 4 * row_b));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Four rows of one column of G, rounded once.
+template <typename SG>
+__device__ __forceinline__ void wg_store4(const WgradArgs& q, int m, int n, f32x4 v) {
+  if (n >= q.out) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (m + i >= q.cols) continue;
+    SG* g = static_cast<SG*>(q.G) + (int64_t)(m + i) * q.ld_g + n;
+    const float x = q.beta == 0.f ? v[i] : fmaf(q.beta, cvt<float, SG>(*g), v[i]);
+    *g = from_f32<SG>(x);
+  }
+}
+
+template <typename S, typename SG, int T, int WM, int WN>
+__global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_grad_kernel(WgradArgs q) {
+  using L = WgradTile<S, T, WM, WN>;
+  extern __shared__ __align__(16) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tiles = q.tiles_m * q.tiles_n;
+  const int l = xcd_remap(blockIdx.x, gridDim.x);
+  const int split = l / tiles, t = l % tiles;
+  const int tm = t % q.tiles_m, tn = t / q.tiles_m;
+  const int m0 = tm * T, n0 = tn * T;
+  const int64_t kb = split * q.per_split, ke = min(q.rows, kb + q.per_split);
+  const int stages = (int)((ke - kb + L::kBk - 1) / L::kBk);
+
+  WgradLoader<S, T, WM, WN> ld;
+  ld.init(q, kb, m0, n0, tid);
+  ld.load(q, kb, ke, tid);
+  ld.store(lds, tid);
+  if (stages > 1) ld.load(q, kb + L::kBk, ke, tid);
+
+  // fragment addresses: 16-lane group g reads columns 16 (g & 1).., tokens 8 (g >> 1)..
+  const int wm = wave / L::kWavesN * WM, wn = wave % L::kWavesN * WN;
+  const int token = (lane >> 5) * 8 + ((lane >> 2) & 3), side = (lane >> 4) & 1;
+  int oa[L::kBm], ob[L::kBn];
+#pragma unroll
+  for (int i = 0; i < L::kBm; ++i)
+    oa[i] = token * L::kRowB + ((wm / 16 + 2 * i + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
+#pragma unroll
+  for (int j = 0; j < L::kBn; ++j)
+    ob[j] = L::kPlaneB + token * L::kRowB + ((wn / 16 + 2 * j + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
+
+  wg_acc acc[L::kBm][L::kBn];
+#pragma unroll
+  for (int i = 0; i < L::kBm; ++i)
+#pragma unroll
+    for (int j = 0; j < L::kBn; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  bf16x8 fa[2][L::kBm], fb[2][L::kTerms][L::kBn];
+  auto read = [&](const char* stage, int step, int set) {
+#pragma unroll
+    for (int i = 0; i < L::kBm; ++i) fa[set][i] = wg_frag(stage + oa[i] + step * 16 * L::kRowB, L::kRowB);
+#pragma unroll
+    for (int p = 0; p < L::kTerms; ++p)
+#pragma unroll
+      for (int j = 0; j < L::kBn; ++j)
+        fb[set][p][j] = wg_frag(stage + ob[j] + p * L::kPlaneB + step * 16 * L::kRowB, L::kRowB);
+  };
+  auto multiply = [&](int set) {
+#pragma unroll
+    for (int p = L::kTerms - 1; p >= 0; --p)  // the smallest terms first
+#pragma unroll
+      for (int j = 0; j < L::kBn; ++j)
+#pragma unroll
+        for (int i = 0; i < L::kBm; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[set][i], fb[set][p][j], acc[i][j], 0, 0, 0);
+  };
+
+  __syncthreads();
+  read(lds, 0, 0);
+  for (int s = 0; s < stages; ++s) {
+    const char* cur = lds + (s & 1) * L::kStageB;
+    char* nxt = lds + ((s + 1) & 1) * L::kStageB;
+    if (s + 1 < stages) ld.store(nxt, tid);
+    if (s + 2 < stages) ld.load(q, kb + (int64_t)(s + 2) * L::kBk, ke, tid);
+#pragma unroll
+    for (int step = 0; step < L::kSteps; ++step) {
+      if (step + 1 < L::kSteps) {
+        read(cur, step + 1, (step + 1) & 1);
+      } else if (s + 1 < stages) {
+        __syncthreads();
+        read(nxt, 0, 0);
+      }
+      multiply(step & 1);
+    }
+  }
+
+  if (q.part) {
+    // partial tiles in accumulator order: 16 bytes a lane
+    f32x4* d = reinterpret_cast<f32x4*>(q.part) + (((int64_t)split * tiles + t) * (L::kThr / 64) + wave) *
+                                                      (L::kBm * L::kBn * 4 * 64) + lane;
+#pragma unroll
+    for (int i = 0; i < L::kBm; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          d[((i * L::kBn + j) * 4 + v) * 64] =
+              f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < L::kBm; ++i)
+#pragma unroll
+    for (int j = 0; j < L::kBn; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        wg_store4<SG>(q, m0 + wm + i * 32 + v * 8 + (lane >> 5) * 4, n0 + wn + j * 32 + (lane & 31),
+                      f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]});
+}
+
+// G from the partial tiles, added in split order: one wave per 4 accumulator
+// elements of a 32 x 32 block.
+template <typename SG, int T, int WM, int WN>
+__global__ __launch_bounds__(kThreads) void weight_grad_sum_kernel(WgradArgs q) {
+  constexpr int kPerTile = (T / 32) * (T / 32) * 4;  // 64-lane pieces of a tile
+  const int lane = threadIdx.x & 63;
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int tiles = q.tiles_m * q.tiles_n;
+  if (w >= (int64_t)tiles * kPerTile) return;
+  const int t = (int)(w / kPerTile), piece = (int)(w % kPerTile);
+  const int v = piece & 3, blk = piece >> 2;
+  constexpr int kBm = WM / 32, kBn = WN / 32;
+  const int wave = blk / (kBm * kBn), i = blk % (kBm * kBn) / kBn, j = blk % kBn;
+  const int m = t % q.tiles_m * T + wave / (T / WN) * WM + i * 32 + v * 8 + (lane >> 5) * 4;
+  const int n = t / q.tiles_m * T + wave % (T / WN) * WN + j * 32 + (lane & 31);
+  const f32x4* d = reinterpret_cast<const f32x4*>(q.part) + w * 64 + lane;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < q.splits; ++s) sum += d[(int64_t)s * tiles * kPerTile * 64];
+  wg_store4<SG>(q, m, n, sum);
+}
+
+// No tokens: G = beta G.
+template <typename SG>
+__global__ __launch_bounds__(kThreads) void weight_grad_scale_kernel(WgradArgs q) {
+  const int64_t n = (int64_t)q.cols * q.out, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += step) {
+    SG* g = static_cast<SG*>(q.G) + i / q.out * q.ld_g + i % q.out;
+    *g = from_f32<SG>(q.beta == 0.f ? 0.f : q.beta * cvt<float, SG>(*g));
   }
 }
 
