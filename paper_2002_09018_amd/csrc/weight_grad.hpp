@@ -65,13 +65,19 @@ struct WgradTile {
   static constexpr int kThr = (T / WM) * (T / WN) * 64;
   static constexpr int kRowB = 2 * T;  // bytes of one token of one operand
   static constexpr int kPlaneB = kBk * kRowB;
-  static constexpr int kStageB = (1 + kTerms) * kPlaneB;
+  static constexpr int kStageB = (1 + kTerms) * kPlaneB;  // a power of two: the buffers are one bit apart
   static constexpr int kLdsB = 2 * kStageB;
   static constexpr int kBm = WM / 32, kBn = WN / 32;
   static constexpr int kUa = kBk * (T / 16) / kThr;  // 16-code units of a thread
   static constexpr int kUb = kBk * (T / 8) / kThr;   // 8-column units of a thread
+  static constexpr int kTa = kThr / (T / 16), kTb = kThr / (T / 8);  // tokens between a thread's units
   static constexpr int kSteps = kBk / 16;
+  static_assert((kStageB & (kStageB - 1)) == 0 && kSteps % 2 == 0 && kTa % 4 == 0 && kTb % 4 == 0, "");
 };
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 __device__ __forceinline__ int wg_swz(int token) { return (token & 3) ^ ((token & 1) << 2); }
 
@@ -80,146 +86,141 @@ __device__ __forceinline__ uint32_t wg_pack(float x, float y) {
   return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
 }
 
+// The share of a thread in staging: kUa units of 16 codes and kUb units of 8
+// gradients, each kind in one column range at tokens kTa and kTb apart.
 template <typename S, int T, int WM, int WN>
 struct WgradLoader {
   using L = WgradTile<S, T, WM, WN>;
-  static constexpr int kTa = L::kThr / (T / 16), kTb = L::kThr / (T / 8);  // tokens between a thread's units
+  static constexpr int kV = sizeof(S) / 2;  // 16-byte loads of a gradient unit
   const char* pa;
   const uint8_t* ps;
   const S* pb;
-  int nb;  // columns of the thread's units inside G
+  int la, lb;  // LDS offsets of the first units
   u32x4 a[L::kUa];
   uint32_t sc[L::kUa];
-  uint32_t b[L::kUb][sizeof(S) == 2 ? 4 : 8];
+  u32x4u b[L::kUb][kV];
 
-  // A thread's units lie in the same columns: 16 codes, 8 gradient columns.
-  static __device__ __forceinline__ void unit_a(int tid, int u, int& token, int& piece) {
-    token = tid / (T / 16) + u * kTa;
-    piece = tid % (T / 16);
-  }
-  static __device__ __forceinline__ void unit_b(int tid, int u, int& token, int& c8) {
-    token = tid / (T / 8) + u * kTb;
-    c8 = tid % (T / 8);
-  }
-
-  __device__ __forceinline__ void init(const WgradArgs& q, int64_t k0, int m0, int n0, int tid) {
-    int token, piece;
-    unit_a(tid, 0, token, piece);
-    // columns past the codes only feed rows of G that are not stored: any codes do
-    int64_t m = m0 + piece * 16;
+  __device__ __forceinline__ void init(const WgradArgs& q, int m0, int n0, int tid) {
+    const int ta = tid / (T / 16), piece = tid % (T / 16);
+    la = ta * L::kRowB + (piece ^ wg_swz(ta)) * 32;
+    const int tb = tid / (T / 8), c8 = tid % (T / 8);
+    lb = L::kPlaneB + tb * L::kRowB + ((c8 >> 1) ^ wg_swz(tb)) * 32 + (c8 & 1) * 16;
+    // codes past a row's end and gradients past `out` only feed elements of G
+    // that are not stored: any column does, and a unit may run into the next row
+    int m = m0 + piece * 16, n = n0 + c8 * 8;
     if (m >= q.ldq) m = 0;
-    pa = q.codes + (k0 + token) * q.ldq + m;
-    ps = q.scales + (k0 + token) * (q.ldq / kActGroup) + m / kActGroup;
-    unit_b(tid, 0, token, piece);
-    const int n = n0 + piece * 8;
-    nb = min(8, max(0, q.out - n));
-    pb = static_cast<const S*>(q.dY) + (k0 + token) * q.ld_dy + n;
+    if (n >= q.out) n = 0;
+    pa = q.codes + ta * q.ldq + m;
+    ps = q.scales + ta * (q.ldq / kActGroup) + m / kActGroup;
+    pb = static_cast<const S*>(q.dY) + tb * q.ld_dy + n;
   }
 
-  // Stage of tokens k0..; tokens at or past k_end are zeros.
-  __device__ __forceinline__ void load(const WgradArgs& q, int64_t k0, int64_t k_end, int tid) {
-    const int64_t left = k_end - k0;
-    const bool full = left >= L::kBk;
+  __device__ __forceinline__ void load_a(const WgradArgs& q, int64_t k0, int u) {
+    a[u] = gload<u32x4>(pa + (k0 + u * L::kTa) * q.ldq);
+    sc[u] = gload<uint8_t>(ps + (k0 + u * L::kTa) * (q.ldq / kActGroup));
+  }
+  __device__ __forceinline__ void load_b(const WgradArgs& q, int64_t k0, int u) {
 #pragma unroll
-    for (int u = 0; u < L::kUa; ++u) {
-      int token, piece;
-      unit_a(tid, u, token, piece);
-      if (full || token < left) {
-        a[u] = gload<u32x4>(pa + u * kTa * q.ldq);
-        sc[u] = gload<uint8_t>(ps + u * kTa * (q.ldq / kActGroup));
+    for (int h = 0; h < kV; ++h) b[u][h] = gload<u32x4u>(pb + (k0 + u * L::kTb) * q.ld_dy + 4 * h);
+  }
+
+  __device__ __forceinline__ void store_a(lds_char* stage, int u) {
+    const float s = act_scale(sc[u]);
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t x = a[u][i / 2] >> (16 * (i & 1));
+      w[i] = wg_pack((float)(int8_t)(x & 0xff) * s, (float)(int8_t)((x >> 8) & 0xff) * s);
+    }
+    lds_u32x4* d = (lds_u32x4*)(stage + la + u * L::kTa * L::kRowB);
+    d[0] = u32x4{w[0], w[1], w[2], w[3]};
+    d[1] = u32x4{w[4], w[5], w[6], w[7]};
+  }
+
+  // One unit of gradients, in its terms.
+  static __device__ __forceinline__ void put_b(lds_char* d, const u32x4u (&v)[kV]) {
+    if constexpr (sizeof(S) == 2) {
+      *(lds_u32x4*)d = u32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
+    } else {
+      uint32_t p[3][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[3][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // a NaN is made quiet, so that its upper half is one too
+          const float y = __builtin_canonicalizef(__uint_as_float(v[i / 2][2 * (i % 2) + h]));
+          x[0][h] = y;
+          // infinities and NaN are the first term alone
+          const float r = finite_f32(y) ? y - __uint_as_float(__float_as_uint(y) & 0xffff0000u) : 0.f;
+          x[1][h] = r;
+          x[2][h] = r - __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t) p[t][i] = wg_pack(x[t][0], x[t][1]);
+      }
+#pragma unroll
+      for (int t = 0; t < 3; ++t) *(lds_u32x4*)(d + t * L::kPlaneB) = u32x4{p[t][0], p[t][1], p[t][2], p[t][3]};
+    }
+  }
+  __device__ __forceinline__ void store_b(lds_char* stage, int u) {
+    put_b(stage + lb + u * L::kTb * L::kRowB, b[u]);
+  }
+
+  // Part g of `parts` of the stage in the registers: to LDS, and (LOAD) the
+  // same units of the stage at token k0 into their place.
+  template <bool LOAD>
+  __device__ __forceinline__ void pass_on(const WgradArgs& q, lds_char* stage, int64_t k0, int g, int parts) {
+    constexpr int kU = L::kUa + L::kUb;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      if (u * parts / kU != g) continue;
+      if (u < L::kUa) {
+        store_a(stage, u);
+        if (LOAD) load_a(q, k0, u);
       } else {
-        a[u] = u32x4{0, 0, 0, 0};
-        sc[u] = 0;
+        store_b(stage, u - L::kUa);
+        if (LOAD) load_b(q, k0, u - L::kUa);
       }
     }
-    pa += L::kBk * q.ldq;
-    ps += L::kBk * (q.ldq / kActGroup);
+  }
+
+  // A stage that reaches past the split's or the tensor's end, straight to LDS:
+  // tokens at or past k_end are zeros, columns at or past `out` zeros too.
+  __device__ __forceinline__ void tail(const WgradArgs& q, lds_char* stage, int64_t k0, int64_t k_end, int n0,
+                                       int tid) {
+    const int left = (int)(k_end - k0), ta = tid / (T / 16), tb = tid / (T / 8), n = n0 + tid % (T / 8) * 8;
 #pragma unroll
+    for (int u = 0; u < L::kUa; ++u) {
+      a[u] = u32x4{0, 0, 0, 0};
+      sc[u] = 0;
+      if (ta + u * L::kTa < left) load_a(q, k0, u);
+      store_a(stage, u);
+    }
+#pragma unroll 1
     for (int u = 0; u < L::kUb; ++u) {
-      int token, c8;
-      unit_b(tid, u, token, c8);
-      const int have = full || token < left ? nb : 0;
-      const S* p = pb + u * kTb * q.ld_dy;
-      if (have == 8) {
-        const u32x4u v = *(const __attribute__((address_space(1))) u32x4u*)(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[u][i] = v[i];
-        if constexpr (sizeof(S) == 4) {
-          const u32x4u w = *(const __attribute__((address_space(1))) u32x4u*)(p + 4);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) b[u][4 + i] = w[i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if constexpr (sizeof(S) == 4) {
-            b[u][i] = i < have ? gload<uint32_t>(p + i) : 0u;
-          } else {
-            const uint32_t v = i < have ? (uint32_t)gload<uint16_t>(p + i) : 0u;
-            b[u][i / 2] = i & 1 ? b[u][i / 2] | v << 16 : v;
-          }
-        }
-      }
-    }
-    pb += L::kBk * q.ld_dy;
-  }
-
-  __device__ __forceinline__ void store(char* stage, int tid) {
-#pragma unroll
-    for (int u = 0; u < L::kUa; ++u) {
-      int token, piece;
-      unit_a(tid, u, token, piece);
-      const float s = act_scale(sc[u]);
-      uint32_t w[8];
+      const int have = tb + u * L::kTb < left ? q.out - n : 0;
+      const S* p = pb + (k0 + u * L::kTb) * q.ld_dy;
+      u32x4u v[kV];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t x = a[u][i / 2] >> (16 * (i & 1));
-        w[i] = wg_pack((float)(int8_t)(x & 0xff) * s, (float)(int8_t)((x >> 8) & 0xff) * s);
-      }
-      u32x4* d = reinterpret_cast<u32x4*>(stage + token * L::kRowB + (piece ^ wg_swz(token)) * 32);
-      d[0] = u32x4{w[0], w[1], w[2], w[3]};
-      d[1] = u32x4{w[4], w[5], w[6], w[7]};
-    }
-    char* sb = stage + L::kPlaneB;
-#pragma unroll
-    for (int u = 0; u < L::kUb; ++u) {
-      int token, c8;
-      unit_b(tid, u, token, c8);
-      char* d = sb + token * L::kRowB + ((c8 >> 1) ^ wg_swz(token)) * 32 + (c8 & 1) * 16;
-      if constexpr (sizeof(S) == 2) {
-        *reinterpret_cast<u32x4*>(d) = u32x4{b[u][0], b[u][1], b[u][2], b[u][3]};
-      } else {
-        uint32_t p[3][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x[3][2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // a NaN is made quiet, so that its upper half is one too
-            const float y = __builtin_canonicalizef(__uint_as_float(b[u][2 * i + h]));
-            x[0][h] = y;
-            // infinities and NaN are the first term alone
-            const float r = finite_f32(y) ? y - __uint_as_float(__float_as_uint(y) & 0xffff0000u) : 0.f;
-            x[1][h] = r;
-            x[2][h] = r - __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-          }
-#pragma unroll
-          for (int t = 0; t < 3; ++t) p[t][i] = wg_pack(x[t][0], x[t][1]);
+        if constexpr (sizeof(S) == 4) {
+          v[i / 4][i % 4] = i < have ? gload<uint32_t>(p + i) : 0u;
+        } else {
+          const uint32_t w = i < have ? (uint32_t)gload<uint16_t>(p + i) : 0u;
+          v[0][i / 2] = i & 1 ? v[0][i / 2] | w << 16 : w;
         }
-#pragma unroll
-        for (int t = 0; t < 3; ++t)
-          *reinterpret_cast<u32x4*>(d + t * L::kPlaneB) = u32x4{p[t][0], p[t][1], p[t][2], p[t][3]};
       }
+      put_b(stage + lb + u * L::kTb * L::kRowB, v);
     }
   }
 };
 
-typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-
 // The 8 tokens of a lane: two transposing reads, 4 rows apart.
-__device__ __forceinline__ bf16x8 wg_frag(const char* p, int row_b) {
+template <int ROW_B>
+__device__ __forceinline__ bf16x8 wg_frag(lds_char* p) {
   const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
-  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 4 * row_b));
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 4 * ROW_B));
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -239,7 +240,8 @@ __device__ __forceinline__ void wg_store4(const WgradArgs& q, int m, int n, f32x
 template <typename S, typename SG, int T, int WM, int WN>
 __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_grad_kernel(WgradArgs q) {
   using L = WgradTile<S, T, WM, WN>;
-  extern __shared__ __align__(16) char lds[];
+  extern __shared__ __align__(16) char lds_bytes[];
+  lds_char* lds = (lds_char*)lds_bytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tiles = q.tiles_m * q.tiles_n;
   const int l = xcd_remap(blockIdx.x, gridDim.x);
@@ -247,15 +249,18 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
   const int tm = t % q.tiles_m, tn = t / q.tiles_m;
   const int m0 = tm * T, n0 = tn * T;
   const int64_t kb = split * q.per_split, ke = min(q.rows, kb + q.per_split);
+  // Stages from the front that lie whole in the split and whose units of
+  // gradients are all readable: where a row's last unit runs past `out`, it
+  // must not be the tensor's last row (last 8 rows when rows are closer than
+  // a unit).  The one or two others go first.
+  const int64_t safe = q.out % 8 == 0 ? q.rows : q.rows - (q.ld_dy >= 8 ? 1 : 8);
   const int stages = (int)((ke - kb + L::kBk - 1) / L::kBk);
+  const int plain = max(0, (int)((min(ke, safe) - kb) / L::kBk));
 
   WgradLoader<S, T, WM, WN> ld;
-  ld.init(q, kb, m0, n0, tid);
-  ld.load(q, kb, ke, tid);
-  ld.store(lds, tid);
-  if (stages > 1) ld.load(q, kb + L::kBk, ke, tid);
+  ld.init(q, m0, n0, tid);
 
-  // fragment addresses: 16-lane group g reads columns 16 (g & 1).., tokens 8 (g >> 1)..
+  // fragment offsets: 16-lane group g reads columns 16 (g & 1).., tokens 8 (g >> 1)..
   const int wm = wave / L::kWavesN * WM, wn = wave % L::kWavesN * WN;
   const int token = (lane >> 5) * 8 + ((lane >> 2) & 3), side = (lane >> 4) & 1;
   int oa[L::kBm], ob[L::kBn];
@@ -274,44 +279,92 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  bf16x8 fa[2][L::kBm], fb[2][L::kTerms][L::kBn];
-  auto read = [&](const char* stage, int step, int set) {
-#pragma unroll
-    for (int i = 0; i < L::kBm; ++i) fa[set][i] = wg_frag(stage + oa[i] + step * 16 * L::kRowB, L::kRowB);
+  bf16x8 fa[L::kBm], fb[2][L::kTerms][L::kBn];
+  auto read_a = [&](lds_char* stage, int step, int i) { fa[i] = wg_frag<L::kRowB>(stage + oa[i] + step * 16 * L::kRowB); };
+  auto read_b = [&](lds_char* stage, int step, int set) {
 #pragma unroll
     for (int p = 0; p < L::kTerms; ++p)
 #pragma unroll
       for (int j = 0; j < L::kBn; ++j)
-        fb[set][p][j] = wg_frag(stage + ob[j] + p * L::kPlaneB + step * 16 * L::kRowB, L::kRowB);
+        fb[set][p][j] = wg_frag<L::kRowB>(stage + ob[j] + p * L::kPlaneB + step * 16 * L::kRowB);
   };
-  auto multiply = [&](int set) {
+  auto read_first = [&](lds_char* stage) {
+    read_b(stage, 0, 0);
 #pragma unroll
-    for (int p = L::kTerms - 1; p >= 0; --p)  // the smallest terms first
-#pragma unroll
-      for (int j = 0; j < L::kBn; ++j)
-#pragma unroll
-        for (int i = 0; i < L::kBm; ++i)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[set][i], fb[set][p][j], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < L::kBm; ++i) read_a(stage, 0, i);
   };
 
-  __syncthreads();
-  read(lds, 0, 0);
-  for (int s = 0; s < stages; ++s) {
-    const char* cur = lds + (s & 1) * L::kStageB;
-    char* nxt = lds + ((s + 1) & 1) * L::kStageB;
-    if (s + 1 < stages) ld.store(nxt, tid);
-    if (s + 2 < stages) ld.load(q, kb + (int64_t)(s + 2) * L::kBk, ke, tid);
+  // The products of one staged stage.  STORE: the stage in the registers is
+  // written to the other buffer beside the products of all steps but the last,
+  // and the last step reads the first fragments of it; LOAD: the registers are
+  // filled with the stage at token k0.  A row block's fragment is read again as
+  // soon as its products are issued; the scheduler may move the conversion
+  // between products, but not the reads (left free it reads a whole stage's
+  // fragments first and spills).
+  auto stage = [&](lds_char* cur, int64_t k0, auto store, auto load) {
+    lds_char* nxt = lds + ((int)(cur - lds) ^ L::kStageB);
 #pragma unroll
     for (int step = 0; step < L::kSteps; ++step) {
-      if (step + 1 < L::kSteps) {
-        read(cur, step + 1, (step + 1) & 1);
-      } else if (s + 1 < stages) {
-        __syncthreads();
-        read(nxt, 0, 0);
+      const bool last = step == L::kSteps - 1;
+      if (last && decltype(store)::value) __syncthreads();
+      if (!last) read_b(cur, step + 1, (step + 1) & 1);
+      else if (decltype(store)::value) read_b(nxt, 0, 0);
+#pragma unroll
+      for (int i = 0; i < L::kBm; ++i) {
+#pragma unroll
+        for (int p = L::kTerms - 1; p >= 0; --p)  // the smallest terms first
+#pragma unroll
+          for (int j = 0; j < L::kBn; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[step & 1][p][j], acc[i][j], 0, 0, 0);
+        if (!last) read_a(cur, step + 1, i);
+        else if (decltype(store)::value) read_a(nxt, 0, i);
+        if (!last && decltype(store)::value)
+          ld.template pass_on<decltype(load)::value>(q, nxt, k0, step * L::kBm + i, (L::kSteps - 1) * L::kBm);
+        __builtin_amdgcn_sched_barrier(0x206);
       }
-      multiply(step & 1);
     }
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+
+  lds_char* cur = lds;
+  auto flip = [&] { cur = lds + ((int)(cur - lds) ^ L::kStageB); };
+  int next = 0;  // the plain stage that goes to the registers next
+  for (int s = stages - 1; s >= plain; --s) {
+    if (s < stages - 1) {
+      __syncthreads();
+      read_first(cur);
+      stage(cur, 0, no, no);
+      flip();
+    }
+    ld.tail(q, cur, kb + (int64_t)s * L::kBk, ke, n0, tid);
   }
+  auto fill = [&](int64_t k0) {
+#pragma unroll
+    for (int u = 0; u < L::kUa; ++u) ld.load_a(q, k0, u);
+#pragma unroll
+    for (int u = 0; u < L::kUb; ++u) ld.load_b(q, k0, u);
+  };
+  if (stages == plain) {
+    fill(kb);
+#pragma unroll
+    for (int u = 0; u < L::kUa; ++u) ld.store_a(cur, u);
+#pragma unroll
+    for (int u = 0; u < L::kUb; ++u) ld.store_b(cur, u);
+    next = 1;
+  }
+  if (next < plain) fill(kb + (int64_t)next * L::kBk);
+  __syncthreads();
+  read_first(cur);
+  for (; next + 1 < plain; ++next) {
+    stage(cur, kb + (int64_t)(next + 1) * L::kBk, yes, yes);
+    flip();
+  }
+  if (next < plain) {
+    stage(cur, 0, yes, no);
+    flip();
+  }
+  stage(cur, 0, no, no);
 
   if (q.part) {
     // partial tiles in accumulator order: 16 bytes a lane
