@@ -690,42 +690,96 @@ def shampoo_graft_lamb(handle, blocks, eta0, beta1=0.0, use_shampoo=True, norms=
 
 
 # ------------------------------------------------------------------ from the loss to the gradient
-def _check_matrix(t, what, shape=None, dtype=None):
-    """(rows, cols, row stride, dtype code) of an fp32 or bf16 matrix whose columns are adjacent."""
+# Each call first looks its tensors over with cheap accessors; only where
+# something is off does the detailed check run, to raise with the reason.
+def _layout(t):
+    """(rows, cols, row stride, dtype code, device, pointer) of an fp32 or bf16
+    matrix of adjacent columns, or None.  One row, or none, uses no stride; rows
+    that overlap (an expanded view) are no layout the library takes."""
+    dt = t.dtype
+    torch = _torch_mod or _torch()
+    code = SHAMPOO_F32 if dt is torch.float32 else SHAMPOO_BF16 if dt is torch.bfloat16 else -1
+    if code < 0 or t.dim() != 2:
+        return None
+    m, n = t.shape
+    ld, sc = t.stride()
+    if m <= 1:
+        ld = n
+    if ld < n or (sc != 1 and n > 1):
+        return None
+    return m, n, ld, code, t.get_device(), t.data_ptr()
+
+
+def _plain(t, dtype, shape, dev):
+    """A contiguous tensor of this type, shape and device, or None given."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev)
+
+
+def _room(t, nbytes, dev):
+    """A contiguous uint8 buffer of at least nbytes on dev (None where none are needed)."""
+    if t is None:
+        return nbytes == 0
+    return (t.dtype is _torch_mod.uint8 and t.numel() >= nbytes and t.is_contiguous() and t.get_device() == dev)
+
+
+def _apart(a, b):
+    """Whether two matrices (as from _layout) share no memory."""
+    if a[0] == 0 or b[0] == 0 or a[1] == 0 or b[1] == 0:
+        return True
+    a_end = a[5] + ((a[0] - 1) * a[2] + a[1]) * (4 - 2 * a[3])
+    b_end = b[5] + ((b[0] - 1) * b[2] + b[1]) * (4 - 2 * b[3])
+    return a_end <= b[5] or b_end <= a[5]
+
+
+def _alike(out, src):
+    """out has src's shape, type and device, and is src itself or apart from it."""
+    return (out is not None and out[0] == src[0] and out[1] == src[1] and out[3] == src[3] and out[4] == src[4] and
+            ((out[5] == src[5] and out[2] == src[2]) or _apart(out, src)))
+
+
+def _on_handle(handle, dev):
+    """dev is a GPU, the handle's where that is known."""
+    return dev >= 0 and _handle_device.get(handle.value if handle is not None else None, dev) == dev
+
+
+def _stream_on(stream, dev):
+    """The stream of a call: the one given, else the current one of dev."""
+    if stream is not None:
+        return stream if isinstance(stream, int) else stream.cuda_stream
+    return _torch_mod._C._cuda_getCurrentRawStream(dev)
+
+
+def _refuse(handle, tensors, checks):
+    """Runs the detailed checks, each of which raises with its reason, then the device check."""
+    for check in checks:
+        check()
+    _devices(handle, tensors)
+    raise ValueError("tensors of one call must all be on one GPU, the handle's")
+
+
+def _check_matrix(t, what, like=None):
     torch = _torch()
     dt = t.dtype
     _need(t.dim() == 2, f"{what}: {t.dim()} dimensions, expected 2")
     _need(dt is torch.float32 or dt is torch.bfloat16, f"{what}: dtype {dt}, expected float32 or bfloat16")
-    _need(dtype is None or dt is dtype, f"{what}: dtype {dt}, expected {dtype}")
     m, n = t.shape
-    _need(shape is None or (m, n) == shape, f"{what}: shape {(m, n)}, expected {shape}")
+    if like is not None:
+        _need(dt is like.dtype, f"{what}: dtype {dt}, expected {like.dtype}")
+        _need(t.shape == like.shape, f"{what}: shape {(m, n)}, expected {tuple(like.shape)}")
     ld, sc = t.stride()
     _need(n <= 1 or sc == 1, f"{what}: columns must be adjacent (stride(1) == 1)")
-    # one row, or none, uses no stride; rows that overlap (an expanded view)
-    # are no layout the library takes
-    if m <= 1:
-        ld = n
-    _need(ld >= n, f"{what}: row stride {ld} < {n} columns")
-    return m, n, ld, SHAMPOO_F32 if dt is torch.float32 else SHAMPOO_BF16
+    _need(m <= 1 or ld >= n, f"{what}: row stride {ld} < {n} columns")
 
 
-def _check_rows(t, rows, what, kind="float32"):
-    """A contiguous vector of `rows` elements, or None."""
+def _check_shape(t, shape, what, kind="float32"):
     if t is None:
         return
     (_int32 if kind == "int32" else _fp32)(t, what)
-    _need(tuple(t.shape) == (rows,), f"{what}: shape {tuple(t.shape)}, expected ({rows},)")
-    _contig(t, what)
-
-
-def _check_top(t, rows, k, what, kind="float32"):
-    (_int32 if kind == "int32" else _fp32)(t, what)
-    _need(tuple(t.shape) == (rows, k), f"{what}: shape {tuple(t.shape)}, expected ({rows}, {k})")
+    _need(tuple(t.shape) == shape, f"{what}: shape {tuple(t.shape)}, expected {shape}")
     _contig(t, what)
 
 
 def _check_bytes(t, nbytes, what):
-    """A contiguous uint8 buffer of at least nbytes (None where none are needed)."""
     if t is None:
         _need(nbytes == 0, f"{what}: {nbytes} bytes needed, got None")
         return
@@ -734,24 +788,10 @@ def _check_bytes(t, nbytes, what):
     _min_numel(t, nbytes, what)
 
 
-def _overlap(a, b):
-    """Whether the memory ranges of two tensors meet."""
-    if a is None or b is None or a.numel() == 0 or b.numel() == 0:
-        return False
-
-    def span(t):
-        size = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1
-        return t.data_ptr(), t.data_ptr() + size * t.element_size()
-    a0, a1 = span(a)
-    b0, b1 = span(b)
-    return a0 < b1 and b0 < a1
-
-
-def _in_place(out, src, what):
-    """out is src itself (same view) or shares no memory with it."""
-    _need(not _overlap(out, src) or (out.data_ptr() == src.data_ptr() and
-                                     (out.shape[0] <= 1 or out.stride(0) == src.stride(0))),
-          f"{what} overlap without being the same view")
+def _check_apart(a, b, what, same_allowed):
+    x, y = _layout(a), _layout(b)
+    _need(_apart(x, y) or (same_allowed and x[5] == y[5] and x[2] == y[2]),
+          f"{what} overlap" + (" without being the same view" if same_allowed else ""))
 
 
 def shampoo_token_logprobs_workspace_bytes(rows, vocab, k=0):
@@ -762,27 +802,46 @@ def shampoo_token_logprobs(handle, logits, targets, logp, lse, entropy=None, top
                            workspace=None, stream=None):
     """logits: rows x vocab, fp32 or bf16 (row-major view); targets int32 [rows]
     and logp fp32 [rows] (both or neither); lse, entropy: fp32 [rows]; top_ids
-    int32 and top_logp fp32, rows x k, for the k largest alternatives."""
-    rows, vocab, ld, dt = _check_matrix(logits, "logits")
+    int32 and top_logp fp32, rows x k, for the k largest alternatives; workspace:
+    uint8, shampoo_token_logprobs_workspace_bytes(rows, vocab, k)."""
+    z = _layout(logits)
+    ok = z is not None and lse is not None and (targets is None) == (logp is None) and (
+        top_ids is None) == (top_logp is None)
+    if ok:
+        rows, vocab, ld, dt, dev, ptr = z
+        f32, i32 = _torch_mod.float32, _torch_mod.int32
+        k = top_ids.shape[-1] if top_ids is not None and top_ids.dim() == 2 else 0
+        vec = (rows,)
+        ok = (_plain(lse, f32, vec, dev) and _plain(targets, i32, vec, dev) and _plain(logp, f32, vec, dev) and
+              _plain(entropy, f32, vec, dev) and _plain(top_ids, i32, (rows, k), dev) and
+              _plain(top_logp, f32, (rows, k), dev) and _on_handle(handle, dev) and
+              _room(workspace, _lib.shampoo_token_logprobs_workspace_bytes(rows, vocab, k), dev))
+    if not ok:
+        _refuse_logprobs(handle, logits, targets, logp, lse, entropy, top_ids, top_logp, workspace)
+    _check(handle, _lib.shampoo_token_logprobs(handle, ptr, dt, rows, vocab, ld, _ptr(targets), _ptr(logp),
+                                               lse.data_ptr(), _ptr(entropy), k, _ptr(top_ids), _ptr(top_logp),
+                                               _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                               _stream_on(stream, dev)))
+
+
+def _refuse_logprobs(handle, logits, targets, logp, lse, entropy, top_ids, top_logp, workspace):
+    _check_matrix(logits, "logits")
+    rows, vocab = logits.shape
     _need((targets is None) == (logp is None), "targets and logp go together")
     _need((top_ids is None) == (top_logp is None), "top_ids and top_logp go together")
-    _check_rows(targets, rows, "targets", "int32")
-    _check_rows(logp, rows, "logp")
     _need(lse is not None, "lse is required")
-    _check_rows(lse, rows, "lse")
-    _check_rows(entropy, rows, "entropy")
     k = 0
     if top_ids is not None:
         _need(top_ids.dim() == 2, f"top_ids: {top_ids.dim()} dimensions, expected 2")
         k = int(top_ids.shape[1])
-        _check_top(top_ids, rows, k, "top_ids", "int32")
-        _check_top(top_logp, rows, k, "top_logp")
-    _check_bytes(workspace, _lib.shampoo_token_logprobs_workspace_bytes(rows, vocab, k), "workspace")
-    _devices(handle, (("logits", logits), ("targets", targets), ("logp", logp), ("lse", lse), ("entropy", entropy),
-                      ("top_ids", top_ids), ("top_logp", top_logp), ("workspace", workspace)))
-    _check(handle, _lib.shampoo_token_logprobs(handle, _ptr(logits), dt, rows, vocab, ld, _ptr(targets), _ptr(logp),
-                                               _ptr(lse), _ptr(entropy), k, _ptr(top_ids), _ptr(top_logp),
-                                               _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    _refuse(handle, (("logits", logits), ("targets", targets), ("logp", logp), ("lse", lse), ("entropy", entropy),
+                     ("top_ids", top_ids), ("top_logp", top_logp), ("workspace", workspace)),
+            (lambda: _check_shape(targets, (rows,), "targets", "int32"), lambda: _check_shape(logp, (rows,), "logp"),
+             lambda: _check_shape(lse, (rows,), "lse"), lambda: _check_shape(entropy, (rows,), "entropy"),
+             lambda: _check_shape(top_ids, (rows, k), "top_ids", "int32"),
+             lambda: _check_shape(top_logp, (rows, k), "top_logp"),
+             lambda: _check_bytes(workspace, _lib.shampoo_token_logprobs_workspace_bytes(rows, vocab, k),
+                                  "workspace")))
 
 
 def shampoo_token_logprobs_grad(handle, logits, targets, lse, dlogits, g_logp=None, g_lse=None, entropy=None,
@@ -790,31 +849,47 @@ def shampoo_token_logprobs_grad(handle, logits, targets, lse, dlogits, g_logp=No
     """dlogits (logits' shape and type; may be logits) from the gradients of
     shampoo_token_logprobs' outputs: g_logp (with targets), g_lse, g_entropy
     (with entropy): fp32 [rows]; g_top (with top_ids): fp32 rows x k."""
-    rows, vocab, ld, dt = _check_matrix(logits, "logits")
-    _, _, ld_d, _ = _check_matrix(dlogits, "dlogits", (rows, vocab), logits.dtype)
-    _in_place(dlogits, logits, "dlogits and logits")
+    z, d = _layout(logits), _layout(dlogits)
+    ok = (z is not None and _alike(d, z) and lse is not None and (g_logp is None or targets is not None) and
+          (g_entropy is None or entropy is not None) and (g_top is None or top_ids is not None))
+    if ok:
+        rows, vocab, ld, dt, dev, ptr = z
+        f32, i32 = _torch_mod.float32, _torch_mod.int32
+        k = top_ids.shape[-1] if top_ids is not None and top_ids.dim() == 2 else 0
+        vec = (rows,)
+        ok = (_plain(lse, f32, vec, dev) and _plain(targets, i32, vec, dev) and _plain(g_logp, f32, vec, dev) and
+              _plain(g_lse, f32, vec, dev) and _plain(entropy, f32, vec, dev) and _plain(g_entropy, f32, vec, dev) and
+              _plain(top_ids, i32, (rows, k), dev) and _plain(g_top, f32, (rows, k), dev) and
+              _on_handle(handle, dev))
+    if not ok:
+        _refuse_logprobs_grad(handle, logits, targets, lse, dlogits, g_logp, g_lse, entropy, g_entropy, top_ids, g_top)
+    _check(handle, _lib.shampoo_token_logprobs_grad(handle, ptr, dt, rows, vocab, ld, _ptr(targets), lse.data_ptr(),
+                                                    _ptr(entropy), k, _ptr(top_ids), _ptr(g_logp), _ptr(g_lse),
+                                                    _ptr(g_entropy), _ptr(g_top), d[5], d[2],
+                                                    _stream_on(stream, dev)))
+
+
+def _refuse_logprobs_grad(handle, logits, targets, lse, dlogits, g_logp, g_lse, entropy, g_entropy, top_ids, g_top):
+    _check_matrix(logits, "logits")
+    rows = logits.shape[0]
+    _check_matrix(dlogits, "dlogits", logits)
+    _check_apart(dlogits, logits, "dlogits and logits", True)
     _need(g_logp is None or targets is not None, "g_logp needs targets")
     _need(g_entropy is None or entropy is not None, "g_entropy needs entropy")
     _need(g_top is None or top_ids is not None, "g_top needs top_ids")
     _need(lse is not None, "lse is required")
-    _check_rows(targets, rows, "targets", "int32")
-    for what, t in (("lse", lse), ("g_logp", g_logp), ("g_lse", g_lse), ("entropy", entropy),
-                    ("g_entropy", g_entropy)):
-        _check_rows(t, rows, what)
     k = 0
     if top_ids is not None:
         _need(top_ids.dim() == 2, f"top_ids: {top_ids.dim()} dimensions, expected 2")
         k = int(top_ids.shape[1])
-        _check_top(top_ids, rows, k, "top_ids", "int32")
-        if g_top is not None:
-            _check_top(g_top, rows, k, "g_top")
-    _devices(handle, (("logits", logits), ("dlogits", dlogits), ("targets", targets), ("lse", lse),
-                      ("g_logp", g_logp), ("g_lse", g_lse), ("entropy", entropy), ("g_entropy", g_entropy),
-                      ("top_ids", top_ids), ("g_top", g_top)))
-    _check(handle, _lib.shampoo_token_logprobs_grad(handle, _ptr(logits), dt, rows, vocab, ld, _ptr(targets),
-                                                    _ptr(lse), _ptr(entropy), k, _ptr(top_ids), _ptr(g_logp),
-                                                    _ptr(g_lse), _ptr(g_entropy), _ptr(g_top), _ptr(dlogits), ld_d,
-                                                    _stream(stream)))
+    rest = (("lse", lse), ("g_logp", g_logp), ("g_lse", g_lse), ("entropy", entropy), ("g_entropy", g_entropy))
+    for what, t in rest:
+        _check_shape(t, (rows,), what)
+    _refuse(handle, (("logits", logits), ("dlogits", dlogits), ("targets", targets), ("top_ids", top_ids),
+                     ("g_top", g_top)) + rest,
+            (lambda: _check_shape(targets, (rows,), "targets", "int32"),
+             lambda: _check_shape(top_ids, (rows, k), "top_ids", "int32"),
+             lambda: _check_shape(g_top, (rows, k), "g_top")))
 
 
 def shampoo_act_checkpoint_bytes(rows, cols):
@@ -830,37 +905,50 @@ def shampoo_act_encode(handle, X, ckpt_x=None, act=ACT_NONE, Y=None, ckpt_y=None
     """X: rows x cols, fp32 or bf16 (row-major view); Y = act(X): X's shape and
     type (may be X), or None; ckpt_x, ckpt_y: uint8 tensors of
     shampoo_act_checkpoint_bytes(rows, cols), or None."""
-    rows, cols, ld, dt = _check_matrix(X, "X")
-    ld_y = 0
-    if Y is not None:
-        _, _, ld_y, _ = _check_matrix(Y, "Y", (rows, cols), X.dtype)
-        _in_place(Y, X, "Y and X")
-    _check_ckpt(ckpt_x, rows, cols, "ckpt_x")
-    _check_ckpt(ckpt_y, rows, cols, "ckpt_y")
-    _devices(handle, (("X", X), ("Y", Y), ("ckpt_x", ckpt_x), ("ckpt_y", ckpt_y)))
-    _check(handle, _lib.shampoo_act_encode(handle, _ptr(X), dt, rows, cols, ld, int(act), _ptr(Y), ld_y,
-                                           _ptr(ckpt_x), _ptr(ckpt_y), _stream(stream)))
+    x, y = _layout(X), None if Y is None else _layout(Y)
+    ok = x is not None and (Y is None or _alike(y, x))
+    if ok:
+        rows, cols, ld, dt, dev, ptr = x
+        need = _lib.shampoo_act_checkpoint_bytes(rows, cols)
+        ok = ((ckpt_x is None or _room(ckpt_x, need, dev)) and (ckpt_y is None or _room(ckpt_y, need, dev)) and
+              _on_handle(handle, dev))
+    if not ok:
+        _check_matrix(X, "X")
+        if Y is not None:
+            _check_matrix(Y, "Y", X)
+            _check_apart(Y, X, "Y and X", True)
+        _refuse(handle, (("X", X), ("Y", Y), ("ckpt_x", ckpt_x), ("ckpt_y", ckpt_y)),
+                (lambda: _check_ckpt(ckpt_x, *X.shape, "ckpt_x"), lambda: _check_ckpt(ckpt_y, *X.shape, "ckpt_y")))
+    _check(handle, _lib.shampoo_act_encode(handle, ptr, dt, rows, cols, ld, int(act), None if y is None else y[5],
+                                           0 if y is None else y[2], _ptr(ckpt_x), _ptr(ckpt_y),
+                                           _stream_on(stream, dev)))
 
 
 def shampoo_act_decode(handle, ckpt, X, stream=None):
     """X: rows x cols, fp32 or bf16: the values that the checkpoint holds."""
-    rows, cols, ld, dt = _check_matrix(X, "X")
-    _need(ckpt is not None, "ckpt is required")
-    _check_ckpt(ckpt, rows, cols, "ckpt")
-    _devices(handle, (("ckpt", ckpt), ("X", X)))
-    _check(handle, _lib.shampoo_act_decode(handle, _ptr(ckpt), rows, cols, _ptr(X), dt, ld, _stream(stream)))
+    x = _layout(X)
+    if x is None or ckpt is None or not _on_handle(handle, x[4]) or not _room(
+            ckpt, _lib.shampoo_act_checkpoint_bytes(x[0], x[1]), x[4]):
+        _check_matrix(X, "X")
+        _need(ckpt is not None, "ckpt is required")
+        _refuse(handle, (("ckpt", ckpt), ("X", X)), (lambda: _check_ckpt(ckpt, *X.shape, "ckpt"),))
+    rows, cols, ld, dt, dev, ptr = x
+    _check(handle, _lib.shampoo_act_decode(handle, ckpt.data_ptr(), rows, cols, ptr, dt, ld, _stream_on(stream, dev)))
 
 
 def shampoo_act_grad(handle, ckpt, act, dY, dX, stream=None):
     """dX = dY o act'(x^), x^ the checkpoint's values; dX: dY's shape and type (may be dY)."""
-    rows, cols, ld_dy, dt = _check_matrix(dY, "dY")
-    _, _, ld_dx, _ = _check_matrix(dX, "dX", (rows, cols), dY.dtype)
-    _in_place(dX, dY, "dX and dY")
-    _need(ckpt is not None, "ckpt is required")
-    _check_ckpt(ckpt, rows, cols, "ckpt")
-    _devices(handle, (("ckpt", ckpt), ("dY", dY), ("dX", dX)))
-    _check(handle, _lib.shampoo_act_grad(handle, _ptr(ckpt), rows, cols, int(act), _ptr(dY), dt, ld_dy, _ptr(dX),
-                                         ld_dx, _stream(stream)))
+    y, x = _layout(dY), _layout(dX)
+    if y is None or not _alike(x, y) or ckpt is None or not _on_handle(handle, y[4]) or not _room(
+            ckpt, _lib.shampoo_act_checkpoint_bytes(y[0], y[1]), y[4]):
+        _check_matrix(dY, "dY")
+        _check_matrix(dX, "dX", dY)
+        _check_apart(dX, dY, "dX and dY", True)
+        _need(ckpt is not None, "ckpt is required")
+        _refuse(handle, (("ckpt", ckpt), ("dY", dY), ("dX", dX)), (lambda: _check_ckpt(ckpt, *dY.shape, "ckpt"),))
+    rows, cols, ld_dy, dt, dev, ptr = y
+    _check(handle, _lib.shampoo_act_grad(handle, ckpt.data_ptr(), rows, cols, int(act), ptr, dt, ld_dy, x[5], x[2],
+                                         _stream_on(stream, dev)))
 
 
 def shampoo_act_weight_grad_workspace_bytes(rows, cols, out):
@@ -869,18 +957,30 @@ def shampoo_act_weight_grad_workspace_bytes(rows, cols, out):
 
 def shampoo_act_weight_grad(handle, ckpt, dY, G, beta=0.0, workspace=None, stream=None):
     """G (cols x out) = beta G + X^^T dY, X^ the rows x cols values of the
-    checkpoint, dY rows x out; dY and G fp32 or bf16, each its own."""
-    cols, out, ld_g, g_dt = _check_matrix(G, "G")
-    rows, _, ld_dy, dt = _check_matrix(dY, "dY")
-    _need(int(dY.shape[1]) == out, f"dY: {int(dY.shape[1])} columns, G has {out}")
-    _need(ckpt is not None, "ckpt is required")
-    _check_ckpt(ckpt, rows, cols, "ckpt")
-    _need(not _overlap(G, dY), "G and dY overlap")
-    _check_bytes(workspace, _lib.shampoo_act_weight_grad_workspace_bytes(rows, cols, out), "workspace")
-    _devices(handle, (("ckpt", ckpt), ("dY", dY), ("G", G), ("workspace", workspace)))
-    _check(handle, _lib.shampoo_act_weight_grad(handle, _ptr(ckpt), rows, cols, _ptr(dY), dt, out, ld_dy, _ptr(G),
-                                                g_dt, ld_g, float(beta), _ptr(workspace), _nbytes(workspace),
-                                                _stream(stream)))
+    checkpoint, dY rows x out; dY and G fp32 or bf16, each its own; workspace:
+    uint8, shampoo_act_weight_grad_workspace_bytes(rows, cols, out)."""
+    y, g = _layout(dY), _layout(G)
+    ok = y is not None and g is not None and y[1] == g[1] and y[4] == g[4] and ckpt is not None and _apart(y, g)
+    if ok:
+        rows, out, ld_dy, dt, dev, ptr = y
+        cols = g[0]
+        ok = (_room(ckpt, _lib.shampoo_act_checkpoint_bytes(rows, cols), dev) and _on_handle(handle, dev) and
+              _room(workspace, _lib.shampoo_act_weight_grad_workspace_bytes(rows, cols, out), dev))
+    if not ok:
+        _check_matrix(G, "G")
+        _check_matrix(dY, "dY")
+        _need(dY.shape[1] == G.shape[1], f"dY: {int(dY.shape[1])} columns, G has {int(G.shape[1])}")
+        _need(ckpt is not None, "ckpt is required")
+        _check_apart(G, dY, "G and dY", False)
+        rows, cols, out = int(dY.shape[0]), int(G.shape[0]), int(G.shape[1])
+        _refuse(handle, (("ckpt", ckpt), ("dY", dY), ("G", G), ("workspace", workspace)),
+                (lambda: _check_ckpt(ckpt, rows, cols, "ckpt"),
+                 lambda: _check_bytes(workspace, _lib.shampoo_act_weight_grad_workspace_bytes(rows, cols, out),
+                                      "workspace")))
+    _check(handle, _lib.shampoo_act_weight_grad(handle, ckpt.data_ptr(), rows, cols, ptr, dt, out, ld_dy, g[5], g[3],
+                                                g[2], beta, _ptr(workspace),
+                                                0 if workspace is None else workspace.numel(),
+                                                _stream_on(stream, dev)))
 
 
 def shampoo_timing_enable(handle, enable=True):
