@@ -5,6 +5,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 #include <type_traits>
 
@@ -93,28 +94,68 @@ struct WgradPlan {
   size_t ws = 0;
 };
 
+// Estimated time (us) of `blocks` workgroups that work on a stage at a time:
+// full rounds of the chip, then the rest.  `alone` is a stage's time on a
+// lightly filled chip, `full` with every slot taken (clock and bandwidth then
+// are shared), measured over 12 shapes from 300 x 300 x 300 to 65536 x 1024 x
+// 4096; the estimate was within 15% wherever it matters.
+double wgrad_rounds(int64_t blocks, int64_t slots, double alone, double full) {
+  const int64_t rest = blocks % slots;
+  const double part = rest == 0           ? 0
+                      : 2 * rest <= slots ? alone
+                      : slots == 512      ? full  // some compute unit holds two
+                                          : alone + (full - alone) * (2 * rest - slots) / slots;
+  return (double)(blocks / slots) * full + part;
+}
+
+// The cheapest of 256 x 256 tiles (one workgroup per compute unit) and 128 x
+// 128 tiles (two) with the token axis in up to 128 parts.  Parts cost their
+// partial tiles' way to memory and back (0.2 us per MB) and a second launch:
+//   65536 x 1024 x 4096 (64 large tiles): 1 part 1318 us, 2 673, 4 470, 8 499;
+//     small tiles 632
+//   32768 x 512 x 512: large tiles in 48 parts 36 us; small in 16 34, in 32 33
+//   2048 x 1024 x 1024: large in 6 parts 28 us, small in 2 22
 WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
-  WgradPlan p;
-  const int64_t bk = dtype == SHAMPOO_BF16 ? 64 : 32;
-  const int64_t t256 = cdiv64(cols, 256) * cdiv64(out, 256);
-  p.tile = t256 >= 64 ? 256 : 128;
-  p.tiles_m = cdiv64(cols, p.tile);
-  p.tiles_n = cdiv64(out, p.tile);
-  const int64_t tiles = p.tiles_m * p.tiles_n, slots = p.tile == 256 ? 256 : 512;
-  const int64_t stages = std::max<int64_t>(1, cdiv64(rows, bk));
-  p.splits = (int)std::min(std::max<int64_t>(1, slots / tiles), cdiv64(stages, 4));
-  p.per_split = cdiv64(stages, p.splits) * bk;
-  p.splits = (int)std::max<int64_t>(1, cdiv64(rows, p.per_split));
-  if (p.splits > 1) p.ws = (size_t)(p.splits * tiles) * p.tile * p.tile * sizeof(float);
-  return p;
+  const bool bf16 = dtype == SHAMPOO_BF16;
+  const int64_t bk = bf16 ? 64 : 32, stages = std::max<int64_t>(1, cdiv64(rows, bk));
+  WgradPlan best;
+  double best_us = 0;
+  for (int tile : {128, 256}) {
+    const int64_t tm = cdiv64(cols, tile), tn = cdiv64(out, tile), tiles = tm * tn;
+    const int64_t slots = tile == 256 ? 256 : 512;
+    const double alone = tile == 256 ? (bf16 ? 1.28 : 2.1) : (bf16 ? 0.69 : 0.9);
+    const double full = tile == 256 ? (bf16 ? 1.79 : 2.7) : (bf16 ? 1.23 : 1.62);
+    for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
+      if (want > stages || (want > 1 && want * tiles > 2 * slots)) break;
+      const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
+      const size_t ws = splits > 1 ? (size_t)(splits * tiles) * tile * tile * sizeof(float) : 0;
+      const double us = wgrad_rounds(tiles * splits, slots, alone, full) * (double)per +
+                        (splits > 1 ? 5 + 0.2e-6 * (double)ws : 0);
+      if (best_us == 0 || us < best_us) {
+        best_us = us;
+        best.tile = tile;
+        best.splits = (int)splits;
+        best.per_split = per * bk;
+        best.tiles_m = tm;
+        best.tiles_n = tn;
+        best.ws = ws;
+      }
+    }
+  }
+  return best;
 }
 
 template <typename S, typename SG, int T, int WM, int WN>
 shampoo_status wgrad_launch(Handle* h, const WgradArgs& q, hipStream_t s) {
   using L = WgradTile<S, T, WM, WN>;
   auto k = weight_grad_kernel<S, SG, T, WM, WN>;
-  // more LDS than a launch may take by default
-  HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, L::kLdsB));
+  // more LDS than a launch may take by default: asked for once per device
+  static std::atomic<uint64_t> asked{0};
+  const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
+  if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
+    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, L::kLdsB));
+    asked.fetch_or(bit, std::memory_order_relaxed);
+  }
   const int64_t tiles = (int64_t)q.tiles_m * q.tiles_n;
   STATUS_TRY(launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
     hipLaunchKernelGGL(k, dim3((unsigned)(tiles * q.splits)), dim3(L::kThr), L::kLdsB, s, q);

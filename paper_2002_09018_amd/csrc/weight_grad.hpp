@@ -320,7 +320,7 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
         else if (decltype(store)::value) read_a(nxt, 0, i);
         if (!last && decltype(store)::value)
           ld.template pass_on<decltype(load)::value>(q, nxt, k0, step * L::kBm + i, (L::kSteps - 1) * L::kBm);
-        __builtin_amdgcn_sched_barrier(0x206);
+        __builtin_amdgcn_sched_barrier(0x2);
       }
     }
   };
