@@ -87,6 +87,30 @@ void with_type(int dtype, F&& f) {
   else f((uint16_t*)nullptr);
 }
 
+// How a row of logits is cut: waves of a workgroup to a row, and workgroups
+// (parts) of a row where there are few rows.
+struct LogprobPlan {
+  int waves = 1, parts = 1, per_part = 0;
+  size_t ws = 0;
+};
+
+LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int k, int dtype) {
+  LogprobPlan p;
+  const int64_t block = dtype == SHAMPOO_BF16 ? LogitBlock<uint16_t>::kN : LogitBlock<float>::kN;
+  p.waves = vocab <= 2 * block ? 1 : 4;
+  if (p.waves == 4) {
+    const int64_t steps = cdiv64(vocab, 4 * block);
+    const int64_t parts = std::min<int64_t>({cdiv64(2048, rows), steps, 64});
+    const int64_t per = cdiv64(steps, parts);
+    p.parts = (int)cdiv64(steps, per);
+    p.per_part = (int)std::min<int64_t>(per * 4 * block, vocab);
+  } else {
+    p.per_part = (int)vocab;
+  }
+  if (p.parts > 1) p.ws = (size_t)(rows * p.parts * logprob_record(k)) * sizeof(float);
+  return p;
+}
+
 // How a weight gradient is cut: the tile, and the splits of the token axis.
 struct WgradPlan {
   int tile = 256, splits = 1;
@@ -174,7 +198,10 @@ extern "C" {
 
 // ---------------------------------------------------------------- loss
 size_t shampoo_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int k) {
-  return 0;
+  if (rows < 1 || rows >= kMaxTokens || vocab < 1 || vocab > kMaxVocab || k < 0 || k > SHAMPOO_MAX_TOP) return 0;
+  size_t need = 0;
+  for (int dtype : {SHAMPOO_F32, SHAMPOO_BF16}) need = std::max(need, logprob_plan(rows, vocab, k, dtype).ws);
+  return need;
 }
 
 shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
@@ -189,13 +216,26 @@ shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtyp
     const size_t need = shampoo_token_logprobs_workspace_bytes(rows, vocab, k);
     if (need && (!workspace || ws_bytes < need))
       return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    if (!aligned16(workspace)) return fail(h, SHAMPOO_EINVAL, "workspace not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const LogprobPlan p = logprob_plan(rows, vocab, k, dtype);
+    LogprobArgs q{logits, ld, rows, (int)vocab, targets, logp, lse, entropy, k, top_ids, top_logp,
+                  p.parts, p.per_part, static_cast<float*>(workspace)};
+    STATUS_TRY(launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        const dim3 grid((unsigned)(p.waves == 1 ? cdiv64(rows, 4) : rows * p.parts));
+        auto k1 = p.waves == 1 ? (entropy ? logprobs_kernel<S, 1, true> : logprobs_kernel<S, 1, false>)
+                               : (entropy ? logprobs_kernel<S, 4, true> : logprobs_kernel<S, 4, false>);
+        hipLaunchKernelGGL(k1, grid, dim3(kThreads), 0, s, q);
+      });
+    }));
+    if (p.parts == 1) return SHAMPOO_OK;
     return launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
-        hipLaunchKernelGGL(logprobs_kernel<S>, dim3((unsigned)rows), dim3(kThreads), 0, s, (const S*)logits, ld,
-                           (int)vocab, targets, logp, lse, entropy, k, top_ids, top_logp);
+        hipLaunchKernelGGL(logprobs_join_kernel<S>, dim3((unsigned)rows), dim3(64), 0, s, q);
       });
     });
   });
