@@ -88,7 +88,14 @@ void with_type(int dtype, F&& f) {
 }
 
 // How a row of logits is cut: waves of a workgroup to a row, and workgroups
-// (parts) of a row where there are few rows.
+// (parts) of a row where there are few rows.  About two waves per SIMD are
+// wanted: fewer do not keep enough bytes in flight, and each wave of a row pays
+// for finding its own first alternatives.  Rows x 131072 in bf16, 8
+// alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 384 / 385 / 388 / 409, 1024
+// rows 71 / 53 / 51 / 70, 256 rows (4 / 8 / 4 in two parts) 28 / 25 / 27; without
+// alternatives 8192 rows 379 / 374 / 356 / 356.  Below 256 rows parts of 4 waves
+// and a second launch to join them: one row 13 us, by one workgroup of 16
+// waves 19; 64 rows 16 (8 waves without parts 21).
 struct LogprobPlan {
   int waves = 1, parts = 1, per_part = 0;
   size_t ws = 0;
@@ -97,16 +104,15 @@ struct LogprobPlan {
 LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int k, int dtype) {
   LogprobPlan p;
   const int64_t block = dtype == SHAMPOO_BF16 ? LogitBlock<uint16_t>::kN : LogitBlock<float>::kN;
-  p.waves = vocab <= 2 * block ? 1 : 4;
-  if (p.waves == 4) {
-    const int64_t steps = cdiv64(vocab, 4 * block);
-    const int64_t parts = std::min<int64_t>({cdiv64(2048, rows), steps, 64});
-    const int64_t per = cdiv64(steps, parts);
-    p.parts = (int)cdiv64(steps, per);
-    p.per_part = (int)std::min<int64_t>(per * 4 * block, vocab);
-  } else {
-    p.per_part = (int)vocab;
-  }
+  const int64_t blocks = cdiv64(vocab, block);
+  const int64_t want = std::min(std::max<int64_t>(cdiv64(2048, rows), k == 0 ? 4 : 1), blocks);
+  const int most = rows >= 256 ? 8 : 4;
+  while (p.waves < want && p.waves < most) p.waves *= 2;
+  const int64_t steps = cdiv64(blocks, p.waves);
+  const int64_t parts = rows >= 256 ? 1 : std::min<int64_t>(cdiv64(want, p.waves), 64);
+  const int64_t per = cdiv64(steps, parts);
+  p.parts = (int)cdiv64(steps, per);
+  p.per_part = (int)std::min<int64_t>(per * p.waves * block, vocab);
   if (p.parts > 1) p.ws = (size_t)(rows * p.parts * logprob_record(k)) * sizeof(float);
   return p;
 }
@@ -226,9 +232,15 @@ shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtyp
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
         const dim3 grid((unsigned)(p.waves == 1 ? cdiv64(rows, 4) : rows * p.parts));
-        auto k1 = p.waves == 1 ? (entropy ? logprobs_kernel<S, 1, true> : logprobs_kernel<S, 1, false>)
-                               : (entropy ? logprobs_kernel<S, 4, true> : logprobs_kernel<S, 4, false>);
-        hipLaunchKernelGGL(k1, grid, dim3(kThreads), 0, s, q);
+        auto pick = [&](auto ent) {
+          constexpr bool kEnt = decltype(ent)::value;
+          return p.waves == 1   ? logprobs_kernel<S, 1, kEnt>
+                 : p.waves == 2 ? logprobs_kernel<S, 2, kEnt>
+                 : p.waves == 4 ? logprobs_kernel<S, 4, kEnt>
+                                : logprobs_kernel<S, 8, kEnt>;
+        };
+        auto k1 = entropy ? pick(std::true_type()) : pick(std::false_type());
+        hipLaunchKernelGGL(k1, grid, dim3(p.waves == 1 ? kThreads : 64 * p.waves), 0, s, q);
       });
     }));
     if (p.parts == 1) return SHAMPOO_OK;

@@ -64,44 +64,21 @@ __device__ __forceinline__ LseStat lse_wave(LseStat a) {
   return a;
 }
 
-// The k largest entries of a wave, sorted over its lanes (lane i: the i-th).
-struct TopList {
-  float v;
-  int i;
-  // No entry below cut is wanted, and of those equal to it only the ones before
-  // entry `last`: the k-th entry of the list, or a bound where it is not full.
-  float cut;
-  int last;
-
-  __device__ __forceinline__ void clear() { v = cut = -INFINITY, i = last = INT32_MAX; }
-  __device__ __forceinline__ bool wants(float x, int j) const { return better(x, j, cut, last) && x > -INFINITY; }
-  // One entry, the same in every lane.
-  __device__ __forceinline__ void insert(float x, int j, int k, int lane) {
-    const int pos = __popcll(__ballot(better(v, i, x, j)));
-    const float pv = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x138, 0xf, 0xf, false));
-    const int pi = __builtin_amdgcn_update_dpp(0, i, 0x138, 0xf, 0xf, false);  // lane - 1's
-    if (lane == pos) v = x, i = j;
-    else if (lane > pos) v = pv, i = pi;
-    cut = fmaxf(cut, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k - 1)));
-    last = __builtin_amdgcn_readlane(i, k - 1);
-  }
-  // One entry of each lane, in any order.
-  __device__ __forceinline__ void insert_lanes(float x, int j, int k, int lane) {
-    uint64_t todo = __ballot(wants(x, j));
-    while (todo) {
-      const int l = __builtin_ctzll(todo);
-      insert(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)), __builtin_amdgcn_readlane(j, l), k, lane);
-      todo &= ~(uint64_t(1) << l) & __ballot(wants(x, j));
-    }
-  }
-};
-
 // The largest float below x (x not NaN); -inf stays.
 __device__ __forceinline__ float float_below(float x) {
   const uint32_t b = __float_as_uint(x);
   if (x == 0.f) return -1.401298464e-45f;
   if (x == -INFINITY) return x;
   return __uint_as_float(x > 0.f ? b - 1 : b + 1);
+}
+
+// LDS written by some lanes of a wave and read by others: a wave's LDS accesses
+// keep their order, the compiler has to keep it too.
+__device__ __forceinline__ void wave_lds_order() { asm volatile("" ::: "memory"); }
+
+// Lanes of the wave below this one that are in the mask.
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
 // A cut below the k-th largest of the lanes' values x, by bisection over the
@@ -120,6 +97,109 @@ __device__ __forceinline__ float first_cut(float x, int k) {
   // at or below the order of -inf: every allowed entry passes
   return at <= 0x007fu ? -INFINITY : float_below(__uint_as_float(f));
 }
+
+// The k largest entries of a wave, sorted over its lanes (lane i: the i-th).
+struct TopList {
+  float v;
+  int i;
+
+  __device__ __forceinline__ void clear() { v = -INFINITY, i = INT32_MAX; }
+  // One entry, the same in every lane.
+  __device__ __forceinline__ void insert(float x, int j, int lane) {
+    const int pos = __popcll(__ballot(better(v, i, x, j)));
+    const float pv = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x138, 0xf, 0xf, false));
+    const int pi = __builtin_amdgcn_update_dpp(0, i, 0x138, 0xf, 0xf, false);  // lane - 1's
+    if (lane == pos) v = x, i = j;
+    else if (lane > pos) v = pv, i = pi;
+  }
+  // One entry of each lane, in any order.
+  __device__ __forceinline__ void insert_lanes(float x, int j, int k, int lane) {
+    for (;;) {
+      const float kv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k - 1));
+      const int ki = __builtin_amdgcn_readlane(i, k - 1);
+      const uint64_t todo = __ballot(x > -INFINITY && better(x, j, kv, ki));
+      if (!todo) return;
+      const int l = __builtin_ctzll(todo);
+      insert(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)), __builtin_amdgcn_readlane(j, l), lane);
+      if (lane == l) x = -INFINITY;
+    }
+  }
+  // The n <= 64 entries (x, j) of lanes 0..n-1, sorted: each lane counts the
+  // entries before its own and passes it to that lane.
+  __device__ __forceinline__ void sort(float x, int j, int n, int lane) {
+    int rank = lane < n ? 0 : lane;
+    for (int o = 0; o < n; ++o) {
+      const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), o));
+      const int i2 = __builtin_amdgcn_readlane(j, o);
+      rank += lane < n && better(y, i2, x, j);
+    }
+    if (lane >= n) x = -INFINITY, j = INT32_MAX;
+    v = __uint_as_float(__builtin_amdgcn_ds_permute(rank * 4, __float_as_uint(x)));
+    i = __builtin_amdgcn_ds_permute(rank * 4, j);
+  }
+};
+
+// The k best of `top` and of `sets` sets of 64 N entries: get(c, x, j) gives a
+// lane's N of set c, of consecutive indices from j (x = -inf: none).  No entry up
+// to `low` is wanted.  What is above it is gathered in LDS and sorted; where
+// that is more than 64 entries (equal values, large k), one by one.
+template <int N, typename G>
+__device__ __forceinline__ void top_select(TopList& top, int sets, float low, int k, int lane, float* pv, int* pi,
+                                           G&& get) {
+  int n = 0;
+  auto gather = [&](float x, int j) {
+    const uint64_t in = __ballot(x > low);
+    const int at = n + lanes_below(in);
+    if (x > low && at < 64) pv[at] = x, pi[at] = j;
+    n += __popcll(in);
+  };
+  gather(top.v, top.i);
+  for (int c = 0; c < sets; ++c) {
+    float x[N];
+    int j;
+    get(c, x, j);
+#pragma unroll
+    for (int i = 0; i < N; ++i) gather(x[i], j + i);
+  }
+  wave_lds_order();
+  if (n <= 64) {
+    top.sort(pv[lane], pi[lane], n, lane);
+    wave_lds_order();
+    return;
+  }
+  for (int c = 0; c < sets; ++c) {
+    float x[N];
+    int j;
+    get(c, x, j);
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      float y = x[0];  // x[i]
+#pragma unroll
+      for (int o = 1; o < N; ++o) y = i == o ? x[o] : y;
+      top.insert_lanes(y > low ? y : -INFINITY, j + i, k, lane);
+    }
+  }
+}
+
+// The entries of a wave that may be among the k largest, while it walks its
+// blocks: 16-byte pieces that hold one, with their first index, in LDS.
+struct TopPieces {
+  static constexpr int kCap = 320;  // 64, and the 256 of a block
+  u32x4 raw[kCap];
+  int at[kCap];
+  float pv[64];  // for top_select
+  int pi[64];
+};
+struct TopState {
+  TopList list;  // the best so far of the pieces already gone through
+  float most;    // the lane's largest entry so far
+  float low;     // no entry of the row up to it is wanted
+  float bar;     // no later entry of this wave up to it is wanted
+  int n, blocks;
+
+  __device__ __forceinline__ void clear() { list.clear(), most = low = bar = -INFINITY, n = blocks = 0; }
+  __device__ __forceinline__ void raise(float x) { low = fmaxf(low, x), bar = fmaxf(bar, x); }
+};
 
 // A block of a wave: kU 16-byte loads of each lane, 64 lanes apart.
 template <typename S>
@@ -156,26 +236,31 @@ struct LogitBlock {
     return __uint_as_float(i & 1 ? raw[u][i / 2] & 0xffff0000u : raw[u][i / 2] << 16);
   }
 
-  template <bool ENT, bool HUGE_>
-  __device__ __forceinline__ void sums(float n, float c, bool clamp, float& s, float& t) const {
+  // The block's s and t against reference n, c = L n.  SAFE: also where n is
+  // beyond kHugeLogit (`far`), and t without the NaN of entries that are not
+  // allowed (0 times -inf).
+  template <bool ENT, bool SAFE>
+  __device__ __forceinline__ void sums(float n, float c, bool far, float& s, float& t) const {
     s = t = 0.f;
 #pragma unroll
     for (int u = 0; u < kU; ++u)
 #pragma unroll
       for (int i = 0; i < kV; ++i) {
         const float z = at(u, i);
-        float x = HUGE_ ? (z - n) * kLog2e : fmaf(z, kLog2e, -c);
+        float x = fmaf(z, kLog2e, -c);
+        if (SAFE) x = far ? (z - n) * kLog2e : x;
         const float e = __builtin_amdgcn_exp2f(x);
         s += e;
-        if (HUGE_ || clamp) x = fmaxf(x, -1e30f);  // 0, not NaN, for an entry that is not allowed
+        if (SAFE) x = fmaxf(x, -1e30f);
         if (ENT) t = fmaf(x, e, t);
       }
   }
 
-  // Adds the block to st and the wave's alternatives; its first entry is entry
-  // `base` of the row.
+  // Adds the block to st and keeps its pieces that hold a wanted entry; its
+  // first entry is entry `base` of the row, no entry up to `floor_` is wanted.
   template <bool ENT>
-  __device__ __forceinline__ void add(LseStat& st, TopList& top, bool& fresh, int base, int k, int lane) const {
+  __device__ __forceinline__ void add(LseStat& st, TopState& top, TopPieces* pieces, float floor_, int base, int k,
+                                      int lane) const {
     float um[kU], bm;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
@@ -185,41 +270,66 @@ struct LogitBlock {
     }
     bm = fmaxf(fmaxf(um[0], um[1]), fmaxf(um[2], um[3]));
     float s, t;
-    const float n0 = st.s == 0.f && bm > -INFINITY ? bm : fmaxf(st.m, bm);
-    const bool far = fabsf(n0) > kHugeLogit;
-    if (__builtin_expect(__any(far), 0)) {
-      if (far) sums<ENT, true>(n0, 0.f, true, s, t);
-      else sums<ENT, false>(n0, lse_ref(n0), true, s, t);
-      st = lse_join(st, {n0, s, t});
+    const float n = st.s == 0.f && bm > -INFINITY ? bm : fmaxf(st.m, bm), c = lse_ref(n);
+    const bool far = fabsf(n) > kHugeLogit;
+    sums<ENT, false>(n, c, false, s, t);
+    if (__any((ENT && t != t) || far)) {
+      LogitBlock again = *this;
+      // a copy the compiler does not know to be one: it would keep 64 values of
+      // the first pass in registers for this rare one
+#pragma unroll
+      for (int u = 0; u < kU; ++u) asm volatile("" : "+v"(again.raw[u]));
+      again.template sums<ENT, true>(n, c, far, s, t);
+    }
+    if (__any(far || fabsf(st.m) > kHugeLogit)) {
+      st = lse_join(st, {n, s, t});
     } else {
-      const float n = fmaxf(st.m, bm), c = lse_ref(n);
       const float d = fmaxf(lse_ref(st.m) - c, -1e30f), f = __builtin_amdgcn_exp2f(d);
-      sums<ENT, false>(n, c, false, s, t);
-      if (ENT && __any(t != t)) sums<ENT, false>(n, c, true, s, t);
       st.t = (st.t + d * st.s) * f + t;
       st.s = st.s * f + s;
       st.m = n;
     }
     if (k == 0) return;
-    if (fresh) top.cut = first_cut(bm, k);
-    fresh = false;
-    // entries equal to the cut count only in the block that holds `last`
-    if (!__any(base <= top.last ? bm >= top.cut : bm > top.cut)) return;
+    top.most = fmaxf(top.most, bm);
+    top.raise(floor_);
+    // k lanes hold an entry at or above the k-th of the lanes' largest: a bound
+    // worth its 16 ballots whenever the number of blocks has doubled
+    ++top.blocks;
+    if ((top.blocks & (top.blocks - 1)) == 0) top.raise(first_cut(top.most, k));
+    if (!__any(bm > top.bar)) return;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      if (!__any(um[u] >= top.cut)) continue;
-      const int first = base + (u * 64 + lane) * kV;
-#pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        uint64_t todo = __ballot(top.wants(at(u, i), first + i));
-        while (todo) {
-          const int l = __builtin_ctzll(todo);
-          top.insert(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(at(u, i)), l)),
-                     base + (u * 64 + l) * kV + i, k, lane);
-          todo &= ~(uint64_t(1) << l) & __ballot(top.wants(at(u, i), first + i));
-        }
+      const bool hit = um[u] > top.bar;
+      const uint64_t hits = __ballot(hit);
+      if (!hits) continue;
+      const int to = top.n + lanes_below(hits);
+      if (hit) {
+        pieces->raw[to] = raw[u];
+        pieces->at[to] = base + (u * 64 + lane) * kV;
       }
+      top.n += __popcll(hits);
     }
+    if (top.n > TopPieces::kCap - 64 * kU) settle(top, pieces, k, lane);
+  }
+
+  // The wave's k best of its list and its pieces.
+  static __device__ __forceinline__ void settle(TopState& top, TopPieces* pieces, int k, int lane) {
+    wave_lds_order();
+    top_select<kV>(top.list, (top.n + 63) / 64, top.low, k, lane, pieces->pv, pieces->pi,
+                   [&](int c, float (&x)[kV], int& j) {
+                     const int e = c * 64 + lane;
+                     LogitBlock one;
+                     one.raw[0] = pieces->raw[e < top.n ? e : 0];
+                     j = pieces->at[e < top.n ? e : 0];
+#pragma unroll
+                     for (int i = 0; i < kV; ++i) x[i] = e < top.n ? one.at(0, i) : -INFINITY;
+                   });
+    top.n = 0;
+    wave_lds_order();
+    // later entries come after these: they must exceed the k-th
+    const float kth = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top.list.v), k - 1));
+    top.low = fmaxf(top.low, float_below(kth));
+    top.bar = fmaxf(top.bar, kth);
   }
 };
 
@@ -270,61 +380,85 @@ __device__ __forceinline__ int logprobs_target(const LogprobArgs& q, int64_t r, 
   return tg < 0 ? -1 : tg;
 }
 
-// W waves to a row (or to a part of it), 4 / W rows to a workgroup; the waves
-// take its blocks in turn.
+// A workgroup of W waves to a row (or to a part of it), which take its blocks in
+// turn; W = 1: four rows to a workgroup.
 template <typename S, int W, bool ENT>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs q) {
+__global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(LogprobArgs q) {
   using Block = LogitBlock<S>;
-  __shared__ float sm[W > 1 ? W : 1][3];
-  __shared__ float sv[W > 1 ? W : 1][SHAMPOO_MAX_TOP];
-  __shared__ int si[W > 1 ? W : 1][SHAMPOO_MAX_TOP];
+  constexpr int kWaves = W == 1 ? 4 : W;
+  __shared__ TopPieces pieces_[kWaves];
+  __shared__ float floors[W];
+  __shared__ float sm[W][3];
+  __shared__ float sv[W][SHAMPOO_MAX_TOP];
+  __shared__ int si[W][SHAMPOO_MAX_TOP];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t item = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
+  const int64_t item = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   if (item >= q.rows * q.parts) return;
   const int64_t r = item / q.parts;
   const int part = (int)(item % q.parts), w = W == 1 ? 0 : wave;
+  TopPieces* pieces = &pieces_[wave];
   const S* z = static_cast<const S*>(q.logits) + r * q.ld;
   const int begin = part * q.per_part, end = min(q.vocab, begin + q.per_part);
   float zt = 0.f;
   const int tg = q.parts == 1 && w == 0 ? logprobs_target<S>(q, r, zt) : -1;
 
   LseStat st = {-kHugeLogit, 0.f, 0.f};
-  TopList top;
+  TopState top;
   top.clear();
-  bool fresh = true;
-  int at = begin + w * Block::kN;
+  // What a wave does not want its neighbours do not want either, up to equal
+  // values: they read each other's bounds, unsynchronised (an old one only lets
+  // more entries through).
+  volatile float* shared = floors;
+  if (W > 1 && q.k) {
+    if (lane == 0) shared[w] = -INFINITY;
+    __syncthreads();
+  }
   Block blk, nxt;
-  if (at + Block::kN <= end) nxt.load(z + at, lane);
-  for (; at + Block::kN <= end; at += W * Block::kN) {
+  auto fetch = [&](int at) {
+    if (at + Block::kN <= end) nxt.load(z + at, lane);
+    else if (at < end) nxt.load_part(z + at, end - at, lane);
+  };
+  int at = begin + w * Block::kN;
+  fetch(at);
+  for (; at < end; at += W * Block::kN) {
     blk = nxt;
-    if (at + (W + 1) * Block::kN <= end) nxt.load(z + at + W * Block::kN, lane);
-    blk.template add<ENT>(st, top, fresh, at, q.k, lane);
+    fetch(at + W * Block::kN);
+    float floor_ = -INFINITY;
+    if (W > 1 && q.k) {
+#pragma unroll
+      for (int o = 0; o < W; ++o) floor_ = fmaxf(floor_, shared[o]);
+      floor_ = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(floor_)));
+    }
+    const float old = top.low;
+    blk.template add<ENT>(st, top, pieces, floor_, at, q.k, lane);
+    if (W > 1 && q.k && top.low > fmaxf(old, floor_) && lane == 0) shared[w] = top.low;
   }
-  if (at < end) {
-    blk.load_part(z + at, end - at, lane);
-    blk.template add<ENT>(st, top, fresh, at, q.k, lane);
-  }
+  if (q.k) Block::settle(top, pieces, q.k, lane);
   st = lse_wave(st);
   if constexpr (W > 1) {
     if (lane == 0) sm[w][0] = st.m, sm[w][1] = st.s, sm[w][2] = st.t;
-    if (lane < q.k) sv[w][lane] = top.v, si[w][lane] = top.i;
+    if (lane < q.k) sv[w][lane] = top.list.v, si[w][lane] = top.list.i;
     __syncthreads();
     if (w != 0) return;
 #pragma unroll
     for (int o = 1; o < W; ++o) st = lse_join(st, {sm[o][0], sm[o][1], sm[o][2]});
-    for (int e = lane; e - lane < (W - 1) * q.k; e += 64) {  // the best of each wave first
-      const bool in = e < (W - 1) * q.k;
-      const int o = 1 + e % (W - 1), i = e / (W - 1);
-      top.insert_lanes(in ? sv[o][i] : -INFINITY, in ? si[o][i] : INT32_MAX, q.k, lane);
+    if (q.k) {
+      const int n = (W - 1) * q.k;
+      auto get = [&](int c, float (&x)[1], int& j) {
+        const int e = c * 64 + lane, o = 1 + e % (W - 1), i = e / (W - 1);
+        x[0] = e < n ? sv[o][i] : -INFINITY;
+        j = e < n ? si[o][i] : INT32_MAX;
+      };
+      top_select<1>(top.list, (n + 63) / 64, top.low, q.k, lane, pieces->pv, pieces->pi, get);
     }
   }
   if (q.parts == 1) {
-    logprobs_finish(q, r, st, top, tg, zt, lane);
+    logprobs_finish(q, r, st, top.list, tg, zt, lane);
     return;
   }
   float* rec = q.ws + item * logprob_record(q.k);
   if (lane == 0) rec[0] = st.m, rec[1] = st.s, rec[2] = st.t;
-  if (lane < q.k) rec[4 + lane] = top.v, rec[4 + q.k + lane] = __int_as_float(top.i);
+  if (lane < q.k) rec[4 + lane] = top.list.v, rec[4 + q.k + lane] = __int_as_float(top.list.i);
 }
 
 // Joins the parts of a row (at most 64), one wave to a row.
@@ -341,12 +475,26 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
     st = {p[0], p[1], p[2]};
   }
   st = lse_wave(st);
+  __shared__ float pv[64];
+  __shared__ int pi[64];
   TopList top;
   top.clear();
-  for (int e = lane; e - lane < q.parts * q.k; e += 64) {
-    const bool in = e < q.parts * q.k;
-    const float* p = rec + (in ? e % q.parts * logprob_record(q.k) + 4 + e / q.parts : 0);
-    top.insert_lanes(in ? p[0] : -INFINITY, in ? __float_as_int(p[q.k]) : INT32_MAX, q.k, lane);
+  if (q.k) {
+    const int n = q.parts * q.k;
+    auto get = [&](int c, float (&x)[1], int& j) {
+      const int e = c * 64 + lane;
+      const float* p = rec + (e < n ? e % q.parts * logprob_record(q.k) + 4 + e / q.parts : 0);
+      x[0] = e < n ? p[0] : -INFINITY;
+      j = e < n ? __float_as_int(p[q.k]) : INT32_MAX;
+    };
+    float most = -INFINITY;
+    for (int c = 0; c * 64 < n; ++c) {
+      float x[1];
+      int j;
+      get(c, x, j);
+      most = fmaxf(most, x[0]);
+    }
+    top_select<1>(top, (n + 63) / 64, first_cut(most, q.k), q.k, lane, pv, pi, get);
   }
   logprobs_finish(q, r, st, top, tg, zt, lane);
 }
