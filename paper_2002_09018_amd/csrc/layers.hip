@@ -87,6 +87,8 @@ void with_type(int dtype, F&& f) {
   else f((uint16_t*)nullptr);
 }
 
+constexpr int64_t kMostItems = 1 << 22;  // parts of rows of one launch
+
 // How a row of logits is cut: waves of a workgroup to a row, and workgroups
 // (parts) of a row where there are few rows.  About two waves per SIMD are
 // wanted: fewer do not keep enough bytes in flight, and each wave of a row pays
@@ -227,22 +229,26 @@ shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtyp
     hipStream_t s = static_cast<hipStream_t>(stream);
     const LogprobPlan p = logprob_plan(rows, vocab, k, dtype);
     LogprobArgs q{logits, ld, rows, (int)vocab, targets, logp, lse, entropy, k, top_ids, top_logp,
-                  p.parts, p.per_part, static_cast<float*>(workspace)};
-    STATUS_TRY(launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
-      with_type(dtype, [&](auto* type) {
-        using S = std::remove_pointer_t<decltype(type)>;
-        const dim3 grid((unsigned)(p.waves == 1 ? cdiv64(rows, 4) : rows * p.parts));
-        auto pick = [&](auto ent) {
-          constexpr bool kEnt = decltype(ent)::value;
-          return p.waves == 1   ? logprobs_kernel<S, 1, kEnt>
-                 : p.waves == 2 ? logprobs_kernel<S, 2, kEnt>
-                 : p.waves == 4 ? logprobs_kernel<S, 4, kEnt>
-                                : logprobs_kernel<S, 8, kEnt>;
-        };
-        auto k1 = entropy ? pick(std::true_type()) : pick(std::false_type());
-        hipLaunchKernelGGL(k1, grid, dim3(p.waves == 1 ? kThreads : 64 * p.waves), 0, s, q);
-      });
-    }));
+                  p.parts, p.per_part, 0, static_cast<float*>(workspace)};
+    // a launch holds fewer than 2^32 threads: more rows than that take several
+    for (q.first = 0; q.first < rows * p.parts; q.first += kMostItems) {
+      STATUS_TRY(launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
+        with_type(dtype, [&](auto* type) {
+          using S = std::remove_pointer_t<decltype(type)>;
+          const int64_t n = std::min(rows * p.parts - q.first, kMostItems);
+          const dim3 grid((unsigned)(p.waves == 1 ? cdiv64(n, 4) : n));
+          auto pick = [&](auto ent) {
+            constexpr bool kEnt = decltype(ent)::value;
+            return p.waves == 1   ? logprobs_kernel<S, 1, kEnt>
+                   : p.waves == 2 ? logprobs_kernel<S, 2, kEnt>
+                   : p.waves == 4 ? logprobs_kernel<S, 4, kEnt>
+                                  : logprobs_kernel<S, 8, kEnt>;
+          };
+          auto k1 = entropy ? pick(std::true_type()) : pick(std::false_type());
+          hipLaunchKernelGGL(k1, grid, dim3(p.waves == 1 ? kThreads : 64 * p.waves), 0, s, q);
+        });
+      }));
+    }
     if (p.parts == 1) return SHAMPOO_OK;
     return launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
       with_type(dtype, [&](auto* type) {
@@ -268,12 +274,21 @@ shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int
     if (dlogits == logits && ld_d != ld) return fail(h, SHAMPOO_EINVAL, "in place, ld_d %lld must be ld %lld", (long long)ld_d, (long long)ld);
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    LossGradArgs q{logits, ld, rows, (int)vocab, targets, lse, entropy, g_top ? k : 0, top_ids, g_logp, g_lse,
+                   g_entropy, g_top, dlogits, ld_d, 1, 1};
+    const int64_t block = dtype == SHAMPOO_BF16 ? LogitBlock<uint16_t>::kN : LogitBlock<float>::kN;
+    const int64_t blocks = cdiv64(vocab + 7, block);  // a row may begin up to 7 entries into its first
+    // one block to a wave (8192 x 131072 in bf16: 729 us; two 766, four 792), two
+    // in short rows, where a row's own values cost more (8192 x 5000 with 32
+    // alternatives: 44.6 -> 41.7)
+    q.per = blocks > 16 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(2, rows * blocks / 4096));
+    q.segs = (int)cdiv64(blocks, q.per);
     return launch(h, SHAMPOO_KCLASS_LOGPROBS, s, [&] {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
-        hipLaunchKernelGGL(logprobs_grad_kernel<S>, dim3((unsigned)rows), dim3(kThreads), 0, s, (const S*)logits, ld,
-                           (int)vocab, targets, lse, entropy, g_top ? k : 0, top_ids, g_logp, g_lse, g_entropy, g_top,
-                           (S*)dlogits, ld_d);
+        auto k1 = g_entropy ? logprobs_grad_kernel<S, true> : logprobs_grad_kernel<S, false>;
+        hipLaunchKernelGGL(k1, dim3((unsigned)std::min<int64_t>(cdiv64(rows * q.segs, 4), 1 << 20)), dim3(kThreads), 0,
+                           s, q);
       });
     });
   });

@@ -6,7 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "fp32_block.hpp"
+#include "split_mfma.hpp"
 #include "shampoo.h"
 #include "tile_mfma.hpp"
 
@@ -211,20 +211,21 @@ struct LogitBlock {
 #pragma unroll
     for (int u = 0; u < kU; ++u) raw[u] = gload<u32x4u>(z + (u * 64 + lane) * kV);
   }
-  // Only n entries; the others are not allowed.
-  __device__ __forceinline__ void load_part(const S* z, int n, int lane) {
+  // Only entries lo..hi of it; the others are not allowed.
+  __device__ __forceinline__ void load_part(const S* z, int lo, int hi, int lane) {
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       const int at = (u * 64 + lane) * kV;
-      if (at + kV <= n) {
+      if (at >= lo && at + kV <= hi) {
         raw[u] = gload<u32x4u>(z + at);
       } else {
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
+          const bool in = at + i >= lo && at + i < hi;
           if constexpr (sizeof(S) == 4) {
-            raw[u][i] = at + i < n ? gload<uint32_t>(z + at + i) : 0xff800000u;
+            raw[u][i] = in ? gload<uint32_t>(z + at + i) : 0xff800000u;
           } else {
-            const uint32_t w = at + i < n ? (uint32_t)gload<uint16_t>(z + at + i) : 0xff80u;
+            const uint32_t w = in ? (uint32_t)gload<uint16_t>(z + at + i) : 0xff80u;
             raw[u][i / 2] = i & 1 ? raw[u][i / 2] | w << 16 : w;
           }
         }
@@ -236,10 +237,10 @@ struct LogitBlock {
     return __uint_as_float(i & 1 ? raw[u][i / 2] & 0xffff0000u : raw[u][i / 2] << 16);
   }
 
-  // The block's s and t against reference n, c = L n.  SAFE: also where n is
-  // beyond kHugeLogit (`far`), and t without the NaN of entries that are not
-  // allowed (0 times -inf).
-  template <bool ENT, bool SAFE>
+  // The block's s and t against reference n, c = L n.  FAR: also where n is
+  // beyond kHugeLogit (`far`).  The lower bound on x makes an entry that is not
+  // allowed add 0 to t (it would be 0 times -inf).
+  template <bool ENT, bool FAR>
   __device__ __forceinline__ void sums(float n, float c, bool far, float& s, float& t) const {
     s = t = 0.f;
 #pragma unroll
@@ -248,11 +249,10 @@ struct LogitBlock {
       for (int i = 0; i < kV; ++i) {
         const float z = at(u, i);
         float x = fmaf(z, kLog2e, -c);
-        if (SAFE) x = far ? (z - n) * kLog2e : x;
+        if (FAR) x = far ? (z - n) * kLog2e : x;
         const float e = __builtin_amdgcn_exp2f(x);
         s += e;
-        if (SAFE) x = fmaxf(x, -1e30f);
-        if (ENT) t = fmaf(x, e, t);
+        if (ENT) t = fmaf(fmaxf(x, -1e30f), e, t);
       }
   }
 
@@ -273,7 +273,7 @@ struct LogitBlock {
     const float n = st.s == 0.f && bm > -INFINITY ? bm : fmaxf(st.m, bm), c = lse_ref(n);
     const bool far = fabsf(n) > kHugeLogit;
     sums<ENT, false>(n, c, false, s, t);
-    if (__any((ENT && t != t) || far)) {
+    if (__any(far)) {
       LogitBlock again = *this;
       // a copy the compiler does not know to be one: it would keep 64 values of
       // the first pass in registers for this rare one
@@ -344,6 +344,7 @@ struct LogprobArgs {
   float* top_logp;
   int parts;     // workgroups of a row
   int per_part;  // entries of one
+  int64_t first; // the launch's first part of all rows' parts
   float* ws;     // a record for each part of each row: m, s, t, -, k values, k indices
 };
 __host__ __device__ __forceinline__ int64_t logprob_record(int k) { return 4 + 2 * (int64_t)k; }
@@ -392,11 +393,12 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
   __shared__ float sv[W][SHAMPOO_MAX_TOP];
   __shared__ int si[W][SHAMPOO_MAX_TOP];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t item = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int w = W == 1 ? 0 : wave;
+  TopPieces* pieces = &pieces_[wave];
+  const int64_t item = q.first + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x);
   if (item >= q.rows * q.parts) return;
   const int64_t r = item / q.parts;
-  const int part = (int)(item % q.parts), w = W == 1 ? 0 : wave;
-  TopPieces* pieces = &pieces_[wave];
+  const int part = (int)(item % q.parts);
   const S* z = static_cast<const S*>(q.logits) + r * q.ld;
   const int begin = part * q.per_part, end = min(q.vocab, begin + q.per_part);
   float zt = 0.f;
@@ -409,14 +411,14 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
   // values: they read each other's bounds, unsynchronised (an old one only lets
   // more entries through).
   volatile float* shared = floors;
-  if (W > 1 && q.k) {
+  if (W > 1) {
     if (lane == 0) shared[w] = -INFINITY;
     __syncthreads();
   }
   Block blk, nxt;
   auto fetch = [&](int at) {
     if (at + Block::kN <= end) nxt.load(z + at, lane);
-    else if (at < end) nxt.load_part(z + at, end - at, lane);
+    else if (at < end) nxt.load_part(z + at, 0, end - at, lane);
   };
   int at = begin + w * Block::kN;
   fetch(at);
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
 template <typename S>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
   const int lane = threadIdx.x;
-  const int64_t r = blockIdx.x;
+  const int64_t r = blockIdx.x;  // fewer than 256 rows are cut into parts
   float zt;
   const int tg = logprobs_target<S>(q, r, zt);
   const float* rec = q.ws + r * q.parts * logprob_record(q.k);
@@ -499,55 +501,119 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
   logprobs_finish(q, r, st, top, tg, zt, lane);
 }
 
-// One workgroup per row of the gradient.  The entries that also take a
-// target's or an alternative's gradient are read before any entry is
-// written (the gradient may overwrite the logits) and written again last.
-template <typename S>
-__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(
-    const S* logits, int64_t ld, int vocab, const int32_t* __restrict__ targets, const float* __restrict__ lse_in,
-    const float* __restrict__ entropy, int k, const int32_t* __restrict__ top_ids, const float* __restrict__ g_logp,
-    const float* __restrict__ g_lse, const float* __restrict__ g_entropy, const float* __restrict__ g_top, S* dlogits,
-    int64_t ld_d) {
-  __shared__ float part[SHAMPOO_MAX_TOP + 1];
-  __shared__ int ids[SHAMPOO_MAX_TOP + 1];
-  const int64_t r = blockIdx.x;
-  const S* z = logits + r * ld;
-  S* dz = dlogits + r * ld_d;
-  const int tid = threadIdx.x;
-  const float lse = lse_in[r];
-  const float H = g_entropy ? entropy[r] : 0.f, ge = g_entropy ? g_entropy[r] : 0.f;
-  // slot 0: the target; slot 1 + i: alternative i
-  if (tid <= k) {
-    int64_t id = -1;
-    float g = 0.f;
-    if (tid == 0) {
-      if (g_logp) id = targets[r], g = g_logp[r];
-    } else if (g_top) {
-      id = top_ids[r * k + tid - 1], g = g_top[r * k + tid - 1];
+// ---------------------------------------------------------------- gradient
+struct LossGradArgs {
+  const void* logits;
+  int64_t ld, rows;
+  int vocab;
+  const int32_t* targets;
+  const float *lse, *entropy;
+  int k;
+  const int32_t* top_ids;
+  const float *g_logp, *g_lse, *g_entropy, *g_top;
+  void* dlogits;
+  int64_t ld_d;
+  int per, segs;  // blocks of a wave, and waves of a row
+};
+
+// A wave to `per` blocks of a row, which start where stores to the row are aligned
+// (a row of odd length or stride begins with a part of a block).  Lane 0 holds
+// the target, lane i an alternative.  The entries of these take the outputs'
+// own gradients too: their lanes read them before anything of the row is
+// written (the gradient may overwrite the logits; no other wave touches these
+// blocks) and write them again when the wave's stores have arrived.
+template <typename S, bool ENT>
+__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LossGradArgs q) {
+  using Block = LogitBlock<S>;
+  constexpr int kV = Block::kV, kU = Block::kU, kN = Block::kN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < q.rows * q.segs; item += (int64_t)gridDim.x * 4) {
+    const int64_t r = item / q.segs;
+    const S* z = static_cast<const S*>(q.logits) + r * q.ld;
+    S* dz = static_cast<S*>(q.dlogits) + r * q.ld_d;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(dz) / sizeof(S) % kV);
+    const int begin = (int)(item % q.segs) * q.per * kN - shift, end = min(q.vocab, begin + q.per * kN);
+    Block blk, nxt;
+    auto fetch = [&](int at) {
+      if (at >= 0 && at + kN <= end) nxt.load(z + at, lane);
+      else if (at < end) nxt.load_part(z + at, -at, end - at, lane);
+    };
+    fetch(begin);
+    const float lse = q.lse[r];
+    const float H = ENT ? q.entropy[r] : 0.f, ge = ENT ? q.g_entropy[r] : 0.f;
+    float base = q.g_lse ? q.g_lse[r] : 0.f;
+    // up to 65 of them: alternative 64 is lane 0's second
+    int id[2] = {-1, -1};
+    float g[2] = {0.f, 0.f};
+    if (lane == 0 && q.g_logp) id[0] = q.targets[r], g[0] = q.g_logp[r];
+    if (lane > 0 && lane <= q.k) id[0] = q.top_ids[r * q.k + lane - 1], g[0] = q.g_top[r * q.k + lane - 1];
+    if (lane == 0 && q.k > 63) id[1] = q.top_ids[r * q.k + 63], g[1] = q.g_top[r * q.k + 63];
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      if (id[o] < 0 || id[o] >= q.vocab) id[o] = -1, g[o] = 0.f;
+    base -= wave_sum(g[0] + g[1]);
+    const bool empty = lse == -INFINITY;  // no entry is allowed: no gradient
+    if (ENT) base -= ge * H;
+    auto value = [&](float x) {
+      const float lp = x - lse;
+      const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+      // exp(-200) is 0: the bound keeps 0 times -inf out
+      return empty ? 0.f : p * (ENT ? fmaf(-ge, fmaxf(lp, -200.f), base) : base);
+    };
+    float own[2];
+    bool mine[2];
+    uint64_t owners[2];
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      mine[o] = id[o] >= begin && id[o] >= 0 && id[o] < end && !empty;
+      owners[o] = __ballot(mine[o]);
+      own[o] = mine[o] ? value(cvt<float, S>(z[id[o]])) : 0.f;
     }
-    const bool on = id >= 0 && id < vocab;
-    ids[tid] = on ? (int)id : -1;
-    part[tid] = on ? g : 0.f;
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      for (uint64_t todo = owners[o]; todo; todo &= todo - 1) {
+        const int l = __builtin_ctzll(todo);
+        const int at = __builtin_amdgcn_readlane(id[o], l);
+        const float add = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g[o]), l));
+        own[0] += id[0] == at ? add : 0.f;
+        own[1] += id[1] == at ? add : 0.f;
+      }
+
+    for (int at = begin; at < end; at += kN) {
+      blk = nxt;
+      fetch(at + kN);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int first = at + (u * 64 + lane) * kV;
+        u32x4u w;
+        if constexpr (sizeof(S) == 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(value(blk.at(u, i)));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack_bf16(value(blk.at(u, 2 * i)), value(blk.at(u, 2 * i + 1)));
+        }
+        if (first >= 0 && first + kV <= end) {
+          gstore<u32x4u>(dz + first, w);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kV; ++i) {
+            if (first + i < 0 || first + i >= end) continue;
+            if constexpr (sizeof(S) == 4) gstore<uint32_t>(dz + first + i, w[i]);
+            else gstore<uint16_t>(dz + first + i, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]));
+          }
+        }
+      }
+    }
+    if (owners[0] | owners[1]) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+        if (mine[o]) gstore<S>(dz + id[o], from_f32<S>(own[o]));
+    }
   }
-  __syncthreads();
-  float total = g_lse ? g_lse[r] : 0.f;
-  for (int i = 0; i <= k; ++i) total -= part[i];
-  const bool empty = lse == -INFINITY;
-  auto value = [&](float x) {
-    const float lp = x - lse;
-    const float p = expf(lp);
-    return empty ? 0.f : p * (total - ge * (fmaxf(lp, -1e30f) + H));
-  };
-  float own = 0.f;
-  if (tid <= k && ids[tid] >= 0) {
-    own = value(cvt<float, S>(z[ids[tid]]));
-    for (int i = 0; i <= k; ++i)
-      if (ids[i] == ids[tid]) own += part[i];
-  }
-  __syncthreads();
-  for (int j = tid; j < vocab; j += kThreads) dz[j] = from_f32<S>(value(cvt<float, S>(z[j])));
-  __syncthreads();
-  if (tid <= k && ids[tid] >= 0 && !empty) dz[ids[tid]] = from_f32<S>(own);
 }
 
 }  // namespace shp
