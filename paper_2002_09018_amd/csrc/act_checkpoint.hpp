@@ -42,92 +42,248 @@ __device__ __forceinline__ float act_scale(uint32_t s) { return __uint_as_float(
 // 2^-(s - 127), s <= 248.
 __device__ __forceinline__ float act_unscale(uint32_t s) { return __uint_as_float((254u - s) << 23); }
 
-template <int ACT>
+// Phi(x), the normal distribution function, and e = exp(-x^2 / 2) beside it, for
+// results kept in bf16: Abramowitz and Stegun 7.1.26 (erf of |x| / sqrt 2 to
+// 1.5e-7), one exponential and one reciprocal.
+__device__ __forceinline__ float normal_cdf(float x, float& e) {
+  const float a = fabsf(x) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
+  e = __builtin_amdgcn_exp2f(a * a * -1.44269504f);
+  // half of the complement: halves of the published coefficients
+  float h = fmaf(0.5307027145f, t, -0.7265760135f);
+  h = fmaf(h, t, 0.7107068705f);
+  h = fmaf(h, t, -0.142248368f);
+  h = fmaf(h, t, 0.127414796f);
+  h = h * t * e;
+  return x < 0.f ? h : 1.f - h;
+}
+__device__ __forceinline__ float fast_sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
+}
+
+// FAST: for results kept in bf16 (errors of a few 2^-22 of the terms), where the
+// library functions' 20 to 40 instructions a value would bound the pass; fp32
+// passes move twice the bytes and call them.
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_value(float x) {
-  if constexpr (ACT == SHAMPOO_ACT_RELU) return x > 0.f ? x : (x != x ? x : 0.f);
-  if constexpr (ACT == SHAMPOO_ACT_GELU) return 0.5f * x * (1.f + erff(x * 0.70710678f));
-  if constexpr (ACT == SHAMPOO_ACT_GELU_TANH)
-    return x / (1.f + expf(-1.59576912f * (x + 0.044715f * x * x * x)));
-  if constexpr (ACT == SHAMPOO_ACT_SILU) return x / (1.f + expf(-x));
+  if constexpr (ACT == SHAMPOO_ACT_RELU) return x < 0.f ? 0.f : x;
+  if constexpr (ACT == SHAMPOO_ACT_GELU) {
+    float e;
+    return FAST ? x * normal_cdf(x, e) : 0.5f * x * (1.f + erff(x * 0.70710678f));
+  }
+  if constexpr (ACT == SHAMPOO_ACT_GELU_TANH) {
+    const float w = 1.59576912f * (x + 0.044715f * x * x * x);
+    return FAST ? x * fast_sigmoid(w) : x / (1.f + expf(-w));
+  }
+  if constexpr (ACT == SHAMPOO_ACT_SILU) return FAST ? x * fast_sigmoid(x) : x / (1.f + expf(-x));
   return x;
 }
 
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == SHAMPOO_ACT_RELU) return x > 0.f ? 1.f : (x != x ? x : 0.f);
-  if constexpr (ACT == SHAMPOO_ACT_GELU)
+  if constexpr (ACT == SHAMPOO_ACT_GELU) {
+    if (FAST) {
+      float e;
+      const float p = normal_cdf(x, e);
+      return fmaf(x * 0.39894228f, e, p);
+    }
     return 0.5f * (1.f + erff(x * 0.70710678f)) + x * (0.39894228f * expf(-0.5f * x * x));
+  }
   if constexpr (ACT == SHAMPOO_ACT_GELU_TANH) {
-    const float p = 1.f / (1.f + expf(-1.59576912f * (x + 0.044715f * x * x * x)));
+    const float w = 1.59576912f * (x + 0.044715f * x * x * x);
+    const float p = FAST ? fast_sigmoid(w) : 1.f / (1.f + expf(-w));
     // beyond 20 the second term is below 2^-24 and its factors overflow
     return fabsf(x) > 20.f ? p : p + x * p * (1.f - p) * (1.59576912f + 0.21406659f * x * x);
   }
   if constexpr (ACT == SHAMPOO_ACT_SILU) {
-    const float p = 1.f / (1.f + expf(-x));
+    const float p = FAST ? fast_sigmoid(x) : 1.f / (1.f + expf(-x));
     return p + x * p * (1.f - p);
   }
   return 1.f;
 }
 
-// Codes and scale of one group of up to 32 values.
-__device__ __forceinline__ void act_encode_group(const float* v, char* ckpt, const ActCkpt& c, int64_t r, int64_t g) {
-  uint32_t top = 0;
-  for (int i = 0; i < kActGroup; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-  const uint32_t s = act_scale_byte(top);
-  int8_t* q = reinterpret_cast<int8_t*>(ckpt) + r * c.ldq + g * kActGroup;
-  for (int i = 0; i < kActGroup; ++i) q[i] = s == 255u ? 0 : (int8_t)fminf(fmaxf(rintf(v[i] * act_unscale(s)), -127.f), 127.f);
-  reinterpret_cast<uint8_t*>(ckpt)[c.scales + r * (c.ldq / kActGroup) + g] = (uint8_t)s;
-}
+// ---------------------------------------------------------------- passes
+// All passes move units of 8 columns, one to a lane: 16 or 32 bytes of a tensor,
+// 8 of the codes; the 4 lanes of a group agree on its scale.  A wave takes 64
+// units of a row, or (rows of up to 32 units) whole rows of 2^lp lanes.
+// blockIdx.x walks along a row, so that neighbouring workgroups touch
+// neighbouring memory.  Bound by memory: 16384 x 4096 in bf16, activation with
+// both checkpoints and their values in 147 us (5.5 TB/s), its gradient in 60 us
+// (5.6 TB/s); two or four units to a lane were 6 and 16% slower.
+struct ActShape {
+  int64_t rows;
+  int cols, upr;   // columns, and units of a row (ldq / 8)
+  int lp;          // log2 of the lanes of a row, 6 where it takes a wave or more
+  int64_t groups;  // items along blockIdx.y: rows, or sets of rows
+};
 
-// One thread per group of 32 columns.  X and Y may be the same buffer.
-template <typename S, int ACT>
-__global__ __launch_bounds__(kThreads) void act_encode_kernel(const S* X, int64_t ld_x, int64_t rows, int64_t cols,
-                                                             S* Y, int64_t ld_y, char* ckpt_x, char* ckpt_y) {
-  const ActCkpt c = act_ckpt(rows, cols);
-  const int64_t ng = c.ldq / kActGroup;
-  const int64_t step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * ng; i += step) {
-    const int64_t r = i / ng, g = i % ng;
-    float v[kActGroup];
-    for (int j = 0; j < kActGroup; ++j)
-      v[j] = g * kActGroup + j < cols ? cvt<float, S>(X[r * ld_x + g * kActGroup + j]) : 0.f;
-    if (ckpt_x) act_encode_group(v, ckpt_x, c, r, g);
-    if (!Y && !ckpt_y) continue;
-    for (int j = 0; j < kActGroup; ++j) {
-      const S y = from_f32<S>(act_value<ACT>(v[j]));
-      if (Y && g * kActGroup + j < cols) Y[r * ld_y + g * kActGroup + j] = y;
-      v[j] = g * kActGroup + j < cols ? cvt<float, S>(y) : 0.f;
-    }
-    if (ckpt_y) act_encode_group(v, ckpt_y, c, r, g);
+// Calls f(row, unit, in) for each unit of the lane; `in` is false past the tensor
+// (the lanes of a group are in or out together).
+template <typename F>
+__device__ __forceinline__ void act_units(const ActShape& h, F&& f) {
+  const int lane = threadIdx.x & 63, unit = blockIdx.x * 64 + (lane & ((1 << h.lp) - 1));
+  for (int64_t g = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); g < h.groups; g += (int64_t)gridDim.y * 4) {
+    const int64_t row = (g << (6 - h.lp)) + (lane >> h.lp);
+    f(row, unit, row < h.rows && unit < h.upr);
   }
 }
 
-__device__ __forceinline__ float act_load(const char* ckpt, const ActCkpt& c, int64_t r, int64_t j) {
-  const float q = (float)reinterpret_cast<const int8_t*>(ckpt)[r * c.ldq + j];
-  return q * act_scale(reinterpret_cast<const uint8_t*>(ckpt)[c.scales + r * (c.ldq / kActGroup) + j / kActGroup]);
+// 8 elements of a tensor.
+template <typename S>
+struct ActVec {
+  u32x4u raw[sizeof(S) / 2];
+
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(S) == 4) return __uint_as_float(raw[i / 4][i % 4]);
+    return __uint_as_float(i & 1 ? raw[0][i / 2] & 0xffff0000u : raw[0][i / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(S) == 4) {
+        raw[0][i] = __float_as_uint(v[i]);
+        raw[1][i] = __float_as_uint(v[4 + i]);
+      } else {
+        raw[0][i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+      }
+    }
+  }
+  // n of the 8 lie in the row; the others are zeros.
+  __device__ __forceinline__ void load(const S* p, int n) {
+    if (n >= 8) {
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(S) / 2; ++h) raw[h] = gload<u32x4u>(p + 4 * h);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(S) == 4) {
+        raw[i / 4][i % 4] = i < n ? gload<uint32_t>(p + i) : 0u;
+      } else {
+        const uint32_t w = i < n ? (uint32_t)gload<uint16_t>(p + i) : 0u;
+        raw[0][i / 2] = i & 1 ? raw[0][i / 2] | w << 16 : w;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(S* p, int n) const {
+    if (n >= 8) {
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(S) / 2; ++h) gstore<u32x4u>(p + 4 * h, raw[h]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i >= n) continue;
+      if constexpr (sizeof(S) == 4) gstore<uint32_t>(p + i, raw[i / 4][i % 4]);
+      else gstore<uint16_t>(p + i, (uint16_t)(i & 1 ? raw[0][i / 2] >> 16 : raw[0][i / 2]));
+    }
+  }
+};
+
+// Codes and scale byte of a lane's unit, with its 3 neighbours of the group.
+// x 2^-e + 1.5 2^23 rounds to the nearest even integer, whose low byte is the code.
+__device__ __forceinline__ uint32_t act_quantize(const float (&v)[8], u32x2& codes) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, true));  // lane ^ 1
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, true));  // lane ^ 2
+  const uint32_t s = act_scale_byte(top);
+  const float us = act_unscale(s);
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], us, 12582912.f));
+  if (__builtin_expect(__any(s >= 248u), 0)) {  // the largest scale, where 128 becomes 127, and NaN
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (s == 248u) b[i] = __float_as_uint(fminf(fmaxf(v[i] * us, -127.f), 127.f) + 12582912.f);
+      if (s == 255u) b[i] = 0;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    codes[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x0c0c0400u),
+                                     __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x0c0c0400u), 0x05040100u);
+  return s;
+}
+
+// The 8 values of a unit.
+__device__ __forceinline__ void act_expand(u32x2 codes, uint32_t s, float (&v)[8]) {
+  const float scale = act_scale(s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(codes[i / 4] >> (8 * (i % 4))) * scale;
+}
+
+struct ActCkptPtr {
+  char* codes;  // NULL: no checkpoint
+  uint8_t* scales;
+};
+
+// X and Y may be the same buffer.
+template <typename S, int ACT>
+__global__ __launch_bounds__(kThreads) void act_encode_kernel(ActShape h, const S* X, int64_t ld_x, S* Y, int64_t ld_y,
+                                                             ActCkptPtr cx, ActCkptPtr cy) {
+  act_units(h, [&](int64_t row, int unit, bool in) {
+    ActVec<S> x;
+    x.load(X + row * ld_x + unit * 8, in ? h.cols - unit * 8 : 0);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x.at(i);
+    auto keep = [&](const ActCkptPtr& c) {
+      u32x2 q;
+      const uint32_t s = act_quantize(v, q);
+      const int64_t at = row * h.upr + unit;
+      if (in) gstore<u32x2>(c.codes + at * 8, q);
+      if (in && (unit & 3) == 0) gstore<uint8_t>(c.scales + at / 4, (uint8_t)s);
+    };
+    if (cx.codes) keep(cx);
+    if (!Y && !cy.codes) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_value<ACT, sizeof(S) == 2>(v[i]);
+    ActVec<S> y;
+    y.set(v);
+    if (Y && in) y.store(Y + row * ld_y + unit * 8, h.cols - unit * 8);
+    if (cy.codes) {  // of y as stored
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = y.at(i);
+      keep(cy);
+    }
+  });
 }
 
 template <typename S>
-__global__ __launch_bounds__(kThreads) void act_decode_kernel(const char* __restrict__ ckpt, int64_t rows,
-                                                             int64_t cols, S* __restrict__ X, int64_t ld_x) {
-  const ActCkpt c = act_ckpt(rows, cols);
-  const int64_t step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * cols; i += step) {
-    const int64_t r = i / cols, j = i % cols;
-    X[r * ld_x + j] = from_f32<S>(act_load(ckpt, c, r, j));
-  }
+__global__ __launch_bounds__(kThreads) void act_decode_kernel(ActShape h, ActCkptPtr c, S* __restrict__ X,
+                                                             int64_t ld_x) {
+  act_units(h, [&](int64_t row, int unit, bool in) {
+    if (!in) return;
+    const int64_t at = row * h.upr + unit;
+    float v[8];
+    act_expand(gload<u32x2>(c.codes + at * 8), gload<uint8_t>(c.scales + at / 4), v);
+    ActVec<S> x;
+    x.set(v);
+    x.store(X + row * ld_x + unit * 8, h.cols - unit * 8);
+  });
 }
 
 // dX may be dY.
 template <typename S, int ACT>
-__global__ __launch_bounds__(kThreads) void act_grad_kernel(const char* __restrict__ ckpt, int64_t rows, int64_t cols,
-                                                           const S* dY, int64_t ld_dy, S* dX, int64_t ld_dx) {
-  const ActCkpt c = act_ckpt(rows, cols);
-  const int64_t step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * cols; i += step) {
-    const int64_t r = i / cols, j = i % cols;
-    dX[r * ld_dx + j] = from_f32<S>(cvt<float, S>(dY[r * ld_dy + j]) * act_slope<ACT>(act_load(ckpt, c, r, j)));
-  }
+__global__ __launch_bounds__(kThreads) void act_grad_kernel(ActShape h, ActCkptPtr c, const S* dY, int64_t ld_dy,
+                                                           S* dX, int64_t ld_dx) {
+  act_units(h, [&](int64_t row, int unit, bool in) {
+    if (!in) return;
+    const int64_t at = row * h.upr + unit;
+    const u32x2 q = gload<u32x2>(c.codes + at * 8);
+    const uint32_t s = gload<uint8_t>(c.scales + at / 4);
+    ActVec<S> d;
+    d.load(dY + row * ld_dy + unit * 8, h.cols - unit * 8);
+    float v[8];
+    act_expand(q, s, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = d.at(i) * act_slope<ACT, sizeof(S) == 2>(v[i]);
+    d.set(v);
+    d.store(dX + row * ld_dx + unit * 8, h.cols - unit * 8);
+  });
 }
 
 }  // namespace shp

@@ -68,6 +68,25 @@ unsigned act_grid(int64_t n) { return (unsigned)std::min<int64_t>(cdiv64(n, kThr
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// How a pass over a rows x cols tensor and its checkpoint is laid out.
+ActShape act_shape(int64_t rows, int64_t cols) {
+  ActShape h{};
+  h.rows = rows;
+  h.cols = (int)cols;
+  h.upr = (int)(act_ckpt(rows, cols).ldq / 8);
+  h.lp = 2;
+  while (h.lp < 6 && (1 << h.lp) < h.upr) ++h.lp;
+  h.groups = cdiv64(rows, 64 >> h.lp);
+  return h;
+}
+dim3 act_grid2(const ActShape& h) {
+  return dim3((unsigned)cdiv(h.upr, 64), (unsigned)std::min<int64_t>(cdiv64(h.groups, 4), 65535));
+}
+ActCkptPtr act_parts(const void* ckpt, int64_t rows, int64_t cols) {
+  char* p = static_cast<char*>(const_cast<void*>(ckpt));
+  return {p, p ? reinterpret_cast<uint8_t*>(p) + act_ckpt(rows, cols).scales : nullptr};
+}
+
 // Calls f with the activation as a compile-time constant.
 template <typename F>
 void with_act(int act, F&& f) {
@@ -312,14 +331,14 @@ shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_
     if (!aligned16(ckpt_x) || !aligned16(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t n = rows * (act_ckpt(rows, cols).ldq / kActGroup);
+    const ActShape sh = act_shape(rows, cols);
     return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
         with_act(act, [&](auto a) {
-          hipLaunchKernelGGL((act_encode_kernel<S, decltype(a)::value>), dim3(act_grid(n)),
-                             dim3(kThreads), 0, s, (const S*)X, ld_x, rows, cols, (S*)Y, ld_y, (char*)ckpt_x,
-                             (char*)ckpt_y);
+          hipLaunchKernelGGL((act_encode_kernel<S, decltype(a)::value>), act_grid2(sh), dim3(kThreads), 0, s, sh,
+                             (const S*)X, ld_x, (S*)Y, ld_y, act_parts(ckpt_x, rows, cols),
+                             act_parts(ckpt_y, rows, cols));
         });
       });
     });
@@ -336,11 +355,12 @@ shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, 
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const ActShape sh = act_shape(rows, cols);
     return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
-        hipLaunchKernelGGL(act_decode_kernel<S>, dim3(act_grid(rows * cols)), dim3(kThreads), 0, s,
-                           (const char*)ckpt, rows, cols, (S*)X, ld_x);
+        hipLaunchKernelGGL(act_decode_kernel<S>, act_grid2(sh), dim3(kThreads), 0, s, sh, act_parts(ckpt, rows, cols),
+                           (S*)X, ld_x);
       });
     });
   });
@@ -358,12 +378,13 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const ActShape sh = act_shape(rows, cols);
     return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
         with_act(act, [&](auto a) {
-          hipLaunchKernelGGL((act_grad_kernel<S, decltype(a)::value>), dim3(act_grid(rows * cols)),
-                             dim3(kThreads), 0, s, (const char*)ckpt, rows, cols, (const S*)dY, ld_dy, (S*)dX, ld_dx);
+          hipLaunchKernelGGL((act_grad_kernel<S, decltype(a)::value>), act_grid2(sh), dim3(kThreads), 0, s, sh,
+                             act_parts(ckpt, rows, cols), (const S*)dY, ld_dy, (S*)dX, ld_dx);
         });
       });
     });
