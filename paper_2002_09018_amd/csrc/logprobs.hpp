@@ -401,8 +401,6 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
   const int part = (int)(item % q.parts);
   const S* z = static_cast<const S*>(q.logits) + r * q.ld;
   const int begin = part * q.per_part, end = min(q.vocab, begin + q.per_part);
-  float zt = 0.f;
-  const int tg = q.parts == 1 && w == 0 ? logprobs_target<S>(q, r, zt) : -1;
 
   LseStat st = {-kHugeLogit, 0.f, 0.f};
   TopState top;
@@ -422,6 +420,8 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
   };
   int at = begin + w * Block::kN;
   fetch(at);
+  float zt = 0.f;
+  const int tg = q.parts == 1 && w == 0 ? logprobs_target<S>(q, r, zt) : -1;
   for (; at < end; at += W * Block::kN) {
     blk = nxt;
     fetch(at + W * Block::kN);
