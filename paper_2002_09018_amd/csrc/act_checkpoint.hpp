@@ -104,30 +104,28 @@ __device__ __forceinline__ float act_slope(float x) {
 }
 
 // ---------------------------------------------------------------- passes
-// All passes move units of 8 columns, one to a lane: 16 or 32 bytes of a tensor,
-// 8 of the codes; the 4 lanes of a group agree on its scale.  A wave takes 64
-// units of a row, or (rows of up to 32 units) whole rows of 2^lp lanes.
-// blockIdx.x walks along a row, so that neighbouring workgroups touch
-// neighbouring memory.  Bound by memory: 16384 x 4096 in bf16, activation with
-// both checkpoints and their values in 147 us (5.5 TB/s), its gradient in 60 us
-// (5.6 TB/s); two or four units to a lane were 6 and 16% slower.
+// All passes move units of 8 columns, one to a lane in row order: 16 or 32 bytes
+// of a tensor, 8 of the codes; the 4 lanes of a group agree on its scale.  Bound
+// by memory: 16384 x 4096 in bf16, activation with both checkpoints and their
+// values in 144 us (5.6 TB/s), its gradient in 60 us (5.6 TB/s).  Two or four
+// units to a lane were 6 and 16% slower; rows of 4095 take 72 us.
 struct ActShape {
-  int64_t rows;
-  int cols, upr;   // columns, and units of a row (ldq / 8)
-  int lp;          // log2 of the lanes of a row, 6 where it takes a wave or more
-  int64_t groups;  // items along blockIdx.y: rows, or sets of rows
+  int64_t row0, units;   // first row, and units of the launch (below 2^31)
+  int cols, upr;         // columns, and units of a row (ldq / 8)
+  uint32_t magic, shift; // n / upr = (t + (n - t) / 2) >> shift, t the upper half of n magic
 };
 
-// Calls f(row, unit, in) for each unit of the lane; `in` is false past the tensor
+// Calls f(row, unit, in) for the unit of the lane; `in` is false past the tensor
 // (the lanes of a group are in or out together).
 template <typename F>
 __device__ __forceinline__ void act_units(const ActShape& h, F&& f) {
-  const int lane = threadIdx.x & 63, unit = blockIdx.x * 64 + (lane & ((1 << h.lp) - 1));
-  for (int64_t g = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); g < h.groups; g += (int64_t)gridDim.y * 4) {
-    const int64_t row = (g << (6 - h.lp)) + (lane >> h.lp);
-    f(row, unit, row < h.rows && unit < h.upr);
-  }
+  const uint32_t n = blockIdx.x * kThreads + threadIdx.x;
+  const uint32_t t = __umulhi(n, h.magic), row = (t + ((n - t) >> 1)) >> h.shift;
+  f(h.row0 + row, (int)(n - row * h.upr), n < h.units);
 }
+
+// (at element alignment)
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
 
 // 8 elements of a tensor.
 template <typename S>
@@ -149,21 +147,40 @@ struct ActVec {
       }
     }
   }
-  // n of the 8 lie in the row; the others are zeros.
+  // n of the 8 lie in the row; the others are zeros.  A part is 4, 2 and 1
+  // elements (one by one, the last unit of a row of 4095 made the activation
+  // gradient take 84 us instead of 66).
   __device__ __forceinline__ void load(const S* p, int n) {
     if (n >= 8) {
 #pragma unroll
       for (int h = 0; h < (int)sizeof(S) / 2; ++h) raw[h] = gload<u32x4u>(p + 4 * h);
       return;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (sizeof(S) == 4) {
-        raw[i / 4][i % 4] = i < n ? gload<uint32_t>(p + i) : 0u;
-      } else {
-        const uint32_t w = i < n ? (uint32_t)gload<uint16_t>(p + i) : 0u;
-        raw[0][i / 2] = i & 1 ? raw[0][i / 2] | w << 16 : w;
+    const bool four = n > 0 && n & 4, two = n > 0 && n & 2, one = n > 0 && n & 1;
+    const S* p2 = p + (four ? 4 : 0);
+    const S* p1 = p2 + (two ? 2 : 0);
+    if constexpr (sizeof(S) == 4) {
+      u32x4u a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+      if (four) a = gload<u32x4u>(p);
+      if (two) {
+        const u32x2u w = gload<u32x2u>(p2);
+        b[0] = w[0], b[1] = w[1];
       }
+      if (one) {
+        const uint32_t w = gload<uint32_t>(p1);
+        if (two) b[2] = w;
+        else b[0] = w;
+      }
+      raw[0] = four ? a : b;
+      raw[1] = four ? b : a;
+    } else {
+      u32x2u a = {0, 0};
+      uint32_t b = 0, c = 0;
+      if (four) a = gload<u32x2u>(p);
+      if (two) b = gload<u32u>(p2);
+      if (one) c = gload<uint16_t>(p1);
+      const uint32_t lo = two ? b : c, hi = two ? c : 0;
+      raw[0] = four ? u32x4u{a[0], a[1], lo, hi} : u32x4u{lo, hi, 0, 0};
     }
   }
   __device__ __forceinline__ void store(S* p, int n) const {
@@ -172,11 +189,19 @@ struct ActVec {
       for (int h = 0; h < (int)sizeof(S) / 2; ++h) gstore<u32x4u>(p + 4 * h, raw[h]);
       return;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i >= n) continue;
-      if constexpr (sizeof(S) == 4) gstore<uint32_t>(p + i, raw[i / 4][i % 4]);
-      else gstore<uint16_t>(p + i, (uint16_t)(i & 1 ? raw[0][i / 2] >> 16 : raw[0][i / 2]));
+    const bool four = n > 0 && n & 4, two = n > 0 && n & 2, one = n > 0 && n & 1;
+    S* p2 = p + (four ? 4 : 0);
+    S* p1 = p2 + (two ? 2 : 0);
+    if constexpr (sizeof(S) == 4) {
+      if (four) gstore<u32x4u>(p, raw[0]);
+      const u32x4u b = four ? raw[1] : raw[0];
+      if (two) gstore<u32x2u>(p2, u32x2u{b[0], b[1]});
+      if (one) gstore<uint32_t>(p1, two ? b[2] : b[0]);
+    } else {
+      if (four) gstore<u32x2u>(p, u32x2u{raw[0][0], raw[0][1]});
+      const uint32_t b = four ? raw[0][2] : raw[0][0], c = four ? raw[0][3] : raw[0][1];
+      if (two) gstore<u32u>(p2, b);
+      if (one) gstore<uint16_t>(p1, (uint16_t)(two ? c : b));
     }
   }
 };

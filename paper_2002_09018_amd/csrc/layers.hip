@@ -68,19 +68,23 @@ unsigned act_grid(int64_t n) { return (unsigned)std::min<int64_t>(cdiv64(n, kThr
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// How a pass over a rows x cols tensor and its checkpoint is laid out.
-ActShape act_shape(int64_t rows, int64_t cols) {
-  ActShape h{};
-  h.rows = rows;
-  h.cols = (int)cols;
-  h.upr = (int)(act_ckpt(rows, cols).ldq / 8);
-  h.lp = 2;
-  while (h.lp < 6 && (1 << h.lp) < h.upr) ++h.lp;
-  h.groups = cdiv64(rows, 64 >> h.lp);
-  return h;
-}
-dim3 act_grid2(const ActShape& h) {
-  return dim3((unsigned)cdiv(h.upr, 64), (unsigned)std::min<int64_t>(cdiv64(h.groups, 4), 65535));
+// The launches of a pass over a rows x cols tensor and its checkpoint: f(shape,
+// grid) for each.
+template <typename F>
+shampoo_status act_launches(Handle* h, int64_t rows, int64_t cols, hipStream_t s, F&& f) {
+  ActShape sh{};
+  sh.cols = (int)cols;
+  sh.upr = (int)(act_ckpt(rows, cols).ldq / 8);  // at least 4
+  int bits = 0;
+  while ((int64_t(1) << bits) < sh.upr) ++bits;
+  sh.magic = (uint32_t)((((uint64_t(1) << bits) - (uint64_t)sh.upr) << 32) / (uint64_t)sh.upr + 1);
+  sh.shift = (uint32_t)bits - 1;
+  const int64_t most = INT32_MAX / sh.upr;
+  for (sh.row0 = 0; sh.row0 < rows; sh.row0 += most) {
+    sh.units = std::min(most, rows - sh.row0) * sh.upr;
+    STATUS_TRY(launch(h, SHAMPOO_KCLASS_ACT, s, [&] { f(sh, dim3((unsigned)cdiv64(sh.units, kThreads))); }));
+  }
+  return SHAMPOO_OK;
 }
 ActCkptPtr act_parts(const void* ckpt, int64_t rows, int64_t cols) {
   char* p = static_cast<char*>(const_cast<void*>(ckpt));
@@ -331,12 +335,11 @@ shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_
     if (!aligned16(ckpt_x) || !aligned16(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const ActShape sh = act_shape(rows, cols);
-    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+    return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
         with_act(act, [&](auto a) {
-          hipLaunchKernelGGL((act_encode_kernel<S, decltype(a)::value>), act_grid2(sh), dim3(kThreads), 0, s, sh,
+          hipLaunchKernelGGL((act_encode_kernel<S, decltype(a)::value>), grid, dim3(kThreads), 0, s, sh,
                              (const S*)X, ld_x, (S*)Y, ld_y, act_parts(ckpt_x, rows, cols),
                              act_parts(ckpt_y, rows, cols));
         });
@@ -355,11 +358,10 @@ shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, 
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const ActShape sh = act_shape(rows, cols);
-    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+    return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
-        hipLaunchKernelGGL(act_decode_kernel<S>, act_grid2(sh), dim3(kThreads), 0, s, sh, act_parts(ckpt, rows, cols),
+        hipLaunchKernelGGL(act_decode_kernel<S>, grid, dim3(kThreads), 0, s, sh, act_parts(ckpt, rows, cols),
                            (S*)X, ld_x);
       });
     });
@@ -378,12 +380,11 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const ActShape sh = act_shape(rows, cols);
-    return launch(h, SHAMPOO_KCLASS_ACT, s, [&] {
+    return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
       with_type(dtype, [&](auto* type) {
         using S = std::remove_pointer_t<decltype(type)>;
         with_act(act, [&](auto a) {
-          hipLaunchKernelGGL((act_grad_kernel<S, decltype(a)::value>), act_grid2(sh), dim3(kThreads), 0, s, sh,
+          hipLaunchKernelGGL((act_grad_kernel<S, decltype(a)::value>), grid, dim3(kThreads), 0, s, sh,
                              act_parts(ckpt, rows, cols), (const S*)dY, ld_dy, (S*)dX, ld_dx);
         });
       });

@@ -238,6 +238,24 @@ def test_large_checkpoint(env):
     assert not bool(torch.any(out[:-2] != 0))
 
 
+def test_more_units_than_a_launch_takes(env):
+    """Beyond 2^31 units of 8 columns a pass takes several launches."""
+    torch, B, dev, h = env
+    n, c = 131075, 131072
+    say("act several launches", n, c)
+    assert n * (c // 8) > 2 ** 31
+    x = torch.zeros(n, c, device=dev, dtype=torch.bfloat16)
+    x[-5:] = torch.from_numpy(act_input(5, c, 17)).bfloat16().to(dev)
+    last = host(x[-5:].double())
+    cx = torch.empty(B.shampoo_act_checkpoint_bytes(n, c), device=dev, dtype=torch.uint8)
+    B.shampoo_act_encode(h, x, ckpt_x=cx)
+    x.fill_(3.0)
+    B.shampoo_act_decode(h, cx, x)
+    torch.cuda.synchronize()
+    assert np.array_equal(host(x[-5:].double()), L.checkpoint_values(*L.checkpoint(last), c))
+    assert not bool(torch.any(x[:-5] != 0))
+
+
 def test_other_stream_and_graph(env):
     torch, B, dev, h = env
     say("act stream and graph")

@@ -287,6 +287,32 @@ def test_gradient_matches_differences(env):
     assert abs(got - quotient) <= 1e-3 * max(1.0, abs(got))
 
 
+def test_more_rows_than_a_launch_takes(env):
+    """Millions of short rows: the calls split their launches; rows on both
+    sides of every split against the oracle."""
+    torch, B, dev, h = env
+    n, v, k = (1 << 23) + 77, 9, 2
+    say("logprobs many rows", n, v)
+    g = torch.Generator(device=dev).manual_seed(5)
+    z = torch.randn(n, v, device=dev, generator=g)
+    t = torch.randint(0, v, (n,), device=dev, generator=g).to(torch.int32)
+    out = [torch.full((n,), float("nan"), device=dev) for _ in range(3)]
+    ids, top = torch.zeros(n, k, device=dev, dtype=torch.int32), torch.zeros(n, k, device=dev)
+    B.shampoo_token_logprobs(h, z, t, out[0], out[1], entropy=out[2], top_ids=ids, top_logp=top)
+    dz = torch.full_like(z, float("nan"))
+    ones = torch.ones(n, device=dev)
+    B.shampoo_token_logprobs_grad(h, z, t, out[1], dz, g_logp=ones)
+    torch.cuda.synchronize()
+    assert not any(bool(torch.isnan(x).any()) for x in out + [dz])
+    some = torch.cat([torch.arange(c - 3, min(c + 3, n)) for c in (3, 1 << 20, 1 << 21, 1 << 22, 1 << 23, n - 3)])
+    zz, tt = host(z[some.to(dev)].double()), host(t[some.to(dev)])
+    ref = L.token_logprobs(zz, tt, k)
+    for a, b in zip([x[some.to(dev)] for x in out] + [ids[some.to(dev)], top[some.to(dev)]], ref):
+        close(host(a), b, 64 * U * (1 + np.abs(b)), "many rows")
+    dref = L.token_logprobs_grad(zz, tt, host(out[1][some.to(dev)]), g_logp=np.ones(len(tt)))
+    close(host(dz[some.to(dev)].double()), dref, 64 * U, "many rows dlogits")
+
+
 def test_offsets_past_32_bits(env):
     """Rows whose offsets pass 2^31 elements."""
     torch, B, dev, h = env
