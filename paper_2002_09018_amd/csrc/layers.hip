@@ -144,16 +144,14 @@ LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int k, int dtype) {
 
 // How a weight gradient is cut: the tile, and the splits of the token axis.
 struct WgradPlan {
-  int tile = 256, splits = 1;
+  int tile_m = 256, tile_n = 256, splits = 1;
   int64_t per_split = 0, tiles_m = 0, tiles_n = 0;
   size_t ws = 0;
 };
 
-// Estimated time (us) of `blocks` workgroups that work on a stage at a time:
-// full rounds of the chip, then the rest.  `alone` is a stage's time on a
-// lightly filled chip, `full` with every slot taken (clock and bandwidth then
-// are shared), measured over 12 shapes from 300 x 300 x 300 to 65536 x 1024 x
-// 4096; the estimate was within 15% wherever it matters.
+// Estimated time (us) of a stage of every one of `blocks` workgroups: full rounds
+// of the chip, then the rest.  `alone` is a stage's time on a lightly filled
+// chip, `full` with every slot taken (clock and bandwidth then are shared).
 double wgrad_rounds(int64_t blocks, int64_t slots, double alone, double full) {
   const int64_t rest = blocks % slots;
   const double part = rest == 0           ? 0
@@ -163,32 +161,39 @@ double wgrad_rounds(int64_t blocks, int64_t slots, double alone, double full) {
   return (double)(blocks / slots) * full + part;
 }
 
-// The cheapest of 256 x 256 tiles (one workgroup per compute unit) and 128 x
-// 128 tiles (two) with the token axis in up to 128 parts.  Parts cost their
-// partial tiles' way to memory and back (0.2 us per MB) and a second launch:
-//   65536 x 1024 x 4096 (64 large tiles): 1 part 1318 us, 2 673, 4 470, 8 499;
-//     small tiles 632
-//   32768 x 512 x 512: large tiles in 48 parts 36 us; small in 16 34, in 32 33
-//   2048 x 1024 x 1024: large in 6 parts 28 us, small in 2 22
+// The cheapest tile, with the token axis in up to 128 parts, by an estimate from
+// the measured time of a stage; parts cost their partial tiles' way to memory
+// and back (0.2 us per MB) and a second launch.  One workgroup of 256 x 256 or
+// 128 x 256 (bf16 gradients only) takes a compute unit, two of 128 x 128 share
+// one.  Measured (bf16, us, best number of parts of 256 x 256 / 128 x 256 / 128 x
+// 128): 65536 x 1024 x 4096 492 / 579 / 672; 16384 x 1024 x 1024 53 / 48 / 54;
+// 30000 x 300 x 1000 48 / 39 / 44; 2048 x 1024 x 1024 28 / 22 / 20; one part instead
+// of the best: 65536 x 1024 x 4096 1321, 32768 x 512 x 512 (128 x 128) 343 instead of 33.
 WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
   const bool bf16 = dtype == SHAMPOO_BF16;
   const int64_t bk = bf16 ? 64 : 32, stages = std::max<int64_t>(1, cdiv64(rows, bk));
   WgradPlan best;
   double best_us = 0;
-  for (int tile : {128, 256}) {
-    const int64_t tm = cdiv64(cols, tile), tn = cdiv64(out, tile), tiles = tm * tn;
-    const int64_t slots = tile == 256 ? 256 : 512;
-    const double alone = tile == 256 ? (bf16 ? 1.28 : 2.1) : (bf16 ? 0.69 : 0.9);
-    const double full = tile == 256 ? (bf16 ? 1.79 : 2.7) : (bf16 ? 1.23 : 1.62);
+  struct Tile {
+    int m, n, slots;
+    double alone, full, start;  // us: a stage, and a launch beside its stages
+  };
+  static const Tile bf16_tiles[] = {{128, 128, 512, 0.69, 1.23, 3}, {128, 256, 256, 0.81, 1.10, 3}, {256, 256, 256, 1.28, 1.79, 6}};
+  static const Tile f32_tiles[] = {{128, 128, 512, 0.90, 1.62, 3}, {256, 256, 256, 2.10, 2.70, 6}};
+  const Tile* tiles_of = bf16 ? bf16_tiles : f32_tiles;
+  for (int i = 0; i < (bf16 ? 3 : 2); ++i) {
+    const Tile& t = tiles_of[i];
+    const int64_t tm = cdiv64(cols, t.m), tn = cdiv64(out, t.n), tiles = tm * tn;
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
-      if (want > stages || (want > 1 && want * tiles > 2 * slots)) break;
+      if (want > stages || (want > 1 && want * tiles > 2 * t.slots)) break;
       const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
-      const size_t ws = splits > 1 ? (size_t)(splits * tiles) * tile * tile * sizeof(float) : 0;
-      const double us = wgrad_rounds(tiles * splits, slots, alone, full) * (double)per +
+      const size_t ws = splits > 1 ? (size_t)(splits * tiles) * t.m * t.n * sizeof(float) : 0;
+      const double us = t.start + wgrad_rounds(tiles * splits, t.slots, t.alone, t.full) * (double)per +
                         (splits > 1 ? 5 + 0.2e-6 * (double)ws : 0);
       if (best_us == 0 || us < best_us) {
         best_us = us;
-        best.tile = tile;
+        best.tile_m = t.m;
+        best.tile_n = t.n;
         best.splits = (int)splits;
         best.per_split = per * bk;
         best.tiles_m = tm;
@@ -200,10 +205,10 @@ WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
   return best;
 }
 
-template <typename S, typename SG, int T, int WM, int WN>
+template <typename S, typename SG, int TM, int TN, int WM, int WN>
 shampoo_status wgrad_launch(Handle* h, const WgradArgs& q, hipStream_t s) {
-  using L = WgradTile<S, T, WM, WN>;
-  auto k = weight_grad_kernel<S, SG, T, WM, WN>;
+  using L = WgradTile<S, TM, TN, WM, WN>;
+  auto k = weight_grad_kernel<S, SG, TM, TN, WM, WN>;
   // more LDS than a launch may take by default: asked for once per device
   static std::atomic<uint64_t> asked{0};
   const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
@@ -216,9 +221,9 @@ shampoo_status wgrad_launch(Handle* h, const WgradArgs& q, hipStream_t s) {
     hipLaunchKernelGGL(k, dim3((unsigned)(tiles * q.splits)), dim3(L::kThr), L::kLdsB, s, q);
   }));
   if (q.splits == 1) return SHAMPOO_OK;
-  const int64_t pieces = tiles * (T / 32) * (T / 32) * 4;
+  const int64_t pieces = tiles * (TM / 32) * (TN / 32) * 4;
   return launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
-    hipLaunchKernelGGL((weight_grad_sum_kernel<SG, T, WM, WN>), dim3((unsigned)cdiv64(pieces, kThreads / 64)),
+    hipLaunchKernelGGL((weight_grad_sum_kernel<SG, TM, TN, WM, WN>), dim3((unsigned)cdiv64(pieces, kThreads / 64)),
                        dim3(kThreads), 0, s, q);
   });
 }
@@ -449,10 +454,12 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
           st = launch(h, SHAMPOO_KCLASS_WGRAD, s, [&] {
             hipLaunchKernelGGL(weight_grad_scale_kernel<SG>, dim3(act_grid(cols * out)), dim3(kThreads), 0, s, q);
           });
-        else if (p.tile == 256)
-          st = wgrad_launch<S, SG, 256, 128, 64>(h, q, s);
-        else
-          st = wgrad_launch<S, SG, 128, 64, 64>(h, q, s);
+        else if (p.tile_m == 256)
+          st = wgrad_launch<S, SG, 256, 256, 128, 64>(h, q, s);
+        else if (p.tile_n == 128)
+          st = wgrad_launch<S, SG, 128, 128, 64, 64>(h, q, s);
+        else if constexpr (sizeof(S) == 2)
+          st = wgrad_launch<S, SG, 128, 256, 64, 64>(h, q, s);
       });
     });
     return st;

@@ -56,23 +56,26 @@ struct WgradArgs {
   int tiles_m, tiles_n;
 };
 
-// T x T tiles of G; waves of WM x WN.
-template <typename S, int T, int WM, int WN>
+// TM x TN tiles of G; waves of WM x WN.
+template <typename S, int TM, int TN, int WM, int WN>
 struct WgradTile {
   static constexpr int kTerms = sizeof(S) == 2 ? 1 : 3;
   static constexpr int kBk = sizeof(S) == 2 ? 64 : 32;  // tokens of a stage
-  static constexpr int kWavesN = T / WN;
-  static constexpr int kThr = (T / WM) * (T / WN) * 64;
-  static constexpr int kRowB = 2 * T;  // bytes of one token of one operand
-  static constexpr int kPlaneB = kBk * kRowB;
-  static constexpr int kStageB = (1 + kTerms) * kPlaneB;  // a power of two: the buffers are one bit apart
-  static constexpr int kLdsB = 2 * kStageB;
+  static constexpr int kWavesN = TN / WN;
+  static constexpr int kThr = (TM / WM) * (TN / WN) * 64;
+  static constexpr int kRowA = 2 * TM, kRowB = 2 * TN;  // bytes of one token
+  static constexpr int kPlaneA = kBk * kRowA, kPlaneB = kBk * kRowB;
+  static constexpr int kUsedB = kPlaneA + kTerms * kPlaneB;
+  // the buffers are one address bit apart
+  static constexpr int kStageB = kUsedB <= 32768 ? 32768 : 65536;
+  static constexpr int kLdsB = kStageB + kUsedB;
   static constexpr int kBm = WM / 32, kBn = WN / 32;
-  static constexpr int kUa = kBk * (T / 16) / kThr;  // 16-code units of a thread
-  static constexpr int kUb = kBk * (T / 8) / kThr;   // 8-column units of a thread
-  static constexpr int kTa = kThr / (T / 16), kTb = kThr / (T / 8);  // tokens between a thread's units
+  static constexpr int kUa = kBk * (TM / 16) / kThr;  // 16-code units of a thread
+  static constexpr int kUb = kBk * (TN / 8) / kThr;   // 8-column units of a thread
+  static constexpr int kTa = kThr / (TM / 16), kTb = kThr / (TN / 8);  // tokens between a thread's units
   static constexpr int kSteps = kBk / 16;
-  static_assert((kStageB & (kStageB - 1)) == 0 && kSteps % 2 == 0 && kTa % 4 == 0 && kTb % 4 == 0, "");
+  static_assert(kUsedB <= kStageB && kSteps % 2 == 0 && kTa % 4 == 0 && kTb % 4 == 0 && kUa * kTa == kBk &&
+                    kUb * kTb == kBk, "");
 };
 
 typedef __attribute__((address_space(3))) char lds_char;
@@ -88,9 +91,9 @@ __device__ __forceinline__ uint32_t wg_pack(float x, float y) {
 
 // The share of a thread in staging: kUa units of 16 codes and kUb units of 8
 // gradients, each kind in one column range at tokens kTa and kTb apart.
-template <typename S, int T, int WM, int WN>
+template <typename S, int TM, int TN, int WM, int WN>
 struct WgradLoader {
-  using L = WgradTile<S, T, WM, WN>;
+  using L = WgradTile<S, TM, TN, WM, WN>;
   static constexpr int kV = sizeof(S) / 2;  // 16-byte loads of a gradient unit
   const char* pa;
   const uint8_t* ps;
@@ -101,10 +104,10 @@ struct WgradLoader {
   u32x4u b[L::kUb][kV];
 
   __device__ __forceinline__ void init(const WgradArgs& q, int m0, int n0, int tid) {
-    const int ta = tid / (T / 16), piece = tid % (T / 16);
-    la = ta * L::kRowB + (piece ^ wg_swz(ta)) * 32;
-    const int tb = tid / (T / 8), c8 = tid % (T / 8);
-    lb = L::kPlaneB + tb * L::kRowB + ((c8 >> 1) ^ wg_swz(tb)) * 32 + (c8 & 1) * 16;
+    const int ta = tid / (TM / 16), piece = tid % (TM / 16);
+    la = ta * L::kRowA + (piece ^ wg_swz(ta)) * 32;
+    const int tb = tid / (TN / 8), c8 = tid % (TN / 8);
+    lb = L::kPlaneA + tb * L::kRowB + ((c8 >> 1) ^ wg_swz(tb)) * 32 + (c8 & 1) * 16;
     // codes past a row's end and gradients past `out` only feed elements of G
     // that are not stored: any column does, and a unit may run into the next row
     int m = m0 + piece * 16, n = n0 + c8 * 8;
@@ -132,7 +135,7 @@ struct WgradLoader {
       const uint32_t x = a[u][i / 2] >> (16 * (i & 1));
       w[i] = wg_pack((float)(int8_t)(x & 0xff) * s, (float)(int8_t)((x >> 8) & 0xff) * s);
     }
-    lds_u32x4* d = (lds_u32x4*)(stage + la + u * L::kTa * L::kRowB);
+    lds_u32x4* d = (lds_u32x4*)(stage + la + u * L::kTa * L::kRowA);
     d[0] = u32x4{w[0], w[1], w[2], w[3]};
     d[1] = u32x4{w[4], w[5], w[6], w[7]};
   }
@@ -189,7 +192,7 @@ struct WgradLoader {
   // tokens at or past k_end are zeros, columns at or past `out` zeros too.
   __device__ __forceinline__ void tail(const WgradArgs& q, lds_char* stage, int64_t k0, int64_t k_end, int n0,
                                        int tid) {
-    const int left = (int)(k_end - k0), ta = tid / (T / 16), tb = tid / (T / 8), n = n0 + tid % (T / 8) * 8;
+    const int left = (int)(k_end - k0), ta = tid / (TM / 16), tb = tid / (TN / 8), n = n0 + tid % (TN / 8) * 8;
 #pragma unroll
     for (int u = 0; u < L::kUa; ++u) {
       a[u] = u32x4{0, 0, 0, 0};
@@ -237,9 +240,9 @@ __device__ __forceinline__ void wg_store4(const WgradArgs& q, int m, int n, f32x
   }
 }
 
-template <typename S, typename SG, int T, int WM, int WN>
-__global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_grad_kernel(WgradArgs q) {
-  using L = WgradTile<S, T, WM, WN>;
+template <typename S, typename SG, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__((WgradTile<S, TM, TN, WM, WN>::kThr), 2) void weight_grad_kernel(WgradArgs q) {
+  using L = WgradTile<S, TM, TN, WM, WN>;
   extern __shared__ __align__(16) char lds_bytes[];
   lds_char* lds = (lds_char*)lds_bytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -247,7 +250,7 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
   const int l = xcd_remap(blockIdx.x, gridDim.x);
   const int split = l / tiles, t = l % tiles;
   const int tm = t % q.tiles_m, tn = t / q.tiles_m;
-  const int m0 = tm * T, n0 = tn * T;
+  const int m0 = tm * TM, n0 = tn * TN;
   const int64_t kb = split * q.per_split, ke = min(q.rows, kb + q.per_split);
   // Stages from the front that lie whole in the split and whose units of
   // gradients are all readable: where a row's last unit runs past `out`, it
@@ -257,7 +260,7 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
   const int stages = (int)((ke - kb + L::kBk - 1) / L::kBk);
   const int plain = max(0, (int)((min(ke, safe) - kb) / L::kBk));
 
-  WgradLoader<S, T, WM, WN> ld;
+  WgradLoader<S, TM, TN, WM, WN> ld;
   ld.init(q, m0, n0, tid);
 
   // fragment offsets: 16-lane group g reads columns 16 (g & 1).., tokens 8 (g >> 1)..
@@ -266,10 +269,10 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
   int oa[L::kBm], ob[L::kBn];
 #pragma unroll
   for (int i = 0; i < L::kBm; ++i)
-    oa[i] = token * L::kRowB + ((wm / 16 + 2 * i + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
+    oa[i] = token * L::kRowA + ((wm / 16 + 2 * i + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
 #pragma unroll
   for (int j = 0; j < L::kBn; ++j)
-    ob[j] = L::kPlaneB + token * L::kRowB + ((wn / 16 + 2 * j + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
+    ob[j] = L::kPlaneA + token * L::kRowB + ((wn / 16 + 2 * j + side) ^ wg_swz(token)) * 32 + (lane & 3) * 8;
 
   wg_acc acc[L::kBm][L::kBn];
 #pragma unroll
@@ -280,7 +283,7 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
   bf16x8 fa[L::kBm], fb[2][L::kTerms][L::kBn];
-  auto read_a = [&](lds_char* stage, int step, int i) { fa[i] = wg_frag<L::kRowB>(stage + oa[i] + step * 16 * L::kRowB); };
+  auto read_a = [&](lds_char* stage, int step, int i) { fa[i] = wg_frag<L::kRowA>(stage + oa[i] + step * 16 * L::kRowA); };
   auto read_b = [&](lds_char* stage, int step, int set) {
 #pragma unroll
     for (int p = 0; p < L::kTerms; ++p)
@@ -392,9 +395,9 @@ __global__ __launch_bounds__((WgradTile<S, T, WM, WN>::kThr), 2) void weight_gra
 
 // G from the partial tiles, added in split order: one wave per 4 accumulator
 // elements of a 32 x 32 block.
-template <typename SG, int T, int WM, int WN>
+template <typename SG, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(kThreads) void weight_grad_sum_kernel(WgradArgs q) {
-  constexpr int kPerTile = (T / 32) * (T / 32) * 4;  // 64-lane pieces of a tile
+  constexpr int kPerTile = (TM / 32) * (TN / 32) * 4;  // 64-lane pieces of a tile
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   const int tiles = q.tiles_m * q.tiles_n;
@@ -403,8 +406,8 @@ __global__ __launch_bounds__(kThreads) void weight_grad_sum_kernel(WgradArgs q) 
   const int v = piece & 3, blk = piece >> 2;
   constexpr int kBm = WM / 32, kBn = WN / 32;
   const int wave = blk / (kBm * kBn), i = blk % (kBm * kBn) / kBn, j = blk % kBn;
-  const int m = t % q.tiles_m * T + wave / (T / WN) * WM + i * 32 + v * 8 + (lane >> 5) * 4;
-  const int n = t / q.tiles_m * T + wave % (T / WN) * WN + j * 32 + (lane & 31);
+  const int m = t % q.tiles_m * TM + wave / (TN / WN) * WM + i * 32 + v * 8 + (lane >> 5) * 4;
+  const int n = t / q.tiles_m * TN + wave % (TN / WN) * WN + j * 32 + (lane & 31);
   const f32x4* d = reinterpret_cast<const f32x4*>(q.part) + w * 64 + lane;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
