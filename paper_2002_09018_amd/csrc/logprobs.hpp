@@ -127,13 +127,15 @@ struct TopList {
   // The n <= 64 entries (x, j) of lanes 0..n-1, sorted: each lane counts the
   // entries before its own and passes it to that lane.
   __device__ __forceinline__ void sort(float x, int j, int n, int lane) {
-    int rank = lane < n ? 0 : lane;
-    for (int o = 0; o < n; ++o) {
-      const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), o));
-      const int i2 = __builtin_amdgcn_readlane(j, o);
-      rank += lane < n && better(y, i2, x, j);
-    }
     if (lane >= n) x = -INFINITY, j = INT32_MAX;
+    int rank = lane < n ? 0 : lane - n;  // all n come before an absent one, none after
+    for (int o = 0; o < n; o += 4)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), o + u));
+        const int i2 = __builtin_amdgcn_readlane(j, o + u);
+        rank += better(y, i2, x, j);
+      }
     v = __uint_as_float(__builtin_amdgcn_ds_permute(rank * 4, __float_as_uint(x)));
     i = __builtin_amdgcn_ds_permute(rank * 4, j);
   }
@@ -179,6 +181,27 @@ __device__ __forceinline__ void top_select(TopList& top, int sets, float low, in
       top.insert_lanes(y > low ? y : -INFINITY, j + i, k, lane);
     }
   }
+}
+
+// The k best of n entries, get(e, x, j) the e-th.
+template <typename G>
+__device__ __forceinline__ void top_join(TopList& top, int n, int k, int lane, float* pv, int* pi, G&& get) {
+  auto set = [&](int c, float (&x)[1], int& j) {
+    const int e = c * 64 + lane;
+    x[0] = -INFINITY, j = INT32_MAX;
+    if (e < n) get(e, x[0], j);
+  };
+  const int sets = (n + 63) / 64;
+  float most = -INFINITY;
+#pragma unroll 4
+  for (int c = 0; c < sets; ++c) {
+    float x[1];
+    int j;
+    set(c, x, j);
+    most = fmaxf(most, x[0]);
+  }
+  top.clear();
+  top_select<1>(top, sets, first_cut(most, k), k, lane, pv, pi, set);
 }
 
 // The entries of a wave that may be among the k largest, while it walks its
@@ -444,15 +467,11 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
     if (w != 0) return;
 #pragma unroll
     for (int o = 1; o < W; ++o) st = lse_join(st, {sm[o][0], sm[o][1], sm[o][2]});
-    if (q.k) {
-      const int n = (W - 1) * q.k;
-      auto get = [&](int c, float (&x)[1], int& j) {
-        const int e = c * 64 + lane, o = 1 + e % (W - 1), i = e / (W - 1);
-        x[0] = e < n ? sv[o][i] : -INFINITY;
-        j = e < n ? si[o][i] : INT32_MAX;
-      };
-      top_select<1>(top.list, (n + 63) / 64, top.low, q.k, lane, pieces->pv, pieces->pi, get);
-    }
+    if (q.k)
+      top_join(top.list, W * q.k, q.k, lane, pieces->pv, pieces->pi, [&](int e, float& x, int& j) {
+        x = sv[e % W][e / W];
+        j = si[e % W][e / W];
+      });
   }
   if (q.parts == 1) {
     logprobs_finish(q, r, st, top.list, tg, zt, lane);
@@ -481,23 +500,12 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
   __shared__ int pi[64];
   TopList top;
   top.clear();
-  if (q.k) {
-    const int n = q.parts * q.k;
-    auto get = [&](int c, float (&x)[1], int& j) {
-      const int e = c * 64 + lane;
-      const float* p = rec + (e < n ? e % q.parts * logprob_record(q.k) + 4 + e / q.parts : 0);
-      x[0] = e < n ? p[0] : -INFINITY;
-      j = e < n ? __float_as_int(p[q.k]) : INT32_MAX;
-    };
-    float most = -INFINITY;
-    for (int c = 0; c * 64 < n; ++c) {
-      float x[1];
-      int j;
-      get(c, x, j);
-      most = fmaxf(most, x[0]);
-    }
-    top_select<1>(top, (n + 63) / 64, first_cut(most, q.k), q.k, lane, pv, pi, get);
-  }
+  if (q.k)
+    top_join(top, q.parts * q.k, q.k, lane, pv, pi, [&](int e, float& x, int& j) {
+      const float* p = rec + e % q.parts * logprob_record(q.k) + 4 + e / q.parts;
+      x = p[0];
+      j = __float_as_int(p[q.k]);
+    });
   logprobs_finish(q, r, st, top, tg, zt, lane);
 }
 
