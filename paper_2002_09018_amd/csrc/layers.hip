@@ -116,11 +116,13 @@ constexpr int64_t kMostItems = 1 << 22;  // parts of rows of one launch
 // (parts) of a row where there are few rows.  About two waves per SIMD are
 // wanted: fewer do not keep enough bytes in flight, and each wave of a row pays
 // for finding its own first alternatives.  Rows x 131072 in bf16, 8
-// alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 384 / 385 / 388 / 409, 1024
-// rows 71 / 53 / 51 / 70, 256 rows (4 / 8 / 4 in two parts) 28 / 25 / 27; without
-// alternatives 8192 rows 379 / 374 / 356 / 356.  Below 256 rows parts of 4 waves
-// and a second launch to join them: one row 13 us, by one workgroup of 16
-// waves 19; 64 rows 16 (8 waves without parts 21).
+// alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 388 / 384 / 382 / 445, 1024
+// rows 74 / 56 / 52 / 60, 256 rows 69 / 43 / 28 / 23; without alternatives 8192
+// rows 381 / 377 / 356 / 361.  Below 256 rows long rows are cut into parts of 4
+// waves and a second launch joins them: one row 12 us, by one workgroup of 8
+// waves 19; 64 rows 15 and 20.  Rows of few blocks to a wave do without: 1 x 32768
+// 10.0 us, in parts 11.9, 128 x 32768 10.7 and 13.1; 1 x 65536 13.3 and 11.3, without
+// alternatives 8.8 and 10.8.
 struct LogprobPlan {
   int waves = 1, parts = 1, per_part = 0;
   size_t ws = 0;
@@ -131,10 +133,11 @@ LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int k, int dtype) {
   const int64_t block = dtype == SHAMPOO_BF16 ? LogitBlock<uint16_t>::kN : LogitBlock<float>::kN;
   const int64_t blocks = cdiv64(vocab, block);
   const int64_t want = std::min(std::max<int64_t>(cdiv64(2048, rows), k == 0 ? 4 : 1), blocks);
-  const int most = rows >= 256 ? 8 : 4;
+  const bool whole = rows >= 256 || blocks <= (k == 0 ? 48 : 16);
+  const int most = whole ? 8 : 4;
   while (p.waves < want && p.waves < most) p.waves *= 2;
   const int64_t steps = cdiv64(blocks, p.waves);
-  const int64_t parts = rows >= 256 ? 1 : std::min<int64_t>(cdiv64(want, p.waves), 64);
+  const int64_t parts = whole ? 1 : std::min<int64_t>(cdiv64(want, p.waves), 64);
   const int64_t per = cdiv64(steps, parts);
   p.parts = (int)cdiv64(steps, per);
   p.per_part = (int)std::min<int64_t>(per * p.waves * block, vocab);
