@@ -107,8 +107,8 @@ __device__ __forceinline__ float act_slope(float x) {
 // All passes move units of 8 columns, one to a lane in row order: 16 or 32 bytes
 // of a tensor, 8 of the codes; the 4 lanes of a group agree on its scale.  Bound
 // by memory: 16384 x 4096 in bf16, activation with both checkpoints and their
-// values in 144 us (5.6 TB/s), its gradient in 60 us (5.6 TB/s).  Two or four
-// units to a lane were 6 and 16% slower; rows of 4095 take 72 us.
+// values in 142 us (5.7 TB/s), its gradient in 60 us (5.6 TB/s).  Two or four
+// units to a lane were 6 and 16% slower; rows of 4095 take 167 and 65 us.
 struct ActShape {
   int64_t row0, units;   // first row, and units of the launch (below 2^31)
   int cols, upr;         // columns, and units of a row (ldq / 8)
@@ -149,7 +149,7 @@ struct ActVec {
   }
   // n of the 8 lie in the row; the others are zeros.  A part is 4, 2 and 1
   // elements (one by one, the last unit of a row of 4095 made the activation
-  // gradient take 84 us instead of 66).
+  // gradient take 84 us instead of 65).
   __device__ __forceinline__ void load(const S* p, int n) {
     if (n >= 8) {
 #pragma unroll

