@@ -540,9 +540,13 @@ struct LossGradArgs {
 //   dz_j = p_j (S - g_H (ln p_j + H)) + the outputs' gradients at their entries,
 //   S = g_lse - g_logp - the sum of the alternatives' gradients.
 // Bound by memory: 8192 x 131072 in bf16, with entropy and 8 alternatives, in 731
-// us (5.9 TB/s); 1021 x 50001 in 39 us (5.2 TB/s).
+// us (5.9 TB/s); 1021 x 50001 in 39 us (5.2 TB/s).  More waves on the chip than the
+// memory needs cost time: fp32 rows take 3 to a SIMD (4096 x 131072: 733 us, 804
+// with 4, 828 with 2; 4096 x 5000: 35.0, 33.5 and 39.6), bf16 rows the 4 that their
+// registers leave (large 737, with 3 788; 8192 x 5000: 36.9 and 42.0).
 template <typename S, bool ENT>
-__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LossGradArgs q) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, sizeof(S) == 4 ? 3 : 4)))
+void logprobs_grad_kernel(LossGradArgs q) {
   using Block = LogitBlock<S>;
   constexpr int kV = Block::kV, kU = Block::kU, kN = Block::kN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
