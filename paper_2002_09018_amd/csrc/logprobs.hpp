@@ -39,7 +39,7 @@ __device__ __forceinline__ bool better(float v, int i, float w, int j) { return 
 // (in LDS), and they are ranked once, at the end.  8192 x 131072 in bf16 with 8
 // alternatives: 390 us, 5.5 TB/s, bound by memory; 1 x 32768: 10 us, the latency of
 // a launch, a load and the ranking.  Small rows are bound by the ranking: 8192 x
-// 5000 in 32 us (2.5 TB/s).
+// 5000 in 32 us (2.5 TB/s), 92 with 64 alternatives.
 constexpr float kLog2e = 1.44269502f;
 constexpr float kHugeLogit = 1e6f;
 
@@ -88,16 +88,28 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// A cut below the k-th largest of the lanes' values x, by bisection over the
-// upper 16 bits of their order.
-__device__ __forceinline__ float first_cut(float x, int k) {
-  const uint32_t b = __float_as_uint(x + 0.f);  // -0 orders with 0
-  const uint32_t key = ((b & 0x80000000u) ? ~b : b | 0x80000000u) >> 16;
+// A cut below the k-th largest of the lanes' values x and y, by bisection over
+// the upper 16 bits of their order.  Up to k = 32 the larger of a lane's two
+// stands for both: half the ballots, and nearly as good a cut.
+__device__ __forceinline__ float first_cut(float x, float y, int k) {
+  auto order = [](float v) {
+    const uint32_t b = __float_as_uint(v + 0.f);  // -0 orders with 0
+    return ((b & 0x80000000u) ? ~b : b | 0x80000000u) >> 16;
+  };
   uint32_t at = 0;
+  if (k <= 32) {
+    const uint32_t key = order(fmaxf(x, y));
 #pragma unroll
-  for (int bit = 15; bit >= 0; --bit) {
-    const uint32_t t = at | 1u << bit;
-    if (__popcll(__ballot(key >= t)) >= k) at = t;
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t t = at | 1u << bit;
+      if (__popcll(__ballot(key >= t)) >= k) at = t;
+    }
+  } else {
+    const uint32_t kx = order(x), ky = order(y);
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t t = at | 1u << bit;
+      if (__popcll(__ballot(kx >= t)) + __popcll(__ballot(ky >= t)) >= k) at = t;
+    }
   }
   const uint32_t o = at << 16;
   const uint32_t f = (o & 0x80000000u) ? o & 0x7fffffffu : ~o;
@@ -146,12 +158,31 @@ struct TopList {
     v = __uint_as_float(__builtin_amdgcn_ds_permute(rank * 4, __float_as_uint(x)));
     i = __builtin_amdgcn_ds_permute(rank * 4, j);
   }
+  // The 64 best of the 64 < n <= 128 entries in pv and pi (LDS), sorted.
+  __device__ __forceinline__ void sort_two(float* pv, int* pi, int n, int lane) {
+    const float x = pv[lane], y = lane + 64 < n ? pv[lane + 64] : -INFINITY;
+    const int j = pi[lane], l = lane + 64 < n ? pi[lane + 64] : INT32_MAX;
+    wave_lds_order();
+    int rx = 0, ry = 0;
+    auto count = [&](float a, int b, int o) {
+      const float z = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(a), o));
+      const int i2 = __builtin_amdgcn_readlane(b, o);
+      rx += better(z, i2, x, j), ry += better(z, i2, y, l);
+    };
+#pragma unroll 4
+    for (int o = 0; o < 64; ++o) count(x, j, o);
+    for (int o = 0; o < n - 64; ++o) count(y, l, o);
+    if (rx < 64) pv[rx] = x, pi[rx] = j;
+    if (ry < 64) pv[ry] = y, pi[ry] = l;  // an absent one comes after all n
+    wave_lds_order();
+    v = pv[lane], i = pi[lane];
+  }
 };
 
 // The k best of `top` and of `sets` sets of 64 N entries: get(c, x, j) gives a
 // lane's N of set c, of consecutive indices from j (x = -inf: none).  No entry up
 // to `low` is wanted.  What is above it is gathered in LDS and sorted; where
-// that is more than 64 entries (equal values, large k), one by one.
+// that is more than 128 entries (equal values), one by one.
 template <int N, typename G>
 __device__ __forceinline__ void top_select(TopList& top, int sets, float low, int k, int lane, float* pv, int* pi,
                                            G&& get) {
@@ -159,7 +190,7 @@ __device__ __forceinline__ void top_select(TopList& top, int sets, float low, in
   auto gather = [&](float x, int j) {
     const uint64_t in = __ballot(x > low);
     const int at = n + lanes_below(in);
-    if (x > low && at < 64) pv[at] = x, pi[at] = j;
+    if (x > low && at < 128) pv[at] = x, pi[at] = j;
     n += __popcll(in);
   };
   gather(top.v, top.i);
@@ -173,6 +204,11 @@ __device__ __forceinline__ void top_select(TopList& top, int sets, float low, in
   wave_lds_order();
   if (n <= 64) {
     top.sort(pv[lane], pi[lane], n, lane);
+    wave_lds_order();
+    return;
+  }
+  if (n <= 128) {
+    top.sort_two(pv, pi, n, lane);
     wave_lds_order();
     return;
   }
@@ -199,16 +235,18 @@ __device__ __forceinline__ void top_join(TopList& top, int n, int k, int lane, f
     if (e < n) get(e, x[0], j);
   };
   const int sets = (n + 63) / 64;
-  float most = -INFINITY;
-#pragma unroll 4
-  for (int c = 0; c < sets; ++c) {
-    float x[1];
-    int j;
-    set(c, x, j);
-    most = fmaxf(most, x[0]);
-  }
+  float most[2] = {-INFINITY, -INFINITY};  // of even and odd sets
+#pragma unroll 2
+  for (int c = 0; c < sets; c += 2)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[1];
+      int j;
+      set(c + h, x, j);
+      most[h] = fmaxf(most[h], x[0]);
+    }
   top.clear();
-  top_select<1>(top, sets, first_cut(most, k), k, lane, pv, pi, set);
+  top_select<1>(top, sets, first_cut(most[0], most[1], k), k, lane, pv, pi, set);
 }
 
 // The entries of a wave that may be among the k largest, while it walks its
@@ -217,17 +255,17 @@ struct TopPieces {
   static constexpr int kCap = 320;  // 64, and the 256 of a block
   u32x4 raw[kCap];
   int at[kCap];
-  float pv[64];  // for top_select
-  int pi[64];
+  float pv[128];  // for top_select
+  int pi[128];
 };
 struct TopState {
   TopList list;  // the best so far of the pieces already gone through
-  float most;    // the lane's largest entry so far
+  float most[2]; // the lane's largest entries so far, of the first and the second halves of blocks
   float low;     // no entry of the row up to it is wanted
   float bar;     // no later entry of this wave up to it is wanted
   int n, blocks;
 
-  __device__ __forceinline__ void clear() { list.clear(), most = low = bar = -INFINITY, n = blocks = 0; }
+  __device__ __forceinline__ void clear() { list.clear(), most[0] = most[1] = low = bar = -INFINITY, n = blocks = 0; }
   __device__ __forceinline__ void raise(float x) { low = fmaxf(low, x), bar = fmaxf(bar, x); }
 };
 
@@ -320,12 +358,13 @@ struct LogitBlock {
       st.m = n;
     }
     if (k == 0) return;
-    top.most = fmaxf(top.most, bm);
+    top.most[0] = fmaxf(top.most[0], fmaxf(um[0], um[1]));
+    top.most[1] = fmaxf(top.most[1], fmaxf(um[2], um[3]));
     top.raise(floor_);
-    // k lanes hold an entry at or above the k-th of the lanes' largest: a bound
+    // k entries are at or above the k-th of the lanes' largest: a bound
     // worth its 16 ballots whenever the number of blocks has doubled
     ++top.blocks;
-    if ((top.blocks & (top.blocks - 1)) == 0) top.raise(first_cut(top.most, k));
+    if ((top.blocks & (top.blocks - 1)) == 0) top.raise(first_cut(top.most[0], top.most[1], k));
     if (!__any(bm > top.bar)) return;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
@@ -503,8 +542,8 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
     st = {p[0], p[1], p[2]};
   }
   st = lse_wave(st);
-  __shared__ float pv[64];
-  __shared__ int pi[64];
+  __shared__ float pv[128];
+  __shared__ int pi[128];
   TopList top;
   top.clear();
   if (q.k)

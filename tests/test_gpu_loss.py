@@ -143,6 +143,17 @@ def test_orders_and_ties(env, kind, k):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k", [31, 32, 33, 48, 63, 64])
+def test_many_alternatives(env, k, dtype):
+    """Large k in rows of one block, of several waves and of several parts."""
+    torch, B, dev, h = env
+    for n, v in ((5, 70), (300, 1000), (9, 5000), (2, 32768), (3, 131072), (257, 9001)):
+        say("logprobs many alternatives", n, v, k, dtype)
+        z, t = logits(n, v, v + k)
+        check(env, place(torch, dev, z, getattr(torch, dtype), 1)[1], t, k)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("v", [40, 1000, 33000])
 def test_extreme_values(env, v, dtype):
     """The type's lowest value as a mask (alone it is a uniform row), values
