@@ -154,39 +154,41 @@ struct WgradPlan {
 
 // Estimated time (us) of a stage of every one of `blocks` workgroups: full rounds
 // of the chip, then the rest.  `alone` is a stage's time on a lightly filled
-// chip, `full` with every slot taken (clock and bandwidth then are shared).
+// chip, `full` with every slot taken (clock and bandwidth then are shared, and
+// compute units where a workgroup leaves room for a second).
 double wgrad_rounds(int64_t blocks, int64_t slots, double alone, double full) {
   const int64_t rest = blocks % slots;
-  const double part = rest == 0           ? 0
-                      : 2 * rest <= slots ? alone
-                      : slots == 512      ? full  // some compute unit holds two
-                                          : alone + (full - alone) * (2 * rest - slots) / slots;
+  const double part = rest == 0      ? 0
+                      : slots == 512 ? (rest <= 256 ? alone * (1 + rest / 1280.0) : full)
+                      : rest <= 128  ? alone
+                                     : alone + (full - alone) * (rest - 128) / 128;
   return (double)(blocks / slots) * full + part;
 }
 
 // The cheapest tile, with the token axis in up to 128 parts, by an estimate from
 // the measured time of a stage; parts cost their partial tiles' way to memory
-// and back (0.2 us per MB) and a second launch.  One workgroup of 256 x 256 or
-// 128 x 256 (bf16 gradients only) takes a compute unit, two of 128 x 128 share
-// one.  Measured (bf16, us, best number of parts of 256 x 256 / 128 x 256 / 128 x
-// 128): 65536 x 1024 x 4096 492 / 579 / 672; 16384 x 1024 x 1024 53 / 48 / 54;
-// 30000 x 300 x 1000 48 / 39 / 44; 2048 x 1024 x 1024 28 / 22 / 20; one part instead
-// of the best: 65536 x 1024 x 4096 1321, 32768 x 512 x 512 (128 x 128) 343 instead of 33.
+// and back (0.2 us per MB) and a second launch.  One workgroup takes a compute
+// unit; two of 128 x 128 share one with bf16 gradients, for which alone there is
+// 128 x 256.  Measured (bf16, us, best number of parts of 256 x 256 / 128 x 256 /
+// 128 x 128): 65536 x 1024 x 4096 492 / 579 / 666; 16384 x 1024 x 1024 53 / 48 / 55;
+// 30000 x 300 x 1000 48 / 39 / 43; 2048 x 1024 x 1024 28 / 22 / 19; one part instead of
+// the best: 65536 x 1024 x 4096 1321, 32768 x 512 x 512 (128 x 128) 288 instead of 31.
 WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
   const bool bf16 = dtype == SHAMPOO_BF16;
-  const int64_t bk = bf16 ? 64 : 32, stages = std::max<int64_t>(1, cdiv64(rows, bk));
   WgradPlan best;
   double best_us = 0;
   struct Tile {
-    int m, n, slots;
+    int m, n, bk, slots;        // bk: tokens of a stage
     double alone, full, start;  // us: a stage, and a launch beside its stages
   };
-  static const Tile bf16_tiles[] = {{128, 128, 512, 0.69, 1.23, 3}, {128, 256, 256, 0.81, 1.10, 3}, {256, 256, 256, 1.28, 1.79, 6}};
-  static const Tile f32_tiles[] = {{128, 128, 512, 0.90, 1.62, 3}, {256, 256, 256, 2.10, 2.70, 6}};
+  static const Tile bf16_tiles[] = {
+      {128, 128, 64, 512, 0.56, 1.31, 3}, {128, 256, 64, 256, 0.81, 1.10, 3}, {256, 256, 64, 256, 1.28, 1.79, 6}};
+  static const Tile f32_tiles[] = {{128, 128, 64, 256, 1.37, 1.60, 3}, {256, 256, 32, 256, 2.10, 2.70, 6}};
   const Tile* tiles_of = bf16 ? bf16_tiles : f32_tiles;
   for (int i = 0; i < (bf16 ? 3 : 2); ++i) {
     const Tile& t = tiles_of[i];
     const int64_t tm = cdiv64(cols, t.m), tn = cdiv64(out, t.n), tiles = tm * tn;
+    const int64_t stages = std::max<int64_t>(1, cdiv64(rows, t.bk));
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
       if (want > stages || (want > 1 && want * tiles > 2 * t.slots)) break;
       const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
@@ -198,7 +200,7 @@ WgradPlan wgrad_plan(int64_t rows, int64_t cols, int64_t out, int dtype) {
         best.tile_m = t.m;
         best.tile_n = t.n;
         best.splits = (int)splits;
-        best.per_split = per * bk;
+        best.per_split = per * t.bk;
         best.tiles_m = tm;
         best.tiles_n = tn;
         best.ws = ws;
@@ -460,7 +462,7 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
         else if (p.tile_m == 256)
           st = wgrad_launch<S, SG, 256, 256, 128, 64>(h, q, s);
         else if (p.tile_n == 128)
-          st = wgrad_launch<S, SG, 128, 128, 64, 64>(h, q, s);
+          st = wgrad_launch<S, SG, 128, 128, 64, 32>(h, q, s);
         else if constexpr (sizeof(S) == 2)
           st = wgrad_launch<S, SG, 128, 256, 64, 64>(h, q, s);
       });
