@@ -118,7 +118,8 @@ constexpr int64_t kMostItems = 1 << 22;  // parts of rows of one launch
 // for finding its own first alternatives.  Rows x 131072 in bf16, 8
 // alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 388 / 384 / 382 / 445, 1024
 // rows 74 / 56 / 52 / 60, 256 rows 69 / 43 / 28 / 23; without alternatives 8192
-// rows 381 / 377 / 356 / 361.  Below 256 rows long rows are cut into parts of 4
+// rows 381 / 377 / 356 / 361, of 65536 205 / 195 / 188 / 203, of 20000 66 / 67 / 75 /
+// 106.  Below 256 rows long rows are cut into parts of 4
 // waves and a second launch joins them: one row 12 us, by one workgroup of 8
 // waves 19; 64 rows 15 and 20.  Rows of few blocks to a wave do without: 1 x 32768
 // 10.0 us, in parts 11.9, 128 x 32768 10.7 and 13.1; 1 x 65536 13.3 and 11.3, without
@@ -132,7 +133,7 @@ LogprobPlan logprob_plan(int64_t rows, int64_t vocab, int k, int dtype) {
   LogprobPlan p;
   const int64_t block = dtype == SHAMPOO_BF16 ? LogitBlock<uint16_t>::kN : LogitBlock<float>::kN;
   const int64_t blocks = cdiv64(vocab, block);
-  const int64_t want = std::min(std::max<int64_t>(cdiv64(2048, rows), k == 0 ? 4 : 1), blocks);
+  const int64_t want = std::min(std::max<int64_t>(cdiv64(2048, rows), k == 0 && blocks >= 32 ? 4 : 1), blocks);
   const bool whole = rows >= 256 || blocks <= (k == 0 ? 48 : 16);
   const int most = whole ? 8 : 4;
   while (p.waves < want && p.waves < most) p.waves *= 2;

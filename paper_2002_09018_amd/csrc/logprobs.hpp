@@ -286,6 +286,8 @@ struct LogitBlock {
       const int at = (u * 64 + lane) * kV;
       if (at >= lo && at + kV <= hi) {
         raw[u] = gload<u32x4u>(z + at);
+      } else if (at + kV <= lo || at >= hi) {
+        raw[u] = sizeof(S) == 4 ? 0xff800000u : 0xff80ff80u;
       } else {
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
