@@ -26,13 +26,14 @@ __device__ __forceinline__ bool better(float v, int i, float w, int j) { return 
 
 // ---------------------------------------------------------------- statistics
 // One pass over a row.  Each lane keeps the largest entry m so far and
-//   s = sum 2^(L z - c),  t = sum (L z - c) 2^(L z - c),  c = L m,
-// L the fp32 value of log2 e, so that lse = (c + log2 s) / L and the entropy is
-// (log2 s - t / s) / L.  Everything is relative to the fp32 number c: one fma
-// gives an exponent, and c's own rounding cancels (the largest entry's exponent
-// is that rounding, at most 2^-24 |c|, not 0).  A largest entry beyond 1e6 in
-// size (a type's lowest value used as a mask, alone in its row) would lose too
-// much so: it takes (z - m) L instead.
+//   s = sum e^(z - m),  t = sum (z - m) e^(z - m),
+// so that lse = m + log s and the entropy is log s - t / s.  The differences are
+// taken before they are scaled for the base-2 exponential: one instruction more
+// than a fused L z - L m, whose rounded L m would be another reference than m.
+// So the largest term is exactly 1, s >= 1 and t <= 0 hold through every join,
+// log probabilities never exceed 0 and entropies never fall below it, and
+// logits of any size (a type's lowest value used as a mask, alone in its row) are
+// as exact as small ones.
 //
 // A wave walks its blocks of 4 KB with the next one in flight.  The alternatives
 // cost a comparison with a bound per 16-byte piece: only pieces above it are kept
@@ -41,27 +42,19 @@ __device__ __forceinline__ bool better(float v, int i, float w, int j) { return 
 // a launch, a load and the ranking.  Small rows are bound by the ranking: 8192 x
 // 5000 in 31 us (2.6 TB/s), 92 with 64 alternatives.
 constexpr float kLog2e = 1.44269502f;
-constexpr float kHugeLogit = 1e6f;
+constexpr float kLowest = -3.40282347e38f;
 
 struct LseStat {
-  float m, s, t;  // m = -kHugeLogit and s = 0 before any entry
+  float m, s, t;  // m = kLowest and s = 0 before any entry
 };
 
-// c as a rounded number: fused into a later sum it would be another one.
-__device__ __forceinline__ float lse_ref(float m) {
-#pragma clang fp contract(off)
-  return m * kLog2e;
-}
-// Exponent of the factor that carries sums from reference m to reference n >= m.
-__device__ __forceinline__ float lse_shift(float m, float n) {
-  float d = fabsf(m) > kHugeLogit || fabsf(n) > kHugeLogit ? (m - n) * kLog2e : lse_ref(m) - lse_ref(n);
-  if (m == n) d = 0.f;
-  return fminf(fmaxf(d, -1e30f), 0.f);  // finite: it multiplies s, which may be 0
-}
+// What carries sums from reference m to reference n >= m: m - n, finite, for it
+// multiplies s, which may be 0.
+__device__ __forceinline__ float lse_shift(float m, float n) { return fmaxf(m - n, -1e20f); }
+__device__ __forceinline__ float lse_exp(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 __device__ __forceinline__ LseStat lse_join(LseStat a, LseStat b) {
-  const float n = a.s == 0.f ? b.m : b.s == 0.f ? a.m : fmaxf(a.m, b.m);
-  const float da = lse_shift(a.m, n), db = lse_shift(b.m, n);
-  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  const float n = fmaxf(a.m, b.m), da = lse_shift(a.m, n), db = lse_shift(b.m, n);
+  const float fa = lse_exp(da), fb = lse_exp(db);
   return {n, a.s * fa + b.s * fb, (a.t + da * a.s) * fa + (b.t + db * b.s) * fb};
 }
 __device__ __forceinline__ LseStat lse_wave(LseStat a) {
@@ -307,24 +300,21 @@ struct LogitBlock {
     return __uint_as_float(i & 1 ? raw[u][i / 2] & 0xffff0000u : raw[u][i / 2] << 16);
   }
 
-  // The block's s and t against reference n, c = L n; only its first `count`
-  // entries may be allowed (quarters past them are left out: 8192 x 1000 in bf16 17.8
-  // -> 17.0 us).  FAR: also where n is beyond kHugeLogit (`far`).  The lower bound
-  // on x makes an entry that is not allowed add 0 to t (it would be 0 times -inf).
-  template <bool ENT, bool FAR>
-  __device__ __forceinline__ void sums(float n, float c, bool far, int count, float& s, float& t) const {
+  // The block's s and t against reference n; only its first `count` entries may
+  // be allowed (quarters past them are left out: 8192 x 1000 in bf16 17.8 -> 17.0
+  // us).  The lower bound on d makes an entry that is not allowed add 0 to t (it
+  // would be 0 times -inf).
+  template <bool ENT>
+  __device__ __forceinline__ void sums(float n, int count, float& s, float& t) const {
     s = t = 0.f;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       if (u * 64 * kV >= count) break;
 #pragma unroll
       for (int i = 0; i < kV; ++i) {
-        const float z = at(u, i);
-        float x = fmaf(z, kLog2e, -c);
-        if (FAR) x = far ? (z - n) * kLog2e : x;
-        const float e = __builtin_amdgcn_exp2f(x);
+        const float d = at(u, i) - n, e = lse_exp(d);
         s += e;
-        if (ENT) t = fmaf(fmaxf(x, -1e30f), e, t);
+        if (ENT) t = fmaf(fmaxf(d, -1e30f), e, t);
       }
     }
   }
@@ -344,25 +334,11 @@ struct LogitBlock {
     }
     bm = fmaxf(fmaxf(um[0], um[1]), fmaxf(um[2], um[3]));
     float s, t;
-    const float n = st.s == 0.f && bm > -INFINITY ? bm : fmaxf(st.m, bm), c = lse_ref(n);
-    const bool far = fabsf(n) > kHugeLogit;
-    sums<ENT, false>(n, c, false, count, s, t);
-    if (__any(far)) {
-      LogitBlock again = *this;
-      // a copy the compiler does not know to be one: it would keep 64 values of
-      // the first pass in registers for this rare one
-#pragma unroll
-      for (int u = 0; u < kU; ++u) asm volatile("" : "+v"(again.raw[u]));
-      again.template sums<ENT, true>(n, c, far, count, s, t);
-    }
-    if (__any(far || fabsf(st.m) > kHugeLogit)) {
-      st = lse_join(st, {n, s, t});
-    } else {
-      const float d = fmaxf(lse_ref(st.m) - c, -1e30f), f = __builtin_amdgcn_exp2f(d);
-      st.t = (st.t + d * st.s) * f + t;
-      st.s = st.s * f + s;
-      st.m = n;
-    }
+    const float n = fmaxf(st.m, bm), d = lse_shift(st.m, n), f = lse_exp(d);
+    sums<ENT>(n, count, s, t);
+    st.t = (st.t + d * st.s) * f + t;
+    st.s = st.s * f + s;
+    st.m = n;
     if (k == 0) return;
     top.most[0] = fmaxf(top.most[0], fmaxf(um[0], um[1]));
     top.most[1] = fmaxf(top.most[1], fmaxf(um[2], um[3]));
@@ -428,22 +404,17 @@ __host__ __device__ __forceinline__ int64_t logprob_record(int k) { return 4 + 2
 // the target's logit in lane 0 (where there is one).
 __device__ __forceinline__ void logprobs_finish(const LogprobArgs& q, int64_t r, LseStat st, const TopList& top, int tg,
                                                 float zt, int lane) {
-  const bool huge = fabsf(st.m) > kHugeLogit, empty = st.s == 0.f;
-  const float c = lse_ref(st.m), ls = log2f(st.s);
-  auto logprob = [&](float z) {
-    // log2 p = L z - c - log2 s
-    return huge || fabsf(z) > kHugeLogit ? (z - st.m) - ls * (1.f / kLog2e) : (fmaf(z, kLog2e, -c) - ls) / kLog2e;
-  };
+  const bool empty = st.s == 0.f;
+  const float ls = logf(st.s);  // NaN in a row that holds one or +inf
   if (lane == 0) {
-    const double l = huge ? (double)st.m + (double)ls / kLog2e : ((double)c + (double)ls) / kLog2e;
-    q.lse[r] = empty ? -INFINITY : st.s != st.s ? NAN : (float)l;
-    if (q.entropy) q.entropy[r] = empty ? 0.f : (ls - st.t / st.s) / kLog2e;
-    if (q.logp) q.logp[r] = tg < 0 ? 0.f : empty ? -INFINITY : st.s != st.s ? NAN : logprob(zt);
+    q.lse[r] = empty ? -INFINITY : st.m + ls;
+    if (q.entropy) q.entropy[r] = empty ? 0.f : ls - st.t / st.s;
+    if (q.logp) q.logp[r] = tg < 0 ? 0.f : empty ? -INFINITY : (zt - st.m) - ls;
   }
   if (lane < q.k) {
     const bool bad = st.s != st.s, none = bad || top.v == -INFINITY;
     q.top_ids[r * q.k + lane] = none ? -1 : top.i;
-    q.top_logp[r * q.k + lane] = bad ? NAN : none ? -INFINITY : logprob(top.v);
+    q.top_logp[r * q.k + lane] = bad ? NAN : none ? -INFINITY : (top.v - st.m) - ls;
   }
 }
 
@@ -477,7 +448,7 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void logprobs_kernel(Lo
   const S* z = static_cast<const S*>(q.logits) + r * q.ld;
   const int begin = part * q.per_part, end = min(q.vocab, begin + q.per_part);
 
-  LseStat st = {-kHugeLogit, 0.f, 0.f};
+  LseStat st = {kLowest, 0.f, 0.f};
   TopState top;
   top.clear();
   // What a wave does not want its neighbours do not want either, up to equal
@@ -542,7 +513,7 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs q) {
   float zt;
   const int tg = logprobs_target<S>(q, r, zt);
   const float* rec = q.ws + r * q.parts * logprob_record(q.k);
-  LseStat st = {-kHugeLogit, 0.f, 0.f};
+  LseStat st = {kLowest, 0.f, 0.f};
   if (lane < q.parts) {
     const float* p = rec + lane * logprob_record(q.k);
     st = {p[0], p[1], p[2]};

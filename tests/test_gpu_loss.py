@@ -382,3 +382,41 @@ def test_other_stream_and_graph(env):
             torch.cuda.synchronize()
             for a, b in zip((logp, lse, ent, ids, top, dz), eager[1:] + (want,)):
                 assert torch.equal(a, b), rep
+
+
+@pytest.mark.parametrize("n,v", [(40, 64), (5, 700), (2100, 2500), (9, 5000), (3, 70001)])
+@pytest.mark.parametrize("centre", [1e6, -1e6, 3e5, 2e7])
+def test_large_logits(env, centre, n, v):
+    """fp32 logits a few units apart around large values (their spacing is 1/16
+    at 1e6): mixed within lanes, and rising or falling so that lanes, blocks,
+    waves and parts of a row lie on either side.  Differences of such values
+    are exact, so the bounds are those of small logits."""
+    torch, B, dev, h = env
+    say("logprobs large logits", centre, n, v)
+    r = np.random.default_rng(v)
+    z = 2 * r.standard_normal((n, v))
+    z[1::3] = np.linspace(-12, 12, v)
+    z[2::3] = np.linspace(12, -12, v)
+    t = r.integers(0, v, n)
+    check(env, place(torch, dev, (centre + z).astype(np.float32), torch.float32, 1)[1], t, 7)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,v", [(3000, 64), (2100, 4100), (300, 1000), (9, 9000), (2, 131072)])
+def test_outputs_stay_in_their_range(env, n, v, dtype):
+    """Log probabilities are at most 0 and entropies at least 0: exactly 0 with a
+    single allowed entry, whose logit is the log-sum-exp."""
+    torch, B, dev, h = env
+    say("logprobs range", n, v, dtype)
+    for mask, lift in (("one", 0), ("none", 30), ("none", 9)):
+        z, t = logits(n, v, n + v, mask)
+        z += np.float32(5.3)
+        if lift:
+            z[np.arange(n), t] = lift + np.abs(z).max()
+        _, view = place(torch, dev, z, getattr(torch, dtype))
+        _, logp, lse, ent, ids, top = forward(env, view, t, 3)
+        torch.cuda.synchronize()
+        assert bool(torch.all(logp <= 0)) and bool(torch.all(ent >= 0)) and bool(torch.all(top <= 0))
+        if mask == "one":
+            assert not bool(torch.any(logp[torch.from_numpy(t).to(dev) >= 0])) and not bool(torch.any(ent))
+            assert torch.equal(lse, view.float().amax(1)) and not bool(torch.any(top[:, 0]))
