@@ -82,7 +82,7 @@ def act(x, kind):
     if kind == GELU:
         return 0.5 * x * (1 + erf(x / math.sqrt(2)))
     if kind == GELU_TANH:
-        return 0.5 * x * (1 + np.tanh(math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)))
+        return x * expit(2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3))
     if kind == SILU:
         return x * expit(x)
     return x
@@ -96,7 +96,7 @@ def act_slope(x, kind):
         return 0.5 * (1 + erf(x / math.sqrt(2))) + x * np.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
     if kind == GELU_TANH:
         u = math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)
-        return 0.5 * (1 + np.tanh(u)) + 0.5 * x / np.cosh(np.clip(u, -300, 300)) ** 2 * math.sqrt(2 / math.pi) * (
+        return expit(2 * u) + 0.5 * x / np.cosh(np.clip(u, -300, 300)) ** 2 * math.sqrt(2 / math.pi) * (
             1 + 3 * 0.044715 * x * x)
     if kind == SILU:
         s = expit(x)

@@ -94,7 +94,7 @@ __device__ __forceinline__ float act_slope(float x) {
     const float w = 1.59576912f * (x + 0.044715f * x * x * x);
     const float p = FAST ? fast_sigmoid(w) : 1.f / (1.f + expf(-w));
     // beyond 20 the second term is below 2^-24 and its factors overflow
-    return fabsf(x) > 20.f ? p : p + x * p * (1.f - p) * (1.59576912f + 0.21406659f * x * x);
+    return fabsf(x) > 20.f ? p : p + x * p * (1.f - p) * (1.59576912f + 0.21406445f * x * x);
   }
   if constexpr (ACT == SHAMPOO_ACT_SILU) {
     const float p = FAST ? fast_sigmoid(x) : 1.f / (1.f + expf(-x));

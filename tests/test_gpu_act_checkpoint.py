@@ -287,3 +287,28 @@ def test_other_stream_and_graph(env):
         torch.cuda.synchronize()
         for a, b in zip(got, (want_c, want_y, want_v, want_d)):
             assert torch.equal(a, b), rep
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("kind", [L.GELU_TANH, L.SILU])
+def test_negative_tail(env, kind, dtype):
+    """Activations and slopes on [-9, -3] to a relative bound: the results fall to
+    1e-28, far below any bound in the size of x.  The exponent, which grows to
+    about x^2, carries a few roundings; exp is a few ulp off."""
+    torch, B, dev, h = env
+    say("act negative tail", kind, dtype)
+    dt = getattr(torch, dtype)
+    x = -np.linspace(3, 9, 64 * 96).reshape(64, 96).astype(np.float32)
+    _, v = place(torch, dev, x, dt)
+    xx = host(v.double())
+    y = torch.empty_like(v)
+    ck = blank(env, 64, 96)
+    B.shampoo_act_encode(h, v, ckpt_x=ck, act=kind, Y=y)
+    dx = torch.empty_like(v)
+    B.shampoo_act_grad(h, ck, kind, torch.ones_like(v), dx)
+    torch.cuda.synchronize()
+    held = L.checkpoint_values(*L.checkpoint(xx), 96)
+    for got, at, ref in ((y, xx, L.act(xx, kind)), (dx, held, L.act_slope(held, kind))):
+        bound = 2.0 ** -8 + 2.0 ** -15 if dt is torch.bfloat16 else U * (40 + 4 * at * at)
+        err = np.abs(host(got.double()) / ref - 1)
+        assert np.all(err <= bound), float((err / bound).max())
