@@ -5,7 +5,7 @@ include/shampoo.h; no code shared with the GPU path.  Test infrastructure."""
 import math
 
 import numpy as np
-from scipy.special import erf, expit
+from scipy.special import erfc, expit
 
 NONE, RELU, GELU, GELU_TANH, SILU = range(5)
 GROUP = 32
@@ -80,7 +80,7 @@ def act(x, kind):
     if kind == RELU:
         return np.where(x > 0, x, np.where(np.isnan(x), x, 0.0))
     if kind == GELU:
-        return 0.5 * x * (1 + erf(x / math.sqrt(2)))
+        return 0.5 * x * erfc(-x / math.sqrt(2))
     if kind == GELU_TANH:
         return x * expit(2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3))
     if kind == SILU:
@@ -93,7 +93,7 @@ def act_slope(x, kind):
     if kind == RELU:
         return np.where(x > 0, 1.0, np.where(np.isnan(x), x, 0.0))
     if kind == GELU:
-        return 0.5 * (1 + erf(x / math.sqrt(2))) + x * np.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
+        return 0.5 * erfc(-x / math.sqrt(2)) + x * np.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
     if kind == GELU_TANH:
         u = math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)
         return expit(2 * u) + 0.5 * x / np.cosh(np.clip(u, -300, 300)) ** 2 * math.sqrt(2 / math.pi) * (

@@ -42,26 +42,31 @@ __device__ __forceinline__ float act_scale(uint32_t s) { return __uint_as_float(
 // 2^-(s - 127), s <= 248.
 __device__ __forceinline__ float act_unscale(uint32_t s) { return __uint_as_float((254u - s) << 23); }
 
-// Phi(x), the normal distribution function, and e = exp(-x^2 / 2) beside it, for
-// results kept in bf16: Abramowitz and Stegun 7.1.26 (erf of |x| / sqrt 2 to
-// 1.5e-7), one exponential and one reciprocal.
-__device__ __forceinline__ float normal_cdf(float x, float& e) {
-  const float a = fabsf(x) * 0.70710678f;
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
-  e = __builtin_amdgcn_exp2f(a * a * -1.44269504f);
-  // half of the complement: halves of the published coefficients
-  float h = fmaf(0.5307027145f, t, -0.7265760135f);
-  h = fmaf(h, t, 0.7107068705f);
-  h = fmaf(h, t, -0.142248368f);
-  h = fmaf(h, t, 0.127414796f);
-  h = h * t * e;
-  return x < 0.f ? h : 1.f - h;
+// The normal distribution's lower tail Phi(-|x|) = R e, e = exp(-x^2 / 2): R, with
+// e beside it.  gelu and its slope are formed from it without the cancellation of
+// 1 + erf, so that their negative tails keep all bits.  FAST: R is a polynomial in
+// 1 / (1 + p |x|) that was fitted for the least relative error, 4e-6 for |x| up to
+// 14 (where Phi leaves fp32's normal range).
+template <bool FAST>
+__device__ __forceinline__ float normal_tail(float x, float& e) {
+  if constexpr (!FAST) {
+    e = expf(-0.5f * x * x);
+    return 0.5f * erfcxf(fabsf(x) * 0.70710678f);
+  }
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.30815624f, fabsf(x), 1.f));
+  e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);
+  float h = fmaf(-0.0753979f, t, 0.18913349f);
+  h = fmaf(h, t, 0.00769323f);
+  h = fmaf(h, t, 0.13641141f);
+  h = fmaf(h, t, 0.11897507f);
+  h = fmaf(h, t, 0.12318278f);
+  return h * t;
 }
 __device__ __forceinline__ float fast_sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
 }
 
-// FAST: for results kept in bf16 (errors of a few 2^-22 of the terms), where the
+// FAST: for results kept in bf16 (relative errors of at most 2^-15 down to -9), where the
 // library functions' 20 to 40 instructions a value would bound the pass; fp32
 // passes move twice the bytes and call them.
 template <int ACT, bool FAST>
@@ -69,7 +74,8 @@ __device__ __forceinline__ float act_value(float x) {
   if constexpr (ACT == SHAMPOO_ACT_RELU) return x < 0.f ? 0.f : x;
   if constexpr (ACT == SHAMPOO_ACT_GELU) {
     float e;
-    return FAST ? x * normal_cdf(x, e) : 0.5f * x * (1.f + erff(x * 0.70710678f));
+    const float p = normal_tail<FAST>(x, e) * e;
+    return x * (x < 0.f ? p : 1.f - p);
   }
   if constexpr (ACT == SHAMPOO_ACT_GELU_TANH) {
     const float w = 1.59576912f * (x + 0.044715f * x * x * x);
@@ -83,12 +89,10 @@ template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == SHAMPOO_ACT_RELU) return x > 0.f ? 1.f : (x != x ? x : 0.f);
   if constexpr (ACT == SHAMPOO_ACT_GELU) {
-    if (FAST) {
-      float e;
-      const float p = normal_cdf(x, e);
-      return fmaf(x * 0.39894228f, e, p);
-    }
-    return 0.5f * (1.f + erff(x * 0.70710678f)) + x * (0.39894228f * expf(-0.5f * x * x));
+    // Phi(x) + x phi(x), at -|x|; the slopes at x and -x add up to 1
+    float e;
+    const float p = fmaf(-0.39894228f, fabsf(x), normal_tail<FAST>(x, e)) * e;
+    return x < 0.f ? p : 1.f - p;
   }
   if constexpr (ACT == SHAMPOO_ACT_GELU_TANH) {
     const float w = 1.59576912f * (x + 0.044715f * x * x * x);
