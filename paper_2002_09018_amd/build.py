@@ -9,7 +9,8 @@ LIB = os.path.join(HERE, "libshampoo.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "layers.hip")]
 HEADERS = [os.path.join(HERE, "csrc", f) for f in ("kernels.hpp", "tile_mfma.hpp", "fp32_block.hpp", "split_mfma.hpp",
                                                    "direct_mma.hpp", "small_root.hpp", "embedding.hpp", "handle.hpp",
-                                                   "logprobs.hpp", "act_checkpoint.hpp", "weight_grad.hpp")]
+                                                   "layer_plans.hpp", "logprobs.hpp", "act_checkpoint.hpp",
+                                                   "weight_grad.hpp")]
 HEADERS.append(os.path.join(ROOT, "include", "shampoo.h"))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "layer_plans.hpp"
 #include "split_mfma.hpp"
 #include "shampoo.h"
 #include "tile_mfma.hpp"
@@ -396,9 +397,8 @@ struct LogprobArgs {
   int parts;     // workgroups of a row
   int per_part;  // entries of one
   int64_t first; // the launch's first part of all rows' parts
-  float* ws;     // a record for each part of each row: m, s, t, -, k values, k indices
+  float* ws;     // a record (logprob_record) for each part of each row
 };
-__host__ __device__ __forceinline__ int64_t logprob_record(int k) { return 4 + 2 * (int64_t)k; }
 
 // The outputs of a row, from a wave that holds its sums and alternatives; zt is
 // the target's logit in lane 0 (where there is one).

@@ -420,3 +420,78 @@ def test_outputs_stay_in_their_range(env, n, v, dtype):
         if mask == "one":
             assert not bool(torch.any(logp[torch.from_numpy(t).to(dev) >= 0])) and not bool(torch.any(ent))
             assert torch.equal(lse, view.float().amax(1)) and not bool(torch.any(top[:, 0]))
+
+
+# Rows of several blocks to a wave for every number of waves of a workgroup (and
+# parts of a row); test_layer_plans.py checks that the dispatch rules send them there.
+LONG = [(2049, 9001), (1100, 20011), (600, 40001), (300, 70001), (2049, 70001), (5, 131075), (100, 131075)]
+LONG_K = [0, 8, 64]
+# Two blocks to a wave of the gradient: (rows, vocab, type).
+LONG_GRAD = [(521, 16001, "float32"), (551, 31003, "bfloat16")]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k", LONG_K)
+@pytest.mark.parametrize("n,v", LONG)
+def test_long_rows(env, n, v, k, dtype):
+    """All rows against 64-bit torch operations, some of them and their
+    alternatives' indices against the oracle; with and without entropy."""
+    torch, B, dev, h = env
+    say("logprobs long rows", n, v, k, dtype)
+    g = torch.Generator(device=dev).manual_seed(n + v + k)
+    z = 3 * torch.randn(n, v, device=dev, generator=g)
+    z[torch.rand(n, v, device=dev, generator=g) < 0.2] = -float("inf")
+    z[1] = torch.linspace(-20, 20, v, device=dev)
+    z[2] = torch.linspace(20, -20, v, device=dev)
+    z[3] = 1.25
+    z[4] = -float("inf")
+    buf = torch.full((n * (v + 5) + 1,), 7.5, device=dev, dtype=getattr(torch, dtype))
+    view = buf[1:].view(n, v + 5)[:, :v]
+    view.copy_(z)
+    del z
+    t = np.random.default_rng(v).integers(-1, v, n)
+    tt, logp, lse, ent, ids, top = forward(env, view, t, k)
+    lse2, ids2, top2 = (None if x is None else torch.zeros_like(x) for x in (lse, ids, top))
+    nws = B.shampoo_token_logprobs_workspace_bytes(n, v, k)
+    ws = torch.empty(nws, device=dev, dtype=torch.uint8) if nws else None
+    B.shampoo_token_logprobs(h, view, None, None, lse2, top_ids=ids2, top_logp=top2, workspace=ws)
+    torch.cuda.synchronize()
+    e = U * (16 + np.sqrt(v))
+    for a, b in ((lse2, lse), (top2, top)):
+        if a is not None:
+            close(host(a), host(b).astype(np.float64), 2 * e + 8 * U * np.abs(np.where(np.isfinite(host(b)), host(b), 0)),
+                  "without entropy")
+    assert k == 0 or torch.equal(ids, ids2)
+    some = np.unique(np.concatenate([np.arange(min(n, 6)), np.random.default_rng(1).integers(0, n, 14), [n - 1]]))
+    at = torch.from_numpy(some).to(dev)
+    ref = L.token_logprobs(host(view[at].double()), t[some], k)
+    for a, b, what, f in zip((logp, lse, ent, None, top), ref, ("logp", "lse", "entropy", "ids", "top"),
+                             (1, 1, 40, 1, 1)):
+        if a is not None:
+            close(host(a[at]), b, f * e + 4 * U * np.abs(np.where(np.isfinite(b), b, 0)), what)
+    if k:
+        assert np.array_equal(host(ids[at]), ref[3])
+    for r in range(0, n, 256):
+        x = view[r:r + 256].double()
+        want = torch.logsumexp(x, 1)
+        tr = tt[r:r + 256].long()
+        picked = torch.where(tr >= 0, x.gather(1, tr.clamp(min=0).unsqueeze(1))[:, 0] - want, torch.zeros_like(want))
+        picked = torch.where((tr >= 0) & torch.isneginf(want), want, picked)
+        p = torch.exp(x - want.unsqueeze(1)).nan_to_num_(0)
+        lp = torch.where(p > 0, x - want.unsqueeze(1), torch.zeros_like(x))
+        pairs = [(logp, picked, 1), (lse, want, 1), (ent, -(p * lp).sum(1), 40)]
+        if k:
+            best = torch.topk(x, k, dim=1).values - want.unsqueeze(1)
+            pairs.append((top, torch.where(torch.isnan(best), torch.full_like(best, -float("inf")), best), 1))
+        for a, b, f in pairs:
+            b = host(b)
+            close(host(a[r:r + 256]), b, f * e + 4 * U * np.abs(np.where(np.isfinite(b), b, 0)), ("all rows", r))
+
+
+@pytest.mark.parametrize("n,v,dtype", LONG_GRAD)
+def test_gradient_of_long_rows(env, n, v, dtype):
+    torch = env[0]
+    for mask, k, pad, entropy, in_place in (("none", 0, 0, False, False), ("some", 17, 3, True, True)):
+        say("logprobs grad long rows", n, v, dtype, mask, k, pad, entropy, in_place)
+        z, t = logits(n, v, n + k, mask)
+        grad_case(env, z, t, k, getattr(torch, dtype), pad, entropy, entropy, in_place)

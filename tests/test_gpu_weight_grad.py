@@ -248,3 +248,47 @@ def test_offsets_past_32_bits(env):
     call(env, ck, d, G, n)
     torch.cuda.synchronize()
     assert bool(torch.all(G[-40:] == 6)) and bool(torch.all(G[:-40] == 0))
+
+
+# Sizes for every tile, in one part of the tokens and in several, none a multiple
+# of a tile or a stage; test_layer_plans.py checks that the dispatch rules send
+# them there.
+LARGE = [(65, 3073, 4090), (70, 2051, 2055), (321, 2053, 4090), (1027, 1283, 3079), (8195, 1025, 515),
+         (16389, 1537, 771)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,c,o", LARGE)
+def test_large_tiles(env, n, c, o, dtype):
+    torch = env[0]
+    for g_dtype, pad, shift, beta in (("float32", 0, 0, 0.0), ("float32", 3, 1, -0.5), ("bfloat16", 6, 0, 1.0)):
+        say("weight grad large", n, c, o, dtype, g_dtype, pad, shift, beta)
+        check(env, n, c, o, getattr(torch, dtype), getattr(torch, g_dtype), pad, shift, beta)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,c,o", LARGE)
+def test_large_tiles_contain_bad_values(env, n, c, o, dtype):
+    """A NaN group spoils the rows of its columns, a NaN in dY its column; every
+    other element keeps its bits."""
+    torch, B, dev, h = env
+    dt = getattr(torch, dtype)
+    say("weight grad large bad values", n, c, o, dtype)
+    g = torch.Generator(device=dev).manual_seed(n)
+    x, dy = torch.randn(n, c, device=dev, generator=g), torch.randn(n, o, device=dev, generator=g).to(dt)
+    ck = torch.empty(B.shampoo_act_checkpoint_bytes(n, c), device=dev, dtype=torch.uint8)
+    B.shampoo_act_encode(h, x, ckpt_x=ck)
+    want, G = torch.empty(c, o, device=dev), torch.empty(c, o, device=dev)
+    call(env, ck, dy, want, n)
+    x[n - 1, c - 1] = float("nan")   # the last, shorter group
+    x[n // 2, 40] = float("inf")
+    B.shampoo_act_encode(h, x, ckpt_x=ck)
+    dy[0, o - 1] = float("nan")
+    dy[n - 1, 130] = float("nan")
+    call(env, ck, dy, G, n)
+    torch.cuda.synchronize()
+    rows = list(range(32, 64)) + list(range((c - 1) // 32 * 32, c))
+    bad = torch.zeros(c, o, device=dev, dtype=torch.bool)
+    bad[rows] = True
+    bad[:, [130, o - 1]] = True
+    assert bool(torch.all(torch.isnan(G[bad]))) and torch.equal(G[~bad], want[~bad])
