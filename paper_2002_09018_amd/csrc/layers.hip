@@ -46,7 +46,7 @@ shampoo_status check_dtype(Handle* h, int dtype, const char* what) {
 
 shampoo_status check_logits(Handle* h, int dtype, int64_t rows, int64_t vocab, int64_t ld, int k) {
   STATUS_TRY(check_dtype(h, dtype, "logits"));
-  if (rows < 0 || rows >= kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31 - 1)", (long long)rows);
+  if (rows < 0 || rows > kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31)", (long long)rows);
   if (vocab < 1 || vocab > kMaxVocab) return fail(h, SHAMPOO_EINVAL, "vocab = %lld outside [1, 2^30]", (long long)vocab);
   if (ld < vocab) return fail(h, SHAMPOO_EINVAL, "ld %lld < vocab %lld", (long long)ld, (long long)vocab);
   if (k < 0 || k > SHAMPOO_MAX_TOP) return fail(h, SHAMPOO_EINVAL, "k = %d outside [0, %d]", k, SHAMPOO_MAX_TOP);
@@ -55,7 +55,7 @@ shampoo_status check_logits(Handle* h, int dtype, int64_t rows, int64_t vocab, i
 
 shampoo_status check_act(Handle* h, int dtype, int64_t rows, int64_t cols, int act) {
   STATUS_TRY(check_dtype(h, dtype, "activations"));
-  if (rows < 0 || rows >= kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31 - 1)", (long long)rows);
+  if (rows < 0 || rows > kMaxTokens) return fail(h, SHAMPOO_EINVAL, "rows = %lld outside [0, 2^31)", (long long)rows);
   if (cols < 1 || cols > kMaxCols) return fail(h, SHAMPOO_EINVAL, "cols = %lld outside [1, 2^20]", (long long)cols);
   if (act < SHAMPOO_ACT_NONE || act > SHAMPOO_ACT_SILU) return fail(h, SHAMPOO_EINVAL, "bad activation %d", act);
   return SHAMPOO_OK;
@@ -142,7 +142,7 @@ extern "C" {
 
 // ---------------------------------------------------------------- loss
 size_t shampoo_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int k) {
-  if (rows < 1 || rows >= kMaxTokens || vocab < 1 || vocab > kMaxVocab || k < 0 || k > SHAMPOO_MAX_TOP) return 0;
+  if (rows < 1 || rows > kMaxTokens || vocab < 1 || vocab > kMaxVocab || k < 0 || k > SHAMPOO_MAX_TOP) return 0;
   size_t need = 0;
   for (int dtype : {SHAMPOO_F32, SHAMPOO_BF16}) need = std::max(need, logprob_plan(rows, vocab, k, dtype).ws);
   return need;
@@ -228,7 +228,7 @@ shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int
 
 // ---------------------------------------------------------------- activations
 size_t shampoo_act_checkpoint_bytes(int64_t rows, int64_t cols) {
-  if (rows < 0 || rows >= kMaxTokens || cols < 1 || cols > kMaxCols) return 0;
+  if (rows < 0 || rows > kMaxTokens || cols < 1 || cols > kMaxCols) return 0;
   return (size_t)act_ckpt(rows, cols).bytes;
 }
 
@@ -303,7 +303,7 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
 
 // ---------------------------------------------------------------- weight gradient
 size_t shampoo_act_weight_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t out) {
-  if (rows < 0 || rows >= kMaxTokens || cols < 1 || cols > kMaxCols || out < 1 || out > kMaxCols) return 0;
+  if (rows < 0 || rows > kMaxTokens || cols < 1 || cols > kMaxCols || out < 1 || out > kMaxCols) return 0;
   size_t need = 0;
   for (int dtype : {SHAMPOO_F32, SHAMPOO_BF16}) need = std::max(need, wgrad_plan(rows, cols, out, dtype).ws);
   return need;

@@ -32,6 +32,17 @@ def test_sizes():
     assert B.shampoo_act_weight_grad_workspace_bytes(8, 0, 8) == 0
 
 
+def test_most_rows():
+    """2^31 - 1 rows are the most, one more is refused."""
+    most = 2 ** 31 - 1
+    codes = (most * 32 + 255) // 256 * 256
+    assert B.shampoo_act_checkpoint_bytes(most, 1) == codes + (most + 255) // 256 * 256
+    assert B.shampoo_act_weight_grad_workspace_bytes(most, 64, 64) == B.shampoo_act_weight_grad_workspace_bytes(
+        most - 1, 64, 64) > 0
+    assert B.shampoo_act_checkpoint_bytes(most + 1, 1) == 0
+    assert B.shampoo_act_weight_grad_workspace_bytes(most + 1, 64, 64) == 0
+
+
 def test_logprobs_checks():
     n, v, k = 4, 10, 3
 
