@@ -723,12 +723,21 @@ def _room(t, nbytes, dev):
 
 
 def _apart(a, b):
-    """Whether two matrices (as from _layout) share no memory."""
+    """Whether two matrices (as from _layout) share no memory: one lies past the
+    other, or the rows of each lie between those of the other (column ranges
+    of one wider buffer)."""
     if a[0] == 0 or b[0] == 0 or a[1] == 0 or b[1] == 0:
         return True
-    a_end = a[5] + ((a[0] - 1) * a[2] + a[1]) * (4 - 2 * a[3])
-    b_end = b[5] + ((b[0] - 1) * b[2] + b[1]) * (4 - 2 * b[3])
-    return a_end <= b[5] or b_end <= a[5]
+    ea, eb = 4 - 2 * a[3], 4 - 2 * b[3]
+    if a[5] + ((a[0] - 1) * a[2] + a[1]) * ea <= b[5] or b[5] + ((b[0] - 1) * b[2] + b[1]) * eb <= a[5]:
+        return True
+    row_a, row_b, pitch, other = a[1] * ea, b[1] * eb, a[2] * ea, b[2] * eb
+    if a[0] == 1:
+        pitch = other
+    elif b[0] > 1 and other != pitch:
+        return False  # rows drift past each other: taken as shared
+    at = (b[5] - a[5]) % pitch
+    return at >= row_a and at + row_b <= pitch
 
 
 def _alike(out, src):

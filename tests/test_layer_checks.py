@@ -155,3 +155,50 @@ def test_null_handle_is_refused():
     assert lib.shampoo_act_decode(None, None, 1, 1, None, 0, 1, None) == B.SHAMPOO_EINVAL
     assert lib.shampoo_act_weight_grad(None, None, 1, 1, None, 0, 1, 1, None, 0, 1, 0.0, None, 0,
                                        None) == B.SHAMPOO_EINVAL
+
+
+def test_column_ranges_of_one_buffer_are_apart():
+    """Views whose rows lie between each other's share no element: they pass the
+    layout checks (and are refused as CPU tensors only)."""
+    n, v = 4, 10
+
+    def grad(z, d):
+        return lambda: B.shampoo_token_logprobs_grad(None, z, _i32(n), torch.zeros(n), d, g_logp=torch.zeros(n))
+    for dt in (torch.float32, BF16):
+        wide = torch.zeros(n, 2 * v + 3, dtype=dt)
+        _raises(grad(wide[:, :v], wide[:, v:2 * v]), "expected a GPU tensor")
+        _raises(grad(wide[:, v + 3:], wide[:, :v]), "expected a GPU tensor")
+        _raises(grad(wide[:, :v], wide[:, v - 1:2 * v - 1]), "overlap")
+        _raises(grad(wide[:, v:2 * v], wide[:, 1:v + 1]), "overlap")
+        _raises(grad(wide[:, v + 3:], wide[:, v + 2:2 * v + 2]), "overlap")
+    x = torch.zeros(n, 2 * v)
+    _raises(lambda: B.shampoo_act_encode(None, x[:, :v], act=B.ACT_SILU, Y=x[:, v:]), "expected a GPU tensor")
+    _raises(lambda: B.shampoo_act_grad(None, _ckpt(n, v), B.ACT_SILU, x[:, :v], x[:, v:]), "expected a GPU tensor")
+    _raises(lambda: B.shampoo_act_encode(None, x[:, :v], act=B.ACT_SILU, Y=x.view(-1)[v:v + n * v].view(n, v)), "overlap")
+    # one row in the gap of the other's rows, and one that is too long for it
+    g = torch.zeros(3, 40)
+    _raises(lambda: B.shampoo_act_weight_grad(None, _ckpt(1, 3), g[1:2, 20:40], g[:, :20]), "expected a GPU tensor")
+    _raises(lambda: B.shampoo_act_weight_grad(None, _ckpt(1, 3), g.view(-1)[21:61].view(1, 40)[:, :20], g[:, :20]),
+            "overlap")
+
+
+def test_apart_is_exact_for_rows_of_one_stride():
+    """Against the sets of bytes, over every small layout; views of different
+    strides may be taken as shared, never as apart when they are not."""
+    for ma, mb in ((1, 1), (1, 3), (3, 1), (2, 3)):
+        for ca in (1, 3):
+            for cb in (1, 2):
+                for la in range(ca, 7):
+                    for lb in range(cb, 7):
+                        for sa, sb in ((0, 0), (1, 0), (1, 1)):
+                            for off in range(-24, 24):
+                                ea, eb = 4 - 2 * sa, 4 - 2 * sb
+                                a, b = (ma, ca, la, sa, 0, 1000), (mb, cb, lb, sb, 0, 1000 + 2 * off)
+                                x = {a[5] + r * la * ea + i for r in range(ma) for i in range(ca * ea)}
+                                y = {b[5] + r * lb * eb + i for r in range(mb) for i in range(cb * eb)}
+                                if not x.isdisjoint(y):
+                                    assert not B._apart(a, b), (a, b)
+                                elif la * ea == lb * eb and ma > 1 and mb > 1:
+                                    # only the last row of one comes near the first of the other
+                                    edge = min(x) > min(y) + (mb - 1) * lb * eb or min(y) > min(x) + (ma - 1) * la * ea
+                                    assert B._apart(a, b) or edge, (a, b)
