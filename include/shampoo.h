@@ -456,8 +456,8 @@ shampoo_status shampoo_embedding_graft(void* handle, const int32_t* rows, const 
  * call needs none), used exclusively by this call until the stream reaches
  * its end.  rows == 0 does nothing.
  * Errors: EINVAL (NULL pointers, rows outside [0, 2^31), vocab outside
- * [1, 2^30], ld < vocab, k outside [0, SHAMPOO_MAX_TOP], dtype), ENOMEM
- * (workspace too small).
+ * [1, 2^30], ld < vocab, k outside [0, SHAMPOO_MAX_TOP], dtype, a workspace that
+ * overlaps the logits), ENOMEM (workspace too small).
  */
 #define SHAMPOO_MAX_TOP 64
 size_t shampoo_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int k);
@@ -476,10 +476,11 @@ shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtyp
  * target outside [0, vocab) has no g_logp, an alternative outside it no g_top.
  * Rows with lse = -inf have gradient 0.  dlogits has the logits' element type
  * (rounded once, to nearest even) and row stride ld_d >= vocab; it may be the
- * logits themselves (same pointer, ld_d == ld).  Deterministic.
+ * logits themselves (same pointer, ld_d == ld), else it shares no element with
+ * them.  Deterministic.
  * Errors: EINVAL (NULL logits, lse or dlogits; targets NULL with g_logp,
  * entropy NULL with g_entropy, top_ids NULL with g_top; sizes and dtype as
- * above; dlogits == logits with ld_d != ld).
+ * above; dlogits == logits with ld_d != ld, or overlapping them otherwise).
  */
 shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int dtype, int64_t rows, int64_t vocab,
                                            int64_t ld, const int32_t* targets, const float* lse,
@@ -517,9 +518,10 @@ size_t shampoo_act_checkpoint_bytes(int64_t rows, int64_t cols);
  * One pass over X (rows x cols, row stride ld_x, dtype): Y = act(X) (same
  * type, row stride ld_y; NULL: not wanted), the checkpoint of X (ckpt_x) and
  * the checkpoint of Y as stored (ckpt_y); each may be NULL, not all three.
- * Y may be X itself (ld_y == ld_x).
+ * Y may be X itself (ld_y == ld_x); otherwise tensors and checkpoints of a call
+ * share no memory (column ranges of one wider buffer do not).
  * Errors: EINVAL (NULL X, no output, sizes, strides, dtype, act, a checkpoint
- * not aligned to 16 bytes).
+ * not aligned to 16 bytes, overlapping buffers).
  */
 shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld_x,
                                   int act, void* Y, int64_t ld_y, void* ckpt_x, void* ckpt_y, void* stream);
@@ -548,7 +550,7 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
  * shampoo_act_weight_grad_workspace_bytes(rows, cols, out) bytes of device
  * memory (0: none needed), as for shampoo_token_logprobs.
  * Sizes: out in [1, 2^20].  Errors: as above, EINVAL for a non-finite beta or
- * G the same buffer as dY or the checkpoint, ENOMEM (workspace too small).
+ * G or the workspace overlapping another buffer, ENOMEM (workspace too small).
  */
 size_t shampoo_act_weight_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t out);
 shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t rows, int64_t cols, const void* dY,

@@ -1,5 +1,5 @@
-// How the calls from the loss to the gradient cut their work: plain host
-// arithmetic on sizes and types.
+// How the calls from the loss to the gradient cut their work, and whether their
+// buffers overlap: plain host arithmetic on sizes, types and addresses.
 #pragma once
 
 #include <stddef.h>
@@ -12,6 +12,32 @@
 namespace shp {
 
 inline int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The bytes of a buffer: rows of `row` bytes, `pitch` apart.
+struct Span {
+  uintptr_t p;
+  int64_t rows, row, pitch;
+};
+inline Span span(const void* p, int64_t rows, int64_t cols, int64_t ld, int dtype) {
+  const int64_t b = dtype == SHAMPOO_BF16 ? 2 : 4;
+  return {reinterpret_cast<uintptr_t>(p), p ? rows : 0, cols * b, ld * b};
+}
+inline Span span(const void* p, int64_t bytes) { return {reinterpret_cast<uintptr_t>(p), p ? 1 : 0, bytes, bytes}; }
+
+// Whether two buffers share no byte: one lies past the other, or the rows of each
+// lie between those of the other.  (Rows of different pitches in one range are
+// taken as shared.)
+inline bool apart(const Span& a, const Span& b) {
+  if (a.rows == 0 || b.rows == 0 || a.row == 0 || b.row == 0) return true;
+  auto end = [](const Span& x) { return x.p + (uintptr_t)(x.rows - 1) * (uintptr_t)x.pitch + (uintptr_t)x.row; };
+  if (end(a) <= b.p || end(b) <= a.p) return true;
+  if (a.rows == 1 && b.rows == 1) return false;
+  if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return false;
+  const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+  int64_t at = (int64_t)(b.p - a.p) % pitch;
+  if (at < 0) at += pitch;
+  return at >= a.row && at + b.row <= pitch;
+}
 
 constexpr int kLogitBlockB = 4096;  // bytes of a row that a wave takes at a time (LogitBlock)
 // Floats of a part of a row: m, s, t, -, k values, k indices.

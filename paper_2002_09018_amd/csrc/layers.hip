@@ -65,6 +65,11 @@ shampoo_status check_act(Handle* h, int dtype, int64_t rows, int64_t cols, int a
 // launch holds fewer than 2^32 threads, so larger ones take turns.
 unsigned act_grid(int64_t n) { return (unsigned)std::min<int64_t>(cdiv64(n, kThreads), 1 << 20); }
 
+// Buffers of a call that must share no memory.
+shampoo_status check_apart(Handle* h, const Span& a, const char* what_a, const Span& b, const char* what_b) {
+  return apart(a, b) ? SHAMPOO_OK : fail(h, SHAMPOO_EINVAL, "%s and %s overlap", what_a, what_b);
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // The launches of a pass over a rows x cols tensor and its checkpoint: f(shape,
@@ -161,6 +166,7 @@ shampoo_status shampoo_token_logprobs(void* handle, const void* logits, int dtyp
     if (need && (!workspace || ws_bytes < need))
       return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
     if (!aligned16(workspace)) return fail(h, SHAMPOO_EINVAL, "workspace not aligned to 16 bytes");
+    STATUS_TRY(check_apart(h, span(workspace, (int64_t)need), "workspace", span(logits, rows, vocab, ld, dtype), "logits"));
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const LogprobPlan p = logprob_plan(rows, vocab, k, dtype);
@@ -208,6 +214,8 @@ shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int
     if ((g_logp && !targets) || (g_entropy && !entropy) || (g_top && k > 0 && !top_ids))
       return fail(h, SHAMPOO_EINVAL, "g_logp without targets, g_entropy without entropy, or g_top without top_ids");
     if (dlogits == logits && ld_d != ld) return fail(h, SHAMPOO_EINVAL, "in place, ld_d %lld must be ld %lld", (long long)ld_d, (long long)ld);
+    if (dlogits != logits)
+      STATUS_TRY(check_apart(h, span(dlogits, rows, vocab, ld_d, dtype), "dlogits", span(logits, rows, vocab, ld, dtype), "logits"));
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     LossGradArgs q{logits, ld, rows, (int)vocab, targets, lse, entropy, g_top ? k : 0, top_ids, g_logp, g_lse,
@@ -242,6 +250,15 @@ shampoo_status shampoo_act_encode(void* handle, const void* X, int dtype, int64_
     if (!X || (!Y && !ckpt_x && !ckpt_y)) return fail(h, SHAMPOO_EINVAL, "X is NULL, or no output is asked for");
     if (Y == X && ld_y != ld_x) return fail(h, SHAMPOO_EINVAL, "in place, ld_y %lld must be ld_x %lld", (long long)ld_y, (long long)ld_x);
     if (!aligned16(ckpt_x) || !aligned16(ckpt_y)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    const Span x = span(X, rows, cols, ld_x, dtype), y = span(Y, rows, cols, ld_y, dtype);
+    const int64_t bytes = act_ckpt(rows, cols).bytes;
+    const Span cx = span(ckpt_x, bytes), cy = span(ckpt_y, bytes);
+    if (Y != X) STATUS_TRY(check_apart(h, y, "Y", x, "X"));
+    STATUS_TRY(check_apart(h, cx, "ckpt_x", x, "X"));
+    STATUS_TRY(check_apart(h, cx, "ckpt_x", y, "Y"));
+    STATUS_TRY(check_apart(h, cy, "ckpt_y", x, "X"));
+    STATUS_TRY(check_apart(h, cy, "ckpt_y", y, "Y"));
+    STATUS_TRY(check_apart(h, cx, "ckpt_x", cy, "ckpt_y"));
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
@@ -265,6 +282,7 @@ shampoo_status shampoo_act_decode(void* handle, const void* ckpt, int64_t rows, 
     if (rows == 0) return SHAMPOO_OK;
     if (!ckpt || !X) return fail(h, SHAMPOO_EINVAL, "ckpt or X is NULL");
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    STATUS_TRY(check_apart(h, span(ckpt, act_ckpt(rows, cols).bytes), "ckpt", span(X, rows, cols, ld_x, dtype), "X"));
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
@@ -287,6 +305,10 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
     if (!ckpt || !dY || !dX) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or dX is NULL");
     if (dX == dY && ld_dx != ld_dy) return fail(h, SHAMPOO_EINVAL, "in place, ld_dx %lld must be ld_dy %lld", (long long)ld_dx, (long long)ld_dy);
     if (!aligned16(ckpt)) return fail(h, SHAMPOO_EINVAL, "checkpoint not aligned to 16 bytes");
+    const Span c = span(ckpt, act_ckpt(rows, cols).bytes), y = span(dY, rows, cols, ld_dy, dtype);
+    const Span x = span(dX, rows, cols, ld_dx, dtype);
+    if (dX != dY) STATUS_TRY(check_apart(h, x, "dX", y, "dY"));
+    STATUS_TRY(check_apart(h, c, "ckpt", x, "dX"));
     DeviceGuard g(h->device);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return act_launches(h, rows, cols, s, [&](const ActShape& sh, dim3 grid) {
@@ -320,12 +342,18 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
       return fail(h, SHAMPOO_EINVAL, "ld_dy %lld or ld_g %lld < out %lld", (long long)ld_dy, (long long)ld_g, (long long)out);
     if (!isfinite(beta)) return fail(h, SHAMPOO_EINVAL, "beta is not finite");
     if (!G || (rows > 0 && (!ckpt || !dY))) return fail(h, SHAMPOO_EINVAL, "ckpt, dY or G is NULL");
-    if (G == dY || G == ckpt) return fail(h, SHAMPOO_EINVAL, "G must not be dY or the checkpoint");
     if (!aligned16(ckpt) || !aligned16(workspace))
       return fail(h, SHAMPOO_EINVAL, "checkpoint or workspace not aligned to 16 bytes");
     const size_t need = shampoo_act_weight_grad_workspace_bytes(rows, cols, out);
     if (need && (!workspace || ws_bytes < need))
       return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    const Span sg = span(G, cols, out, ld_g, g_dtype), sy = span(dY, rows, out, ld_dy, dtype);
+    const Span sc = span(ckpt, act_ckpt(rows, cols).bytes), sw = span(workspace, (int64_t)need);
+    STATUS_TRY(check_apart(h, sg, "G", sy, "dY"));
+    STATUS_TRY(check_apart(h, sg, "G", sc, "ckpt"));
+    STATUS_TRY(check_apart(h, sw, "workspace", sg, "G"));
+    STATUS_TRY(check_apart(h, sw, "workspace", sy, "dY"));
+    STATUS_TRY(check_apart(h, sw, "workspace", sc, "ckpt"));
     const WgradPlan p = wgrad_plan(rows, cols, out, dtype);
     if (p.tiles_m * p.tiles_n * p.splits > INT32_MAX / 512)
       return fail(h, SHAMPOO_EUNSUPPORTED, "G of %lld x %lld", (long long)cols, (long long)out);

@@ -48,7 +48,32 @@ static WgradPlan wgrad(ll rows, ll cols, ll out, int dtype) {
   return p;
 }
 
+// apart() against the bytes themselves: exact for one row, or rows of one pitch
+// away from each other's ends, and never true for buffers that share a byte.
+static void spans() {
+  for (int rows_a = 1; rows_a <= 3; ++rows_a)
+    for (int rows_b = 1; rows_b <= 3; ++rows_b)
+      for (int a = 1; a <= 4; ++a)
+        for (int b = 1; b <= 4; ++b)
+          for (int pa = a; pa <= 9; ++pa)
+            for (int pb = b; pb <= 9; ++pb)
+              for (int off = -40; off <= 40; ++off) {
+                const Span x = {1000, rows_a, a, pa}, y = {(uintptr_t)(1000 + off), rows_b, b, pb};
+                bool hit = false, inside = false;
+                for (int i = 0; i < rows_a; ++i)
+                  for (int j = 0; j < rows_b; ++j) {
+                    const int s = i * pa, t = off + j * pb;
+                    hit |= s < t + b && t < s + a;
+                    inside |= i > 0 && (s - pa + a <= t && t + b <= s);  // y's row between two of x's
+                  }
+                require(!(hit && apart(x, y)) && apart(x, y) == apart(y, x), "spans", rows_a, rows_b, off, pa * 100 + pb);
+                if (!hit && inside && (rows_b == 1 || pa == pb)) require(apart(x, y), "gap", rows_a, rows_b, off, pa * 100 + pb);
+              }
+  require(apart(span(nullptr, 8), span(nullptr, 8)) && apart({8, 0, 4, 4}, {8, 1, 4, 4}), "empty", 0, 0, 0, 0);
+}
+
 int main() {
+  spans();
   char kind[16];
   ll a, b, c;
   int d;

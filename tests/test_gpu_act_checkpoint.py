@@ -312,3 +312,48 @@ def test_negative_tail(env, kind, dtype):
         bound = 2.0 ** -8 + 2.0 ** -15 if dt is torch.bfloat16 else U * (40 + 4 * at * at)
         err = np.abs(host(got.double()) / ref - 1)
         assert np.all(err <= bound), float((err / bound).max())
+
+
+def test_overlapping_checkpoints_are_refused(env):
+    """A checkpoint shares no memory with the tensors of its call or the other
+    checkpoint; nothing is written then.  One buffer that holds them one after
+    the other is taken."""
+    torch, B, dev, h = env
+    say("act overlapping buffers")
+    n, c = 8, 64
+    nb = B.shampoo_act_checkpoint_bytes(n, c)
+    size = n * c * 2
+    buf = torch.zeros(2 * size + 2 * nb, device=dev, dtype=torch.uint8)
+
+    def tensor(at):
+        return buf[at:at + size].view(torch.bfloat16).view(n, c)
+    x, y, kx, ky = 0, size, 2 * size, 2 * size + nb
+
+    def encode(x, y, kx, ky):
+        B.shampoo_act_encode(h, tensor(x), ckpt_x=buf[kx:kx + nb], act=L.GELU, Y=tensor(y), ckpt_y=buf[ky:ky + nb])
+    for bad in ((x, y, x + size - 16, ky), (x, y, y, ky), (x, y, kx, 16), (x, y, kx, y + 32), (x, y, kx, kx),
+                (x, y, kx, ky - 16)):
+        with pytest.raises(B.ShampooError, match="overlap"):
+            encode(*bad)
+    G = buf[:64 * 4 * 4].view(torch.float32).view(c, 4)
+    with pytest.raises(B.ShampooError, match="overlap"):
+        B.shampoo_act_decode(h, buf[size - 16:size - 16 + nb], tensor(0))
+    with pytest.raises(B.ShampooError, match="overlap"):
+        B.shampoo_act_grad(h, buf[size:size + nb], L.GELU, tensor(0), tensor(size))
+    with pytest.raises(B.ShampooError, match="overlap"):
+        B.shampoo_act_weight_grad(h, buf[16:16 + nb], tensor(2 * size)[:, :4], G)
+    torch.cuda.synchronize()
+    assert not bool(torch.any(buf))
+    tensor(x).copy_(torch.from_numpy(act_input(n, c, 1)).bfloat16())
+    xx = host(tensor(x).double())
+    encode(x, y, kx, ky)
+    torch.cuda.synchronize()
+    tail = torch.full((64,), 0x5A, device=dev, dtype=torch.uint8)
+    same_checkpoint(torch.cat([buf[kx:ky], tail]), xx)
+    same_checkpoint(torch.cat([buf[ky:], tail]), host(tensor(y).double()))
+    # halves of one wider tensor
+    wide = torch.zeros(n, 2 * c, device=dev)
+    wide[:, :c] = tensor(x).float()
+    B.shampoo_act_encode(h, wide[:, :c], act=L.RELU, Y=wide[:, c:])
+    torch.cuda.synchronize()
+    assert np.array_equal(host(wide[:, c:].double()), np.maximum(xx, 0)) and np.array_equal(host(wide[:, :c].double()), xx)
