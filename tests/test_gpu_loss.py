@@ -495,3 +495,31 @@ def test_gradient_of_long_rows(env, n, v, dtype):
         say("logprobs grad long rows", n, v, dtype, mask, k, pad, entropy, in_place)
         z, t = logits(n, v, n + k, mask)
         grad_case(env, z, t, k, getattr(torch, dtype), pad, entropy, entropy, in_place)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k", [8, 64])
+def test_time_does_not_depend_on_the_order(env, k, dtype):
+    """Rows that rise with the index raise the bound on the alternatives in every
+    block.  They may cost a few times what rows in random order do, not tens of
+    times."""
+    torch, B, dev, h = env
+    n, v = 2048, 131072
+    say("logprobs order and time", k, dtype)
+    up = torch.linspace(-20, 20, v, device=dev)
+    mixed = up[torch.randperm(v, device=dev, generator=torch.Generator(device=dev).manual_seed(1))]
+    lse, top = torch.empty(n, device=dev), torch.empty(n, k, device=dev)
+    ids = torch.empty(n, k, device=dev, dtype=torch.int32)
+    times = []
+    for row in (mixed, up):
+        z = row.to(getattr(torch, dtype)).expand(n, v).contiguous()
+        best = float("inf")
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            B.shampoo_token_logprobs(h, z, None, None, lse, top_ids=ids, top_logp=top)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        times.append(best)
+    assert times[1] <= 10 * times[0], times
