@@ -495,9 +495,10 @@ shampoo_status shampoo_token_logprobs_grad(void* handle, const void* logits, int
  *   x^ = q 2^e,  |q| <= 127,  e the smallest exponent in [-126, 121] for which
  *   the group's largest |x| 2^-e rounds to at most 127,  q = x 2^-e rounded to
  *   nearest even
- * (|x - x^| <= 2^(e-1), at most 1/127 of the group's largest |x|; values from
- * 127.5 2^121 on, which would round to 2^128, are held as 127 2^121).  x^ is
- * exact in bfloat16.  A group that holds an infinity or NaN is NaN throughout.
+ * (|x - x^| <= 2^(e-1): for e > -126 at most 1/127 of the group's largest |x|,
+ * for e = -126 multiples of 2^-126, a group up to 2^-127 becoming 0; values from
+ * 127.5 2^121 on, which would round to 2^128, are held as 127 2^121).  x^ is exact
+ * in bfloat16.  A group that holds an infinity or NaN is NaN throughout.
  * Layout, one buffer of shampoo_act_checkpoint_bytes(rows, cols) bytes aligned
  * to 16: with ldq = cols rounded up to 32, rows x ldq codes (0 in the
  * columns at and past cols); then, at the next multiple of 256 bytes, rows x
@@ -544,7 +545,8 @@ shampoo_status shampoo_act_grad(void* handle, const void* ckpt, int64_t rows, in
  *                             beta == 0)
  * dY: rows x out, row stride ld_dy, dtype; G: g_dtype (either type; rounded
  * once at the end).  Products of x^ with bfloat16 gradients are exact and
- * summed in fp32; fp32 gradients are split exactly into three bfloat16 terms.
+ * summed in fp32; fp32 gradients are split into three bfloat16 terms, exactly
+ * from 2^-110 in size on (below, what lies under 2^-133 is cut off).
  * Long sums over few output tiles are cut into parts that are added in a fixed
  * order (deterministic).  `workspace`: at least
  * shampoo_act_weight_grad_workspace_bytes(rows, cols, out) bytes of device

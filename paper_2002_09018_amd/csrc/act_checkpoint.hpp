@@ -111,8 +111,10 @@ __device__ __forceinline__ float act_slope(float x) {
 // All passes move units of 8 columns, one to a lane in row order: 16 or 32 bytes
 // of a tensor, 8 of the codes; the 4 lanes of a group agree on its scale.  Bound
 // by memory: 16384 x 4096 in bf16, activation with both checkpoints and their
-// values in 142 us (5.7 TB/s), its gradient in 60 us (5.6 TB/s).  Two or four
-// units to a lane were 6 and 16% slower; rows of 4095 take 167 and 65 us.
+// values in 142 us (5.7 TB/s), gelu's gradient in 59 us (5.7 TB/s); the activation alone
+// with both checkpoints 69 to 73 us whichever it is (fp32 116, gelu 131: erfcx and
+// exp), the gradients 57 to 61 (fp32 105, gelu 117).  Two or four units to a lane were
+// 6 and 16% slower; rows of 4095 take 167 and 66 us.
 struct ActShape {
   int64_t row0, units;   // first row, and units of the launch (below 2^31)
   int cols, upr;         // columns, and units of a row (ldq / 8)

@@ -47,14 +47,13 @@ constexpr int64_t logprob_record(int k) { return 4 + 2 * (int64_t)k; }
 // (parts) of a row where there are few rows.  About two waves per SIMD are
 // wanted: fewer do not keep enough bytes in flight, and each wave of a row pays
 // for finding its own first alternatives.  Rows x 131072 in bf16, 8
-// alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 388 / 384 / 382 / 445, 1024
-// rows 74 / 56 / 52 / 60, 256 rows 69 / 43 / 28 / 23; without alternatives 8192
-// rows 381 / 377 / 356 / 361, of 65536 205 / 195 / 188 / 203, of 20000 66 / 67 / 75 /
-// 106.  Below 256 rows long rows are cut into parts of 4
-// waves and a second launch joins them: one row 12 us, by one workgroup of 8
-// waves 19; 64 rows 15 and 20.  Rows of few blocks to a wave do without: 1 x 32768
-// 10.0 us, in parts 11.9, 128 x 32768 10.7 and 13.1; 1 x 65536 13.3 and 11.3, without
-// alternatives 8.8 and 10.8.
+// alternatives, us with 1 / 2 / 4 / 8 waves: 8192 rows 390 / 384 / 380 / 436, 1024
+// rows 75 / 58 / 52 / 58, 256 rows 71 / 44 / 28 / 23; without alternatives 8192
+// rows 385 / 377 / 355 / 358, of 65536 205 / 195 / 184 / 187, of 20000 63 / 63 / 67 / 86.
+// Below 256 rows long rows are cut into parts of 4 waves and a second launch joins
+// them: one row 10.6 us, by one workgroup of 8 waves 18; 64 rows 13 and 19.  Rows of
+// few blocks to a wave do without: 1 x 32768 8.8 us, in parts 10.7, 128 x 32768 9.6 and
+// 11.4; 1 x 65536 12.2 and 10.4, without alternatives 7.6 and 9.9.
 struct LogprobPlan {
   int waves = 1, parts = 1, per_part = 0;
   size_t ws = 0;

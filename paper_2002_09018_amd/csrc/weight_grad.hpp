@@ -6,8 +6,8 @@
 // instruction per 16 tokens forms them.  An fp32 gradient is cut into three
 // bf16 terms, y = p0 + p1 + p2 (truncated: 8 bits each, every difference exact;
 // p0 keeps the sign of an infinity and never rounds up to one), which takes
-// three.  (Below 2^-109 the last term reaches bf16's subnormals: it is held to
-// 2^-134 then.)
+// three.  (Below 2^-110 the last term ends below bf16's smallest step: it is cut off at
+// multiples of 2^-133 then.)
 //
 // Both operands lie token by token, and the contraction runs over tokens.  A
 // stage of kBk tokens of both is copied into LDS as it lies,
@@ -27,7 +27,7 @@
 // 65536 x 1024 x 4096 with bf16 gradients: 473 to 495 us (1110 to 1160 TFLOP/s; a
 // library product of the same size, of bf16 operands, 674 us), where the chip
 // lowers its clock.  32768 x 512 x 512: 29 us, 24 of them the products of 24 parts
-// of the tokens (matrix cores and LDS busy in 38% of the cycles each; a second
+// of the tokens (matrix cores and LDS busy in 23% of the cycles each; a second
 // stage of loads in flight gained nothing), the rest the sum of the parts.
 #pragma once
 
