@@ -523,3 +523,32 @@ def test_time_does_not_depend_on_the_order(env, k, dtype):
             best = min(best, a.elapsed_time(b))
         times.append(best)
     assert times[1] <= 10 * times[0], times
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,v", [(2050, 20011), (700, 20011), (5, 131075)])
+def test_largest_in_few_lanes(env, n, v, dtype):
+    """Rows that rise from block to block, with their largest entries in a few of
+    the 16-byte pieces that lanes hold: fewer lanes than alternatives, at several
+    distances, some with a long run of equal values at the bound."""
+    torch, B, dev, h = env
+    say("logprobs few lanes", n, v, dtype)
+    per = 4 if dtype == "float32" else 8  # entries of a piece
+    c = np.arange(v)
+    lane, block = c // per % 64, c // (256 * per)
+    rows = [np.where(lane < lanes, 5.0, 0.0) + 0.05 * block + fine * (c % (256 * per))
+            for lanes in (1, 3, 15) for fine in (0.0, 1e-5)]
+    z = np.tile(np.array(rows), (n // len(rows) + 1, 1))[:n].astype(np.float32)
+    _, view = place(torch, dev, z, getattr(torch, dtype))
+    t = np.random.default_rng(n).integers(0, v, n)
+    for k in (5, 16, 40, 64):
+        _, logp, lse, ent, ids, top = forward(env, view, t, k)
+        torch.cuda.synchronize()
+        some = list(range(min(n, 6))) + [n - 1]
+        ref = L.token_logprobs(host(view[some].double()), t[some], k)
+        e = U * (16 + np.sqrt(v))
+        for a, b, f in ((logp, ref[0], 1), (lse, ref[1], 1), (ent, ref[2], 40), (top, ref[4], 1)):
+            close(host(a[some]), b, f * e + 4 * U * np.abs(b), k)
+        assert np.array_equal(host(ids[some]), ref[3])
+        for i in range(6, n, 6):  # the same rows again
+            assert torch.equal(ids[i], ids[0])
