@@ -560,6 +560,111 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
                                        float beta, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * The layers around the step.  A model's output layer without its logits, a gated
+ * feed-forward block, and dropout, with their gradients: the dW that these calls
+ * write are the gradients that shampoo_update_stats and shampoo_precondition take.
+ * They use no handle scratch: two calls of one handle may overlap on different
+ * streams if their buffers differ.  `workspace`: at least the stated bytes of device
+ * memory (0: none needed), aligned to 16, used exclusively by the call until the
+ * stream reaches its end.  Matrices are row-major with any row stride of at least
+ * their columns and any alignment to their element; bf16 ones whose address is a
+ * multiple of 16 bytes and whose columns and stride are multiples of 8 are read as
+ * they lie, others are copied into the workspace first.  Products of bf16 values
+ * are exact; fp32 values are split into three bf16 terms, exactly from 2^-110 in size on
+ * (below, what lies under 2^-133 is cut off), of whose nine products the six largest
+ * are formed.  Sums are kept in fp32, in a fixed order: results repeat to the bit.  A
+ * NaN spreads as in the formulas; an infinity (in fp32 also a value from 2^128 - 2^119
+ * on) gives an infinity or a NaN where its products reach.
+ */
+
+/*
+ * Log probabilities of given tokens from the last activations: z = X W^T (X: rows x
+ * dim, W: vocab x dim, both dtype), z not kept,
+ *   lse[r]  = log sum_j exp(z_rj)
+ *   logp[r] = z_rt - lse[r], t = targets[r]; 0 when t is outside [0, vocab) (a token
+ *             without loss)
+ * logp and targets may both be NULL.  z is not rounded to dtype.  logp is never above 0.
+ * rows == 0 does nothing.
+ * Errors: EINVAL (NULL pointers, rows outside [0, 2^31), dim outside [1, 2^20],
+ * vocab outside [1, 2^30], strides, dtype, a workspace not aligned to 16, outputs or
+ * workspace that overlap another buffer), ENOMEM (workspace too small), EUNSUPPORTED
+ * (a product of more than 2^22 tiles).
+ */
+size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype);
+shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W, int dtype, int64_t rows, int64_t dim,
+                                      int64_t vocab, int64_t ld_x, int64_t ld_w, const int32_t* targets, float* logp,
+                                      float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Its gradient.  Given lse and the gradients of the outputs (g_logp with targets, g_lse;
+ * fp32, rows; each may be NULL for zero),
+ *   dz_rj = (g_lse - g_logp) exp(z_rj - lse) + [j = t] g_logp   (no g_logp without a target)
+ *   dX = dz W             (rows x dim, dtype)
+ *   dW = beta dW + dz^T X (vocab x dim, g_dtype; not read when beta == 0)
+ * dX or dW may be NULL.  The logits are formed again, in pieces of the vocabulary.
+ * dz is kept in three bf16 terms where dtype or g_dtype is fp32 (dX of bf16 inputs takes
+ * the first), else in one.  A row whose gradients are all 0 adds nothing to dW if X and
+ * lse are finite there.  rows == 0: dW = beta dW.
+ * Errors: as above, EINVAL for a non-finite beta, g_logp without targets, or neither dX nor
+ * dW.
+ */
+size_t shampoo_vocab_logprobs_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype);
+shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const void* W, int dtype, int64_t rows,
+                                           int64_t dim, int64_t vocab, int64_t ld_x, int64_t ld_w,
+                                           const int32_t* targets, const float* lse, const float* g_logp,
+                                           const float* g_lse, void* dX, int64_t ld_dx, void* dW, int g_dtype,
+                                           int64_t ld_dw, float beta, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Gated feed-forward block: G = X Wg, U = X Wu (X: rows x dim, Wg and Wu: dim x width),
+ *   H = act(G) o U   (act: SHAMPOO_ACT_*, of the sums before they are rounded)
+ * G and U are written too unless both are NULL.  X, weights and outputs: dtype.
+ * rows == 0 does nothing.  Sizes: dim in [1, 2^20], width in [1, 2^19].
+ * Errors: as above, EINVAL for a bad act or only one of G and U.
+ */
+size_t shampoo_gated_ffn_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype);
+shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, const void* Wu, int dtype, int64_t rows,
+                                 int64_t dim, int64_t width, int64_t ld_x, int64_t ld_wg, int64_t ld_wu, int act,
+                                 void* H, int64_t ld_h, void* G, int64_t ld_g, void* U, int64_t ld_u, void* workspace,
+                                 size_t ws_bytes, void* stream);
+
+/*
+ * Its gradients from dH (rows x width, dtype), with G and U as they were kept, or both
+ * NULL: then the projections are formed again and not rounded.
+ *   dG = dH o U o act'(G), dU = dH o act(G)
+ *   dX = dG Wg^T + dU Wu^T          (rows x dim, dtype)
+ *   dWg = beta dWg + X^T dG, dWu = beta dWu + X^T dU   (dim x width, g_dtype; not read
+ *                                                       when beta == 0)
+ * dX may be NULL, or dWg and dWu.  dG and dU are kept in bf16 terms as dz above.
+ * rows == 0: dWg = beta dWg, dWu = beta dWu.
+ * Errors: as above, EINVAL for only one of G and U or of dWg and dWu, or no output.
+ */
+size_t shampoo_gated_ffn_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype);
+shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* Wg, const void* Wu, int dtype,
+                                      int64_t rows, int64_t dim, int64_t width, int64_t ld_x, int64_t ld_wg,
+                                      int64_t ld_wu, int act, const void* dH, int64_t ld_dh, const void* G,
+                                      int64_t ld_g, const void* U, int64_t ld_u, void* dX, int64_t ld_dx, void* dWg,
+                                      int64_t ld_dwg, void* dWu, int64_t ld_dwu, int g_dtype, float beta,
+                                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Dropout: Y = R + [kept] X 65536 / (65536 - n), n = rate 65536 rounded to nearest even; R
+ * may be NULL (zero), Y may be X or R (same row stride).  n = 65536 keeps nothing.  The mask
+ * is that of a counter-based generator, never stored: Philox 4x32 with 10 rounds (Salmon,
+ * Moraes, Dror and Shaw 2011), key = seed (low word, high word), counter = (column / 8,
+ * row, offset low, offset high); of the 128 bits, 16-bit half column % 8 (low halves of
+ * the words first) decides: kept if it is at least n.  The gradient with respect to X is
+ * the same call on dY with R NULL.  What is not kept leaves no trace, NaN included.
+ * Calls whose masks must differ take another seed or offset (one offset covers any
+ * tensor).  Sizes: rows in [0, 2^31), cols in [1, 2^20].
+ * Errors: EINVAL (NULL X or Y, sizes, strides, dtype, rate outside [0, 1], Y overlapping X
+ * or R without being the same).
+ */
+shampoo_status shampoo_dropout(void* handle, const void* X, const void* R, void* Y, int dtype, int64_t rows,
+                               int64_t cols, int64_t ld_x, int64_t ld_r, int64_t ld_y, double rate, uint64_t seed,
+                               uint64_t offset, void* stream);
+
+/*
  * Measurement support.  While enabled, every launch of the timed kernel
  * classes below is bracketed by HIP events on its stream.
  * shampoo_timing_read synchronizes those events, returns the summed duration
@@ -577,7 +682,10 @@ enum {
   SHAMPOO_KCLASS_LOGPROBS = 8,   /* token log probabilities and their gradient */
   SHAMPOO_KCLASS_ACT = 9,        /* activation checkpoints: encode, decode, activation gradient */
   SHAMPOO_KCLASS_WGRAD = 10,     /* weight gradients from checkpoints */
-  SHAMPOO_KCLASS_COUNT = 11
+  SHAMPOO_KCLASS_VOCAB = 11,     /* loss from the last activations and its gradient */
+  SHAMPOO_KCLASS_FFN = 12,       /* gated feed-forward block and its gradient */
+  SHAMPOO_KCLASS_DROPOUT = 13,   /* dropout */
+  SHAMPOO_KCLASS_COUNT = 14
 };
 shampoo_status shampoo_timing_enable(void* handle, int enable);
 shampoo_status shampoo_timing_read(void* handle, int kclass, double* total_ms, int64_t* launches);

@@ -28,9 +28,10 @@ ROOT_CONVERGED, ROOT_STAGNATED, ROOT_MAXITER, ROOT_DIVERGED, ROOT_NOT_PD = 0, 1,
 PRECISION_FP32, PRECISION_AUTO, PRECISION_FP64 = 0, 1, 2
 SCALING_FROBENIUS, SCALING_POWER4 = 0, 1
 (KCLASS_NEWTON_F32, KCLASS_NEWTON_F64, KCLASS_STATS, KCLASS_PRECOND, KCLASS_GRAFT, KCLASS_ROOT_AUX, KCLASS_EMB,
- KCLASS_NEWTON_WARM, KCLASS_LOGPROBS, KCLASS_ACT, KCLASS_WGRAD) = range(11)
+ KCLASS_NEWTON_WARM, KCLASS_LOGPROBS, KCLASS_ACT, KCLASS_WGRAD, KCLASS_VOCAB, KCLASS_FFN,
+ KCLASS_DROPOUT) = range(14)
 KCLASS_NAMES = ["newton_f32", "newton_f64", "stats", "precond", "graft", "root_aux", "emb", "newton_warm", "logprobs",
-                "act", "wgrad"]
+                "act", "wgrad", "vocab", "ffn", "dropout"]
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
 MAX_TOP = 64
 
@@ -94,6 +95,19 @@ _sig = {
     "shampoo_act_grad": (_i, [_vp, _vp, _i64, _i64, _i, _vp, _i, _i64, _vp, _i64, _vp]),
     "shampoo_act_weight_grad_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "shampoo_act_weight_grad": (_i, [_vp, _vp, _i64, _i64, _vp, _i, _i64, _i64, _vp, _i, _i64, _f, _vp, _sz, _vp]),
+    "shampoo_vocab_logprobs_workspace_bytes": (_sz, [_i64, _i64, _i64, _i]),
+    "shampoo_vocab_logprobs": (_i, [_vp, _vp, _vp, _i, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "shampoo_vocab_logprobs_grad_workspace_bytes": (_sz, [_i64, _i64, _i64, _i, _i]),
+    "shampoo_vocab_logprobs_grad": (_i, [_vp, _vp, _vp, _i, _i64, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64,
+                                         _vp, _i, _i64, _f, _vp, _sz, _vp]),
+    "shampoo_gated_ffn_workspace_bytes": (_sz, [_i64, _i64, _i64, _i]),
+    "shampoo_gated_ffn": (_i, [_vp, _vp, _vp, _vp, _i, _i64, _i64, _i64, _i64, _i64, _i64, _i, _vp, _i64, _vp, _i64,
+                               _vp, _i64, _vp, _sz, _vp]),
+    "shampoo_gated_ffn_grad_workspace_bytes": (_sz, [_i64, _i64, _i64, _i, _i]),
+    "shampoo_gated_ffn_grad": (_i, [_vp, _vp, _vp, _vp, _i, _i64, _i64, _i64, _i64, _i64, _i64, _i, _vp, _i64, _vp,
+                                    _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i, _f, _vp, _sz, _vp]),
+    "shampoo_dropout": (_i, [_vp, _vp, _vp, _vp, _i, _i64, _i64, _i64, _i64, _i64, C.c_double, C.c_uint64, C.c_uint64,
+                             _vp]),
     "shampoo_timing_enable": (_i, [_vp, _i]),
     "shampoo_timing_read": (_i, [_vp, _i, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
 }
@@ -990,6 +1004,257 @@ def shampoo_act_weight_grad(handle, ckpt, dY, G, beta=0.0, workspace=None, strea
                                                 g[2], beta, _ptr(workspace),
                                                 0 if workspace is None else workspace.numel(),
                                                 _stream_on(stream, dev)))
+
+
+# ------------------------------------------------------------------ the layers around the step
+def _code(dtype):
+    """The library's code of a torch type (its codes stand for themselves)."""
+    torch = _torch_mod or _torch()
+    if dtype is torch.float32:
+        return SHAMPOO_F32
+    if dtype is torch.bfloat16:
+        return SHAMPOO_BF16
+    _need(isinstance(dtype, int), f"dtype {dtype}, expected float32 or bfloat16")
+    return dtype
+
+
+def _mat(t, rows, cols, code, dev):
+    """The layout of t if it has this shape, type (None: either) and device, else None."""
+    x = _layout(t)
+    ok = x is not None and x[0] == rows and x[1] == cols and (code is None or x[3] == code) and x[4] == dev
+    return x if ok else None
+
+
+def _opt(x):
+    """Pointer and row stride of a layout that may be None."""
+    return (None, 0) if x is None else (x[5], x[2])
+
+
+def _check_all_apart(written, read):
+    """Every written matrix (name, tensor) is apart from every other."""
+    for i, (name, t) in enumerate(written):
+        for other, u in written[i + 1:] + read:
+            if t is not None and u is not None:
+                _check_apart(t, u, f"{name} and {other}", False)
+
+
+def _all_apart(written, read):
+    """The same of layouts (None: not given)."""
+    for i, a in enumerate(written):
+        if a is not None:
+            for b in written[i + 1:] + read:
+                if b is not None and not _apart(a, b):
+                    return False
+    return True
+
+
+def _check_like(t, what, rows, cols, dtype=None):
+    if t is None:
+        return
+    _check_matrix(t, what)
+    _need(tuple(t.shape) == (rows, cols), f"{what}: shape {tuple(t.shape)}, expected {(rows, cols)}")
+    _need(dtype is None or t.dtype is dtype, f"{what}: dtype {t.dtype}, expected {dtype}")
+
+
+def shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dtype):
+    return int(_lib.shampoo_vocab_logprobs_workspace_bytes(int(rows), int(dim), int(vocab), _code(dtype)))
+
+
+def shampoo_vocab_logprobs(handle, X, W, targets, logp, lse, workspace=None, stream=None):
+    """X: rows x dim, W: vocab x dim, both fp32 or both bf16 (row-major views);
+    targets int32 [rows] and logp fp32 [rows] (both or neither); lse fp32 [rows];
+    workspace: uint8, shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, X.dtype)."""
+    x, w = _layout(X), _layout(W)
+    ok = (x is not None and w is not None and x[1] == w[1] and x[3] == w[3] and x[4] == w[4] and lse is not None and
+          (targets is None) == (logp is None))
+    if ok:
+        rows, dim, ld, dt, dev, ptr = x
+        vocab = w[0]
+        f32, vec = _torch_mod.float32, (rows,)
+        ok = (_plain(lse, f32, vec, dev) and _plain(logp, f32, vec, dev) and _on_handle(handle, dev) and
+              _plain(targets, _torch_mod.int32, vec, dev) and
+              _room(workspace, _lib.shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dt), dev))
+    if not ok:
+        _refuse_vocab(handle, X, W, targets, lse, (("logp", logp),), workspace,
+                      lambda r, d, v: _lib.shampoo_vocab_logprobs_workspace_bytes(r, d, v, _code(X.dtype)),
+                      lambda: _need((targets is None) == (logp is None), "targets and logp go together"))
+    _check(handle, _lib.shampoo_vocab_logprobs(handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets),
+                                               _ptr(logp), lse.data_ptr(), _ptr(workspace),
+                                               0 if workspace is None else workspace.numel(),
+                                               _stream_on(stream, dev)))
+
+
+def _refuse_vocab(handle, X, W, targets, lse, vecs, workspace, room, pairs, more=()):
+    _check_matrix(X, "X")
+    _check_like(W, "W", int(W.shape[0]) if W.dim() else 0, int(X.shape[1]), X.dtype)
+    (rows, dim), vocab = X.shape, int(W.shape[0])
+    pairs()
+    _need(lse is not None, "lse is required")
+    for what, t in (("lse", lse),) + vecs:
+        _check_shape(t, (rows,), what)
+    _check_shape(targets, (rows,), "targets", "int32")
+    _refuse(handle, (("X", X), ("W", W), ("targets", targets), ("lse", lse), ("workspace", workspace)) + vecs + more,
+            (lambda: _check_bytes(workspace, room(rows, dim, vocab), "workspace"),))
+
+
+def shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dtype, g_dtype):
+    return int(_lib.shampoo_vocab_logprobs_grad_workspace_bytes(int(rows), int(dim), int(vocab), _code(dtype),
+                                                                _code(g_dtype)))
+
+
+def shampoo_vocab_logprobs_grad(handle, X, W, targets, lse, dX=None, dW=None, g_logp=None, g_lse=None, beta=0.0,
+                                workspace=None, stream=None):
+    """dX (X's shape and type, or None) and dW = beta dW + ... (W's shape, fp32 or bf16, or
+    None) from the gradients of shampoo_vocab_logprobs' outputs: g_logp (with targets),
+    g_lse: fp32 [rows]; workspace: uint8, shampoo_vocab_logprobs_grad_workspace_bytes(rows,
+    dim, vocab, X.dtype, dW.dtype) (without dW: X.dtype twice)."""
+    x, w = _layout(X), _layout(W)
+    ok = (x is not None and w is not None and x[1] == w[1] and x[3] == w[3] and x[4] == w[4] and lse is not None and
+          (g_logp is None or targets is not None) and (dX is not None or dW is not None))
+    if ok:
+        rows, dim, ld, dt, dev, ptr = x
+        vocab = w[0]
+        dx, dw = None if dX is None else _mat(dX, rows, dim, dt, dev), None if dW is None else _mat(dW, vocab, dim, None, dev)
+        gdt = dt if dw is None else dw[3]
+        f32, vec = _torch_mod.float32, (rows,)
+        ok = ((dx is None) == (dX is None) and (dw is None) == (dW is None) and _plain(lse, f32, vec, dev) and
+              _plain(g_logp, f32, vec, dev) and _plain(g_lse, f32, vec, dev) and
+              _plain(targets, _torch_mod.int32, vec, dev) and _on_handle(handle, dev) and
+              _all_apart([dx, dw], [x, w]) and
+              _room(workspace, _lib.shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dt, gdt), dev))
+    if not ok:
+        def pairs():
+            _need(g_logp is None or targets is not None, "g_logp needs targets")
+            _need(dX is not None or dW is not None, "dX or dW is required")
+            _check_like(dX, "dX", *X.shape, X.dtype)
+            _check_like(dW, "dW", *W.shape)
+            _check_all_apart([("dX", dX), ("dW", dW)], [("X", X), ("W", W)])
+        _refuse_vocab(handle, X, W, targets, lse, (("g_logp", g_logp), ("g_lse", g_lse)), workspace,
+                      lambda r, d, v: _lib.shampoo_vocab_logprobs_grad_workspace_bytes(
+                          r, d, v, _code(X.dtype), _code(X.dtype if dW is None else dW.dtype)), pairs,
+                      (("dX", dX), ("dW", dW)))
+    _check(handle, _lib.shampoo_vocab_logprobs_grad(
+        handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets), lse.data_ptr(), _ptr(g_logp), _ptr(g_lse),
+        *_opt(dx), _opt(dw)[0], gdt, _opt(dw)[1], float(beta), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_on(stream, dev)))
+
+
+def shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype):
+    return int(_lib.shampoo_gated_ffn_workspace_bytes(int(rows), int(dim), int(width), _code(dtype)))
+
+
+def _ffn_shapes(X, Wg, Wu, wide):
+    """Layouts of X, Wg, Wu and of the rows x width matrices `wide`, or None where one
+    does not fit the others."""
+    x, wg = _layout(X), _layout(Wg)
+    if x is None or wg is None or wg[0] != x[1] or wg[3] != x[3] or wg[4] != x[4]:
+        return None
+    rows, dim, _, dt, dev, _ = x
+    wu = _mat(Wu, dim, wg[1], dt, dev)
+    rest = [None if t is None else _mat(t, rows, wg[1], dt, dev) for t in wide]
+    if wu is None or any((a is None) != (t is None) for a, t in zip(rest, wide)):
+        return None
+    return x, wg, wu, rest
+
+
+def _refuse_ffn(handle, X, Wg, Wu, wide, more, written, read, room, workspace):
+    _check_matrix(X, "X")
+    _check_like(Wg, "Wg", int(X.shape[1]), int(Wg.shape[-1]), X.dtype)
+    _check_like(Wu, "Wu", *Wg.shape, X.dtype)
+    (rows, dim), width = X.shape, int(Wg.shape[1])
+    for name, t in wide:
+        _check_like(t, name, rows, width, X.dtype)
+    for check in more:
+        check(rows, dim, width)
+    base = [("X", X), ("Wg", Wg), ("Wu", Wu)]
+    _check_all_apart(written, base + read)
+    _refuse(handle, tuple(base + written + read) + (("workspace", workspace),),
+            (lambda: _check_bytes(workspace, room(rows, dim, width), "workspace"),))
+
+
+def shampoo_gated_ffn(handle, X, Wg, Wu, H, act=ACT_SILU, G=None, U=None, workspace=None, stream=None):
+    """H (rows x width) = act(X Wg) o (X Wu); X: rows x dim, Wg and Wu: dim x width; G and U
+    (both or neither): the projections, rows x width; all fp32 or all bf16 (row-major
+    views); workspace: uint8, shampoo_gated_ffn_workspace_bytes(rows, dim, width, X.dtype)."""
+    s = _ffn_shapes(X, Wg, Wu, (H, G, U)) if H is not None and (G is None) == (U is None) else None
+    ok = s is not None
+    if ok:
+        x, wg, wu, (lh, lg, lu) = s
+        rows, dim, ld, dt, dev, ptr = x
+        width = wg[1]
+        ok = (_all_apart([lh, lg, lu], [x, wg, wu]) and _on_handle(handle, dev) and
+              _room(workspace, _lib.shampoo_gated_ffn_workspace_bytes(rows, dim, width, dt), dev))
+    if not ok:
+        _need(H is not None, "H is required")
+        _need((G is None) == (U is None), "G and U go together")
+        _refuse_ffn(handle, X, Wg, Wu, (("H", H), ("G", G), ("U", U)), (), [("H", H), ("G", G), ("U", U)], [],
+                    lambda r, d, w: _lib.shampoo_gated_ffn_workspace_bytes(r, d, w, _code(X.dtype)), workspace)
+    _check(handle, _lib.shampoo_gated_ffn(handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], int(act),
+                                          *_opt(lh), *_opt(lg), *_opt(lu), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel(), _stream_on(stream, dev)))
+
+
+def shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype):
+    return int(_lib.shampoo_gated_ffn_grad_workspace_bytes(int(rows), int(dim), int(width), _code(dtype),
+                                                           _code(g_dtype)))
+
+
+def shampoo_gated_ffn_grad(handle, X, Wg, Wu, dH, act=ACT_SILU, G=None, U=None, dX=None, dWg=None, dWu=None, beta=0.0,
+                           workspace=None, stream=None):
+    """Gradients of shampoo_gated_ffn from dH (rows x width): dX (X's shape and type, or
+    None), dWg and dWu = beta dW + ... (Wg's shape, both fp32 or both bf16; both or
+    neither).  G and U: the projections as kept, or None to form them again; workspace: uint8,
+    shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, X.dtype, dWg.dtype) (without
+    dWg: X.dtype twice)."""
+    pairs = (G is None) == (U is None) and (dWg is None) == (dWu is None) and (dX is not None or dWg is not None)
+    s = _ffn_shapes(X, Wg, Wu, (dH, G, U)) if dH is not None and pairs else None
+    ok = s is not None
+    if ok:
+        x, wg, wu, (lh, lg, lu) = s
+        rows, dim, ld, dt, dev, ptr = x
+        width = wg[1]
+        dx = None if dX is None else _mat(dX, rows, dim, dt, dev)
+        dg = None if dWg is None else _mat(dWg, dim, width, None, dev)
+        gdt = dt if dg is None else dg[3]
+        du = None if dWu is None else _mat(dWu, dim, width, gdt, dev)
+        ok = ((dx is None) == (dX is None) and (dg is None) == (dWg is None) and (du is None) == (dWu is None) and
+              _all_apart([dx, dg, du], [x, wg, wu, lh, lg, lu]) and _on_handle(handle, dev) and
+              _room(workspace, _lib.shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dt, gdt), dev))
+    if not ok:
+        _need(dH is not None, "dH is required")
+        _need((G is None) == (U is None), "G and U go together")
+        _need((dWg is None) == (dWu is None), "dWg and dWu go together")
+        _need(dX is not None or dWg is not None, "dX, or dWg and dWu, are required")
+        _refuse_ffn(handle, X, Wg, Wu, (("dH", dH), ("G", G), ("U", U)),
+                    (lambda r, d, w: _check_like(dX, "dX", r, d, X.dtype), lambda r, d, w: _check_like(dWg, "dWg", d, w),
+                     lambda r, d, w: _check_like(dWu, "dWu", d, w, None if dWg is None else dWg.dtype)),
+                    [("dX", dX), ("dWg", dWg), ("dWu", dWu)], [("dH", dH), ("G", G), ("U", U)],
+                    lambda r, d, w: _lib.shampoo_gated_ffn_grad_workspace_bytes(
+                        r, d, w, _code(X.dtype), _code(X.dtype if dWg is None else dWg.dtype)), workspace)
+    _check(handle, _lib.shampoo_gated_ffn_grad(
+        handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], int(act), *_opt(lh), *_opt(lg), *_opt(lu),
+        *_opt(dx), *_opt(dg), *_opt(du), gdt, float(beta), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+        _stream_on(stream, dev)))
+
+
+def shampoo_dropout(handle, X, Y, rate, seed, offset=0, R=None, stream=None):
+    """Y = R + kept X / (1 - rate) (R None: zero); X, Y, R: one shape and type, fp32 or bf16
+    (row-major views; Y may be X or R).  seed and offset (64-bit) give the mask; the
+    gradient with respect to X is the same call on dY without R."""
+    x, y, r = _layout(X), _layout(Y), None if R is None else _layout(R)
+    ok = x is not None and y is not None and _alike(y, x) and (R is None or (r is not None and _alike(y, r)))
+    if not ok or not _on_handle(handle, x[4]) or not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        _need(0 <= seed < 1 << 64 and 0 <= offset < 1 << 64, f"seed {seed} or offset {offset} outside [0, 2^64)")
+        _check_matrix(X, "X")
+        _check_matrix(Y, "Y", X)
+        _check_apart(Y, X, "Y and X", True)
+        if R is not None:
+            _check_matrix(R, "R", X)
+            _check_apart(Y, R, "Y and R", True)
+        _refuse(handle, (("X", X), ("Y", Y), ("R", R)), ())
+    rows, cols, ld, dt, dev, ptr = x
+    _check(handle, _lib.shampoo_dropout(handle, ptr, _opt(r)[0], y[5], dt, rows, cols, ld, _opt(r)[1], y[2],
+                                        float(rate), seed, offset, _stream_on(stream, dev)))
 
 
 def shampoo_timing_enable(handle, enable=True):

@@ -6,11 +6,12 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libshampoo.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "layers.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "layers.hip", "model_layers.hip")]
 HEADERS = [os.path.join(HERE, "csrc", f) for f in ("kernels.hpp", "tile_mfma.hpp", "fp32_block.hpp", "split_mfma.hpp",
                                                    "direct_mma.hpp", "small_root.hpp", "embedding.hpp", "handle.hpp",
                                                    "layer_plans.hpp", "logprobs.hpp", "act_checkpoint.hpp",
-                                                   "weight_grad.hpp")]
+                                                   "weight_grad.hpp", "layer_host.hpp", "stream_plans.hpp", "stream_mma.hpp",
+                                                   "vocab_loss.hpp", "gated_ffn.hpp", "dropout.hpp")]
 HEADERS.append(os.path.join(ROOT, "include", "shampoo.h"))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

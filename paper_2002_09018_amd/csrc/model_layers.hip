@@ -1,0 +1,520 @@
+// Host side of the calls of a model's own layers: the loss from the last activations,
+// the gated feed-forward block, dropout (vocab_loss.hpp, gated_ffn.hpp, dropout.hpp).
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+#include <initializer_list>
+
+#include "dropout.hpp"
+#include "gated_ffn.hpp"
+#include "layer_host.hpp"
+#include "shampoo.h"
+#include "stream_plans.hpp"
+#include "vocab_loss.hpp"
+
+using namespace shp;
+
+namespace {
+
+using FewShape = MmaShape<32, 128, 32, 64, 4>;
+using MidShape = MmaShape<128, 128, 64, 64, 4>;
+using BigShape = MmaShape<256, 256, 128, 64, 4>;
+
+// A buffer of a call and what to call it.
+struct Named {
+  Span s;
+  const char* name;
+};
+
+// Every buffer that is written shares no memory with any other.
+shampoo_status check_all_apart(Handle* h, std::initializer_list<Named> written, std::initializer_list<Named> read) {
+  for (const Named* a = written.begin(); a != written.end(); ++a) {
+    for (const Named* b = a + 1; b != written.end(); ++b) STATUS_TRY(check_apart(h, a->s, a->name, b->s, b->name));
+    for (const Named& b : read) STATUS_TRY(check_apart(h, a->s, a->name, b.s, b.name));
+  }
+  return SHAMPOO_OK;
+}
+
+shampoo_status check_room(Handle* h, const void* workspace, size_t ws_bytes, size_t need) {
+  if (need && (!workspace || ws_bytes < need))
+    return fail(h, SHAMPOO_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+  if (!aligned16(workspace)) return fail(h, SHAMPOO_EINVAL, "workspace not aligned to 16 bytes");
+  return SHAMPOO_OK;
+}
+
+shampoo_status check_size(Handle* h, int64_t v, int64_t lo, int64_t hi, const char* what) {
+  if (v < lo || v > hi)
+    return fail(h, SHAMPOO_EINVAL, "%s = %lld outside [%lld, %lld]", what, (long long)v, (long long)lo, (long long)hi);
+  return SHAMPOO_OK;
+}
+shampoo_status check_ld(Handle* h, int64_t ld, int64_t cols, const char* what) {
+  if (ld < cols || ld > (int64_t(1) << 40))
+    return fail(h, SHAMPOO_EINVAL, "%s %lld outside [%lld, 2^40]", what, (long long)ld, (long long)cols);
+  return SHAMPOO_OK;
+}
+
+// Whether the products can read a matrix as it lies: 16-byte chunks that lie whole in
+// its rows, and tiles whose offsets fit 31 bits.
+bool as_it_lies(const void* p, int64_t ld, int64_t cols, int dtype) {
+  return dtype == SHAMPOO_BF16 && aligned16(p) && cols % 8 == 0 && ld % 8 == 0 && ld <= (1 << 21);
+}
+
+// An operand's planes: p and the elements from one plane to the next.
+struct Planes16 {
+  const uint16_t* p;
+  int64_t ld, plane;
+};
+const uint16_t* plane_of(const Planes16& x, int i) { return x.p + i * x.plane; }
+
+// X as the products read it, copied to `room` first where it has to be.
+shampoo_status packed(Handle* h, int cls, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld, bool pack,
+                      const PackPlan& p, void* room, hipStream_t s, Planes16* out) {
+  if (!pack) {
+    *out = {static_cast<const uint16_t*>(X), ld, 0};
+    return SHAMPOO_OK;
+  }
+  *out = {static_cast<const uint16_t*>(room), p.ld, p.plane};
+  return unit_launches(h, cls, rows, cols, p.ld / 8, s, [&](const ActShape& sh, dim3 grid) {
+    with_type(dtype, [&](auto* type) {
+      using S = std::remove_pointer_t<decltype(type)>;
+      hipLaunchKernelGGL(pack_kernel<S>, grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(X), ld,
+                         static_cast<uint16_t*>(room), p.plane);
+    });
+  });
+}
+
+// Products of two operands' terms, the smallest first: all six pairs of three planes
+// that count, or the terms of B (or A) alone.
+void add_segs(MmaArgs& q, const Planes16& a, int na, const Planes16& b, int nb, const Planes16* b2 = nullptr) {
+  for (int s = std::min(na + nb - 2, 2); s >= 0; --s)
+    for (int i = std::min(s, na - 1); i >= 0; --i) {
+      const int j = s - i;
+      if (j >= nb) continue;
+      MmaSeg& g = q.seg[q.segs++];
+      g = {plane_of(a, i), plane_of(b, j), b2 ? plane_of(*b2, j) : nullptr, (int)a.ld, (int)b.ld, b2 ? (int)b2->ld : 0};
+    }
+}
+
+// Fills what the plan says; ka and kb are rounded up to 8 where the contraction
+// lies along rows (their padding is zeros).
+void use_plan(MmaArgs& q, const MmaPlan& p, int64_t M, int64_t N, int64_t K, int la, int lb, void* part) {
+  q.M = (int)M;
+  q.N = (int)N;
+  q.ka = (int)(la == kLayoutRow ? cdiv64(K, 8) * 8 : K);
+  q.kb = (int)(lb == kLayoutRow ? cdiv64(K, 8) * 8 : K);
+  q.seg_stages = (int)p.seg_stages;
+  q.tiles_m = (int)p.tiles_m;
+  q.tiles_n = (int)p.tiles_n;
+  q.splits = p.splits;
+  q.per_split = p.per_split;
+  q.part = p.part ? static_cast<float*>(part) : nullptr;
+  q.ld_part = p.ld_part;
+}
+
+template <typename T, int LA, int LB, typename E>
+shampoo_status mma_launch(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_t s) {
+  auto k = mma_kernel<T, LA, LB, E>;
+  // more LDS than a launch may take by default: asked for once per device
+  static std::atomic<uint64_t> asked{0};
+  const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
+  if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
+    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLdsB));
+    asked.fetch_or(bit, std::memory_order_relaxed);
+  }
+  const int64_t groups = (int64_t)q.tiles_m * q.tiles_n * q.splits;
+  if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "a product of %d x %d", q.M, q.N);
+  return launch(h, cls, s, [&] { hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(T::kThr), T::kLdsB, s, q, e); });
+}
+
+// The product; what was cut is left in q.part.
+template <int LA, int LB, typename E>
+shampoo_status product(Handle* h, int cls, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
+  if constexpr (LA == kLayoutRow)
+    if (shape == kShapeFew) return mma_launch<FewShape, LA, LB>(h, cls, q, e, s);
+  if (shape == kShapeMid) return mma_launch<MidShape, LA, LB>(h, cls, q, e, s);
+  return mma_launch<BigShape, LA, LB>(h, cls, q, e, s);
+}
+
+// The epilogue over the parts.
+template <typename E>
+shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_t s) {
+  const int64_t units = (int64_t)q.M * cdiv64(q.N, 8);
+  return launch(h, cls, s, [&] {
+    hipLaunchKernelGGL(mma_join_kernel<E>, dim3(act_grid(units)), dim3(kThreads), 0, s, q, e);
+  });
+}
+
+template <int LA, int LB, typename E>
+shampoo_status product_whole(Handle* h, int cls, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
+  STATUS_TRY((product<LA, LB>(h, cls, shape, q, e, s)));
+  return q.part ? join(h, cls, q, e, s) : SHAMPOO_OK;
+}
+
+shampoo_status scaled(Handle* h, int cls, void* C, int dtype, int64_t rows, int64_t cols, int64_t ld, float beta,
+                      hipStream_t s) {
+  return launch(h, cls, s, [&] {
+    with_type(dtype, [&](auto* type) {
+      using S = std::remove_pointer_t<decltype(type)>;
+      hipLaunchKernelGGL(scale_kernel<S>, dim3(act_grid(rows * cols)), dim3(kThreads), 0, s, static_cast<S*>(C), rows,
+                         cols, ld, beta);
+    });
+  });
+}
+
+const char* typed(const void* p, int64_t elements, int dtype) {
+  return static_cast<const char*>(p) + elements * (dtype == SHAMPOO_BF16 ? 2 : 4);
+}
+
+shampoo_status check_vocab(Handle* h, int dtype, int64_t rows, int64_t dim, int64_t vocab, int64_t ld_x, int64_t ld_w) {
+  STATUS_TRY(check_dtype(h, dtype, "X and W"));
+  STATUS_TRY(check_size(h, rows, 0, kMaxTokens, "rows"));
+  STATUS_TRY(check_size(h, dim, 1, kMaxCols, "dim"));
+  STATUS_TRY(check_size(h, vocab, 1, kMaxVocab, "vocab"));
+  STATUS_TRY(check_ld(h, ld_x, dim, "ld_x"));
+  return check_ld(h, ld_w, dim, "ld_w");
+}
+
+shampoo_status check_ffn(Handle* h, int dtype, int64_t rows, int64_t dim, int64_t width, int64_t ld_x, int64_t ld_wg,
+                         int64_t ld_wu, int act) {
+  STATUS_TRY(check_dtype(h, dtype, "X, Wg and Wu"));
+  STATUS_TRY(check_size(h, rows, 0, kMaxTokens, "rows"));
+  STATUS_TRY(check_size(h, dim, 1, kMaxCols, "dim"));
+  STATUS_TRY(check_size(h, width, 1, kMaxCols / 2, "width"));
+  if (act < SHAMPOO_ACT_NONE || act > SHAMPOO_ACT_SILU) return fail(h, SHAMPOO_EINVAL, "bad activation %d", act);
+  STATUS_TRY(check_ld(h, ld_x, dim, "ld_x"));
+  STATUS_TRY(check_ld(h, ld_wg, width, "ld_wg"));
+  return check_ld(h, ld_wu, width, "ld_wu");
+}
+
+bool sizes_ok(int64_t rows, int64_t dim, int64_t n, int64_t most, int dtype) {
+  return rows >= 0 && rows <= kMaxTokens && dim >= 1 && dim <= kMaxCols && n >= 1 && n <= most &&
+         (dtype == SHAMPOO_F32 || dtype == SHAMPOO_BF16);
+}
+
+}  // namespace
+
+extern "C" {
+
+// ---------------------------------------------------------------- loss
+size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype) {
+  if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
+  size_t need = 0;
+  for (int i = dtype == SHAMPOO_F32 ? 3 : 0; i < 4; ++i)
+    need = std::max(need, vocab_plan(rows, dim, vocab, dtype, i & 1, i & 2).bytes);
+  return need;
+}
+
+shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W, int dtype, int64_t rows, int64_t dim,
+                                      int64_t vocab, int64_t ld_x, int64_t ld_w, const int32_t* targets, float* logp,
+                                      float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_vocab(h, dtype, rows, dim, vocab, ld_x, ld_w));
+    if (rows == 0) return SHAMPOO_OK;
+    if (!X || !W || !lse || !logp != !targets)
+      return fail(h, SHAMPOO_EINVAL, "X, W or lse, or one of targets and logp is NULL");
+    const size_t need = shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dtype);
+    STATUS_TRY(check_room(h, workspace, ws_bytes, need));
+    STATUS_TRY(check_all_apart(
+        h, {{span(workspace, (int64_t)need), "workspace"}, {span(logp, rows * 4), "logp"}, {span(lse, rows * 4), "lse"}},
+        {{span(X, rows, dim, ld_x, dtype), "X"}, {span(W, vocab, dim, ld_w, dtype), "W"}, {span(targets, rows * 4), "targets"}}));
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    constexpr int kCls = SHAMPOO_KCLASS_VOCAB;
+    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
+    const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
+    Planes16 x, w;
+    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, s, &x));
+    auto* stat = reinterpret_cast<f32x2p*>(ws + p.at_stat);
+    auto* z_target = reinterpret_cast<float*>(ws + p.at_target);
+    int64_t entry0 = 0;
+    for (int64_t i = 0; i < p.pieces; ++i) {
+      const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
+      const MmaPlan& m = p.mma[i == p.pieces - 1];
+      STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
+      MmaArgs q{};
+      add_segs(q, x, p.x.planes, w, p.w.planes);
+      use_plan(q, m, rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
+      const LseEpilogue e{{targets, (int)vocab, (int)v0}, stat + entry0, p.entries, z_target};
+      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, m.shape, q, e, s)));
+      if (q.part) {
+        const int64_t groups = cdiv64(rows * cdiv64(n, kStatCols), kThreads / 64);
+        if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
+        STATUS_TRY(launch(h, kCls, s, [&] {
+          hipLaunchKernelGGL(logit_stat_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, q, e);
+        }));
+      }
+      entry0 += vocab_entries(m, n);
+    }
+    return launch(h, kCls, s, [&] {
+      const int64_t groups = std::min<int64_t>(cdiv64(rows, kThreads / 64), 1 << 20);
+      hipLaunchKernelGGL(lse_join_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, rows, (int)p.entries, stat,
+                         VocabTargets{targets, (int)vocab, 0}, z_target, logp, lse);
+    });
+  });
+}
+
+size_t shampoo_vocab_logprobs_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype) {
+  if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
+  if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
+  size_t need = 0;
+  for (int i = dtype == SHAMPOO_F32 ? 3 : 0; i < 4; ++i)
+    need = std::max(need, vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, i & 1, i & 2).bytes);
+  return need;
+}
+
+shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const void* W, int dtype, int64_t rows,
+                                           int64_t dim, int64_t vocab, int64_t ld_x, int64_t ld_w,
+                                           const int32_t* targets, const float* lse, const float* g_logp,
+                                           const float* g_lse, void* dX, int64_t ld_dx, void* dW, int g_dtype,
+                                           int64_t ld_dw, float beta, void* workspace, size_t ws_bytes, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_vocab(h, dtype, rows, dim, vocab, ld_x, ld_w));
+    STATUS_TRY(check_dtype(h, g_dtype, "dW"));
+    if (dX) STATUS_TRY(check_ld(h, ld_dx, dim, "ld_dx"));
+    if (dW) STATUS_TRY(check_ld(h, ld_dw, dim, "ld_dw"));
+    if (!isfinite(beta)) return fail(h, SHAMPOO_EINVAL, "beta is not finite");
+    if (!dX && !dW) return fail(h, SHAMPOO_EINVAL, "dX and dW are NULL");
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    constexpr int kCls = SHAMPOO_KCLASS_VOCAB;
+    if (rows == 0) return dW ? scaled(h, kCls, dW, g_dtype, vocab, dim, ld_dw, beta, s) : SHAMPOO_OK;
+    if (!X || !W || !lse) return fail(h, SHAMPOO_EINVAL, "X, W or lse is NULL");
+    if (g_logp && !targets) return fail(h, SHAMPOO_EINVAL, "g_logp without targets");
+    const size_t need = shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dtype, g_dtype);
+    STATUS_TRY(check_room(h, workspace, ws_bytes, need));
+    STATUS_TRY(check_all_apart(h,
+                               {{span(workspace, (int64_t)need), "workspace"},
+                                {span(dX, rows, dim, ld_dx, dtype), "dX"},
+                                {span(dW, vocab, dim, ld_dw, g_dtype), "dW"}},
+                               {{span(X, rows, dim, ld_x, dtype), "X"},
+                                {span(W, vocab, dim, ld_w, dtype), "W"},
+                                {span(targets, rows * 4), "targets"},
+                                {span(lse, rows * 4), "lse"},
+                                {span(g_logp, rows * 4), "g_logp"},
+                                {span(g_lse, rows * 4), "g_lse"}}));
+    char* ws = static_cast<char*>(workspace);
+    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
+    const VocabGradPlan p = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, pack_x, pack_w);
+    Planes16 x, w;
+    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, s, &x));
+    uint16_t* dz = reinterpret_cast<uint16_t*>(ws + p.at_dz);
+    const Planes16 pz{dz, p.ld_dz, rows * p.ld_dz};
+    const int nx = p.x.planes, nw = p.w.planes;
+    MmaArgs qx{};
+    const OutEpilogue out_x{{dX, nullptr}, {ld_dx, 0}, 0, (int)dim, dtype == SHAMPOO_BF16, 0.f};
+    for (int64_t i = 0; i < p.pieces; ++i) {
+      const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
+      const bool last = i == p.pieces - 1;
+      STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
+      MmaArgs q{};
+      add_segs(q, x, nx, w, nw);
+      use_plan(q, p.z[last], rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
+      const DlogitEpilogue e{{targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes};
+      STATUS_TRY((product_whole<kLayoutRow, kLayoutRow>(h, kCls, p.z[last].shape, q, e, s)));
+      if (dX) {
+        // a bf16 dX takes the first term alone
+        MmaArgs r{};
+        add_segs(r, pz, nw == 1 ? 1 : p.planes, w, nw);
+        use_plan(r, p.dx[last], rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
+        r.part_add = i > 0;
+        STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, p.dx[last].shape, r, out_x, s)));
+        if (i == 0) qx = r;
+      }
+      if (dW) {
+        MmaArgs r{};
+        add_segs(r, pz, p.planes, x, nx);
+        use_plan(r, p.dw[last], n, dim, rows, kLayoutK, kLayoutK, ws + p.at_part);
+        const OutEpilogue out{{const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)), nullptr}, {ld_dw, 0}, 0, (int)dim,
+                              g_dtype == SHAMPOO_BF16, beta};
+        STATUS_TRY((product_whole<kLayoutK, kLayoutK>(h, kCls, p.dw[last].shape, r, out, s)));
+      }
+    }
+    return dX && qx.part ? join(h, kCls, qx, out_x, s) : SHAMPOO_OK;
+  });
+}
+
+// ---------------------------------------------------------------- feed-forward block
+size_t shampoo_gated_ffn_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype) {
+  if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
+  return ffn_plan(rows, dim, width, dtype, true, true, true).bytes;
+}
+
+shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, const void* Wu, int dtype, int64_t rows,
+                                 int64_t dim, int64_t width, int64_t ld_x, int64_t ld_wg, int64_t ld_wu, int act,
+                                 void* H, int64_t ld_h, void* G, int64_t ld_g, void* U, int64_t ld_u, void* workspace,
+                                 size_t ws_bytes, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_ffn(h, dtype, rows, dim, width, ld_x, ld_wg, ld_wu, act));
+    STATUS_TRY(check_ld(h, ld_h, width, "ld_h"));
+    if (!G != !U) return fail(h, SHAMPOO_EINVAL, "one of G and U is NULL");
+    if (G) STATUS_TRY(check_ld(h, ld_g, width, "ld_g"));
+    if (U) STATUS_TRY(check_ld(h, ld_u, width, "ld_u"));
+    if (rows == 0) return SHAMPOO_OK;
+    if (!X || !Wg || !Wu || !H) return fail(h, SHAMPOO_EINVAL, "X, Wg, Wu or H is NULL");
+    const size_t need = shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype);
+    STATUS_TRY(check_room(h, workspace, ws_bytes, need));
+    STATUS_TRY(check_all_apart(h,
+                               {{span(workspace, (int64_t)need), "workspace"},
+                                {span(H, rows, width, ld_h, dtype), "H"},
+                                {span(G, rows, width, ld_g, dtype), "G"},
+                                {span(U, rows, width, ld_u, dtype), "U"}},
+                               {{span(X, rows, dim, ld_x, dtype), "X"},
+                                {span(Wg, dim, width, ld_wg, dtype), "Wg"},
+                                {span(Wu, dim, width, ld_wu, dtype), "Wu"}}));
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    constexpr int kCls = SHAMPOO_KCLASS_FFN;
+    const bool px = !as_it_lies(X, ld_x, dim, dtype), pg = !as_it_lies(Wg, ld_wg, width, dtype);
+    const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
+    const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
+    Planes16 x, wg, wu;
+    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, px, p.x, ws + p.at_x, s, &x));
+    STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
+    STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
+    MmaArgs q{};
+    add_segs(q, x, p.x.planes, wg, p.wg.planes, &wu);
+    use_plan(q, p.mma, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
+    shampoo_status st = SHAMPOO_OK;
+    with_type(dtype, [&](auto* type) {
+      using S = std::remove_pointer_t<decltype(type)>;
+      const GatedEpilogue<S> e{act, (int)width, static_cast<S*>(H), static_cast<S*>(G), static_cast<S*>(U), ld_h, ld_g, ld_u};
+      st = product_whole<kLayoutRow, kLayoutK>(h, kCls, p.mma.shape, q, e, s);
+    });
+    return st;
+  });
+}
+
+size_t shampoo_gated_ffn_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype) {
+  if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
+  if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
+  return ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, true, true).bytes;
+}
+
+shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* Wg, const void* Wu, int dtype,
+                                      int64_t rows, int64_t dim, int64_t width, int64_t ld_x, int64_t ld_wg,
+                                      int64_t ld_wu, int act, const void* dH, int64_t ld_dh, const void* G,
+                                      int64_t ld_g, const void* U, int64_t ld_u, void* dX, int64_t ld_dx, void* dWg,
+                                      int64_t ld_dwg, void* dWu, int64_t ld_dwu, int g_dtype, float beta,
+                                      void* workspace, size_t ws_bytes, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_ffn(h, dtype, rows, dim, width, ld_x, ld_wg, ld_wu, act));
+    STATUS_TRY(check_dtype(h, g_dtype, "dWg and dWu"));
+    STATUS_TRY(check_ld(h, ld_dh, width, "ld_dh"));
+    if (!G != !U) return fail(h, SHAMPOO_EINVAL, "one of G and U is NULL");
+    if (!dWg != !dWu) return fail(h, SHAMPOO_EINVAL, "one of dWg and dWu is NULL");
+    if (!dX && !dWg) return fail(h, SHAMPOO_EINVAL, "dX, dWg and dWu are NULL");
+    if (G) STATUS_TRY(check_ld(h, ld_g, width, "ld_g"));
+    if (U) STATUS_TRY(check_ld(h, ld_u, width, "ld_u"));
+    if (dX) STATUS_TRY(check_ld(h, ld_dx, dim, "ld_dx"));
+    if (dWg) STATUS_TRY(check_ld(h, ld_dwg, width, "ld_dwg"));
+    if (dWu) STATUS_TRY(check_ld(h, ld_dwu, width, "ld_dwu"));
+    if (!isfinite(beta)) return fail(h, SHAMPOO_EINVAL, "beta is not finite");
+    STATUS_TRY(check_apart(h, span(dWg, dim, width, ld_dwg, g_dtype), "dWg", span(dWu, dim, width, ld_dwu, g_dtype), "dWu"));
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    constexpr int kCls = SHAMPOO_KCLASS_FFN;
+    if (rows == 0) {
+      if (!dWg) return SHAMPOO_OK;
+      STATUS_TRY(scaled(h, kCls, dWg, g_dtype, dim, width, ld_dwg, beta, s));
+      return scaled(h, kCls, dWu, g_dtype, dim, width, ld_dwu, beta, s);
+    }
+    if (!X || !Wg || !Wu || !dH) return fail(h, SHAMPOO_EINVAL, "X, Wg, Wu or dH is NULL");
+    const size_t need = shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype);
+    STATUS_TRY(check_room(h, workspace, ws_bytes, need));
+    STATUS_TRY(check_all_apart(h,
+                               {{span(workspace, (int64_t)need), "workspace"},
+                                {span(dX, rows, dim, ld_dx, dtype), "dX"},
+                                {span(dWg, dim, width, ld_dwg, g_dtype), "dWg"},
+                                {span(dWu, dim, width, ld_dwu, g_dtype), "dWu"}},
+                               {{span(X, rows, dim, ld_x, dtype), "X"},
+                                {span(Wg, dim, width, ld_wg, dtype), "Wg"},
+                                {span(Wu, dim, width, ld_wu, dtype), "Wu"},
+                                {span(dH, rows, width, ld_dh, dtype), "dH"},
+                                {span(G, rows, width, ld_g, dtype), "G"},
+                                {span(U, rows, width, ld_u, dtype), "U"}}));
+    char* ws = static_cast<char*>(workspace);
+    const bool px = (!G || dWg) && !as_it_lies(X, ld_x, dim, dtype);
+    const bool pg = (!G || dX) && !as_it_lies(Wg, ld_wg, width, dtype);
+    const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
+    const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
+    Planes16 x, wg, wu;
+    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, px, p.x, ws + p.at_x, s, &x));
+    STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
+    STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
+    const int nx = p.x.planes, nw = p.wg.planes;
+    uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.at_d);
+    const Planes16 dg{d, 2 * p.ld_d, rows * 2 * p.ld_d}, du{d + p.ld_d, dg.ld, dg.plane};
+    shampoo_status st = SHAMPOO_OK;
+    with_type(dtype, [&](auto* type) {
+      using S = std::remove_pointer_t<decltype(type)>;
+      const GatedGradEpilogue<S> e{act, (int)width, p.planes, static_cast<const S*>(dH), ld_dh, d, d + p.ld_d, dg.ld, dg.plane};
+      if (G) {
+        st = unit_launches(h, kCls, rows, width, p.ld_d / 8, s, [&](const ActShape& sh, dim3 grid) {
+          hipLaunchKernelGGL(gated_grad_kernel<S>, grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(G), ld_g,
+                             static_cast<const S*>(U), ld_u, e);
+        });
+      } else {
+        MmaArgs q{};
+        add_segs(q, x, nx, wg, nw, &wu);
+        use_plan(q, p.gu, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
+        st = product_whole<kLayoutRow, kLayoutK>(h, kCls, p.gu.shape, q, e, s);
+      }
+    });
+    STATUS_TRY(st);
+    if (dX) {
+      MmaArgs q{};
+      add_segs(q, dg, nw == 1 ? 1 : p.planes, wg, nw);
+      add_segs(q, du, nw == 1 ? 1 : p.planes, wu, nw);
+      use_plan(q, p.dx, rows, dim, width, kLayoutRow, kLayoutRow, ws + p.at_part);
+      const OutEpilogue out{{dX, nullptr}, {ld_dx, 0}, 0, (int)dim, dtype == SHAMPOO_BF16, 0.f};
+      STATUS_TRY((product_whole<kLayoutRow, kLayoutRow>(h, kCls, p.dx.shape, q, out, s)));
+    }
+    if (!dWg) return SHAMPOO_OK;
+    MmaArgs q{};
+    add_segs(q, x, nx, dg, p.planes);
+    use_plan(q, p.dw, dim, 2 * p.ld_d, rows, kLayoutK, kLayoutK, ws + p.at_part);
+    const OutEpilogue out{{dWg, dWu}, {ld_dwg, ld_dwu}, (int)p.ld_d, (int)width, g_dtype == SHAMPOO_BF16, beta};
+    return product_whole<kLayoutK, kLayoutK>(h, kCls, p.dw.shape, q, out, s);
+  });
+}
+
+// ---------------------------------------------------------------- dropout
+shampoo_status shampoo_dropout(void* handle, const void* X, const void* R, void* Y, int dtype, int64_t rows,
+                               int64_t cols, int64_t ld_x, int64_t ld_r, int64_t ld_y, double rate, uint64_t seed,
+                               uint64_t offset, void* stream) {
+  return entry(handle, [&](Handle* h) {
+    STATUS_TRY(check_dtype(h, dtype, "X"));
+    STATUS_TRY(check_size(h, rows, 0, kMaxTokens, "rows"));
+    STATUS_TRY(check_size(h, cols, 1, kMaxCols, "cols"));
+    STATUS_TRY(check_ld(h, ld_x, cols, "ld_x"));
+    STATUS_TRY(check_ld(h, ld_y, cols, "ld_y"));
+    if (R) STATUS_TRY(check_ld(h, ld_r, cols, "ld_r"));
+    if (!(rate >= 0 && rate <= 1)) return fail(h, SHAMPOO_EINVAL, "rate %g outside [0, 1]", rate);
+    if (rows == 0) return SHAMPOO_OK;
+    if (!X || !Y) return fail(h, SHAMPOO_EINVAL, "X or Y is NULL");
+    if (Y == X && ld_y != ld_x) return fail(h, SHAMPOO_EINVAL, "in place, ld_y %lld must be ld_x %lld", (long long)ld_y, (long long)ld_x);
+    if (Y == R && ld_y != ld_r) return fail(h, SHAMPOO_EINVAL, "in place, ld_y %lld must be ld_r %lld", (long long)ld_y, (long long)ld_r);
+    const Span y = span(Y, rows, cols, ld_y, dtype);
+    if (Y != X) STATUS_TRY(check_apart(h, y, "Y", span(X, rows, cols, ld_x, dtype), "X"));
+    if (Y != R) STATUS_TRY(check_apart(h, y, "Y", span(R, rows, cols, ld_r, dtype), "R"));
+    DeviceGuard g(h->device);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint32_t least = (uint32_t)nearbyint(rate * 65536);
+    const DropoutArgs q{{(uint32_t)seed, (uint32_t)(seed >> 32)}, {(uint32_t)offset, (uint32_t)(offset >> 32)}, least,
+                        least < 65536 ? 65536.f / (float)(65536 - least) : 0.f};
+    return unit_launches(h, SHAMPOO_KCLASS_DROPOUT, rows, cols, cdiv64(cols, 32) * 4, s, [&](const ActShape& sh, dim3 grid) {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        hipLaunchKernelGGL(dropout_kernel<S>, grid, dim3(kThreads), 0, s, sh, q, static_cast<const S*>(X), ld_x,
+                           static_cast<const S*>(R), ld_r, static_cast<S*>(Y), ld_y);
+      });
+    });
+  });
+}
+
+}  // extern "C"

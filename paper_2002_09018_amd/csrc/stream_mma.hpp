@@ -1,0 +1,479 @@
+// Products C = sum_s A_s B_s of bf16 matrices on the matrix cores
+// (v_mfma_f32_32x32x16_bf16), with what follows them applied to the tile: the
+// core of the loss from the last activations and of the gated feed-forward block.
+//
+// Operands.  An operand lies with its contraction index along its rows (kLayoutRow)
+// or along its columns (kLayoutK), in bf16, 16-byte aligned with strides that are
+// multiples of 8.  An fp32 matrix is three bf16 matrices ("planes", x = p0 + p1 +
+// p2 exactly), and its products are the six of them that count: segments of one
+// long contraction, the smallest first, so that the loop knows bf16 only.  A sum of
+// two products (dG Wg^T + dU Wu^T) is two segments as well.
+//
+// Staging.  Stages of kBk = 32 contraction indices go from memory to LDS without
+// passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a ring
+// of kBufs buffers: kBufs - 1 stages are in flight.  Lanes whose row, column or
+// contraction index lies outside the operand have an offset outside the buffer's
+// range and receive zeros, so that no size needs other code.
+//   kLayoutRow: [row][32 k], 64 bytes a row, its 16-byte chunks stored at chunk ^
+//               (row >> 1 & 3); a fragment (8 k of a row) is one 16-byte read.
+//   kLayoutK:   panels of [k][128 or 64 columns], 32-byte pieces stored at piece ^
+//               swizzle(k), read with the transposing read (ds_read_b64_tr_b16).
+// The destination of a load is fixed (1 KB in lane order), so the swizzle is in
+// the addresses that the lanes load from.
+//
+// Loop.  One barrier per stage, before its last 16 indices are multiplied: all
+// fragments of the stage are in registers then, its buffer is free for the stage
+// kBufs further on, and the first fragments of the next stage are read beside the
+// last products.
+//
+// The instruction's first operand is B and its second A, so that a lane holds one
+// row of C (lane % 32) and runs of four columns: sums along a row are formed in the
+// lane.  Results leave through LDS, 32 rows of a wave at a time, as units of 8
+// neighbouring columns.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "act_checkpoint.hpp"
+#include "layer_plans.hpp"
+#include "split_mfma.hpp"
+#include "tile_mfma.hpp"
+#include "weight_grad.hpp"
+
+namespace shp {
+
+// One product of the sum.
+struct MmaSeg {
+  const uint16_t *a, *b, *b2;  // b2: the second matrix of a pair (columns of the tile's other half)
+  int lda, ldb, ldb2;
+};
+constexpr int kMostSegs = 12;
+
+struct MmaArgs {
+  MmaSeg seg[kMostSegs];
+  int segs;
+  int M, N;            // of C; of a pair: of each of the two
+  int ka, kb;          // contraction indices of A and B (rounded up to 8 where they lie along rows)
+  int seg_stages;      // stages of a segment
+  int tiles_m, tiles_n;
+  int splits, per_split;  // parts of the contraction, and their stages
+  float* part;         // parts of C (splits x M x ld_part, a pair's second matrix at ld_part / 2), or NULL
+  int64_t ld_part;
+  int part_add;        // added to what `part` holds
+};
+
+template <int TM_, int TN_, int WM_, int WN_, int BUFS_>
+struct MmaShape {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, kBufs = BUFS_;
+  static constexpr int kBk = 32;
+  static constexpr int kWavesN = TN / WN, kWaves = (TM / WM) * kWavesN, kThr = 64 * kWaves;
+  static constexpr int kBytesA = TM * kBk * 2, kBytesB = TN * kBk * 2, kStageB = kBytesA + kBytesB;
+  static constexpr int kLoadsA = kBytesA / 1024 / kWaves, kLoadsB = kBytesB / 1024 / kWaves;
+  static constexpr int kLoads = kLoadsA + kLoadsB;
+  static constexpr int kBm = WM / 32, kBn = WN / 32;
+  static constexpr int kPitch = WN * 4 + 16;          // bytes of a row on its way out
+  static constexpr int kOutB = kWaves * 32 * kPitch;
+  static constexpr int kLdsB = kBufs * kStageB;
+  static_assert(kLoadsA * kWaves * 1024 == kBytesA && kLoadsB * kWaves * 1024 == kBytesB && kOutB <= kLdsB, "");
+};
+
+// An offset outside every buffer's range.
+constexpr uint32_t kOutside = 0x80000000u;
+
+template <int W>
+__device__ __forceinline__ int mma_swz(int k) {
+  return W == 128 ? wg_swz(k) : ((k >> 1) & 1) << 1;
+}
+
+// One lane's share of an operand's staging: the offsets it loads from and their
+// contraction indices within a stage.
+template <int LAYOUT, int W, int LOADS, int WAVES>
+struct MmaLoader {
+  static constexpr int kPerPanel = W * 64 / 1024;  // loads of a panel of W columns (kLayoutK)
+  uint32_t off[LOADS];
+  int kl[LOADS];
+
+  // Panels of a pair take their columns from n0 each (PAIR), others go on.
+  template <bool PAIR>
+  __device__ __forceinline__ void init(int i0, int end, int ld, int wave, int lane) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int idx = j * WAVES + wave;
+      if constexpr (LAYOUT == kLayoutRow) {
+        const int row = idx * 16 + (lane >> 2), c = (lane & 3) ^ ((lane >> 3) & 3);
+        kl[j] = c * 8;
+        off[j] = i0 + row < end ? (uint32_t)row * (uint32_t)ld * 2u + c * 16u : kOutside;
+      } else {
+        const int in = idx % kPerPanel, panel = idx / kPerPanel;
+        const int k = W == 128 ? in * 4 + (lane >> 4) : in * 8 + (lane >> 3);
+        const int piece = ((lane >> 1) & (W / 16 - 1)) ^ mma_swz<W>(k);
+        const int col = (PAIR ? 0 : panel * W) + piece * 16 + (lane & 1) * 8;
+        kl[j] = k;
+        off[j] = i0 + col < end ? ((uint32_t)k * (uint32_t)ld + (uint32_t)col) * 2u : kOutside;
+      }
+    }
+  }
+};
+
+// 1 KB from the lanes' offsets to LDS, in lane order.  In asm, as the compiler would
+// have every later transposing read wait for all loads in flight; mma_wait and
+// mma_barrier are what orders them.  (The instruction writes no register; M0 needs
+// one wait state before it.)
+__device__ __forceinline__ void mma_dma(const char* base, uint32_t off, lds_char* to) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);
+  const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               ::"s"((uint32_t)(uintptr_t)to), "v"(off), "s"(rsrc)
+               : "memory", "m0");
+}
+
+template <int N>
+__device__ __forceinline__ void mma_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// All of this wave's LDS reads have arrived; then the workgroup's barrier.
+__device__ __forceinline__ void mma_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Logical tile of a workgroup: groups of 8 tile rows, within them column by column,
+// so that the workgroups that run at once on an XCD share few operand panels.
+__device__ __forceinline__ void mma_tile(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+  constexpr int kGroup = 8;
+  const int64_t whole = (int64_t)kGroup * tiles_n;
+  const int g = (int)(t / whole), in = (int)(t % whole);
+  const int rows = min(kGroup, tiles_m - g * kGroup);
+  tm = g * kGroup + in % rows;
+  tn = in / rows;
+}
+
+// The accumulators of one wave after all stages of its part.
+template <typename T, int LA, int LB, bool PAIR>
+struct MmaCore {
+  static constexpr int kWa = T::TM < 128 ? T::TM : 128, kWb = PAIR ? T::TN / 2 : 128;
+  wg_acc acc[T::kBm][T::kBn];
+  int wm, wn;  // first row of the wave in the tile, and number of its column strip
+
+  // Column of the tile where block j of the wave begins.
+  __device__ __forceinline__ int block_col(int j) const {
+    return PAIR ? j * (T::TN / 2) + wn * 32 * (T::kBn / 2) : wn * T::WN + j * 32;
+  }
+
+  template <int LAYOUT, int W>
+  static __device__ __forceinline__ int frag_at(int first, int lane) {
+    if constexpr (LAYOUT == kLayoutRow)
+      return (first + (lane & 31)) * 64 + ((lane >> 5) ^ ((lane >> 1) & 3)) * 16;
+    const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), side = (lane >> 4) & 1;
+    return first / W * (W * 64) + k * (W * 2) + ((first % W / 16 + side) ^ mma_swz<W>(k)) * 32 + (lane & 3) * 8;
+  }
+  template <int LAYOUT, int W>
+  static __device__ __forceinline__ bf16x8 frag(lds_char* stage, int at, int step) {
+    if constexpr (LAYOUT == kLayoutRow)
+      return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(stage + (at ^ (step * 32))));
+    else
+      return wg_frag<W * 2>(stage + at + step * 16 * W * 2);
+  }
+
+  __device__ __forceinline__ void run(const MmaArgs& q, lds_char* lds, int m0, int n0, int split) {
+    static_assert(T::kBn == 2 || !PAIR, "");
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave / T::kWavesN * T::WM;
+    wn = wave % T::kWavesN;
+    const int first = split * q.per_split;
+    const int stages = min(q.per_split, q.segs * q.seg_stages - first);
+
+    // where the next stage to be loaded lies
+    int seg = first / q.seg_stages, at = first % q.seg_stages, left = stages;
+    const char *pa, *pb, *pb2;
+    int64_t step_a, step_b, step_b2;
+    MmaLoader<LA, kWa, T::kLoadsA, T::kWaves> la;
+    MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> lb;
+    auto open = [&] {
+      const MmaSeg& s = q.seg[seg];
+      step_a = LA == kLayoutRow ? T::kBk * 2 : (int64_t)s.lda * T::kBk * 2;
+      step_b = LB == kLayoutRow ? T::kBk * 2 : (int64_t)s.ldb * T::kBk * 2;
+      step_b2 = PAIR ? (int64_t)s.ldb2 * T::kBk * 2 : 0;
+      pa = reinterpret_cast<const char*>(s.a) + (LA == kLayoutRow ? (int64_t)m0 * s.lda : m0) * 2 + at * step_a;
+      pb = reinterpret_cast<const char*>(s.b) + (LB == kLayoutRow ? (int64_t)n0 * s.ldb : n0) * 2 + at * step_b;
+      if (PAIR) pb2 = reinterpret_cast<const char*>(s.b2) + (int64_t)n0 * 2 + at * step_b2;
+      la.template init<false>(m0, q.M, s.lda, wave, lane);
+      lb.template init<PAIR>(n0, q.N, s.ldb, wave, lane);
+      if (PAIR && s.ldb2 != s.ldb) {
+        // the second panel's loads (all of a wave's loads j >= kLoadsB / 2)
+        MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> l2;
+        l2.template init<PAIR>(n0, q.N, s.ldb2, wave, lane);
+#pragma unroll
+        for (int j = T::kLoadsB / 2; j < T::kLoadsB; ++j) lb.off[j] = l2.off[j];
+      }
+    };
+    open();
+    // Issues the loads of the next stage into the buffer (of zeros past the last).
+    auto issue = [&](lds_char* to) {
+      const int ra = left > 0 ? q.ka - at * T::kBk : 0, rb = left > 0 ? q.kb - at * T::kBk : 0;
+#pragma unroll
+      for (int j = 0; j < T::kLoadsA; ++j)
+        mma_dma(pa, la.kl[j] < ra ? la.off[j] : kOutside, to + (j * T::kWaves + wave) * 1024);
+#pragma unroll
+      for (int j = 0; j < T::kLoadsB; ++j)
+        mma_dma(PAIR && j >= T::kLoadsB / 2 ? pb2 : pb, lb.kl[j] < rb ? lb.off[j] : kOutside,
+                to + T::kBytesA + (j * T::kWaves + wave) * 1024);
+      --left;
+      if (++at == q.seg_stages && left > 0) {
+        ++seg;
+        at = 0;
+        open();
+      } else {
+        pa += step_a;
+        pb += step_b;
+        if (PAIR) pb2 += step_b2;
+      }
+    };
+
+    int oa[T::kBm], ob[T::kBn];
+#pragma unroll
+    for (int i = 0; i < T::kBm; ++i) oa[i] = frag_at<LA, kWa>(wm + i * 32, lane);
+#pragma unroll
+    for (int j = 0; j < T::kBn; ++j) ob[j] = T::kBytesA + frag_at<LB, kWb>(block_col(j), lane);
+#pragma unroll
+    for (int i = 0; i < T::kBm; ++i)
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    bf16x8 fa[2][T::kBm], fb[2][T::kBn];
+    auto read = [&](lds_char* stage, int step) {
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j) fb[step][j] = frag<LB, kWb>(stage, ob[j], step);
+#pragma unroll
+      for (int i = 0; i < T::kBm; ++i) fa[step][i] = frag<LA, kWa>(stage, oa[i], step);
+    };
+    auto multiply = [&](int step) {
+#pragma unroll
+      for (int i = 0; i < T::kBm; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kBn; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step][j], fa[step][i], acc[i][j], 0, 0, 0);
+    };
+
+#pragma unroll
+    for (int b = 0; b < T::kBufs - 1; ++b) issue(lds + b * T::kStageB);
+    mma_wait<(T::kBufs - 2) * T::kLoads>();
+    mma_barrier();
+    int cur = 0;
+    read(lds, 0);
+    issue(lds + (T::kBufs - 1) * T::kStageB);
+#pragma unroll 1
+    for (int s = 0; s < stages; ++s) {
+      lds_char* now = lds + cur;
+      cur = cur == (T::kBufs - 1) * T::kStageB ? 0 : cur + T::kStageB;
+      read(now, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0);
+      __builtin_amdgcn_sched_barrier(0);
+      mma_wait<(T::kBufs - 2) * T::kLoads>();
+      mma_barrier();
+      read(lds + cur, 0);
+      issue(now);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    mma_wait<0>();
+    mma_barrier();
+  }
+};
+
+// Columns of C that a wave's units hold, written to part or given to f(row, col,
+// first values, second values of a pair).
+template <typename T, bool PAIR, typename Core, typename F>
+__device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, lds_char* lds, int m0, int n0, int split,
+                                          F&& f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  lds_char* own = lds + wave * 32 * T::kPitch;
+  constexpr int kUnits = PAIR ? T::WN / 16 : T::WN / 8;  // of a row
+  constexpr int kTurns = 32 * kUnits / 64;
+  const int col0 = n0 + (PAIR ? core.wn * (T::WN / 2) : core.wn * T::WN);
+#pragma unroll 1
+  for (int i = 0; i < T::kBm; ++i) {
+#pragma unroll
+    for (int b = 0; b < T::kBm; ++b) {
+      if (b != i) continue;
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const wg_acc& c = core.acc[b][j];
+          *(lds_f32x4*)(own + (lane & 31) * T::kPitch + (j * 32 + v * 8 + (lane >> 5) * 4) * 4) =
+              f32x4{c[4 * v], c[4 * v + 1], c[4 * v + 2], c[4 * v + 3]};
+        }
+    }
+    wave_lds_order();
+#pragma unroll 1
+    for (int t = 0; t < kTurns; ++t) {
+      const int u = t * 64 + lane, r = u / kUnits, c = u % kUnits * 8;
+      const int row = m0 + core.wm + i * 32 + r, col = col0 + c;
+      float x[8], y[8];
+      auto get = [&](float (&w)[8], int at) {
+        const f32x4 lo = *(lds_f32x4*)(own + r * T::kPitch + at * 4);
+        const f32x4 hi = *(lds_f32x4*)(own + r * T::kPitch + at * 4 + 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = lo[e], w[4 + e] = hi[e];
+      };
+      get(x, c);
+      if (PAIR) get(y, T::WN / 2 + c);
+      if (row >= q.M || col >= q.N) continue;
+      if (q.part) {
+        auto put = [&](const float (&w)[8], float* p) {
+          f32x4 lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
+          if (q.part_add) {
+            lo += *reinterpret_cast<f32x4*>(p);
+            hi += *reinterpret_cast<f32x4*>(p + 4);
+          }
+          *reinterpret_cast<f32x4*>(p) = lo;
+          *reinterpret_cast<f32x4*>(p + 4) = hi;
+        };
+        float* p = q.part + ((int64_t)split * q.M + row) * q.ld_part + col;
+        put(x, p);
+        if (PAIR) put(y, p + q.ld_part / 2);
+      } else {
+        f(row, col, x, y);
+      }
+    }
+    wave_lds_order();
+  }
+}
+
+// C, each unit handed to the epilogue E.  ld_part holds whole units.
+template <typename T, int LA, int LB, typename E>
+__global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
+  extern __shared__ __align__(16) char lds_bytes[];
+  lds_char* lds = (lds_char*)lds_bytes;
+  const int tiles = q.tiles_m * q.tiles_n;
+  const int l = xcd_remap(blockIdx.x, gridDim.x);
+  const int split = l / tiles;
+  int tm, tn;
+  mma_tile(l % tiles, q.tiles_m, q.tiles_n, tm, tn);
+  const int m0 = tm * T::TM, n0 = tn * (E::kPair ? T::TN / 2 : T::TN);
+  MmaCore<T, LA, LB, E::kPair> core;
+  core.run(q, lds, m0, n0, split);
+  if constexpr (E::kWhole) {
+    if (!q.part) {
+      e.template whole<T>(q, core, lds, m0, n0, tn);
+      return;
+    }
+  }
+  mma_units<T, E::kPair>(q, core, lds, m0, n0, split, e);
+}
+
+// The epilogue of a product whose contraction was cut: parts added in order.  One
+// unit of 8 columns to a thread.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void mma_join_kernel(MmaArgs q, E e) {
+  const int units = (q.N + 7) / 8;
+  const int64_t n = (int64_t)q.M * units, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += step) {
+    const int row = (int)(i / units), col = (int)(i % units) * 8;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float (&w)[8], const float* p) {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] += lo[k], w[4 + k] += hi[k];
+    };
+#pragma unroll 4
+    for (int s = 0; s < q.splits; ++s) {
+      const float* p = q.part + ((int64_t)s * q.M + row) * q.ld_part + col;
+      add(x, p);
+      if (E::kPair) add(y, p + q.ld_part / 2);
+    }
+    e(row, col, x, y);
+  }
+}
+
+// x = p0 + p1 + p2 in bf16, each to nearest even: 8 bits apiece, exact from 2^-110 in
+// size on.  A value whose p0 is not finite (infinities, NaN, and what rounds up to
+// an infinity) is p0 alone.
+__device__ __forceinline__ void planes_of(const float (&x)[8], u32x4u (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      p[t][i] = pack_bf16(a, b);
+      const float ha = __uint_as_float(p[t][i] << 16), hb = __uint_as_float(p[t][i] & 0xffff0000u);
+      a = finite_f32(ha) ? a - ha : 0.f;
+      b = finite_f32(hb) ? b - hb : 0.f;
+    }
+  }
+}
+
+// A matrix into bf16 planes with rows of ldp elements, zeros from `cols` on.
+// Bound by memory: one read, one write (three of half the size for fp32).
+template <typename S>
+__global__ __launch_bounds__(kThreads) void pack_kernel(ActShape h, const S* __restrict__ X, int64_t ld,
+                                                       uint16_t* __restrict__ out, int64_t plane) {
+  act_units(h, [&](int64_t row, int unit, bool in) {
+    if (!in) return;
+    ActVec<S> x;
+    x.load(X + row * ld + unit * 8, h.cols - unit * 8);
+    uint16_t* d = out + (row * h.upr + unit) * 8;
+    if constexpr (sizeof(S) == 2) {
+      gstore<u32x4u>(d, x.raw[0]);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = x.at(i);
+      u32x4u p[3];
+      planes_of(v, p);
+#pragma unroll
+      for (int t = 0; t < 3; ++t) gstore<u32x4u>(d + t * plane, p[t]);
+    }
+  });
+}
+
+// C = beta C + the product, in either type.  With `second`, the product's columns from
+// there on are another matrix.
+struct OutEpilogue {
+  static constexpr bool kPair = false, kWhole = false;
+  void* C[2];
+  int64_t ld[2];
+  int second, N;  // N: columns of C
+  int bf16;
+  float beta;
+
+  template <typename S>
+  __device__ __forceinline__ void put(int64_t row, int col, float (&x)[8]) const {
+    const bool b = second && col >= second;
+    if (b) col -= second;
+    S* p = static_cast<S*>(b ? C[1] : C[0]) + row * (b ? ld[1] : ld[0]) + col;
+    ActVec<S> v;
+    if (beta != 0.f) {
+      v.load(p, N - col);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fmaf(beta, v.at(i), x[i]);
+    }
+    v.set(x);
+    v.store(p, N - col);
+  }
+  __device__ __forceinline__ void operator()(int row, int col, float (&x)[8], float (&)[8]) const {
+    if (bf16) put<uint16_t>(row, col, x);
+    else put<float>(row, col, x);
+  }
+};
+
+// C = beta C.
+template <typename S>
+__global__ __launch_bounds__(kThreads) void scale_kernel(S* C, int64_t rows, int64_t cols, int64_t ld, float beta) {
+  const int64_t n = rows * cols, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += step) {
+    S* p = C + i / cols * ld + i % cols;
+    *p = from_f32<S>(beta == 0.f ? 0.f : beta * cvt<float, S>(*p));
+  }
+}
+
+}  // namespace shp

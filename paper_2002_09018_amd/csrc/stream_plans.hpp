@@ -1,0 +1,220 @@
+// How the loss from the last activations and the gated feed-forward block cut their
+// work: plain host arithmetic on sizes and types.
+#pragma once
+
+#include "layer_plans.hpp"
+
+namespace shp {
+
+enum { kShapeFew = 0, kShapeMid = 1, kShapeBig = 2 };
+
+// How a product is cut: tiles of C, and parts of the contraction.
+struct MmaPlan {
+  int shape = kShapeMid, splits = 1, per_split = 0;  // (per_split: stages of a part)
+  int64_t tiles_m = 0, tiles_n = 0, seg_stages = 0;
+  int64_t ld_part = 0;
+  size_t part = 0;  // bytes of the parts
+};
+
+// The cheapest tile and number of parts by estimated time.  A stage of a workgroup takes
+// `work` us of its compute unit, and at least `alone` us on its own; `slots`
+// workgroups share a compute unit.  Parts cost their way to memory and back, and
+// the launch that adds them.
+inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, int segs, bool pair, bool few, int most_splits,
+                        bool always_part) {
+  struct Shape {
+    int m, n, slots;
+    double work, alone, start;
+  };
+  static const Shape shapes[] = {{32, 128, 4, 0.16, 0.35, 3}, {128, 128, 2, 0.27, 0.40, 4}, {256, 256, 1, 0.90, 0.90, 6}};
+  MmaPlan best;
+  double best_us = 0;
+  const int64_t seg_stages = cdiv64(K, 32), stages = seg_stages * segs;
+  for (int i = few ? 0 : 1; i < 3; ++i) {
+    const Shape& t = shapes[i];
+    const int64_t tm = cdiv64(M, t.m), tn = cdiv64(N, pair ? t.n / 2 : t.n);
+    for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (want > stages || want > most_splits || (want > 1 && want * tm * tn > 256 * 2 * t.slots)) break;
+      const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per), groups = tm * tn * splits;
+      const int64_t ld = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
+      const size_t part = splits > 1 || always_part ? (size_t)(splits * M * ld) * sizeof(float) : 0;
+      const double us = t.start + (double)per * std::max((double)cdiv64(groups, 256) * t.work,
+                                                         (double)cdiv64(groups, 256 * t.slots) * t.alone) +
+                        (splits > 1 ? 4 + 0.4e-6 * (double)part : 0);
+      if (best_us == 0 || us < best_us) {
+        best_us = us;
+        best = {i, (int)splits, (int)per, tm, tn, seg_stages, ld, part};
+      }
+    }
+  }
+  return best;
+}
+
+// A matrix copied into bf16 planes: one, or three of an fp32 one.
+struct PackPlan {
+  int planes = 1;
+  int64_t ld = 0, plane = 0;  // elements
+  size_t bytes = 0;
+};
+inline PackPlan pack_plan(int64_t rows, int64_t cols, int dtype) {
+  PackPlan p;
+  p.planes = dtype == SHAMPOO_BF16 ? 1 : 3;
+  p.ld = cdiv64(cols, 64) * 64;
+  p.plane = rows * p.ld;
+  p.bytes = (size_t)(p.plane * p.planes) * 2;
+  return p;
+}
+
+// Offsets of buffers in a workspace, each aligned to 256 bytes.
+struct Room {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  }
+};
+
+// Most bytes of one piece of the vocabulary: of the logits' gradient (it is read twice
+// soon after it was written, and the last-level cache holds 256 MB), and of packed
+// rows of the table.
+constexpr int64_t kPieceB = 256 << 20;
+
+inline int64_t vocab_piece(int64_t vocab, int64_t bytes_each) {
+  const int64_t most = std::max<int64_t>(256, kPieceB / bytes_each / 256 * 256);
+  return std::min(vocab, most);
+}
+
+// Columns of a row of logits whose statistics are one entry, where the logits were
+// formed in parts.
+constexpr int kStatCols = 2048;
+
+// The loss: pieces of the vocabulary (one, where the table is read as it lies).
+struct VocabPlan {
+  int64_t piece = 0, pieces = 0, entries = 0;  // entries: statistics of a row
+  MmaPlan mma[2];  // of a whole piece and of the last
+  PackPlan x, w;
+  size_t at_x = 0, at_w = 0, at_stat = 0, at_target = 0, at_part = 0, bytes = 0;
+};
+inline int64_t vocab_entries(const MmaPlan& p, int64_t n) { return p.part ? cdiv64(n, kStatCols) : p.tiles_n; }
+
+inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, bool pack_x, bool pack_w) {
+  VocabPlan p;
+  Room r;
+  p.x = pack_plan(rows, dim, dtype);
+  if (pack_x) p.at_x = r.take(p.x.bytes);
+  p.piece = pack_w ? vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) : vocab;
+  p.pieces = cdiv64(vocab, p.piece);
+  p.w = pack_plan(p.piece, dim, dtype);
+  if (pack_w) p.at_w = r.take(p.w.bytes);
+  const int64_t last = vocab - (p.pieces - 1) * p.piece;
+  size_t part = 0;
+  for (int i = 0; i < 2; ++i) {
+    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, dtype == SHAMPOO_F32 ? 6 : 1, false, true, 64, false);
+    part = std::max(part, p.mma[i].part);
+  }
+  p.entries = (p.pieces - 1) * vocab_entries(p.mma[0], p.piece) + vocab_entries(p.mma[1], last);
+  p.at_stat = r.take((size_t)(rows * p.entries) * 8);
+  p.at_target = r.take((size_t)rows * 4);
+  p.at_part = r.take(part);
+  p.bytes = r.at;
+  return p;
+}
+
+// Its gradient: the logits of a piece, its share of dX, its rows of dW.
+struct VocabGradPlan {
+  int64_t piece = 0, pieces = 0, ld_dz = 0;
+  int planes = 1;  // bf16 terms of the logits' gradient
+  MmaPlan z[2], dx[2], dw[2];
+  PackPlan x, w;
+  size_t at_x = 0, at_w = 0, at_dz = 0, at_dx = 0, at_part = 0, bytes = 0;
+};
+
+// An fp32 gradient, of inputs of either type, has three terms of dz: with one it
+// would keep 9 bits, with two 17.  A bf16 one takes dz as the framework stores a
+// bf16 gradient of logits, rounded once.
+inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || g_dtype == SHAMPOO_F32 ? 3 : 1; }
+// Products of a weight gradient: an fp32 input's three planes times three terms.
+inline int grad_segs(int dtype, int planes) { return dtype == SHAMPOO_F32 ? 6 : planes; }
+
+inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype, bool pack_x,
+                                     bool pack_w) {
+  VocabGradPlan p;
+  Room r;
+  const bool f32 = dtype == SHAMPOO_F32;
+  p.planes = grad_planes(dtype, g_dtype);
+  p.x = pack_plan(rows, dim, dtype);
+  if (pack_x) p.at_x = r.take(p.x.bytes);
+  p.piece = vocab_piece(vocab, rows * p.planes * 2);
+  if (pack_w) p.piece = std::min(p.piece, vocab_piece(vocab, pack_plan(1, dim, dtype).bytes));
+  p.pieces = cdiv64(vocab, p.piece);
+  p.w = pack_plan(p.piece, dim, dtype);
+  if (pack_w) p.at_w = r.take(p.w.bytes);
+  p.ld_dz = cdiv64(p.piece, 64) * 64;
+  p.at_dz = r.take((size_t)(rows * p.ld_dz * p.planes) * 2);
+  size_t part = 0;
+  const int64_t last = vocab - (p.pieces - 1) * p.piece;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t n = i ? last : p.piece;
+    p.z[i] = mma_plan(rows, n, dim, f32 ? 6 : 1, false, true, 64, false);
+    p.dx[i] = mma_plan(rows, dim, n, f32 ? 6 : 1, false, true, i ? p.dx[0].splits : 64, p.pieces > 1);
+    p.dw[i] = mma_plan(n, dim, rows, grad_segs(dtype, p.planes), false, false, 64, false);
+    part = std::max({part, p.z[i].part, p.dw[i].part});
+  }
+  p.at_dx = r.take(p.dx[0].part);
+  p.at_part = r.take(part);
+  p.bytes = r.at;
+  return p;
+}
+
+// The feed-forward block.
+struct FfnPlan {
+  MmaPlan mma;
+  PackPlan x, wg, wu;
+  size_t at_x = 0, at_wg = 0, at_wu = 0, at_part = 0, bytes = 0;
+};
+inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, bool pack_x, bool pack_wg, bool pack_wu) {
+  FfnPlan p;
+  Room r;
+  p.x = pack_plan(rows, dim, dtype);
+  p.wg = p.wu = pack_plan(dim, width, dtype);
+  if (pack_x) p.at_x = r.take(p.x.bytes);
+  if (pack_wg) p.at_wg = r.take(p.wg.bytes);
+  if (pack_wu) p.at_wu = r.take(p.wu.bytes);
+  p.mma = mma_plan(rows, width, dim, dtype == SHAMPOO_F32 ? 6 : 1, true, true, 64, false);
+  p.at_part = r.take(p.mma.part);
+  p.bytes = r.at;
+  return p;
+}
+
+// Its gradient.  dG and dU lie side by side in rows of 2 ld_d, so that dWg and dWu are
+// one product.
+struct FfnGradPlan {
+  MmaPlan gu, dx, dw;
+  PackPlan x, wg, wu;
+  int64_t ld_d = 0;
+  int planes = 1;
+  size_t at_x = 0, at_wg = 0, at_wu = 0, at_d = 0, at_part = 0, bytes = 0;
+};
+inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype, bool pack_x,
+                                 bool pack_wg, bool pack_wu) {
+  FfnGradPlan p;
+  Room r;
+  const bool f32 = dtype == SHAMPOO_F32;
+  p.planes = grad_planes(dtype, g_dtype);
+  p.x = pack_plan(rows, dim, dtype);
+  p.wg = p.wu = pack_plan(dim, width, dtype);
+  if (pack_x) p.at_x = r.take(p.x.bytes);
+  if (pack_wg) p.at_wg = r.take(p.wg.bytes);
+  if (pack_wu) p.at_wu = r.take(p.wu.bytes);
+  p.ld_d = cdiv64(width, 64) * 64;
+  p.at_d = r.take((size_t)(rows * 2 * p.ld_d * p.planes) * 2);
+  p.gu = mma_plan(rows, width, dim, f32 ? 6 : 1, true, true, 64, false);
+  p.dx = mma_plan(rows, dim, width, f32 ? 12 : 2, false, true, 64, false);
+  p.dw = mma_plan(dim, 2 * p.ld_d, rows, grad_segs(dtype, p.planes), false, false, 64, false);
+  p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part}));
+  p.bytes = r.at;
+  return p;
+}
+
+}  // namespace shp

@@ -1,0 +1,172 @@
+// Device kernels of the loss from the last activations: log probabilities of given
+// tokens from X and the vocabulary's table W, the logits z = X W^T never in memory.
+//
+// Forward: the tile's epilogue takes the largest entry m and sum s = sum e^(z - m) of
+// every row over the tile's columns, and the target's logit where it lies there; a
+// second kernel joins the tiles of a row.  Backward: the logits are formed again in
+// pieces of the vocabulary, dz_j = c p_j + [j = t] g (c = g_lse - g) is stored in
+// bf16 terms, and two products take it to dX and dW.
+#pragma once
+
+#include "stream_mma.hpp"
+#include "stream_plans.hpp"
+
+namespace shp {
+
+struct VocabTargets {
+  const int32_t* targets;  // or NULL
+  int vocab;
+  int first;               // of the piece
+  // Column of the row's target, counted from the piece's first (a target elsewhere
+  // is negative or past it), or kNone.
+  static constexpr int kNone = -(1 << 30);
+  __device__ __forceinline__ int at(int64_t row) const {
+    const int t = targets ? targets[row] : -1;
+    return t >= 0 && t < vocab ? t - first : kNone;
+  }
+};
+
+// (m, s) of a part of a row: s = sum e^(z - m); m = kLowest and s = 0 before any
+// entry.  Differences are taken before they are scaled, as in logprobs.hpp.
+typedef float f32x2p __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ f32x2p ms_join(f32x2p a, f32x2p b) {
+  const float n = fmaxf(a[0], b[0]);
+  return {n, a[1] * lse_exp(lse_shift(a[0], n)) + b[1] * lse_exp(lse_shift(b[0], n))};
+}
+
+struct LseEpilogue {
+  static constexpr bool kPair = false, kWhole = true;
+  VocabTargets t;
+  f32x2p* stat;      // rows x ld_stat
+  int64_t ld_stat;
+  float* z_target;   // rows
+
+  __device__ __forceinline__ void operator()(int, int, float (&)[8], float (&)[8]) const {}
+
+  template <typename T, typename Core>
+  __device__ __forceinline__ void whole(const MmaArgs& q, const Core& core, lds_char* lds, int m0, int n0,
+                                        int tn) const {
+    typedef __attribute__((address_space(3))) f32x2p lds_f32x2;
+    lds_f32x2* rows = (lds_f32x2*)lds;  // [wave column][row]
+    const int lane = threadIdx.x & 63;
+    const int c0 = n0 + core.wn * T::WN + (lane >> 5) * 4;  // column of (j, v): c0 + j 32 + (v / 4) 8 + v % 4
+    const bool full = n0 + T::TN <= q.N;
+#pragma unroll
+    for (int i = 0; i < T::kBm; ++i) {
+      const int r = core.wm + i * 32 + (lane & 31);
+      float z[T::kBn][16];
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          z[j][v] = core.acc[i][j][v];
+          if (!full && c0 + j * 32 + v / 4 * 8 + v % 4 >= q.N) z[j][v] = -INFINITY;
+        }
+      float m = kLowest;
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) m = fmaxf(m, z[j][v]);
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const int at = m0 + r < q.M ? t.at(m0 + r) - c0 : -1;
+      if (__any(at >= 0 && at < T::WN)) {
+#pragma unroll
+        for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (at == j * 32 + v / 4 * 8 + v % 4) z_target[m0 + r] = z[j][v];
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s += lse_exp(z[j][v] - m);
+      s += __shfl_xor(s, 32, 64);
+      if (lane < 32) rows[core.wn * T::TM + r] = f32x2p{m, s};
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < T::TM; r += T::kThr) {
+      f32x2p a = rows[r];
+#pragma unroll
+      for (int w = 1; w < T::kWavesN; ++w) a = ms_join(a, rows[w * T::TM + r]);
+      if (m0 + r < q.M) stat[(int64_t)(m0 + r) * ld_stat + tn] = a;
+    }
+  }
+};
+
+// (m, s) of kStatCols columns of a row of logits that were formed in parts: a wave
+// each.
+__global__ __launch_bounds__(kThreads) inline void logit_stat_kernel(MmaArgs q, LseEpilogue e) {
+  const int lane = threadIdx.x & 63, parts = (q.N + kStatCols - 1) / kStatCols;
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (w >= (int64_t)q.M * parts) return;
+  const int row = (int)(w / parts), p = (int)(w % parts);
+  const int t = e.t.at(row), end = min(q.N, (p + 1) * kStatCols);
+  f32x2p a = {kLowest, 0.f};
+  for (int c = p * kStatCols + lane; c < end; c += 64) {
+    const float* z = q.part + (int64_t)row * q.ld_part + c;
+    float x = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < q.splits; ++s) x += z[(int64_t)s * q.M * q.ld_part];
+    if (c == t) e.z_target[row] = x;
+    const float n = fmaxf(a[0], x);
+    a = {n, a[1] * lse_exp(lse_shift(a[0], n)) + lse_exp(x - n)};
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) a = ms_join(a, f32x2p{__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64)});
+  if (lane == 0) e.stat[(int64_t)row * e.ld_stat + p] = a;
+}
+
+// lse and log probability from the parts of a row: a wave to a row.
+__global__ __launch_bounds__(kThreads) inline void lse_join_kernel(int64_t rows, int parts, const f32x2p* stat,
+                                                                   VocabTargets t, const float* z_target, float* logp,
+                                                                   float* lse) {
+  const int lane = threadIdx.x & 63;
+  const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
+  for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); row < rows; row += step) {
+    f32x2p a = {kLowest, 0.f};
+#pragma unroll 4
+    for (int p = lane; p < parts; p += 64) a = ms_join(a, stat[row * parts + p]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) a = ms_join(a, f32x2p{__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64)});
+    if (lane) continue;
+    const float ls = logf(a[1]);
+    lse[row] = a[0] + ls;
+    if (logp) logp[row] = t.at(row) != t.kNone ? (z_target[row] - a[0]) - ls : 0.f;
+  }
+}
+
+// The gradient of the logits, in one or three bf16 terms.
+struct DlogitEpilogue {
+  static constexpr bool kPair = false, kWhole = false;
+  VocabTargets t;
+  const float *lse, *g_logp, *g_lse;
+  uint16_t* dz;  // M x ld
+  int64_t ld, plane;
+  int N, planes;
+
+  __device__ __forceinline__ void operator()(int row, int col, float (&z)[8], float (&)[8]) const {
+    const int target = t.at(row), at = target - col;
+    const float g = g_logp && target != t.kNone ? g_logp[row] : 0.f;
+    const float c = (g_lse ? g_lse[row] : 0.f) - g, l = lse[row];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      z[i] = c * lse_exp(z[i] - l);
+      if (i == at) z[i] += g;
+      if (col + i >= N || l == -INFINITY) z[i] = 0.f;
+    }
+    uint16_t* d = dz + row * ld + col;
+    if (planes == 1) {
+      ActVec<uint16_t> v;
+      v.set(z);
+      gstore<u32x4u>(d, v.raw[0]);
+    } else {
+      u32x4u p[3];
+      planes_of(z, p);
+#pragma unroll
+      for (int s = 0; s < 3; ++s) gstore<u32x4u>(d + s * plane, p[s]);
+    }
+  }
+};
+
+}  // namespace shp
