@@ -22,13 +22,15 @@ __device__ __forceinline__ void act_switch(int act, F&& f) {
 
 // H, and G and U where they are kept (rounded for themselves: H is of the sums).
 template <typename S>
-struct GatedEpilogue {
-  static constexpr bool kPair = true, kWhole = false;
+struct GatedEpilogue : UnitEpilogue<GatedEpilogue<S>> {
+  static constexpr bool kPair = true;
   int act, N;
   S *H, *G, *U;
   int64_t ld_h, ld_g, ld_u;
 
-  __device__ __forceinline__ void operator()(int row, int col, float (&g)[8], float (&u)[8]) const {
+  GatedEpilogue(int a, int n, S* h, S* g, S* u, int64_t lh, int64_t lg, int64_t lu)
+      : act(a), N(n), H(h), G(g), U(u), ld_h(lh), ld_g(lg), ld_u(lu) {}
+  __device__ __forceinline__ void operator()(int row, const f32x4&, int col, float (&g)[8], float (&u)[8]) const {
     ActVec<S> v;
     if (G) {
       v.set(g);
@@ -48,14 +50,16 @@ struct GatedEpilogue {
 // dG = dH o U o act'(G) and dU = dH o act(G), in one or three bf16 terms with zeros up
 // to a multiple of 8 columns.
 template <typename S>
-struct GatedGradEpilogue {
-  static constexpr bool kPair = true, kWhole = false;
+struct GatedGradEpilogue : UnitEpilogue<GatedGradEpilogue<S>> {
+  static constexpr bool kPair = true;
   int act, N, planes;
   const S* dH;
   int64_t ld_dh;
   uint16_t *dG, *dU;  // M x ld
   int64_t ld, plane;
 
+  GatedGradEpilogue(int a, int n, int np, const S* h, int64_t lh, uint16_t* g, uint16_t* u, int64_t l, int64_t pl)
+      : act(a), N(n), planes(np), dH(h), ld_dh(lh), dG(g), dU(u), ld(l), plane(pl) {}
   __device__ __forceinline__ void put(uint16_t* d, const float (&x)[8]) const {
     if (planes == 1) {
       ActVec<uint16_t> v;
@@ -68,7 +72,7 @@ struct GatedGradEpilogue {
       for (int s = 0; s < 3; ++s) gstore<u32x4u>(d + s * plane, p[s]);
     }
   }
-  __device__ __forceinline__ void operator()(int row, int col, float (&g)[8], float (&u)[8]) const {
+  __device__ __forceinline__ void operator()(int row, const f32x4&, int col, float (&g)[8], float (&u)[8]) const {
     ActVec<S> d;
     d.load(dH + row * ld_dh + col, N - col);
     act_switch(act, [&](auto a) {
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void gated_grad_kernel(ActShape h, const 
     float x[8], y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = g.at(i), y[i] = u.at(i);
-    e((int)row, unit * 8, x, y);
+    e((int)row, f32x4{0.f, 0.f, 0.f, 0.f}, unit * 8, x, y);
   });
 }
 

@@ -19,9 +19,19 @@ using namespace shp;
 
 namespace {
 
-using FewShape = MmaShape<32, 128, 32, 64, 4>;
-using MidShape = MmaShape<128, 128, 64, 64, 4>;
-using BigShape = MmaShape<256, 256, 128, 64, 4>;
+// Shapes of a product whose operands have PA and PB planes.
+template <int PA, int PB>
+struct Shapes {
+  using Few = MmaShape<32, 128, 32, 64, 2, PA, PB>;
+  using Mid = MmaShape<128, 128, 32, 64, 3, PA, PB>;
+  using Big = MmaShape<256, 128, 64, 64, 2, PA, PB>;
+};
+template <>
+struct Shapes<1, 1> {
+  using Few = MmaShape<32, 128, 32, 64, 4>;
+  using Mid = MmaShape<128, 128, 64, 64, 4>;
+  using Big = MmaShape<256, 256, 128, 64, 3>;
+};
 
 // A buffer of a call and what to call it.
 struct Named {
@@ -62,12 +72,11 @@ bool as_it_lies(const void* p, int64_t ld, int64_t cols, int dtype) {
   return dtype == SHAMPOO_BF16 && aligned16(p) && cols % 8 == 0 && ld % 8 == 0 && ld <= (1 << 21);
 }
 
-// An operand's planes: p and the elements from one plane to the next.
+// An operand's planes: the first, and the elements from one to the next.
 struct Planes16 {
   const uint16_t* p;
   int64_t ld, plane;
 };
-const uint16_t* plane_of(const Planes16& x, int i) { return x.p + i * x.plane; }
 
 // X as the products read it, copied to `room` first where it has to be.
 shampoo_status packed(Handle* h, int cls, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld, bool pack,
@@ -86,16 +95,10 @@ shampoo_status packed(Handle* h, int cls, const void* X, int dtype, int64_t rows
   });
 }
 
-// Products of two operands' terms, the smallest first: all six pairs of three planes
-// that count, or the terms of B (or A) alone.
-void add_segs(MmaArgs& q, const Planes16& a, int na, const Planes16& b, int nb, const Planes16* b2 = nullptr) {
-  for (int s = std::min(na + nb - 2, 2); s >= 0; --s)
-    for (int i = std::min(s, na - 1); i >= 0; --i) {
-      const int j = s - i;
-      if (j >= nb) continue;
-      MmaSeg& g = q.seg[q.segs++];
-      g = {plane_of(a, i), plane_of(b, j), b2 ? plane_of(*b2, j) : nullptr, (int)a.ld, (int)b.ld, b2 ? (int)b2->ld : 0};
-    }
+// One more product of the sum.
+void add_seg(MmaArgs& q, const Planes16& a, const Planes16& b, const Planes16* b2 = nullptr) {
+  q.seg[q.segs++] = {a.p, b.p, b2 ? b2->p : nullptr, a.plane, b.plane, b2 ? b2->plane : 0,
+                     (int)a.ld, (int)b.ld, b2 ? (int)b2->ld : 0};
 }
 
 // Fills what the plan says; ka and kb are rounded up to 8 where the contraction
@@ -117,25 +120,32 @@ void use_plan(MmaArgs& q, const MmaPlan& p, int64_t M, int64_t N, int64_t K, int
 template <typename T, int LA, int LB, typename E>
 shampoo_status mma_launch(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_t s) {
   auto k = mma_kernel<T, LA, LB, E>;
+  constexpr int kLds = T::kLdsB + (E::kState ? T::kStateB : 0);
   // more LDS than a launch may take by default: asked for once per device
   static std::atomic<uint64_t> asked{0};
   const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
   if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
-    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, T::kLdsB));
+    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
     asked.fetch_or(bit, std::memory_order_relaxed);
   }
   const int64_t groups = (int64_t)q.tiles_m * q.tiles_n * q.splits;
   if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "a product of %d x %d", q.M, q.N);
-  return launch(h, cls, s, [&] { hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(T::kThr), T::kLdsB, s, q, e); });
+  return launch(h, cls, s, [&] { hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(T::kThr), kLds, s, q, e); });
 }
 
-// The product; what was cut is left in q.part.
-template <int LA, int LB, typename E>
+// The product of operands of PA and PB planes; what was cut is left in q.part.
+template <int LA, int LB, int PA, int PB, typename E>
 shampoo_status product(Handle* h, int cls, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
+  using K = Shapes<PA, PB>;
   if constexpr (LA == kLayoutRow)
-    if (shape == kShapeFew) return mma_launch<FewShape, LA, LB>(h, cls, q, e, s);
-  if (shape == kShapeMid) return mma_launch<MidShape, LA, LB>(h, cls, q, e, s);
-  return mma_launch<BigShape, LA, LB>(h, cls, q, e, s);
+    if (shape == kShapeFew) return mma_launch<typename K::Few, LA, LB>(h, cls, q, e, s);
+  if (shape == kShapeMid) return mma_launch<typename K::Mid, LA, LB>(h, cls, q, e, s);
+  return mma_launch<typename K::Big, LA, LB>(h, cls, q, e, s);
+}
+// ... of operands that both have one or both three.
+template <int LA, int LB, typename E>
+shampoo_status product(Handle* h, int cls, int planes, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
+  return planes == 1 ? product<LA, LB, 1, 1>(h, cls, shape, q, e, s) : product<LA, LB, 3, 3>(h, cls, shape, q, e, s);
 }
 
 // The epilogue over the parts.
@@ -147,9 +157,16 @@ shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_
   });
 }
 
-template <int LA, int LB, typename E>
-shampoo_status product_whole(Handle* h, int cls, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
-  STATUS_TRY((product<LA, LB>(h, cls, shape, q, e, s)));
+// A weight gradient X^T D or D^T X of D's terms: three where X has one plane and D's
+// gradient is kept in fp32.
+template <bool D_FIRST>
+shampoo_status weight_product(Handle* h, int cls, int x_planes, int d_planes, int shape, const MmaArgs& q,
+                              const OutEpilogue& e, hipStream_t s) {
+  constexpr int K = kLayoutK;
+  shampoo_status st;
+  if (x_planes == d_planes) st = product<K, K>(h, cls, x_planes, shape, q, e, s);
+  else st = product<K, K, D_FIRST ? 3 : 1, D_FIRST ? 1 : 3>(h, cls, shape, q, e, s);
+  STATUS_TRY(st);
   return q.part ? join(h, cls, q, e, s) : SHAMPOO_OK;
 }
 
@@ -236,10 +253,10 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
       const MmaPlan& m = p.mma[i == p.pieces - 1];
       STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
       MmaArgs q{};
-      add_segs(q, x, p.x.planes, w, p.w.planes);
+      add_seg(q, x, w);
       use_plan(q, m, rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
-      const LseEpilogue e{{targets, (int)vocab, (int)v0}, stat + entry0, p.entries, z_target};
-      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, m.shape, q, e, s)));
+      const LseEpilogue e({targets, (int)vocab, (int)v0}, stat + entry0, p.entries, z_target, (int)n);
+      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, p.x.planes, m.shape, q, e, s)));
       if (q.part) {
         const int64_t groups = cdiv64(rows * cdiv64(n, kStatCols), kThreads / 64);
         if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
@@ -303,34 +320,35 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, s, &x));
     uint16_t* dz = reinterpret_cast<uint16_t*>(ws + p.at_dz);
     const Planes16 pz{dz, p.ld_dz, rows * p.ld_dz};
-    const int nx = p.x.planes, nw = p.w.planes;
+    const int nx = p.x.planes;
     MmaArgs qx{};
-    const OutEpilogue out_x{{dX, nullptr}, {ld_dx, 0}, 0, (int)dim, dtype == SHAMPOO_BF16, 0.f};
+    const OutEpilogue out_x(dX, ld_dx, nullptr, 0, 0, (int)dim, (int)dim, dtype == SHAMPOO_BF16, 0.f);
     for (int64_t i = 0; i < p.pieces; ++i) {
       const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
       const bool last = i == p.pieces - 1;
       STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
       MmaArgs q{};
-      add_segs(q, x, nx, w, nw);
+      add_seg(q, x, w);
       use_plan(q, p.z[last], rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
-      const DlogitEpilogue e{{targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes};
-      STATUS_TRY((product_whole<kLayoutRow, kLayoutRow>(h, kCls, p.z[last].shape, q, e, s)));
+      const DlogitEpilogue e({targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes);
+      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.z[last].shape, q, e, s)));
+      if (q.part) STATUS_TRY(join(h, kCls, q, e, s));
       if (dX) {
         // a bf16 dX takes the first term alone
         MmaArgs r{};
-        add_segs(r, pz, nw == 1 ? 1 : p.planes, w, nw);
+        add_seg(r, pz, w);
         use_plan(r, p.dx[last], rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
         r.part_add = i > 0;
-        STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, p.dx[last].shape, r, out_x, s)));
+        STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, p.dx[last].shape, r, out_x, s)));
         if (i == 0) qx = r;
       }
       if (dW) {
         MmaArgs r{};
-        add_segs(r, pz, p.planes, x, nx);
+        add_seg(r, pz, x);
         use_plan(r, p.dw[last], n, dim, rows, kLayoutK, kLayoutK, ws + p.at_part);
-        const OutEpilogue out{{const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)), nullptr}, {ld_dw, 0}, 0, (int)dim,
-                              g_dtype == SHAMPOO_BF16, beta};
-        STATUS_TRY((product_whole<kLayoutK, kLayoutK>(h, kCls, p.dw[last].shape, r, out, s)));
+        const OutEpilogue out(const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)), ld_dw, nullptr, 0, 0, (int)dim,
+                              (int)dim, g_dtype == SHAMPOO_BF16, beta);
+        STATUS_TRY(weight_product<true>(h, kCls, nx, p.planes, p.dw[last].shape, r, out, s));
       }
     }
     return dX && qx.part ? join(h, kCls, qx, out_x, s) : SHAMPOO_OK;
@@ -377,13 +395,15 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
     STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
     MmaArgs q{};
-    add_segs(q, x, p.x.planes, wg, p.wg.planes, &wu);
+    add_seg(q, x, wg, &wu);
     use_plan(q, p.mma, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
     shampoo_status st = SHAMPOO_OK;
     with_type(dtype, [&](auto* type) {
       using S = std::remove_pointer_t<decltype(type)>;
-      const GatedEpilogue<S> e{act, (int)width, static_cast<S*>(H), static_cast<S*>(G), static_cast<S*>(U), ld_h, ld_g, ld_u};
-      st = product_whole<kLayoutRow, kLayoutK>(h, kCls, p.mma.shape, q, e, s);
+      const GatedEpilogue<S> e(act, (int)width, static_cast<S*>(H), static_cast<S*>(G), static_cast<S*>(U), ld_h, ld_g, ld_u);
+      constexpr int kP = sizeof(S) == 2 ? 1 : 3;
+      st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.mma.shape, q, e, s);
+      if (st == SHAMPOO_OK && q.part) st = join(h, kCls, q, e, s);
     });
     return st;
   });
@@ -446,13 +466,13 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, px, p.x, ws + p.at_x, s, &x));
     STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
     STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
-    const int nx = p.x.planes, nw = p.wg.planes;
+    const int nx = p.x.planes;
     uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.at_d);
     const Planes16 dg{d, 2 * p.ld_d, rows * 2 * p.ld_d}, du{d + p.ld_d, dg.ld, dg.plane};
     shampoo_status st = SHAMPOO_OK;
     with_type(dtype, [&](auto* type) {
       using S = std::remove_pointer_t<decltype(type)>;
-      const GatedGradEpilogue<S> e{act, (int)width, p.planes, static_cast<const S*>(dH), ld_dh, d, d + p.ld_d, dg.ld, dg.plane};
+      const GatedGradEpilogue<S> e(act, (int)width, p.planes, static_cast<const S*>(dH), ld_dh, d, d + p.ld_d, dg.ld, dg.plane);
       if (G) {
         st = unit_launches(h, kCls, rows, width, p.ld_d / 8, s, [&](const ActShape& sh, dim3 grid) {
           hipLaunchKernelGGL(gated_grad_kernel<S>, grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(G), ld_g,
@@ -460,26 +480,30 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
         });
       } else {
         MmaArgs q{};
-        add_segs(q, x, nx, wg, nw, &wu);
+        add_seg(q, x, wg, &wu);
         use_plan(q, p.gu, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
-        st = product_whole<kLayoutRow, kLayoutK>(h, kCls, p.gu.shape, q, e, s);
+        constexpr int kP = sizeof(S) == 2 ? 1 : 3;
+        st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.gu.shape, q, e, s);
+        if (st == SHAMPOO_OK && q.part) st = join(h, kCls, q, e, s);
       }
     });
     STATUS_TRY(st);
     if (dX) {
       MmaArgs q{};
-      add_segs(q, dg, nw == 1 ? 1 : p.planes, wg, nw);
-      add_segs(q, du, nw == 1 ? 1 : p.planes, wu, nw);
+      add_seg(q, dg, wg);
+      add_seg(q, du, wu);
       use_plan(q, p.dx, rows, dim, width, kLayoutRow, kLayoutRow, ws + p.at_part);
-      const OutEpilogue out{{dX, nullptr}, {ld_dx, 0}, 0, (int)dim, dtype == SHAMPOO_BF16, 0.f};
-      STATUS_TRY((product_whole<kLayoutRow, kLayoutRow>(h, kCls, p.dx.shape, q, out, s)));
+      const OutEpilogue out(dX, ld_dx, nullptr, 0, 0, (int)dim, (int)dim, dtype == SHAMPOO_BF16, 0.f);
+      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.dx.shape, q, out, s)));
+      if (q.part) STATUS_TRY(join(h, kCls, q, out, s));
     }
     if (!dWg) return SHAMPOO_OK;
     MmaArgs q{};
-    add_segs(q, x, nx, dg, p.planes);
+    add_seg(q, x, dg);
     use_plan(q, p.dw, dim, 2 * p.ld_d, rows, kLayoutK, kLayoutK, ws + p.at_part);
-    const OutEpilogue out{{dWg, dWu}, {ld_dwg, ld_dwu}, (int)p.ld_d, (int)width, g_dtype == SHAMPOO_BF16, beta};
-    return product_whole<kLayoutK, kLayoutK>(h, kCls, p.dw.shape, q, out, s);
+    const OutEpilogue out(dWg, ld_dwg, dWu, ld_dwu, (int)p.ld_d, (int)width, (int)(2 * p.ld_d), g_dtype == SHAMPOO_BF16,
+                          beta);
+    return weight_product<false>(h, kCls, nx, p.planes, p.dw.shape, q, out, s);
   });
 }
 

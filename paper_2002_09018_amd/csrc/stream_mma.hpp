@@ -1,13 +1,14 @@
-// Products C = sum_s A_s B_s of bf16 matrices on the matrix cores
-// (v_mfma_f32_32x32x16_bf16), with what follows them applied to the tile: the
-// core of the loss from the last activations and of the gated feed-forward block.
+// Products of bf16 matrices on the matrix cores (v_mfma_f32_32x32x16_bf16), with what
+// follows them applied to the tile: the core of the loss from the last activations
+// and of the gated feed-forward block.
 //
 // Operands.  An operand lies with its contraction index along its rows (kLayoutRow)
 // or along its columns (kLayoutK), in bf16, 16-byte aligned with strides that are
 // multiples of 8.  An fp32 matrix is three bf16 matrices ("planes", x = p0 + p1 +
-// p2 exactly), and its products are the six of them that count: segments of one
-// long contraction, the smallest first, so that the loop knows bf16 only.  A sum of
-// two products (dG Wg^T + dU Wu^T) is two segments as well.
+// p2 exactly); a stage holds all planes of both operands, and each 16 contraction
+// indices are multiplied for the pairs of planes that count (six of nine, or three
+// where the other operand has one), the smallest first.  A sum of two products (dG
+// Wg^T + dU Wu^T) is two segments of one long contraction.
 //
 // Staging.  Stages of kBk = 32 contraction indices go from memory to LDS without
 // passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a ring
@@ -15,7 +16,7 @@
 // contraction index lies outside the operand have an offset outside the buffer's
 // range and receive zeros, so that no size needs other code.
 //   kLayoutRow: [row][32 k], 64 bytes a row, its 16-byte chunks stored at chunk ^
-//               (row >> 1 & 3); a fragment (8 k of a row) is one 16-byte read.
+//               (row >> 2 & 3); a fragment (8 k of a row) is one 16-byte read.
 //   kLayoutK:   panels of [k][128 or 64 columns], 32-byte pieces stored at piece ^
 //               swizzle(k), read with the transposing read (ds_read_b64_tr_b16).
 // The destination of a load is fixed (1 KB in lane order), so the swizzle is in
@@ -45,10 +46,11 @@ namespace shp {
 
 // One product of the sum.
 struct MmaSeg {
-  const uint16_t *a, *b, *b2;  // b2: the second matrix of a pair (columns of the tile's other half)
+  const uint16_t *a, *b, *b2;          // b2: the second matrix of a pair (columns of the tile's other half)
+  int64_t plane_a, plane_b, plane_b2;  // elements from one plane to the next
   int lda, ldb, ldb2;
 };
-constexpr int kMostSegs = 12;
+constexpr int kMostSegs = 2;
 
 struct MmaArgs {
   MmaSeg seg[kMostSegs];
@@ -63,18 +65,20 @@ struct MmaArgs {
   int part_add;        // added to what `part` holds
 };
 
-template <int TM_, int TN_, int WM_, int WN_, int BUFS_>
+template <int TM_, int TN_, int WM_, int WN_, int BUFS_, int PA_ = 1, int PB_ = 1>
 struct MmaShape {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, kBufs = BUFS_;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, kBufs = BUFS_, PA = PA_, PB = PB_;
   static constexpr int kBk = 32;
   static constexpr int kWavesN = TN / WN, kWaves = (TM / WM) * kWavesN, kThr = 64 * kWaves;
-  static constexpr int kBytesA = TM * kBk * 2, kBytesB = TN * kBk * 2, kStageB = kBytesA + kBytesB;
+  static constexpr int kBytesA = TM * kBk * 2, kBytesB = TN * kBk * 2;  // of one plane
+  static constexpr int kStageB = PA * kBytesA + PB * kBytesB;
   static constexpr int kLoadsA = kBytesA / 1024 / kWaves, kLoadsB = kBytesB / 1024 / kWaves;
-  static constexpr int kLoads = kLoadsA + kLoadsB;
+  static constexpr int kLoads = PA * kLoadsA + PB * kLoadsB;
   static constexpr int kBm = WM / 32, kBn = WN / 32;
   static constexpr int kPitch = WN * 4 + 16;          // bytes of a row on its way out
   static constexpr int kOutB = kWaves * 32 * kPitch;
-  static constexpr int kLdsB = kBufs * kStageB;
+  static constexpr int kLdsB = kBufs * kStageB;       // then 16 bytes a row for an epilogue's state
+  static constexpr int kStateB = TM * 16;
   static_assert(kLoadsA * kWaves * 1024 == kBytesA && kLoadsB * kWaves * 1024 == kBytesB && kOutB <= kLdsB, "");
 };
 
@@ -101,7 +105,7 @@ struct MmaLoader {
     for (int j = 0; j < LOADS; ++j) {
       const int idx = j * WAVES + wave;
       if constexpr (LAYOUT == kLayoutRow) {
-        const int row = idx * 16 + (lane >> 2), c = (lane & 3) ^ ((lane >> 3) & 3);
+        const int row = idx * 16 + (lane >> 2), c = (lane & 3) ^ ((lane >> 4) & 3);
         kl[j] = c * 8;
         off[j] = i0 + row < end ? (uint32_t)row * (uint32_t)ld * 2u + c * 16u : kOutside;
       } else {
@@ -118,12 +122,12 @@ struct MmaLoader {
 
 // 1 KB from the lanes' offsets to LDS, in lane order.  In asm, as the compiler would
 // have every later transposing read wait for all loads in flight; mma_wait and
-// mma_barrier are what orders them.  (The instruction writes no register; M0 needs
-// one wait state before it.)
+// mma_barrier are what orders them.  (The instruction writes no register.  The wait states are those that M0, and the
+// scalar registers of the range if the vector unit wrote them, need before it.)
 __device__ __forceinline__ void mma_dma(const char* base, uint32_t off, lds_char* to) {
   const uint64_t at = reinterpret_cast<uint64_t>(base);
   const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                ::"s"((uint32_t)(uintptr_t)to), "v"(off), "s"(rsrc)
                : "memory", "m0");
 }
@@ -165,7 +169,7 @@ struct MmaCore {
   template <int LAYOUT, int W>
   static __device__ __forceinline__ int frag_at(int first, int lane) {
     if constexpr (LAYOUT == kLayoutRow)
-      return (first + (lane & 31)) * 64 + ((lane >> 5) ^ ((lane >> 1) & 3)) * 16;
+      return (first + (lane & 31)) * 64 + ((lane >> 5) ^ ((lane >> 2) & 3)) * 16;
     const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), side = (lane >> 4) & 1;
     return first / W * (W * 64) + k * (W * 2) + ((first % W / 16 + side) ^ mma_swz<W>(k)) * 32 + (lane & 3) * 8;
   }
@@ -177,7 +181,9 @@ struct MmaCore {
       return wg_frag<W * 2>(stage + at + step * 16 * W * 2);
   }
 
-  __device__ __forceinline__ void run(const MmaArgs& q, lds_char* lds, int m0, int n0, int split) {
+  // `between` runs while the first stages are on their way.
+  template <typename F>
+  __device__ __forceinline__ void run(const MmaArgs& q, lds_char* lds, int m0, int n0, int split, F&& between) {
     static_assert(T::kBn == 2 || !PAIR, "");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -189,13 +195,16 @@ struct MmaCore {
     // where the next stage to be loaded lies
     int seg = first / q.seg_stages, at = first % q.seg_stages, left = stages;
     const char *pa, *pb, *pb2;
-    int64_t step_a, step_b, step_b2;
+    int64_t step_a, step_b, step_b2, plane_a, plane_b, plane_b2;  // bytes
     MmaLoader<LA, kWa, T::kLoadsA, T::kWaves> la;
     MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> lb;
     auto open = [&] {
       const MmaSeg& s = q.seg[seg];
       step_a = LA == kLayoutRow ? T::kBk * 2 : (int64_t)s.lda * T::kBk * 2;
       step_b = LB == kLayoutRow ? T::kBk * 2 : (int64_t)s.ldb * T::kBk * 2;
+      plane_a = 2 * s.plane_a;
+      plane_b = 2 * s.plane_b;
+      plane_b2 = 2 * s.plane_b2;
       step_b2 = PAIR ? (int64_t)s.ldb2 * T::kBk * 2 : 0;
       pa = reinterpret_cast<const char*>(s.a) + (LA == kLayoutRow ? (int64_t)m0 * s.lda : m0) * 2 + at * step_a;
       pb = reinterpret_cast<const char*>(s.b) + (LB == kLayoutRow ? (int64_t)n0 * s.ldb : n0) * 2 + at * step_b;
@@ -211,16 +220,22 @@ struct MmaCore {
       }
     };
     open();
-    // Issues the loads of the next stage into the buffer (of zeros past the last).
-    auto issue = [&](lds_char* to) {
-      const int ra = left > 0 ? q.ka - at * T::kBk : 0, rb = left > 0 ? q.kb - at * T::kBk : 0;
-#pragma unroll
-      for (int j = 0; j < T::kLoadsA; ++j)
-        mma_dma(pa, la.kl[j] < ra ? la.off[j] : kOutside, to + (j * T::kWaves + wave) * 1024);
-#pragma unroll
-      for (int j = 0; j < T::kLoadsB; ++j)
-        mma_dma(PAIR && j >= T::kLoadsB / 2 ? pb2 : pb, lb.kl[j] < rb ? lb.off[j] : kOutside,
-                to + T::kBytesA + (j * T::kWaves + wave) * 1024);
+    // Load n of the next stage's kLoads into the buffer (zeros past the last stage), and
+    // the step to the stage after it.
+    auto load = [&](lds_char* to, int n) {
+      if (n < T::PA * T::kLoadsA) {
+        const int p = n / T::kLoadsA, j = n % T::kLoadsA, left_k = left > 0 ? q.ka - at * T::kBk : 0;
+        mma_dma(pa + p * plane_a, la.kl[j] < left_k ? la.off[j] : kOutside,
+                to + p * T::kBytesA + (j * T::kWaves + wave) * 1024);
+      } else {
+        const int m = n - T::PA * T::kLoadsA, p = m / T::kLoadsB, j = m % T::kLoadsB;
+        const int left_k = left > 0 ? q.kb - at * T::kBk : 0;
+        mma_dma(PAIR && j >= T::kLoadsB / 2 ? pb2 + p * plane_b2 : pb + p * plane_b,
+                lb.kl[j] < left_k ? lb.off[j] : kOutside,
+                to + T::PA * T::kBytesA + p * T::kBytesB + (j * T::kWaves + wave) * 1024);
+      }
+    };
+    auto advance = [&] {
       --left;
       if (++at == q.seg_stages && left > 0) {
         ++seg;
@@ -232,12 +247,17 @@ struct MmaCore {
         if (PAIR) pb2 += step_b2;
       }
     };
+    auto issue = [&](lds_char* to) {
+#pragma unroll
+      for (int n = 0; n < T::kLoads; ++n) load(to, n);
+      advance();
+    };
 
     int oa[T::kBm], ob[T::kBn];
 #pragma unroll
     for (int i = 0; i < T::kBm; ++i) oa[i] = frag_at<LA, kWa>(wm + i * 32, lane);
 #pragma unroll
-    for (int j = 0; j < T::kBn; ++j) ob[j] = T::kBytesA + frag_at<LB, kWb>(block_col(j), lane);
+    for (int j = 0; j < T::kBn; ++j) ob[j] = frag_at<LB, kWb>(block_col(j), lane);
 #pragma unroll
     for (int i = 0; i < T::kBm; ++i)
 #pragma unroll
@@ -245,60 +265,92 @@ struct MmaCore {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-    bf16x8 fa[2][T::kBm], fb[2][T::kBn];
-    auto read = [&](lds_char* stage, int step) {
-#pragma unroll
-      for (int j = 0; j < T::kBn; ++j) fb[step][j] = frag<LB, kWb>(stage, ob[j], step);
-#pragma unroll
-      for (int i = 0; i < T::kBm; ++i) fa[step][i] = frag<LA, kWa>(stage, oa[i], step);
+    bf16x8 fa[2][T::PA][T::kBm], fb[2][T::PB][T::kBn];
+    constexpr int kFrags = T::PA * T::kBm + T::PB * T::kBn;
+    auto read_one = [&](lds_char* stage, int step, int n) {
+      if (n < T::PB * T::kBn) {
+        const int p = n / T::kBn, j = n % T::kBn;
+        fb[step][p][j] = frag<LB, kWb>(stage + T::PA * T::kBytesA + p * T::kBytesB, ob[j], step);
+      } else {
+        const int m = n - T::PB * T::kBn, p = m / T::kBm, i = m % T::kBm;
+        fa[step][p][i] = frag<LA, kWa>(stage + p * T::kBytesA, oa[i], step);
+      }
     };
-    auto multiply = [&](int step) {
+    // The products of a step, pairs of planes by size, the smallest first.  beside(n)
+    // puts what else the wave issues behind product n: a product keeps the matrix unit
+    // busy for 32 cycles, in which a few other instructions go out.
+    constexpr int kPairs = T::PA + T::PB == 2 ? 1 : T::PA + T::PB == 4 ? 3 : 6;
+    constexpr int kProducts = kPairs * T::kBm * T::kBn;
+    auto multiply = [&](int step, auto&& beside) {
+      int n = 0;
 #pragma unroll
-      for (int i = 0; i < T::kBm; ++i)
+      for (int s = kPairs > 1 ? 2 : 0; s >= 0; --s)
 #pragma unroll
-        for (int j = 0; j < T::kBn; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step][j], fa[step][i], acc[i][j], 0, 0, 0);
+        for (int p = 0; p < T::PA; ++p) {
+          const int r = s - p;
+          if (r < 0 || r >= T::PB) continue;
+#pragma unroll
+          for (int i = 0; i < T::kBm; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kBn; ++j) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step][r][j], fa[step][p][i], acc[i][j], 0, 0, 0);
+              beside(n++);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    // The fragments of a step go out behind the first three quarters of the products
+    // before it, the loads of a stage behind all of them.
+    constexpr int kEarly = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
+    auto read_beside = [&](lds_char* stage, int step, int n) {
+#pragma unroll
+      for (int k = 0; k < kFrags; ++k)
+        if (k * kEarly / kFrags == n) read_one(stage, step, k);
     };
 
 #pragma unroll
     for (int b = 0; b < T::kBufs - 1; ++b) issue(lds + b * T::kStageB);
+    between();
     mma_wait<(T::kBufs - 2) * T::kLoads>();
     mma_barrier();
     int cur = 0;
-    read(lds, 0);
+#pragma unroll
+    for (int k = 0; k < kFrags; ++k) read_one(lds, 0, k);
     issue(lds + (T::kBufs - 1) * T::kStageB);
 #pragma unroll 1
     for (int s = 0; s < stages; ++s) {
       lds_char* now = lds + cur;
       cur = cur == (T::kBufs - 1) * T::kStageB ? 0 : cur + T::kStageB;
-      read(now, 1);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(0);
-      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, [&](int n) { read_beside(now, 1, n); });
       mma_wait<(T::kBufs - 2) * T::kLoads>();
       mma_barrier();
-      read(lds + cur, 0);
-      issue(now);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(1);
-      __builtin_amdgcn_sched_barrier(0);
+      multiply(1, [&](int n) {
+        read_beside(lds + cur, 0, n);
+#pragma unroll
+        for (int k = 0; k < T::kLoads; ++k)
+          if (k * kProducts / T::kLoads == n) load(now, k);
+      });
+      advance();
     }
     mma_wait<0>();
     mma_barrier();
   }
 };
 
-// Columns of C that a wave's units hold, written to part or given to f(row, col,
-// first values, second values of a pair).
-template <typename T, bool PAIR, typename Core, typename F>
-__device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, lds_char* lds, int m0, int n0, int split,
-                                          F&& f) {
+// The wave's results in units of 8 columns, written to part or given to e(row, its
+// state, column, first values, second values of a pair).  The units of 32 rows are
+// read together, so that their ways through LDS and the epilogue overlap (one unit
+// after another, the logits' gradient took 17 us of a 256 x 256 tile's 45).
+template <typename T, typename Core, typename E>
+__device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, lds_char* lds, lds_char* state, int m0,
+                                          int n0, int split, const E& e) {
+  constexpr bool PAIR = E::kPair;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
   lds_char* own = lds + wave * 32 * T::kPitch;
   constexpr int kUnits = PAIR ? T::WN / 16 : T::WN / 8;  // of a row
   constexpr int kTurns = 32 * kUnits / 64;
-  const int col0 = n0 + (PAIR ? core.wn * (T::WN / 2) : core.wn * T::WN);
+  const int col = n0 + (PAIR ? core.wn * (T::WN / 2) : core.wn * T::WN) + lane % kUnits * 8;
 #pragma unroll 1
   for (int i = 0; i < T::kBm; ++i) {
 #pragma unroll
@@ -314,21 +366,27 @@ __device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, ld
         }
     }
     wave_lds_order();
-#pragma unroll 1
+    float x[kTurns][8], y[kTurns][8];
+    f32x4 st[kTurns];
+#pragma unroll
     for (int t = 0; t < kTurns; ++t) {
-      const int u = t * 64 + lane, r = u / kUnits, c = u % kUnits * 8;
-      const int row = m0 + core.wm + i * 32 + r, col = col0 + c;
-      float x[8], y[8];
+      const int r = t * (64 / kUnits) + lane / kUnits;
       auto get = [&](float (&w)[8], int at) {
         const f32x4 lo = *(lds_f32x4*)(own + r * T::kPitch + at * 4);
         const f32x4 hi = *(lds_f32x4*)(own + r * T::kPitch + at * 4 + 16);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = lo[e], w[4 + e] = hi[e];
+        for (int k = 0; k < 4; ++k) w[k] = lo[k], w[4 + k] = hi[k];
       };
-      get(x, c);
-      if (PAIR) get(y, T::WN / 2 + c);
-      if (row >= q.M || col >= q.N) continue;
-      if (q.part) {
+      get(x[t], lane % kUnits * 8);
+      if (PAIR) get(y[t], T::WN / 2 + lane % kUnits * 8);
+      if (E::kState) st[t] = *(lds_f32x4*)(state + (core.wm + i * 32 + r) * 16);
+    }
+    wave_lds_order();
+    const int row = m0 + core.wm + i * 32 + lane / kUnits;
+    if (q.part) {
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        if (row + t * (64 / kUnits) >= q.M || col >= q.N) continue;
         auto put = [&](const float (&w)[8], float* p) {
           f32x4 lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
           if (q.part_add) {
@@ -338,16 +396,31 @@ __device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, ld
           *reinterpret_cast<f32x4*>(p) = lo;
           *reinterpret_cast<f32x4*>(p + 4) = hi;
         };
-        float* p = q.part + ((int64_t)split * q.M + row) * q.ld_part + col;
-        put(x, p);
-        if (PAIR) put(y, p + q.ld_part / 2);
-      } else {
-        f(row, col, x, y);
+        float* p = q.part + ((int64_t)split * q.M + row + t * (64 / kUnits)) * q.ld_part + col;
+        put(x[t], p);
+        if (PAIR) put(y[t], p + q.ld_part / 2);
       }
+    } else {
+      e.template units<kTurns>(row, 64 / kUnits, q.M, st, col, x, y);
     }
-    wave_lds_order();
   }
 }
+
+// What epilogues have in common: units go to E's operator one by one, unless it takes
+// them together.
+template <typename E>
+struct UnitEpilogue {
+  static constexpr bool kPair = false, kWhole = false, kState = false;
+  template <int N>
+  __device__ __forceinline__ void units(int row, int step, int M, const f32x4 (&st)[N], int col, float (&x)[N][8],
+                                        float (&y)[N][8]) const {
+    const E& e = *static_cast<const E*>(this);
+    if (col >= e.N) return;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+      if (row + t * step < M) e(row + t * step, st[t], col, x[t], y[t]);
+  }
+};
 
 // C, each unit handed to the epilogue E.  ld_part holds whole units.
 template <typename T, int LA, int LB, typename E>
@@ -360,15 +433,24 @@ __global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
   int tm, tn;
   mma_tile(l % tiles, q.tiles_m, q.tiles_n, tm, tn);
   const int m0 = tm * T::TM, n0 = tn * (E::kPair ? T::TN / 2 : T::TN);
+  lds_char* state = lds + T::kLdsB;
+  // what the epilogue needs of each row, loaded behind the first stages
+  auto states = [&] {
+    if constexpr (E::kState) {
+      typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+      for (int r = threadIdx.x; r < T::TM; r += T::kThr)
+        *(lds_f32x4*)(state + r * 16) = m0 + r < q.M ? e.state(m0 + r) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
   MmaCore<T, LA, LB, E::kPair> core;
-  core.run(q, lds, m0, n0, split);
+  core.run(q, lds, m0, n0, split, states);
   if constexpr (E::kWhole) {
     if (!q.part) {
       e.template whole<T>(q, core, lds, m0, n0, tn);
       return;
     }
   }
-  mma_units<T, E::kPair>(q, core, lds, m0, n0, split, e);
+  mma_units<T>(q, core, lds, state, m0, n0, split, e);
 }
 
 // The epilogue of a product whose contraction was cut: parts added in order.  One
@@ -391,7 +473,9 @@ __global__ __launch_bounds__(kThreads) void mma_join_kernel(MmaArgs q, E e) {
       add(x, p);
       if (E::kPair) add(y, p + q.ld_part / 2);
     }
-    e(row, col, x, y);
+    f32x4 st = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (E::kState) st = e.state(row);
+    e(row, st, col, x, y);
   }
 }
 
@@ -438,11 +522,10 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(ActShape h, const S* __r
 
 // C = beta C + the product, in either type.  With `second`, the product's columns from
 // there on are another matrix.
-struct OutEpilogue {
-  static constexpr bool kPair = false, kWhole = false;
+struct OutEpilogue : UnitEpilogue<OutEpilogue> {
   void* C[2];
   int64_t ld[2];
-  int second, N;  // N: columns of C
+  int second, Nc, N;  // where the second begins, columns of one, of the product
   int bf16;
   float beta;
 
@@ -453,14 +536,16 @@ struct OutEpilogue {
     S* p = static_cast<S*>(b ? C[1] : C[0]) + row * (b ? ld[1] : ld[0]) + col;
     ActVec<S> v;
     if (beta != 0.f) {
-      v.load(p, N - col);
+      v.load(p, Nc - col);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = fmaf(beta, v.at(i), x[i]);
     }
     v.set(x);
-    v.store(p, N - col);
+    v.store(p, Nc - col);
   }
-  __device__ __forceinline__ void operator()(int row, int col, float (&x)[8], float (&)[8]) const {
+  OutEpilogue(void* c0, int64_t ld0, void* c1, int64_t ld1, int cols, int n, int n_all, int b, float be)
+      : C{c0, c1}, ld{ld0, ld1}, second(cols), Nc(n), N(n_all), bf16(b), beta(be) {}
+  __device__ __forceinline__ void operator()(int row, const f32x4&, int col, float (&x)[8], float (&)[8]) const {
     if (bf16) put<uint16_t>(row, col, x);
     else put<float>(row, col, x);
   }

@@ -16,31 +16,48 @@ struct MmaPlan {
   size_t part = 0;  // bytes of the parts
 };
 
-// The cheapest tile and number of parts by estimated time.  A stage of a workgroup takes
-// `work` us of its compute unit, and at least `alone` us on its own; `slots`
-// workgroups share a compute unit.  Parts cost their way to memory and back, and
-// the launch that adds them.
-inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, int segs, bool pair, bool few, int most_splits,
+// A tile and what it takes: us of a stage with 1, 2, .. workgroups on a compute unit
+// (`alone`: one, and half the chip idle), us of a launch beside its stages.
+struct MmaCost {
+  int m, n, slots;
+  double alone, stage[4], start;
+};
+// Measured for one plane each (bf16), 3 and 1, 3 and 3 (fp32).  Per compute unit the
+// large tiles reach 5.2 TFLOP/s (one plane), 4.5 and 4.7, where the chip lowers its clock;
+// 8192^3 of the library in bf16 5.1.
+constexpr MmaCost kCost11[] = {{32, 128, 4, 0.28, {0.30, 0.38, 0.49, 0.62}, 4},
+                               {128, 128, 2, 0.29, {0.34, 0.66}, 5},
+                               {256, 256, 1, 0.60, {0.80}, 9}};
+constexpr MmaCost kCost31[] = {{32, 128, 2, 0.40, {0.45, 0.70}, 5}, {128, 128, 1, 0.55, {0.72}, 6}, {256, 128, 1, 1.03, {1.45}, 9}};
+constexpr MmaCost kCost33[] = {{32, 128, 2, 0.70, {0.73, 1.17}, 5}, {128, 128, 1, 0.86, {1.33}, 6}, {256, 128, 1, 1.55, {2.34}, 10}};
+
+// Time of `groups` workgroups of `per` stages: full rounds of the chip, then the rest.
+inline double mma_us(const MmaCost& t, int64_t groups, int64_t per) {
+  const int64_t full = 256 * t.slots, rest = groups % full;
+  double us = (double)(groups / full) * ((double)per * t.stage[t.slots - 1] + t.start);
+  if (rest) us += (double)per * (rest <= 128 ? t.alone : t.stage[(rest - 1) / 256]) + t.start;
+  return us;
+}
+
+// The cheapest tile and number of parts by estimated time, for operands of pa and pb
+// planes.  Parts cost their way to memory and back (more where the last-level cache
+// does not hold them) and the launch that adds them.
+inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, int pa, int pb, int segs, bool pair, bool few, int most_splits,
                         bool always_part) {
-  struct Shape {
-    int m, n, slots;
-    double work, alone, start;
-  };
-  static const Shape shapes[] = {{32, 128, 4, 0.16, 0.35, 3}, {128, 128, 2, 0.27, 0.40, 4}, {256, 256, 1, 0.90, 0.90, 6}};
+  const MmaCost* cost = pa + pb == 2 ? kCost11 : pa + pb == 4 ? kCost31 : kCost33;
   MmaPlan best;
   double best_us = 0;
   const int64_t seg_stages = cdiv64(K, 32), stages = seg_stages * segs;
+  const int64_t ld = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
   for (int i = few ? 0 : 1; i < 3; ++i) {
-    const Shape& t = shapes[i];
+    const MmaCost& t = cost[i];
     const int64_t tm = cdiv64(M, t.m), tn = cdiv64(N, pair ? t.n / 2 : t.n);
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (want > stages || want > most_splits || (want > 1 && want * tm * tn > 256 * 2 * t.slots)) break;
-      const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per), groups = tm * tn * splits;
-      const int64_t ld = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
+      if (want > stages || want > most_splits || (want > 1 && want * tm * tn > 1024)) break;
+      const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
       const size_t part = splits > 1 || always_part ? (size_t)(splits * M * ld) * sizeof(float) : 0;
-      const double us = t.start + (double)per * std::max((double)cdiv64(groups, 256) * t.work,
-                                                         (double)cdiv64(groups, 256 * t.slots) * t.alone) +
-                        (splits > 1 ? 4 + 0.4e-6 * (double)part : 0);
+      const double mb = 1e-6 * (double)part;
+      const double us = mma_us(t, tm * tn * splits, per) + (splits > 1 ? 5 + 0.3 * mb + 0.25 * std::max(0., mb - 256) : 0);
       if (best_us == 0 || us < best_us) {
         best_us = us;
         best = {i, (int)splits, (int)per, tm, tn, seg_stages, ld, part};
@@ -82,12 +99,12 @@ constexpr int64_t kPieceB = 256 << 20;
 
 inline int64_t vocab_piece(int64_t vocab, int64_t bytes_each) {
   const int64_t most = std::max<int64_t>(256, kPieceB / bytes_each / 256 * 256);
-  return std::min(vocab, most);
+  return std::min(vocab, cdiv64(cdiv64(vocab, cdiv64(vocab, most)), 256) * 256);
 }
 
 // Columns of a row of logits whose statistics are one entry, where the logits were
 // formed in parts.
-constexpr int kStatCols = 2048;
+constexpr int kStatCols = 512;  // 8 of a lane
 
 // The loss: pieces of the vocabulary (one, where the table is read as it lies).
 struct VocabPlan {
@@ -110,7 +127,7 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
   const int64_t last = vocab - (p.pieces - 1) * p.piece;
   size_t part = 0;
   for (int i = 0; i < 2; ++i) {
-    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, dtype == SHAMPOO_F32 ? 6 : 1, false, true, 64, false);
+    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, p.x.planes, p.x.planes, 1, false, true, 64, false);
     part = std::max(part, p.mma[i].part);
   }
   p.entries = (p.pieces - 1) * vocab_entries(p.mma[0], p.piece) + vocab_entries(p.mma[1], last);
@@ -134,14 +151,11 @@ struct VocabGradPlan {
 // would keep 9 bits, with two 17.  A bf16 one takes dz as the framework stores a
 // bf16 gradient of logits, rounded once.
 inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || g_dtype == SHAMPOO_F32 ? 3 : 1; }
-// Products of a weight gradient: an fp32 input's three planes times three terms.
-inline int grad_segs(int dtype, int planes) { return dtype == SHAMPOO_F32 ? 6 : planes; }
 
 inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype, bool pack_x,
                                      bool pack_w) {
   VocabGradPlan p;
   Room r;
-  const bool f32 = dtype == SHAMPOO_F32;
   p.planes = grad_planes(dtype, g_dtype);
   p.x = pack_plan(rows, dim, dtype);
   if (pack_x) p.at_x = r.take(p.x.bytes);
@@ -156,9 +170,10 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
   const int64_t last = vocab - (p.pieces - 1) * p.piece;
   for (int i = 0; i < 2; ++i) {
     const int64_t n = i ? last : p.piece;
-    p.z[i] = mma_plan(rows, n, dim, f32 ? 6 : 1, false, true, 64, false);
-    p.dx[i] = mma_plan(rows, dim, n, f32 ? 6 : 1, false, true, i ? p.dx[0].splits : 64, p.pieces > 1);
-    p.dw[i] = mma_plan(n, dim, rows, grad_segs(dtype, p.planes), false, false, 64, false);
+    const int in = p.x.planes;
+    p.z[i] = mma_plan(rows, n, dim, in, in, 1, false, true, 64, false);
+    p.dx[i] = mma_plan(rows, dim, n, in, in, 1, false, true, i ? p.dx[0].splits : 64, p.pieces > 1);
+    p.dw[i] = mma_plan(n, dim, rows, p.planes, in, 1, false, false, 64, false);
     part = std::max({part, p.z[i].part, p.dw[i].part});
   }
   p.at_dx = r.take(p.dx[0].part);
@@ -181,7 +196,7 @@ inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, boo
   if (pack_x) p.at_x = r.take(p.x.bytes);
   if (pack_wg) p.at_wg = r.take(p.wg.bytes);
   if (pack_wu) p.at_wu = r.take(p.wu.bytes);
-  p.mma = mma_plan(rows, width, dim, dtype == SHAMPOO_F32 ? 6 : 1, true, true, 64, false);
+  p.mma = mma_plan(rows, width, dim, p.x.planes, p.x.planes, 1, true, true, 64, false);
   p.at_part = r.take(p.mma.part);
   p.bytes = r.at;
   return p;
@@ -200,7 +215,6 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
                                  bool pack_wg, bool pack_wu) {
   FfnGradPlan p;
   Room r;
-  const bool f32 = dtype == SHAMPOO_F32;
   p.planes = grad_planes(dtype, g_dtype);
   p.x = pack_plan(rows, dim, dtype);
   p.wg = p.wu = pack_plan(dim, width, dtype);
@@ -209,9 +223,10 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   if (pack_wu) p.at_wu = r.take(p.wu.bytes);
   p.ld_d = cdiv64(width, 64) * 64;
   p.at_d = r.take((size_t)(rows * 2 * p.ld_d * p.planes) * 2);
-  p.gu = mma_plan(rows, width, dim, f32 ? 6 : 1, true, true, 64, false);
-  p.dx = mma_plan(rows, dim, width, f32 ? 12 : 2, false, true, 64, false);
-  p.dw = mma_plan(dim, 2 * p.ld_d, rows, grad_segs(dtype, p.planes), false, false, 64, false);
+  const int in = p.x.planes;
+  p.gu = mma_plan(rows, width, dim, in, in, 1, true, true, 64, false);
+  p.dx = mma_plan(rows, dim, width, in, in, 2, false, true, 64, false);
+  p.dw = mma_plan(dim, 2 * p.ld_d, rows, in, p.planes, 1, false, false, 64, false);
   p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part}));
   p.bytes = r.at;
   return p;

@@ -34,14 +34,17 @@ __device__ __forceinline__ f32x2p ms_join(f32x2p a, f32x2p b) {
   return {n, a[1] * lse_exp(lse_shift(a[0], n)) + b[1] * lse_exp(lse_shift(b[0], n))};
 }
 
-struct LseEpilogue {
-  static constexpr bool kPair = false, kWhole = true;
+struct LseEpilogue : UnitEpilogue<LseEpilogue> {
+  static constexpr bool kWhole = true;
   VocabTargets t;
   f32x2p* stat;      // rows x ld_stat
   int64_t ld_stat;
   float* z_target;   // rows
+  int N;
 
-  __device__ __forceinline__ void operator()(int, int, float (&)[8], float (&)[8]) const {}
+  LseEpilogue(VocabTargets tt, f32x2p* s, int64_t ld, float* z, int n)
+      : t(tt), stat(s), ld_stat(ld), z_target(z), N(n) {}
+  __device__ __forceinline__ void operator()(int, const f32x4&, int, float (&)[8], float (&)[8]) const {}
 
   template <typename T, typename Core>
   __device__ __forceinline__ void whole(const MmaArgs& q, const Core& core, lds_char* lds, int m0, int n0,
@@ -95,23 +98,37 @@ struct LseEpilogue {
 };
 
 // (m, s) of kStatCols columns of a row of logits that were formed in parts: a wave
-// each.
+// each, its columns in registers.
 __global__ __launch_bounds__(kThreads) inline void logit_stat_kernel(MmaArgs q, LseEpilogue e) {
   const int lane = threadIdx.x & 63, parts = (q.N + kStatCols - 1) / kStatCols;
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   if (w >= (int64_t)q.M * parts) return;
   const int row = (int)(w / parts), p = (int)(w % parts);
-  const int t = e.t.at(row), end = min(q.N, (p + 1) * kStatCols);
-  f32x2p a = {kLowest, 0.f};
-  for (int c = p * kStatCols + lane; c < end; c += 64) {
-    const float* z = q.part + (int64_t)row * q.ld_part + c;
-    float x = 0.f;
+  constexpr int kEach = kStatCols / 64;
+  const int c0 = p * kStatCols + lane * kEach, t = e.t.at(row) - c0;
+  const float* at = q.part + (int64_t)row * q.ld_part + c0;
+  float z[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) z[i] = 0.f;
+  if (c0 < q.N) {  // whole units of 8 lie in the part
 #pragma unroll 4
-    for (int s = 0; s < q.splits; ++s) x += z[(int64_t)s * q.M * q.ld_part];
-    if (c == t) e.z_target[row] = x;
-    const float n = fmaxf(a[0], x);
-    a = {n, a[1] * lse_exp(lse_shift(a[0], n)) + lse_exp(x - n)};
+    for (int s = 0; s < q.splits; ++s)
+#pragma unroll
+      for (int i = 0; i < kEach / 4; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(at + (int64_t)s * q.M * q.ld_part + 4 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[4 * i + k] += x[k];
+      }
   }
+  f32x2p a = {kLowest, 0.f};
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (c0 + i >= q.N) z[i] = -INFINITY;
+    else if (i == t) e.z_target[row] = z[i];
+    a[0] = fmaxf(a[0], z[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) a[1] += lse_exp(z[i] - a[0]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) a = ms_join(a, f32x2p{__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64)});
   if (lane == 0) e.stat[(int64_t)row * e.ld_stat + p] = a;
@@ -136,24 +153,39 @@ __global__ __launch_bounds__(kThreads) inline void lse_join_kernel(int64_t rows,
   }
 }
 
-// The gradient of the logits, in one or three bf16 terms.
-struct DlogitEpilogue {
-  static constexpr bool kPair = false, kWhole = false;
+// The gradient of the logits, in one or three bf16 terms.  A row's state: c, g (0
+// without a target), lse and the target's column.
+struct DlogitEpilogue : UnitEpilogue<DlogitEpilogue> {
+  static constexpr bool kState = true;
   VocabTargets t;
   const float *lse, *g_logp, *g_lse;
   uint16_t* dz;  // M x ld
   int64_t ld, plane;
   int N, planes;
 
-  __device__ __forceinline__ void operator()(int row, int col, float (&z)[8], float (&)[8]) const {
-    const int target = t.at(row), at = target - col;
-    const float g = g_logp && target != t.kNone ? g_logp[row] : 0.f;
-    const float c = (g_lse ? g_lse[row] : 0.f) - g, l = lse[row];
+  DlogitEpilogue(VocabTargets tt, const float* l, const float* gp, const float* gs, uint16_t* d, int64_t ld_d,
+                 int64_t pl, int n, int np)
+      : t(tt), lse(l), g_logp(gp), g_lse(gs), dz(d), ld(ld_d), plane(pl), N(n), planes(np) {}
+  __device__ __forceinline__ f32x4 state(int row) const {
+    const int target = t.at(row);
+    const float l = lse[row], given = g_logp ? g_logp[row] : 0.f, penalty = g_lse ? g_lse[row] : 0.f;
+    const float g = target != t.kNone ? given : 0.f;
+    return {penalty - g, g, l, __int_as_float(target)};
+  }
+  __device__ __forceinline__ void operator()(int row, const f32x4& st, int col, float (&z)[8], float (&)[8]) const {
+    const float c = st[0], g = st[1], l = st[2];
+    const int at = __float_as_int(st[3]) - col;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      z[i] = c * lse_exp(z[i] - l);
-      if (i == at) z[i] += g;
-      if (col + i >= N || l == -INFINITY) z[i] = 0.f;
+    for (int i = 0; i < 8; ++i) z[i] = c * lse_exp(z[i] - l);
+    if (at >= 0 && at < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i == at) z[i] += g;
+    }
+    if (col + 8 > N || l == -INFINITY) {  // columns past the last, and rows of nothing
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i >= N || l == -INFINITY) z[i] = 0.f;
     }
     uint16_t* d = dz + row * ld + col;
     if (planes == 1) {
