@@ -198,6 +198,8 @@ struct MmaCore {
     int64_t step_a, step_b, step_b2, plane_a, plane_b, plane_b2;  // bytes
     MmaLoader<LA, kWa, T::kLoadsA, T::kWaves> la;
     MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> lb;
+    // whether load j of B is of a pair's second panel
+    auto second = [&](int j) { return PAIR && (j * T::kWaves + wave) * 2 >= T::kLoadsB * T::kWaves; };
     auto open = [&] {
       const MmaSeg& s = q.seg[seg];
       step_a = LA == kLayoutRow ? T::kBk * 2 : (int64_t)s.lda * T::kBk * 2;
@@ -212,11 +214,11 @@ struct MmaCore {
       la.template init<false>(m0, q.M, s.lda, wave, lane);
       lb.template init<PAIR>(n0, q.N, s.ldb, wave, lane);
       if (PAIR && s.ldb2 != s.ldb) {
-        // the second panel's loads (all of a wave's loads j >= kLoadsB / 2)
         MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> l2;
         l2.template init<PAIR>(n0, q.N, s.ldb2, wave, lane);
 #pragma unroll
-        for (int j = T::kLoadsB / 2; j < T::kLoadsB; ++j) lb.off[j] = l2.off[j];
+        for (int j = 0; j < T::kLoadsB; ++j)
+          if (second(j)) lb.off[j] = l2.off[j];
       }
     };
     open();
@@ -230,7 +232,7 @@ struct MmaCore {
       } else {
         const int m = n - T::PA * T::kLoadsA, p = m / T::kLoadsB, j = m % T::kLoadsB;
         const int left_k = left > 0 ? q.kb - at * T::kBk : 0;
-        mma_dma(PAIR && j >= T::kLoadsB / 2 ? pb2 + p * plane_b2 : pb + p * plane_b,
+        mma_dma(second(j) ? pb2 + p * plane_b2 : pb + p * plane_b,
                 lb.kl[j] < left_k ? lb.off[j] : kOutside,
                 to + T::PA * T::kBytesA + p * T::kBytesB + (j * T::kWaves + wave) * 1024);
       }
