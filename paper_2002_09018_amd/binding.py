@@ -1018,16 +1018,21 @@ def _code(dtype):
     return dtype
 
 
-def _mat(t, rows, cols, code, dev):
-    """The layout of t if it has this shape, type (None: either) and device, else None."""
-    x = _layout(t)
-    ok = x is not None and x[0] == rows and x[1] == cols and (code is None or x[3] == code) and x[4] == dev
-    return x if ok else None
+def _fits(a, rows, cols, like):
+    """a (a layout, or None) is rows x cols, of the type and device of the layout `like`."""
+    return a is not None and a[0] == rows and a[1] == cols and a[3] == like[3] and a[4] == like[4]
 
 
-def _opt(x):
+def _opt(a):
     """Pointer and row stride of a layout that may be None."""
-    return (None, 0) if x is None else (x[5], x[2])
+    return (None, 0) if a is None else (a[5], a[2])
+
+
+def _done(handle, rc, written, read):
+    """A call's status.  The library refuses buffers that overlap; which, the tensors tell."""
+    if rc == SHAMPOO_EINVAL:
+        _check_all_apart(written, read)
+    _check(handle, rc)
 
 
 def _check_all_apart(written, read):
@@ -1036,16 +1041,6 @@ def _check_all_apart(written, read):
         for other, u in written[i + 1:] + read:
             if t is not None and u is not None:
                 _check_apart(t, u, f"{name} and {other}", False)
-
-
-def _all_apart(written, read):
-    """The same of layouts (None: not given)."""
-    for i, a in enumerate(written):
-        if a is not None:
-            for b in written[i + 1:] + read:
-                if b is not None and not _apart(a, b):
-                    return False
-    return True
 
 
 def _check_like(t, what, rows, cols, dtype=None):
@@ -1114,13 +1109,14 @@ def shampoo_vocab_logprobs_grad(handle, X, W, targets, lse, dX=None, dW=None, g_
     if ok:
         rows, dim, ld, dt, dev, ptr = x
         vocab = w[0]
-        dx, dw = None if dX is None else _mat(dX, rows, dim, dt, dev), None if dW is None else _mat(dW, vocab, dim, None, dev)
+        dx = None if dX is None else _layout(dX)
+        dw = None if dW is None else _layout(dW)
         gdt = dt if dw is None else dw[3]
         f32, vec = _torch_mod.float32, (rows,)
-        ok = ((dx is None) == (dX is None) and (dw is None) == (dW is None) and _plain(lse, f32, vec, dev) and
-              _plain(g_logp, f32, vec, dev) and _plain(g_lse, f32, vec, dev) and
+        ok = ((dX is None or _fits(dx, rows, dim, x)) and
+              (dW is None or (dw is not None and dw[0] == vocab and dw[1] == dim and dw[4] == dev)) and
+              _plain(lse, f32, vec, dev) and _plain(g_logp, f32, vec, dev) and _plain(g_lse, f32, vec, dev) and
               _plain(targets, _torch_mod.int32, vec, dev) and _on_handle(handle, dev) and
-              _all_apart([dx, dw], [x, w]) and
               _room(workspace, _lib.shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dt, gdt), dev))
     if not ok:
         def pairs():
@@ -1133,28 +1129,15 @@ def shampoo_vocab_logprobs_grad(handle, X, W, targets, lse, dX=None, dW=None, g_
                       lambda r, d, v: _lib.shampoo_vocab_logprobs_grad_workspace_bytes(
                           r, d, v, _code(X.dtype), _code(X.dtype if dW is None else dW.dtype)), pairs,
                       (("dX", dX), ("dW", dW)))
-    _check(handle, _lib.shampoo_vocab_logprobs_grad(
+    _done(handle, _lib.shampoo_vocab_logprobs_grad(
         handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets), lse.data_ptr(), _ptr(g_logp), _ptr(g_lse),
-        *_opt(dx), _opt(dw)[0], gdt, _opt(dw)[1], float(beta), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream_on(stream, dev)))
+        *_opt(dx), _opt(dw)[0], gdt, _opt(dw)[1], beta, _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_on(stream, dev)),
+        [("dX", dX), ("dW", dW)], [("X", X), ("W", W)])
 
 
 def shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype):
     return int(_lib.shampoo_gated_ffn_workspace_bytes(int(rows), int(dim), int(width), _code(dtype)))
-
-
-def _ffn_shapes(X, Wg, Wu, wide):
-    """Layouts of X, Wg, Wu and of the rows x width matrices `wide`, or None where one
-    does not fit the others."""
-    x, wg = _layout(X), _layout(Wg)
-    if x is None or wg is None or wg[0] != x[1] or wg[3] != x[3] or wg[4] != x[4]:
-        return None
-    rows, dim, _, dt, dev, _ = x
-    wu = _mat(Wu, dim, wg[1], dt, dev)
-    rest = [None if t is None else _mat(t, rows, wg[1], dt, dev) for t in wide]
-    if wu is None or any((a is None) != (t is None) for a, t in zip(rest, wide)):
-        return None
-    return x, wg, wu, rest
 
 
 def _refuse_ffn(handle, X, Wg, Wu, wide, more, written, read, room, workspace):
@@ -1176,22 +1159,24 @@ def shampoo_gated_ffn(handle, X, Wg, Wu, H, act=ACT_SILU, G=None, U=None, worksp
     """H (rows x width) = act(X Wg) o (X Wu); X: rows x dim, Wg and Wu: dim x width; G and U
     (both or neither): the projections, rows x width; all fp32 or all bf16 (row-major
     views); workspace: uint8, shampoo_gated_ffn_workspace_bytes(rows, dim, width, X.dtype)."""
-    s = _ffn_shapes(X, Wg, Wu, (H, G, U)) if H is not None and (G is None) == (U is None) else None
-    ok = s is not None
+    x, wg, wu, lh = _layout(X), _layout(Wg), _layout(Wu), None if H is None else _layout(H)
+    lg, lu = None if G is None else _layout(G), None if U is None else _layout(U)
+    ok = x is not None and wg is not None and lh is not None and (G is None) == (U is None)
     if ok:
-        x, wg, wu, (lh, lg, lu) = s
         rows, dim, ld, dt, dev, ptr = x
         width = wg[1]
-        ok = (_all_apart([lh, lg, lu], [x, wg, wu]) and _on_handle(handle, dev) and
+        ok = (_fits(wg, dim, width, x) and _fits(wu, dim, width, x) and _fits(lh, rows, width, x) and
+              (G is None or (_fits(lg, rows, width, x) and _fits(lu, rows, width, x))) and _on_handle(handle, dev) and
               _room(workspace, _lib.shampoo_gated_ffn_workspace_bytes(rows, dim, width, dt), dev))
     if not ok:
         _need(H is not None, "H is required")
         _need((G is None) == (U is None), "G and U go together")
         _refuse_ffn(handle, X, Wg, Wu, (("H", H), ("G", G), ("U", U)), (), [("H", H), ("G", G), ("U", U)], [],
                     lambda r, d, w: _lib.shampoo_gated_ffn_workspace_bytes(r, d, w, _code(X.dtype)), workspace)
-    _check(handle, _lib.shampoo_gated_ffn(handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], int(act),
-                                          *_opt(lh), *_opt(lg), *_opt(lu), _ptr(workspace),
-                                          0 if workspace is None else workspace.numel(), _stream_on(stream, dev)))
+    _done(handle, _lib.shampoo_gated_ffn(handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], act,
+                                         lh[5], lh[2], *_opt(lg), *_opt(lu), _ptr(workspace),
+                                         0 if workspace is None else workspace.numel(), _stream_on(stream, dev)),
+          [("H", H), ("G", G), ("U", U)], [("X", X), ("Wg", Wg), ("Wu", Wu)])
 
 
 def shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype):
@@ -1206,19 +1191,22 @@ def shampoo_gated_ffn_grad(handle, X, Wg, Wu, dH, act=ACT_SILU, G=None, U=None, 
     neither).  G and U: the projections as kept, or None to form them again; workspace: uint8,
     shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, X.dtype, dWg.dtype) (without
     dWg: X.dtype twice)."""
-    pairs = (G is None) == (U is None) and (dWg is None) == (dWu is None) and (dX is not None or dWg is not None)
-    s = _ffn_shapes(X, Wg, Wu, (dH, G, U)) if dH is not None and pairs else None
-    ok = s is not None
+    x, wg, wu, lh = _layout(X), _layout(Wg), _layout(Wu), None if dH is None else _layout(dH)
+    lg, lu = None if G is None else _layout(G), None if U is None else _layout(U)
+    ok = (x is not None and wg is not None and lh is not None and (G is None) == (U is None) and
+          (dWg is None) == (dWu is None) and (dX is not None or dWg is not None))
     if ok:
-        x, wg, wu, (lh, lg, lu) = s
         rows, dim, ld, dt, dev, ptr = x
         width = wg[1]
-        dx = None if dX is None else _mat(dX, rows, dim, dt, dev)
-        dg = None if dWg is None else _mat(dWg, dim, width, None, dev)
+        dx = None if dX is None else _layout(dX)
+        dg = None if dWg is None else _layout(dWg)
+        du = None if dWu is None else _layout(dWu)
         gdt = dt if dg is None else dg[3]
-        du = None if dWu is None else _mat(dWu, dim, width, gdt, dev)
-        ok = ((dx is None) == (dX is None) and (dg is None) == (dWg is None) and (du is None) == (dWu is None) and
-              _all_apart([dx, dg, du], [x, wg, wu, lh, lg, lu]) and _on_handle(handle, dev) and
+        ok = (_fits(wg, dim, width, x) and _fits(wu, dim, width, x) and _fits(lh, rows, width, x) and
+              (G is None or (_fits(lg, rows, width, x) and _fits(lu, rows, width, x))) and
+              (dX is None or _fits(dx, rows, dim, x)) and
+              (dWg is None or (dg is not None and dg[0] == dim and dg[1] == width and dg[4] == dev and
+                               _fits(du, dim, width, dg))) and _on_handle(handle, dev) and
               _room(workspace, _lib.shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dt, gdt), dev))
     if not ok:
         _need(dH is not None, "dH is required")
@@ -1231,10 +1219,11 @@ def shampoo_gated_ffn_grad(handle, X, Wg, Wu, dH, act=ACT_SILU, G=None, U=None, 
                     [("dX", dX), ("dWg", dWg), ("dWu", dWu)], [("dH", dH), ("G", G), ("U", U)],
                     lambda r, d, w: _lib.shampoo_gated_ffn_grad_workspace_bytes(
                         r, d, w, _code(X.dtype), _code(X.dtype if dWg is None else dWg.dtype)), workspace)
-    _check(handle, _lib.shampoo_gated_ffn_grad(
-        handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], int(act), *_opt(lh), *_opt(lg), *_opt(lu),
-        *_opt(dx), *_opt(dg), *_opt(du), gdt, float(beta), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-        _stream_on(stream, dev)))
+    _done(handle, _lib.shampoo_gated_ffn_grad(
+        handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], act, *_opt(lh), *_opt(lg), *_opt(lu),
+        *_opt(dx), *_opt(dg), *_opt(du), gdt, beta, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+        _stream_on(stream, dev)),
+        [("dX", dX), ("dWg", dWg), ("dWu", dWu)], [("X", X), ("Wg", Wg), ("Wu", Wu), ("dH", dH), ("G", G), ("U", U)])
 
 
 def shampoo_dropout(handle, X, Y, rate, seed, offset=0, R=None, stream=None):
@@ -1242,8 +1231,8 @@ def shampoo_dropout(handle, X, Y, rate, seed, offset=0, R=None, stream=None):
     (row-major views; Y may be X or R).  seed and offset (64-bit) give the mask; the
     gradient with respect to X is the same call on dY without R."""
     x, y, r = _layout(X), _layout(Y), None if R is None else _layout(R)
-    ok = x is not None and y is not None and _alike(y, x) and (R is None or (r is not None and _alike(y, r)))
-    if not ok or not _on_handle(handle, x[4]) or not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+    if (x is None or not _fits(y, x[0], x[1], x) or not (R is None or _fits(r, x[0], x[1], x)) or
+            not _on_handle(handle, x[4]) or not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64)):
         _need(0 <= seed < 1 << 64 and 0 <= offset < 1 << 64, f"seed {seed} or offset {offset} outside [0, 2^64)")
         _check_matrix(X, "X")
         _check_matrix(Y, "Y", X)
@@ -1253,8 +1242,13 @@ def shampoo_dropout(handle, X, Y, rate, seed, offset=0, R=None, stream=None):
             _check_apart(Y, R, "Y and R", True)
         _refuse(handle, (("X", X), ("Y", Y), ("R", R)), ())
     rows, cols, ld, dt, dev, ptr = x
-    _check(handle, _lib.shampoo_dropout(handle, ptr, _opt(r)[0], y[5], dt, rows, cols, ld, _opt(r)[1], y[2],
-                                        float(rate), seed, offset, _stream_on(stream, dev)))
+    rc = _lib.shampoo_dropout(handle, ptr, None if r is None else r[5], y[5], dt, rows, cols, ld, 0 if r is None else r[2],
+                              y[2], rate, seed, offset, _stream_on(stream, dev))
+    if rc == SHAMPOO_EINVAL:
+        _check_apart(Y, X, "Y and X", True)
+        if R is not None:
+            _check_apart(Y, R, "Y and R", True)
+    _check(handle, rc)
 
 
 def shampoo_timing_enable(handle, enable=True):

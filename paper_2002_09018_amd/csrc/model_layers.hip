@@ -22,15 +22,21 @@ namespace {
 // Shapes of a product whose operands have PA and PB planes.
 template <int PA, int PB>
 struct Shapes {
+  using Solo = MmaShape<32, 64, 32, 64, 2, PA, PB, 4>;
   using Few = MmaShape<32, 128, 32, 64, 2, PA, PB>;
+  using Thin = MmaShape<64, 64, 32, 32, 2, PA, PB>;
   using Mid = MmaShape<128, 128, 32, 64, 3, PA, PB>;
   using Big = MmaShape<256, 128, 64, 64, 2, PA, PB>;
+  using BigWeight = Big;
 };
 template <>
 struct Shapes<1, 1> {
+  using Solo = MmaShape<32, 64, 32, 64, 3, 1, 1, 8>;
   using Few = MmaShape<32, 128, 32, 64, 4>;
-  using Mid = MmaShape<128, 128, 64, 64, 4>;
-  using Big = MmaShape<256, 256, 128, 64, 3>;
+  using Thin = MmaShape<64, 64, 32, 32, 2>;
+  using Mid = MmaShape<128, 128, 64, 64, 2, 1, 1, 0, 64>;
+  using Big = MmaShape<256, 256, 128, 64, 2, 1, 1, 0, 64>;
+  using BigWeight = MmaShape<256, 256, 128, 64, 3>;
 };
 
 // A buffer of a call and what to call it.
@@ -137,10 +143,16 @@ shampoo_status mma_launch(Handle* h, int cls, const MmaArgs& q, const E& e, hipS
 template <int LA, int LB, int PA, int PB, typename E>
 shampoo_status product(Handle* h, int cls, int shape, const MmaArgs& q, const E& e, hipStream_t s) {
   using K = Shapes<PA, PB>;
-  if constexpr (LA == kLayoutRow)
-    if (shape == kShapeFew) return mma_launch<typename K::Few, LA, LB>(h, cls, q, e, s);
+  if constexpr (LA == kLayoutRow && !E::kWhole)
+    if (shape == kShapeSolo) return mma_launch<typename K::Solo, LA, LB>(h, cls, q, e, s);
+  if (shape == kShapeFew) {
+    if constexpr (LA == kLayoutRow) return mma_launch<typename K::Few, LA, LB>(h, cls, q, e, s);
+    else return mma_launch<typename K::Thin, LA, LB>(h, cls, q, e, s);
+  }
   if (shape == kShapeMid) return mma_launch<typename K::Mid, LA, LB>(h, cls, q, e, s);
-  return mma_launch<typename K::Big, LA, LB>(h, cls, q, e, s);
+  if (shape == kShapeMid) return mma_launch<typename K::Mid, LA, LB>(h, cls, q, e, s);
+  using B = std::conditional_t<LA == kLayoutK, typename K::BigWeight, typename K::Big>;
+  return mma_launch<B, LA, LB>(h, cls, q, e, s);
 }
 // ... of operands that both have one or both three.
 template <int LA, int LB, typename E>
@@ -218,10 +230,9 @@ extern "C" {
 // ---------------------------------------------------------------- loss
 size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype) {
   if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
-  size_t need = 0;
-  for (int i = dtype == SHAMPOO_F32 ? 3 : 0; i < 4; ++i)
-    need = std::max(need, vocab_plan(rows, dim, vocab, dtype, i & 1, i & 2).bytes);
-  return need;
+  // (which matrices are copied hangs on strides and addresses: room for either way)
+  const size_t need = vocab_plan(rows, dim, vocab, dtype, true, true).bytes;
+  return dtype == SHAMPOO_F32 ? need : std::max(need, vocab_plan(rows, dim, vocab, dtype, true, false).bytes);
 }
 
 shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W, int dtype, int64_t rows, int64_t dim,
@@ -277,10 +288,9 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
 size_t shampoo_vocab_logprobs_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype) {
   if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
   if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
-  size_t need = 0;
-  for (int i = dtype == SHAMPOO_F32 ? 3 : 0; i < 4; ++i)
-    need = std::max(need, vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, i & 1, i & 2).bytes);
-  return need;
+  const size_t need = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, true).bytes;
+  return dtype == SHAMPOO_F32 ? need
+                              : std::max(need, vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, false).bytes);
 }
 
 shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const void* W, int dtype, int64_t rows,

@@ -65,36 +65,50 @@ struct MmaArgs {
   int part_add;        // added to what `part` holds
 };
 
-template <int TM_, int TN_, int WM_, int WN_, int BUFS_, int PA_ = 1, int PB_ = 1>
+// Tiles of TM x TN, waves of WM x WN.  SOLO: so many waves that each hold the whole tile
+// and a share of the contraction, with a ring of their own and no barrier; their sums
+// are added in order at the end.
+template <int TM_, int TN_, int WM_, int WN_, int BUFS_, int PA_ = 1, int PB_ = 1, int SOLO_ = 0,
+          int BK_ = 32>
 struct MmaShape {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, kBufs = BUFS_, PA = PA_, PB = PB_;
-  static constexpr int kBk = 32;
-  static constexpr int kWavesN = TN / WN, kWaves = (TM / WM) * kWavesN, kThr = 64 * kWaves;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, kBufs = BUFS_, PA = PA_, PB = PB_, kSolo = SOLO_;
+  static constexpr int kBk = BK_, kSteps = kBk / 16;  // contraction indices of a stage, 16 to a step
+  static constexpr int kWavesN = TN / WN, kWaves = (TM / WM) * kWavesN;  // that share a stage
+  static constexpr int kThr = 64 * kWaves * (kSolo ? kSolo : 1);
   static constexpr int kBytesA = TM * kBk * 2, kBytesB = TN * kBk * 2;  // of one plane
   static constexpr int kStageB = PA * kBytesA + PB * kBytesB;
   static constexpr int kLoadsA = kBytesA / 1024 / kWaves, kLoadsB = kBytesB / 1024 / kWaves;
   static constexpr int kLoads = PA * kLoadsA + PB * kLoadsB;
   static constexpr int kBm = WM / 32, kBn = WN / 32;
   static constexpr int kPitch = WN * 4 + 16;          // bytes of a row on its way out
-  static constexpr int kOutB = kWaves * 32 * kPitch;
-  static constexpr int kLdsB = kBufs * kStageB;       // then 16 bytes a row for an epilogue's state
+  static constexpr int kRingB = kBufs * kStageB;
+  static constexpr int kOutB = kThr / 64 * 32 * kPitch;
+  // the rings or what leaves, then 16 bytes a row for an epilogue's state
+  static constexpr int kLdsB = kSolo ? kRingB * kSolo : kRingB > kOutB ? kRingB : kOutB;
   static constexpr int kStateB = TM * 16;
-  static_assert(kLoadsA * kWaves * 1024 == kBytesA && kLoadsB * kWaves * 1024 == kBytesB && kOutB <= kLdsB, "");
+  static_assert(kLoadsA * kWaves * 1024 == kBytesA && kLoadsB * kWaves * 1024 == kBytesB, "");
+  static_assert(kSolo == 0 || (kWaves == 1 && kBm == 1 && 32 * kPitch <= kRingB && kThr >= TN * 4), "");
 };
 
 // An offset outside every buffer's range.
 constexpr uint32_t kOutside = 0x80000000u;
 
+// What a row's 16-byte chunks are exchanged by: the 16 lanes that LDS serves at a time read
+// one chunk of 16 rows, and 256 bytes hold 2 or 4 rows.
+template <int BK>
+__device__ __forceinline__ int mma_row_swz(int row) {
+  return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
 template <int W>
 __device__ __forceinline__ int mma_swz(int k) {
-  return W == 128 ? wg_swz(k) : ((k >> 1) & 1) << 1;
+  return W == 128 ? wg_swz(k) : W == 64 ? ((k >> 1) & 1) << 1 : 0;
 }
 
 // One lane's share of an operand's staging: the offsets it loads from and their
 // contraction indices within a stage.
-template <int LAYOUT, int W, int LOADS, int WAVES>
+template <int LAYOUT, int W, int BK, int LOADS, int WAVES>
 struct MmaLoader {
-  static constexpr int kPerPanel = W * 64 / 1024;  // loads of a panel of W columns (kLayoutK)
+  static constexpr int kPerPanel = W * BK * 2 / 1024;  // loads of a panel of W columns (kLayoutK)
   uint32_t off[LOADS];
   int kl[LOADS];
 
@@ -105,12 +119,13 @@ struct MmaLoader {
     for (int j = 0; j < LOADS; ++j) {
       const int idx = j * WAVES + wave;
       if constexpr (LAYOUT == kLayoutRow) {
-        const int row = idx * 16 + (lane >> 2), c = (lane & 3) ^ ((lane >> 4) & 3);
+        constexpr int kChunks = BK / 8;  // of a row
+        const int row = idx * (64 / kChunks) + lane / kChunks, c = (lane % kChunks) ^ mma_row_swz<BK>(row);
         kl[j] = c * 8;
         off[j] = i0 + row < end ? (uint32_t)row * (uint32_t)ld * 2u + c * 16u : kOutside;
       } else {
         const int in = idx % kPerPanel, panel = idx / kPerPanel;
-        const int k = W == 128 ? in * 4 + (lane >> 4) : in * 8 + (lane >> 3);
+        const int k = in * (512 / W) + lane / (W / 8);
         const int piece = ((lane >> 1) & (W / 16 - 1)) ^ mma_swz<W>(k);
         const int col = (PAIR ? 0 : panel * W) + piece * 16 + (lane & 1) * 8;
         kl[j] = k;
@@ -136,10 +151,12 @@ template <int N>
 __device__ __forceinline__ void mma_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// All of this wave's LDS reads have arrived; then the workgroup's barrier.
+// All of this wave's LDS reads have arrived; then the barrier of the waves that share
+// its stages.
+template <bool SHARED>
 __device__ __forceinline__ void mma_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
+  if (SHARED) __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
@@ -157,7 +174,7 @@ __device__ __forceinline__ void mma_tile(int t, int tiles_m, int tiles_n, int& t
 // The accumulators of one wave after all stages of its part.
 template <typename T, int LA, int LB, bool PAIR>
 struct MmaCore {
-  static constexpr int kWa = T::TM < 128 ? T::TM : 128, kWb = PAIR ? T::TN / 2 : 128;
+  static constexpr int kWa = T::TM < 128 ? T::TM : 128, kWb = PAIR ? T::TN / 2 : T::TN < 128 ? T::TN : 128;
   wg_acc acc[T::kBm][T::kBn];
   int wm, wn;  // first row of the wave in the tile, and number of its column strip
 
@@ -169,9 +186,10 @@ struct MmaCore {
   template <int LAYOUT, int W>
   static __device__ __forceinline__ int frag_at(int first, int lane) {
     if constexpr (LAYOUT == kLayoutRow)
-      return (first + (lane & 31)) * 64 + ((lane >> 5) ^ ((lane >> 2) & 3)) * 16;
+      return (first + (lane & 31)) * (T::kBk * 2) + ((lane >> 5) ^ mma_row_swz<T::kBk>(lane & 31)) * 16;
     const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), side = (lane >> 4) & 1;
-    return first / W * (W * 64) + k * (W * 2) + ((first % W / 16 + side) ^ mma_swz<W>(k)) * 32 + (lane & 3) * 8;
+    return first / W * (W * T::kBk * 2) + k * (W * 2) + ((first % W / 16 + side) ^ mma_swz<W>(k)) * 32 +
+           (lane & 3) * 8;
   }
   template <int LAYOUT, int W>
   static __device__ __forceinline__ bf16x8 frag(lds_char* stage, int at, int step) {
@@ -186,18 +204,25 @@ struct MmaCore {
   __device__ __forceinline__ void run(const MmaArgs& q, lds_char* lds, int m0, int n0, int split, F&& between) {
     static_assert(T::kBn == 2 || !PAIR, "");
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = T::kSolo ? 0 : all;
     wm = wave / T::kWavesN * T::WM;
     wn = wave % T::kWavesN;
-    const int first = split * q.per_split;
-    const int stages = min(q.per_split, q.segs * q.seg_stages - first);
+    int first = split * q.per_split;
+    int stages = min(q.per_split, q.segs * q.seg_stages - first);
+    if constexpr (T::kSolo > 0) {
+      const int from = stages * all / T::kSolo, to = stages * (all + 1) / T::kSolo;
+      first = from < to ? first + from : 0;
+      stages = to - from;
+      lds += all * T::kRingB;
+    }
+    constexpr bool kShared = T::kSolo == 0;
 
     // where the next stage to be loaded lies
     int seg = first / q.seg_stages, at = first % q.seg_stages, left = stages;
     const char *pa, *pb, *pb2;
     int64_t step_a, step_b, step_b2, plane_a, plane_b, plane_b2;  // bytes
-    MmaLoader<LA, kWa, T::kLoadsA, T::kWaves> la;
-    MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> lb;
+    MmaLoader<LA, kWa, T::kBk, T::kLoadsA, T::kWaves> la;
+    MmaLoader<LB, kWb, T::kBk, T::kLoadsB, T::kWaves> lb;
     // whether load j of B is of a pair's second panel
     auto second = [&](int j) { return PAIR && (j * T::kWaves + wave) * 2 >= T::kLoadsB * T::kWaves; };
     auto open = [&] {
@@ -214,7 +239,7 @@ struct MmaCore {
       la.template init<false>(m0, q.M, s.lda, wave, lane);
       lb.template init<PAIR>(n0, q.N, s.ldb, wave, lane);
       if (PAIR && s.ldb2 != s.ldb) {
-        MmaLoader<LB, kWb, T::kLoadsB, T::kWaves> l2;
+        MmaLoader<LB, kWb, T::kBk, T::kLoadsB, T::kWaves> l2;
         l2.template init<PAIR>(n0, q.N, s.ldb2, wave, lane);
 #pragma unroll
         for (int j = 0; j < T::kLoadsB; ++j)
@@ -272,10 +297,10 @@ struct MmaCore {
     auto read_one = [&](lds_char* stage, int step, int n) {
       if (n < T::PB * T::kBn) {
         const int p = n / T::kBn, j = n % T::kBn;
-        fb[step][p][j] = frag<LB, kWb>(stage + T::PA * T::kBytesA + p * T::kBytesB, ob[j], step);
+        fb[step & 1][p][j] = frag<LB, kWb>(stage + T::PA * T::kBytesA + p * T::kBytesB, ob[j], step);
       } else {
         const int m = n - T::PB * T::kBn, p = m / T::kBm, i = m % T::kBm;
-        fa[step][p][i] = frag<LA, kWa>(stage + p * T::kBytesA, oa[i], step);
+        fa[step & 1][p][i] = frag<LA, kWa>(stage + p * T::kBytesA, oa[i], step);
       }
     };
     // The products of a step, pairs of planes by size, the smallest first.  beside(n)
@@ -295,7 +320,8 @@ struct MmaCore {
           for (int i = 0; i < T::kBm; ++i)
 #pragma unroll
             for (int j = 0; j < T::kBn; ++j) {
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step][r][j], fa[step][p][i], acc[i][j], 0, 0, 0);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step & 1][r][j], fa[step & 1][p][i], acc[i][j], 0, 0,
+                                                                  0);
               beside(n++);
               __builtin_amdgcn_sched_barrier(0);
             }
@@ -314,7 +340,7 @@ struct MmaCore {
     for (int b = 0; b < T::kBufs - 1; ++b) issue(lds + b * T::kStageB);
     between();
     mma_wait<(T::kBufs - 2) * T::kLoads>();
-    mma_barrier();
+    mma_barrier<kShared>();
     int cur = 0;
 #pragma unroll
     for (int k = 0; k < kFrags; ++k) read_one(lds, 0, k);
@@ -323,10 +349,11 @@ struct MmaCore {
     for (int s = 0; s < stages; ++s) {
       lds_char* now = lds + cur;
       cur = cur == (T::kBufs - 1) * T::kStageB ? 0 : cur + T::kStageB;
-      multiply(0, [&](int n) { read_beside(now, 1, n); });
+#pragma unroll
+      for (int t = 0; t < T::kSteps - 1; ++t) multiply(t, [&](int n) { read_beside(now, t + 1, n); });
       mma_wait<(T::kBufs - 2) * T::kLoads>();
-      mma_barrier();
-      multiply(1, [&](int n) {
+      mma_barrier<kShared>();
+      multiply(T::kSteps - 1, [&](int n) {
         read_beside(lds + cur, 0, n);
 #pragma unroll
         for (int k = 0; k < T::kLoads; ++k)
@@ -335,9 +362,44 @@ struct MmaCore {
       advance();
     }
     mma_wait<0>();
-    mma_barrier();
+    mma_barrier<kShared>();
   }
 };
+
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+// Blocks j of a wave's 32 rows to LDS, [row][column].
+template <typename T>
+__device__ __forceinline__ void mma_rows_out(const wg_acc (&acc)[T::kBn], lds_char* own, int lane) {
+#pragma unroll
+  for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      *(lds_f32x4*)(own + (lane & 31) * T::kPitch + (j * 32 + v * 8 + (lane >> 5) * 4) * 4) =
+          f32x4{acc[j][4 * v], acc[j][4 * v + 1], acc[j][4 * v + 2], acc[j][4 * v + 3]};
+}
+__device__ __forceinline__ void lds_add8(float (&w)[8], lds_char* p) {
+  const f32x4 lo = *(lds_f32x4*)p, hi = *(lds_f32x4*)(p + 16);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] += lo[k], w[4 + k] += hi[k];
+}
+// Units to the part of C that this split forms.
+template <bool PAIR>
+__device__ __forceinline__ void mma_part(const MmaArgs& q, int split, int row, int col, const float (&x)[8],
+                                         const float (&y)[8]) {
+  auto put = [&](const float (&w)[8], float* p) {
+    f32x4 lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
+    if (q.part_add) {
+      lo += *reinterpret_cast<f32x4*>(p);
+      hi += *reinterpret_cast<f32x4*>(p + 4);
+    }
+    *reinterpret_cast<f32x4*>(p) = lo;
+    *reinterpret_cast<f32x4*>(p + 4) = hi;
+  };
+  float* p = q.part + ((int64_t)split * q.M + row) * q.ld_part + col;
+  put(x, p);
+  if (PAIR) put(y, p + q.ld_part / 2);
+}
 
 // The wave's results in units of 8 columns, written to part or given to e(row, its
 // state, column, first values, second values of a pair).  The units of 32 rows are
@@ -348,62 +410,51 @@ __device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, ld
                                           int n0, int split, const E& e) {
   constexpr bool PAIR = E::kPair;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-  lds_char* own = lds + wave * 32 * T::kPitch;
   constexpr int kUnits = PAIR ? T::WN / 16 : T::WN / 8;  // of a row
-  constexpr int kTurns = 32 * kUnits / 64;
-  const int col = n0 + (PAIR ? core.wn * (T::WN / 2) : core.wn * T::WN) + lane % kUnits * 8;
+  if constexpr (T::kSolo > 0) {
+    mma_rows_out<T>(core.acc[0], lds + wave * T::kRingB, lane);
+    __syncthreads();
+    const int r = threadIdx.x / kUnits, c = threadIdx.x % kUnits * 8, row = m0 + r, col = n0 + c;
+    if (r >= 32 || row >= q.M || col >= q.N) return;
+    float x[1][8] = {}, y[1][8] = {};
+    f32x4 st[1];
+#pragma unroll
+    for (int w = 0; w < T::kSolo; ++w) {
+      lds_add8(x[0], lds + w * T::kRingB + r * T::kPitch + c * 4);
+      if (PAIR) lds_add8(y[0], lds + w * T::kRingB + r * T::kPitch + (T::WN / 2 + c) * 4);
+    }
+    if (E::kState) st[0] = *(lds_f32x4*)(state + r * 16);
+    if (q.part) mma_part<PAIR>(q, split, row, col, x[0], y[0]);
+    else e.template units<1>(row, 0, q.M, st, col, x, y);
+    return;
+  } else {
+    lds_char* own = lds + wave * 32 * T::kPitch;
+    constexpr int kTurns = 32 * kUnits / 64;
+    const int col = n0 + (PAIR ? core.wn * (T::WN / 2) : core.wn * T::WN) + lane % kUnits * 8;
 #pragma unroll 1
-  for (int i = 0; i < T::kBm; ++i) {
+    for (int i = 0; i < T::kBm; ++i) {
 #pragma unroll
-    for (int b = 0; b < T::kBm; ++b) {
-      if (b != i) continue;
-#pragma unroll
-      for (int j = 0; j < T::kBn; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const wg_acc& c = core.acc[b][j];
-          *(lds_f32x4*)(own + (lane & 31) * T::kPitch + (j * 32 + v * 8 + (lane >> 5) * 4) * 4) =
-              f32x4{c[4 * v], c[4 * v + 1], c[4 * v + 2], c[4 * v + 3]};
-        }
-    }
-    wave_lds_order();
-    float x[kTurns][8], y[kTurns][8];
-    f32x4 st[kTurns];
-#pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-      const int r = t * (64 / kUnits) + lane / kUnits;
-      auto get = [&](float (&w)[8], int at) {
-        const f32x4 lo = *(lds_f32x4*)(own + r * T::kPitch + at * 4);
-        const f32x4 hi = *(lds_f32x4*)(own + r * T::kPitch + at * 4 + 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = lo[k], w[4 + k] = hi[k];
-      };
-      get(x[t], lane % kUnits * 8);
-      if (PAIR) get(y[t], T::WN / 2 + lane % kUnits * 8);
-      if (E::kState) st[t] = *(lds_f32x4*)(state + (core.wm + i * 32 + r) * 16);
-    }
-    wave_lds_order();
-    const int row = m0 + core.wm + i * 32 + lane / kUnits;
-    if (q.part) {
+      for (int b = 0; b < T::kBm; ++b)
+        if (b == i) mma_rows_out<T>(core.acc[b], own, lane);
+      wave_lds_order();
+      float x[kTurns][8] = {}, y[kTurns][8] = {};
+      f32x4 st[kTurns];
 #pragma unroll
       for (int t = 0; t < kTurns; ++t) {
-        if (row + t * (64 / kUnits) >= q.M || col >= q.N) continue;
-        auto put = [&](const float (&w)[8], float* p) {
-          f32x4 lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
-          if (q.part_add) {
-            lo += *reinterpret_cast<f32x4*>(p);
-            hi += *reinterpret_cast<f32x4*>(p + 4);
-          }
-          *reinterpret_cast<f32x4*>(p) = lo;
-          *reinterpret_cast<f32x4*>(p + 4) = hi;
-        };
-        float* p = q.part + ((int64_t)split * q.M + row + t * (64 / kUnits)) * q.ld_part + col;
-        put(x[t], p);
-        if (PAIR) put(y[t], p + q.ld_part / 2);
+        const int r = t * (64 / kUnits) + lane / kUnits;
+        lds_add8(x[t], own + r * T::kPitch + lane % kUnits * 32);
+        if (PAIR) lds_add8(y[t], own + r * T::kPitch + T::WN * 2 + lane % kUnits * 32);
+        if (E::kState) st[t] = *(lds_f32x4*)(state + (core.wm + i * 32 + r) * 16);
       }
-    } else {
-      e.template units<kTurns>(row, 64 / kUnits, q.M, st, col, x, y);
+      wave_lds_order();
+      const int row = m0 + core.wm + i * 32 + lane / kUnits;
+      if (q.part) {
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+          if (row + t * (64 / kUnits) < q.M && col < q.N) mma_part<PAIR>(q, split, row + t * (64 / kUnits), col, x[t], y[t]);
+      } else {
+        e.template units<kTurns>(row, 64 / kUnits, q.M, st, col, x, y);
+      }
     }
   }
 }
@@ -439,14 +490,13 @@ __global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
   // what the epilogue needs of each row, loaded behind the first stages
   auto states = [&] {
     if constexpr (E::kState) {
-      typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
       for (int r = threadIdx.x; r < T::TM; r += T::kThr)
         *(lds_f32x4*)(state + r * 16) = m0 + r < q.M ? e.state(m0 + r) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
   MmaCore<T, LA, LB, E::kPair> core;
   core.run(q, lds, m0, n0, split, states);
-  if constexpr (E::kWhole) {
+  if constexpr (E::kWhole && T::kSolo == 0) {
     if (!q.part) {
       e.template whole<T>(q, core, lds, m0, n0, tn);
       return;
