@@ -124,10 +124,14 @@ struct ActShape {
 // Calls f(row, unit, in) for the unit of the lane; `in` is false past the tensor
 // (the lanes of a group are in or out together).
 template <typename F>
-__device__ __forceinline__ void act_units(const ActShape& h, F&& f) {
-  const uint32_t n = blockIdx.x * kThreads + threadIdx.x;
+__device__ __forceinline__ void act_units_of(const ActShape& h, uint32_t block, F&& f) {
+  const uint32_t n = block * kThreads + threadIdx.x;
   const uint32_t t = __umulhi(n, h.magic), row = (t + ((n - t) >> 1)) >> h.shift;
   f(h.row0 + row, (int)(n - row * h.upr), n < h.units);
+}
+template <typename F>
+__device__ __forceinline__ void act_units(const ActShape& h, F&& f) {
+  act_units_of(h, blockIdx.x, f);
 }
 
 // (at element alignment)

@@ -50,10 +50,8 @@ inline shampoo_status check_apart(Handle* h, const Span& a, const char* what_a, 
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// The launches of a pass over a rows x cols tensor in `upr` units of 8 columns a row
-// (at least 2): f(shape, grid) for each.
-template <typename F>
-shampoo_status unit_launches(Handle* h, int cls, int64_t rows, int64_t cols, int64_t upr, hipStream_t s, F&& f) {
+// A tensor of `cols` columns in `upr` units of 8 columns a row (at least 2).
+inline ActShape unit_shape(int64_t cols, int64_t upr) {
   ActShape sh{};
   sh.cols = (int)cols;
   sh.upr = (int)upr;
@@ -61,6 +59,13 @@ shampoo_status unit_launches(Handle* h, int cls, int64_t rows, int64_t cols, int
   while ((int64_t(1) << bits) < sh.upr) ++bits;
   sh.magic = (uint32_t)((((uint64_t(1) << bits) - (uint64_t)sh.upr) << 32) / (uint64_t)sh.upr + 1);
   sh.shift = (uint32_t)bits - 1;
+  return sh;
+}
+
+// The launches of a pass over a rows x cols tensor: f(shape, grid) for each.
+template <typename F>
+shampoo_status unit_launches(Handle* h, int cls, int64_t rows, int64_t cols, int64_t upr, hipStream_t s, F&& f) {
+  ActShape sh = unit_shape(cols, upr);
   const int64_t most = INT32_MAX / sh.upr;
   for (sh.row0 = 0; sh.row0 < rows; sh.row0 += most) {
     sh.units = std::min(most, rows - sh.row0) * sh.upr;

@@ -84,22 +84,48 @@ struct Planes16 {
   int64_t ld, plane;
 };
 
-// X as the products read it, copied to `room` first where it has to be.
-shampoo_status packed(Handle* h, int cls, const void* X, int dtype, int64_t rows, int64_t cols, int64_t ld, bool pack,
-                      const PackPlan& p, void* room, hipStream_t s, Planes16* out) {
-  if (!pack) {
-    *out = {static_cast<const uint16_t*>(X), ld, 0};
+// Collects the matrices of a call that have to be copied, and launches the copies
+// together (at most 2^31 units of 8 columns a launch).
+struct Packer {
+  Handle* h;
+  int cls, dtype;
+  hipStream_t s;
+  PackArgs q{};
+  uint32_t blocks = 0;
+
+  shampoo_status flush() {
+    if (q.jobs == 0) return SHAMPOO_OK;
+    const dim3 grid(blocks);
+    STATUS_TRY(launch(h, cls, s, [&] {
+      with_type(dtype, [&](auto* type) {
+        using S = std::remove_pointer_t<decltype(type)>;
+        hipLaunchKernelGGL(pack_kernel<S>, grid, dim3(kThreads), 0, s, q);
+      });
+    }));
+    q.jobs = 0;
+    blocks = 0;
     return SHAMPOO_OK;
   }
-  *out = {static_cast<const uint16_t*>(room), p.ld, p.plane};
-  return unit_launches(h, cls, rows, cols, p.ld / 8, s, [&](const ActShape& sh, dim3 grid) {
-    with_type(dtype, [&](auto* type) {
-      using S = std::remove_pointer_t<decltype(type)>;
-      hipLaunchKernelGGL(pack_kernel<S>, grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(X), ld,
-                         static_cast<uint16_t*>(room), p.plane);
-    });
-  });
-}
+  // X (rows x cols) as the products read it: itself, or its planes in `room`.
+  shampoo_status take(const void* X, int64_t rows, int64_t cols, int64_t ld, bool pack, const PackPlan& p, void* room,
+                      Planes16* out) {
+    if (!pack) {
+      *out = {static_cast<const uint16_t*>(X), ld, 0};
+      return SHAMPOO_OK;
+    }
+    *out = {static_cast<const uint16_t*>(room), p.ld, p.plane};
+    ActShape sh = unit_shape(cols, p.ld / 8);
+    const int64_t most = (INT32_MAX / 2) / sh.upr;
+    for (sh.row0 = 0; sh.row0 < rows; sh.row0 += most) {
+      sh.units = std::min(most, rows - sh.row0) * sh.upr;
+      const int64_t n = cdiv64(sh.units, kThreads);
+      if (q.jobs == kMostPacks || blocks + n > (1 << 23)) STATUS_TRY(flush());
+      q.job[q.jobs++] = {sh, X, ld, static_cast<uint16_t*>(room), p.plane, blocks};
+      blocks += (uint32_t)n;
+    }
+    return SHAMPOO_OK;
+  }
+};
 
 // One more product of the sum.
 void add_seg(MmaArgs& q, const Planes16& a, const Planes16& b, const Planes16* b2 = nullptr) {
@@ -255,14 +281,16 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
     const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
     Planes16 x, w;
-    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, s, &x));
+    Packer packer{h, kCls, dtype, s};
+    STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
     auto* stat = reinterpret_cast<f32x2p*>(ws + p.at_stat);
     auto* z_target = reinterpret_cast<float*>(ws + p.at_target);
     int64_t entry0 = 0;
     for (int64_t i = 0; i < p.pieces; ++i) {
       const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
       const MmaPlan& m = p.mma[i == p.pieces - 1];
-      STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
+      STATUS_TRY(packer.take(typed(W, v0 * ld_w, dtype), n, dim, ld_w, pack_w, p.w, ws + p.at_w, &w));
+      STATUS_TRY(packer.flush());
       MmaArgs q{};
       add_seg(q, x, w);
       use_plan(q, m, rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
@@ -327,7 +355,8 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
     const VocabGradPlan p = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, pack_x, pack_w);
     Planes16 x, w;
-    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, s, &x));
+    Packer packer{h, kCls, dtype, s};
+    STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
     uint16_t* dz = reinterpret_cast<uint16_t*>(ws + p.at_dz);
     const Planes16 pz{dz, p.ld_dz, rows * p.ld_dz};
     const int nx = p.x.planes;
@@ -336,7 +365,8 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     for (int64_t i = 0; i < p.pieces; ++i) {
       const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
       const bool last = i == p.pieces - 1;
-      STATUS_TRY(packed(h, kCls, typed(W, v0 * ld_w, dtype), dtype, n, dim, ld_w, pack_w, p.w, ws + p.at_w, s, &w));
+      STATUS_TRY(packer.take(typed(W, v0 * ld_w, dtype), n, dim, ld_w, pack_w, p.w, ws + p.at_w, &w));
+      STATUS_TRY(packer.flush());
       MmaArgs q{};
       add_seg(q, x, w);
       use_plan(q, p.z[last], rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
@@ -401,9 +431,11 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
     Planes16 x, wg, wu;
-    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, px, p.x, ws + p.at_x, s, &x));
-    STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
-    STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
+    Packer packer{h, kCls, dtype, s};
+    STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));
+    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, &wg));
+    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, &wu));
+    STATUS_TRY(packer.flush());
     MmaArgs q{};
     add_seg(q, x, wg, &wu);
     use_plan(q, p.mma, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
@@ -473,9 +505,11 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
     Planes16 x, wg, wu;
-    STATUS_TRY(packed(h, kCls, X, dtype, rows, dim, ld_x, px, p.x, ws + p.at_x, s, &x));
-    STATUS_TRY(packed(h, kCls, Wg, dtype, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, s, &wg));
-    STATUS_TRY(packed(h, kCls, Wu, dtype, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, s, &wu));
+    Packer packer{h, kCls, dtype, s};
+    STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));
+    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, &wg));
+    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, &wu));
+    STATUS_TRY(packer.flush());
     const int nx = p.x.planes;
     uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.at_d);
     const Planes16 dg{d, 2 * p.ld_d, rows * 2 * p.ld_d}, du{d + p.ld_d, dg.ld, dg.plane};

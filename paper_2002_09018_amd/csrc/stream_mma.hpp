@@ -291,6 +291,17 @@ struct MmaCore {
       for (int j = 0; j < T::kBn; ++j)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    // Products of planes that are not both the first are sums of their own: they are 2^-8
+    // of the others, so that these are rounded at the size of the sum once in 16 indices,
+    // not six times.
+    constexpr bool kTwo = T::PA + T::PB > 2;
+    wg_acc small[kTwo ? T::kBm : 1][kTwo ? T::kBn : 1];
+    if constexpr (kTwo) {
+#pragma unroll
+      for (int i = 0; i < T::kBm; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kBn; ++j) small[i][j] = acc[i][j];
+    }
 
     bf16x8 fa[2][T::PA][T::kBm], fb[2][T::PB][T::kBn];
     constexpr int kFrags = T::PA * T::kBm + T::PB * T::kBn;
@@ -320,8 +331,8 @@ struct MmaCore {
           for (int i = 0; i < T::kBm; ++i)
 #pragma unroll
             for (int j = 0; j < T::kBn; ++j) {
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step & 1][r][j], fa[step & 1][p][i], acc[i][j], 0, 0,
-                                                                  0);
+              wg_acc& c = kTwo && s > 0 ? small[kTwo ? i : 0][kTwo ? j : 0] : acc[i][j];
+              c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[step & 1][r][j], fa[step & 1][p][i], c, 0, 0, 0);
               beside(n++);
               __builtin_amdgcn_sched_barrier(0);
             }
@@ -360,6 +371,14 @@ struct MmaCore {
           if (k * kProducts / T::kLoads == n) load(now, k);
       });
       advance();
+    }
+    if constexpr (kTwo) {
+#pragma unroll
+      for (int i = 0; i < T::kBm; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kBn; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[i][j][v] += small[i][j][v];
     }
     mma_wait<0>();
     mma_barrier<kShared>();
@@ -548,26 +567,43 @@ __device__ __forceinline__ void planes_of(const float (&x)[8], u32x4u (&p)[3]) {
   }
 }
 
-// A matrix into bf16 planes with rows of ldp elements, zeros from `cols` on.
-// Bound by memory: one read, one write (three of half the size for fp32).
+// Matrices into bf16 planes with rows of 8 upr elements, zeros from `cols` on; one launch
+// for those of a call.  Bound by memory: one read, one write (three of half the size
+// for fp32).
+struct PackJob {
+  ActShape h;
+  const void* X;
+  int64_t ld;
+  uint16_t* out;
+  int64_t plane;
+  uint32_t first;  // workgroup
+};
+constexpr int kMostPacks = 3;
+struct PackArgs {
+  PackJob job[kMostPacks];
+  int jobs;
+};
+
 template <typename S>
-__global__ __launch_bounds__(kThreads) void pack_kernel(ActShape h, const S* __restrict__ X, int64_t ld,
-                                                       uint16_t* __restrict__ out, int64_t plane) {
-  act_units(h, [&](int64_t row, int unit, bool in) {
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs q) {
+  int i = 0;
+  while (i + 1 < q.jobs && blockIdx.x >= q.job[i + 1].first) ++i;
+  const PackJob& j = q.job[i];
+  act_units_of(j.h, blockIdx.x - j.first, [&](int64_t row, int unit, bool in) {
     if (!in) return;
     ActVec<S> x;
-    x.load(X + row * ld + unit * 8, h.cols - unit * 8);
-    uint16_t* d = out + (row * h.upr + unit) * 8;
+    x.load(static_cast<const S*>(j.X) + row * j.ld + unit * 8, j.h.cols - unit * 8);
+    uint16_t* d = j.out + (row * j.h.upr + unit) * 8;
     if constexpr (sizeof(S) == 2) {
       gstore<u32x4u>(d, x.raw[0]);
     } else {
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = x.at(i);
+      for (int k = 0; k < 8; ++k) v[k] = x.at(k);
       u32x4u p[3];
       planes_of(v, p);
 #pragma unroll
-      for (int t = 0; t < 3; ++t) gstore<u32x4u>(d + t * plane, p[t]);
+      for (int t = 0; t < 3; ++t) gstore<u32x4u>(d + t * j.plane, p[t]);
     }
   });
 }
