@@ -161,7 +161,6 @@ shampoo_status mma_launch(Handle* h, int cls, const MmaArgs& q, const E& e, hipS
     asked.fetch_or(bit, std::memory_order_relaxed);
   }
   const int64_t groups = (int64_t)q.tiles_m * q.tiles_n * q.splits;
-  if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "a product of %d x %d", q.M, q.N);
   return launch(h, cls, s, [&] { hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(T::kThr), kLds, s, q, e); });
 }
 
@@ -217,6 +216,15 @@ shampoo_status scaled(Handle* h, int cls, void* C, int dtype, int64_t rows, int6
                          cols, ld, beta);
     });
   });
+}
+
+// Products that a call would need in more tiles than a launch holds are refused before
+// anything is enqueued.
+shampoo_status check_tiles(Handle* h, std::initializer_list<MmaPlan> plans) {
+  for (const MmaPlan& p : plans)
+    if (!fits(p))
+      return fail(h, SHAMPOO_EUNSUPPORTED, "a product of %lld x %lld tiles", (long long)p.tiles_m, (long long)p.tiles_n);
+  return SHAMPOO_OK;
 }
 
 const char* typed(const void* p, int64_t elements, int dtype) {
@@ -280,6 +288,9 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     constexpr int kCls = SHAMPOO_KCLASS_VOCAB;
     const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
     const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
+    STATUS_TRY(check_tiles(h, {p.mma[0], p.mma[1]}));
+    if (rows * cdiv64(p.piece, kStatCols) / (kThreads / 64) >= kMostTiles)
+      return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
     Planes16 x, w;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
@@ -298,7 +309,6 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
       STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, p.x.planes, m.shape, q, e, s)));
       if (q.part) {
         const int64_t groups = cdiv64(rows * cdiv64(n, kStatCols), kThreads / 64);
-        if (groups > INT32_MAX / 512) return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
         STATUS_TRY(launch(h, kCls, s, [&] {
           hipLaunchKernelGGL(logit_stat_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, q, e);
         }));
@@ -354,6 +364,7 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     char* ws = static_cast<char*>(workspace);
     const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
     const VocabGradPlan p = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, pack_x, pack_w);
+    STATUS_TRY(check_tiles(h, {p.z[0], p.z[1], p.dx[0], p.dx[1], p.dw[0], p.dw[1]}));
     Planes16 x, w;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
@@ -430,6 +441,7 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     const bool px = !as_it_lies(X, ld_x, dim, dtype), pg = !as_it_lies(Wg, ld_wg, width, dtype);
     const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
+    STATUS_TRY(check_tiles(h, {p.mma}));
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));
@@ -504,6 +516,7 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     const bool pg = (!G || dX) && !as_it_lies(Wg, ld_wg, width, dtype);
     const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
+    STATUS_TRY(check_tiles(h, {p.gu, p.dx, p.dw}));
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));

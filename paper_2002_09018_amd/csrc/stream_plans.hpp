@@ -2,15 +2,14 @@
 // work: plain host arithmetic on sizes and types.
 #pragma once
 
-#ifdef SWEEP
-#include <stdio.h>
-#include <stdlib.h>
-#endif
 #include "layer_plans.hpp"
 
 namespace shp {
 
 enum { kShapeSolo = 0, kShapeFew = 1, kShapeMid = 2, kShapeBig = 3 };
+
+// Shapes of a product: tiles of 32 rows whose waves share the contraction (Solo), of 32
+// rows (Few; small tiles of a weight gradient), of 128 x 128, and larger ones.
 
 // How a product is cut: tiles of C, and parts of the contraction.
 struct MmaPlan {
@@ -27,29 +26,37 @@ struct MmaCost {
   double alone, stage[4], start;
   int bk;  // contraction indices of a stage
 };
-// Measured for one plane each (bf16), 3 and 1, 3 and 3 (fp32).  Per compute unit the
-// large tiles reach 5.2 TFLOP/s (one plane), 4.5 and 4.7, where the chip lowers its clock;
-// 8192^3 of the library in bf16 5.1.
-constexpr MmaCost kCost11[] = {{32, 64, 1, 0.09, {0.145}, 4, 32},
-                               {32, 128, 4, 0.28, {0.30, 0.38, 0.49, 0.62}, 4, 32},
-                               {128, 128, 2, 0.50, {0.55, 0.95}, 5, 64},
-                               {256, 256, 1, 1.10, {1.40}, 9, 64}};
-constexpr MmaCost kCost31[] = {{32, 64, 1, 0.3, {0.3}, 5, 32},
-                               {32, 128, 2, 0.40, {0.45, 0.70}, 5, 32},
-                               {128, 128, 1, 0.55, {0.72}, 6, 32},
-                               {256, 128, 1, 1.03, {1.45}, 9, 32}};
-constexpr MmaCost kCost33[] = {{32, 64, 1, 0.24, {0.46}, 5, 32},
-                               {32, 128, 2, 0.70, {0.80, 1.17}, 5, 32},
-                               {128, 128, 1, 0.86, {1.33}, 6, 32},
-                               {256, 128, 1, 1.55, {2.34}, 10, 32}};
-
+// By shape, for operands of one plane (bf16) and of three (fp32).  Measured: at full
+// load a compute unit reaches 5.1 TFLOP/s with the largest tiles of one plane and
+// 4.7 with those of three (six products), 4.0 and 4.7 with 128 x 128; a library product
+// of 8192^3 in bf16 5.1.
+constexpr MmaCost kCost1[] = {{32, 64, 1, 0.09, {0.145}, 4, 32},
+                              {32, 128, 4, 0.28, {0.30, 0.38, 0.49, 0.62}, 4, 32},
+                              {128, 128, 2, 0.58, {0.64, 1.05}, 5, 64},
+                              {256, 256, 1, 1.15, {1.65}, 10, 64}};
+constexpr MmaCost kCost3[] = {{32, 64, 1, 0.24, {0.46}, 5, 32},
+                              {32, 128, 2, 0.70, {0.80, 1.17}, 5, 32},
+                              {128, 128, 1, 0.86, {1.33}, 6, 32},
+                              {256, 128, 1, 1.55, {2.34}, 10, 32}};
 // Weight gradients, whose contraction runs over rows: small tiles take the place of those
-// for few rows, for few rows mean short sums there, and many tiles at once keep the stores
-// flowing.
-constexpr MmaCost kBigWeight11 = {256, 256, 1, 0.57, {0.75}, 9, 32};
-constexpr MmaCost kThin11 = {64, 64, 4, 0.30, {0.30, 0.32, 0.36, 0.45}, 4, 32};
-constexpr MmaCost kThin31 = {64, 64, 4, 0.35, {0.40, 0.45, 0.60, 0.80}, 4, 32};
-constexpr MmaCost kThin33 = {64, 64, 3, 0.50, {0.60, 0.80, 1.10}, 4, 32};
+// for few rows (few rows are short sums there, and many tiles at once keep the stores
+// flowing); for one plane, one and three (three products), three.
+constexpr MmaCost kWeight1[] = {{},
+                                {64, 64, 4, 0.30, {0.30, 0.32, 0.36, 0.45}, 4, 32},
+                                {128, 128, 2, 0.58, {0.64, 1.05}, 5, 64},
+                                {256, 256, 1, 0.57, {0.83}, 9, 32}};
+constexpr MmaCost kWeight31[] = {{},
+                                 {64, 64, 4, 0.35, {0.40, 0.45, 0.60, 0.80}, 4, 32},
+                                 {128, 128, 1, 0.55, {0.72}, 6, 32},
+                                 {256, 128, 1, 1.03, {1.45}, 9, 32}};
+constexpr MmaCost kWeight3[] = {{},
+                                {64, 64, 3, 0.50, {0.60, 0.80, 1.10}, 4, 32},
+                                {128, 128, 1, 0.86, {1.33}, 6, 32},
+                                {256, 128, 1, 1.55, {2.34}, 10, 32}};
+inline const MmaCost* mma_cost(int planes) { return planes == 1 ? kCost1 : kCost3; }
+inline const MmaCost* weight_cost(int x_planes, int d_planes) {
+  return x_planes == 3 ? kWeight3 : d_planes == 3 ? kWeight31 : kWeight1;
+}
 
 // Time of `groups` workgroups of `per` stages: full rounds of the chip, then the rest.
 inline double mma_us(const MmaCost& t, int64_t groups, int64_t per) {
@@ -59,33 +66,19 @@ inline double mma_us(const MmaCost& t, int64_t groups, int64_t per) {
   return us;
 }
 
-// The cheapest tile and number of parts by estimated time, for operands of pa and pb
-// planes.  Parts cost their way to memory and back (more where the last-level cache
-// does not hold them) and the launch that adds them.
-inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, int pa, int pb, int segs, bool pair, int least_shape,
-                        int most_splits, bool always_part, bool weight = false) {
-  const MmaCost* cost = pa + pb == 2 ? kCost11 : pa + pb == 4 ? kCost31 : kCost33;
+// The cheapest tile and number of parts (at most most_splits) by estimated time.  Parts cost
+// their way to memory and back (more where the last-level cache does not hold them) and
+// the launch that adds them.  `segs` products of one contraction length are summed.
+inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, int segs, bool pair, int least_shape,
+                        int most_splits, bool always_part) {
   MmaPlan best;
   double best_us = 0;
   const int64_t ld = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
-  for (int i = least_shape; i < 4; ++i) {
-#ifdef SWEEP
-    int fs = -1, fw = -1;
-    if (getenv("MMA_FORCE")) sscanf(getenv("MMA_FORCE"), "%d,%d", &fs, &fw);
-    if (fs >= 0 && i != std::max(fs, least_shape)) continue;
-#endif
-    const MmaCost& t = !weight           ? cost[i]
-                       : i == kShapeFew   ? (pa + pb == 2 ? kThin11 : pa + pb == 4 ? kThin31 : kThin33)
-                       : i == kShapeBig && pa + pb == 2 ? kBigWeight11
-                                                        : cost[i];
+  for (int i = least_shape; i <= kShapeBig; ++i) {
+    const MmaCost& t = cost[i];
     const int64_t seg_stages = cdiv64(K, t.bk), stages = seg_stages * segs;
     const int64_t tm = cdiv64(M, t.m), tn = cdiv64(N, pair ? t.n / 2 : t.n);
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-#ifdef SWEEP
-      if (want > 1 && fw >= 0) break;
-      if (fw >= 0) want = std::min<int64_t>(fw, stages);
-      else
-#endif
       if (want > stages || want > most_splits || (want > 1 && want * tm * tn > 1024)) break;
       const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
       const size_t part = splits > 1 || always_part ? (size_t)(splits * M * ld) * sizeof(float) : 0;
@@ -99,6 +92,10 @@ inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, int pa, int pb, int seg
   }
   return best;
 }
+
+// Most tiles of a launch (it holds fewer than 2^32 threads, and their numbers 31 bits).
+constexpr int64_t kMostTiles = INT32_MAX / 512;
+inline bool fits(const MmaPlan& p) { return p.tiles_m * p.tiles_n * p.splits <= kMostTiles; }
 
 // A matrix copied into bf16 planes: one, or three of an fp32 one.
 struct PackPlan {
@@ -164,7 +161,7 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
       p.mma[1] = p.mma[0];
       break;
     }
-    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, p.x.planes, p.x.planes, 1, false, kShapeFew, 64, false);
+    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, mma_cost(p.x.planes), 1, false, kShapeFew, 64, false);
     part = std::max(part, p.mma[i].part);
   }
   p.entries = (p.pieces - 1) * vocab_entries(p.mma[0], p.piece) + vocab_entries(p.mma[1], last);
@@ -213,10 +210,10 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
       p.dw[1] = p.dw[0];
       break;
     }
-    const int in = p.x.planes;
-    p.z[i] = mma_plan(rows, n, dim, in, in, 1, false, kShapeSolo, 64, false);
-    p.dx[i] = mma_plan(rows, dim, n, in, in, 1, false, kShapeSolo, i ? p.dx[0].splits : 64, p.pieces > 1);
-    p.dw[i] = mma_plan(n, dim, rows, p.planes, in, 1, false, kShapeFew, 64, false, true);
+    const MmaCost* cost = mma_cost(p.x.planes);
+    p.z[i] = mma_plan(rows, n, dim, cost, 1, false, kShapeSolo, 64, false);
+    p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, i ? p.dx[0].splits : 64, p.pieces > 1);
+    p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
     part = std::max({part, p.z[i].part, p.dw[i].part});
   }
   p.at_dx = r.take(p.dx[0].part);
@@ -239,7 +236,7 @@ inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, boo
   if (pack_x) p.at_x = r.take(p.x.bytes);
   if (pack_wg) p.at_wg = r.take(p.wg.bytes);
   if (pack_wu) p.at_wu = r.take(p.wu.bytes);
-  p.mma = mma_plan(rows, width, dim, p.x.planes, p.x.planes, 1, true, kShapeSolo, 64, false);
+  p.mma = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
   p.at_part = r.take(p.mma.part);
   p.bytes = r.at;
   return p;
@@ -266,10 +263,9 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   if (pack_wu) p.at_wu = r.take(p.wu.bytes);
   p.ld_d = cdiv64(width, 64) * 64;
   p.at_d = r.take((size_t)(rows * 2 * p.ld_d * p.planes) * 2);
-  const int in = p.x.planes;
-  p.gu = mma_plan(rows, width, dim, in, in, 1, true, kShapeSolo, 64, false);
-  p.dx = mma_plan(rows, dim, width, in, in, 2, false, kShapeSolo, 64, false);
-  p.dw = mma_plan(dim, 2 * p.ld_d, rows, in, p.planes, 1, false, kShapeFew, 64, false, true);
+  p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
+  p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false);
+  p.dw = mma_plan(dim, 2 * p.ld_d, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
   p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part}));
   p.bytes = r.at;
   return p;

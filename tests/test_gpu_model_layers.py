@@ -196,6 +196,26 @@ def test_vocab_pieces(env, n, d, v, dtype):
     check_vocab_grad(env, n, d, v, dt, env[0].float32, beta=1.0)
 
 
+# sizes that reach the remaining tiles, whole and in parts (test_stream_plans checks that all are
+# reached): rows, dim, vocab, type, gradient's type, whether the matrices are copied first
+VOCAB_MORE = [(6109, 3490, 72, "bfloat16", "bfloat16", True), (4951, 1163, 408, "float32", "float32", True),
+              (1004, 2479, 1397, "float32", "float32", True), (474, 2138, 14, "bfloat16", "float32", True),
+              (8005, 90, 114, "float32", "bfloat16", True), (524, 3188, 6586, "bfloat16", "bfloat16", True),
+              (1007, 2432, 8, "float32", "bfloat16", True), (3907, 2796, 13, "bfloat16", "bfloat16", True),
+              (2608, 241, 4626, "bfloat16", "float32", True), (843, 1928, 1991, "bfloat16", "float32", True),
+              (922, 196, 31249, "bfloat16", "float32", True), (5525, 80, 14027, "float32", "bfloat16", True),
+              (130, 3330, 23888, "bfloat16", "float32", True), (4870, 136, 17995, "bfloat16", "bfloat16", False),
+              (6903, 914, 15369, "bfloat16", "float32", True)]
+
+
+@pytest.mark.parametrize("n,d,v,dtype,g_dtype,copied", VOCAB_MORE)
+def test_vocab_tiles(env, n, d, v, dtype, g_dtype, copied):
+    say("vocab tiles", n, d, v, dtype, g_dtype, copied)
+    dt, gt, lay = dtype_of(env, dtype), dtype_of(env, g_dtype), (5, 3) if copied else (0, 0)
+    check_vocab(env, n, d, v, dt, *lay)
+    check_vocab_grad(env, n, d, v, dt, gt, *lay)
+
+
 def test_vocab_rows_of_their_own(env):
     """A NaN or an infinity in one row of X stays there; targets outside the vocabulary
     are no targets; a row whose target is far above the rest has log probability 0 to
@@ -381,6 +401,48 @@ def test_gated_ffn_grad(env, n, d, w, dtype, g_dtype):
                 check_ffn_grad(env, n, d, w, dtype_of(env, dtype), dtype_of(env, g_dtype), act, keep, pad, shift)
 
 
+# as VOCAB_MORE: rows, dim, width, type, gradient's type
+FFN_MORE = [(1, 1718, 1871, "float32", "float32"), (1, 3508, 1348, "bfloat16", "bfloat16"),
+            (7225, 3508, 20, "float32", "float32"), (942, 2340, 476, "bfloat16", "bfloat16"),
+            (1441, 2247, 731, "float32", "bfloat16"), (4932, 884, 2504, "bfloat16", "float32"),
+            (7880, 75, 269, "float32", "bfloat16"), (688, 3745, 3026, "bfloat16", "float32"),
+            (5349, 2491, 844, "bfloat16", "bfloat16"), (992, 723, 2295, "bfloat16", "float32"),
+            (7392, 845, 1327, "bfloat16", "float32")]
+
+
+@pytest.mark.parametrize("n,d,w,dtype,g_dtype", FFN_MORE)
+def test_gated_ffn_tiles(env, n, d, w, dtype, g_dtype):
+    say("ffn tiles", n, d, w, dtype, g_dtype)
+    dt, gt = dtype_of(env, dtype), dtype_of(env, g_dtype)
+    check_ffn(env, n, d, w, dt, "SILU")
+    check_ffn_grad(env, n, d, w, dt, gt, "GELU_TANH", False)
+
+
+def test_weights_of_different_strides(env):
+    """Wg and Wu in rows of different lengths, and one that is read as it lies beside one
+    that is copied: the bits of the plain call."""
+    torch, B, dev, h = env
+    for n, d, w in ((3, 64, 136), (40, 72, 1000), (700, 256, 520), (3000, 512, 2056)):
+        for dt in (torch.bfloat16, torch.float32):
+            say("ffn strides", n, d, w, dt)
+            X, g, u = normal(env, 1, n, d).to(dt), (normal(env, 2, d, w) / d).to(dt), (normal(env, 3, d, w) / d).to(dt)
+            ws = room(env, B.shampoo_gated_ffn_workspace_bytes(n, d, w, dt))
+            gws = room(env, B.shampoo_gated_ffn_grad_workspace_bytes(n, d, w, dt, dt))
+            dH = normal(env, 4, n, w).to(dt)
+            got = []
+            for (pg, sg), (pu, su) in (((0, 0), (0, 0)), ((8, 0), (24, 8)), ((3, 1), (16, 0)), ((64, 8), (1, 0))):
+                Wg, Wu = Sheet(env, d, w, dt, pg, sg, g).v, Sheet(env, d, w, dt, pu, su, u).v
+                out = [torch.empty(n, w, device=dev, dtype=dt) for _ in range(3)]
+                B.shampoo_gated_ffn(h, X, Wg, Wu, out[0], B.ACT_SILU, out[1], out[2], workspace=ws)
+                out += [torch.empty_like(X), torch.empty(d, w, device=dev, dtype=dt), torch.empty(d, w, device=dev, dtype=dt)]
+                B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, B.ACT_SILU, dX=out[3], dWg=out[4], dWu=out[5], workspace=gws)
+                got.append(out)
+            torch.cuda.synchronize()
+            for other in got[1:]:
+                for a, b in zip(got[0], other):
+                    assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype,g_dtype", [("bfloat16", "bfloat16"), ("float32", "float32")])
 def test_gated_ffn_grad_options(env, dtype, g_dtype):
     dt, gt = dtype_of(env, dtype), dtype_of(env, g_dtype)
@@ -495,7 +557,16 @@ def test_c_entry_refusals(env):
     refused(lambda: B.shampoo_gated_ffn(h, X, Wg, Wu, H, 9, workspace=fw), "activation")
     for rate in (-0.1, 1.5, float("nan")):
         refused(lambda: B.shampoo_dropout(h, X, dX, rate, 1), "rate")
+    # what overlaps is refused by the library and named by the binding
+    w = torch.zeros(24, 16, device=dev)
+    big = torch.zeros(8 * 8 + 16 * 8 - 1, device=dev)
+    for fn in (lambda: B.shampoo_vocab_logprobs_grad(h, X, w, t, lse, dW=w, g_logp=g, workspace=gw),
+               lambda: B.shampoo_gated_ffn(h, X, big[:128].view(16, 8), Wu, big[127:].view(8, 8), workspace=fw),
+               lambda: B.shampoo_dropout(h, big[:64].view(8, 8), big[1:65].view(8, 8), 0.5, 1)):
+        with pytest.raises(ValueError, match="overlap"):
+            fn()
     torch.cuda.synchronize()
+    assert bool((w == 0).all()) and bool((big == 0).all())
     assert bool((dX == 0).all()) and bool((H == 0).all()) and bool((lse == 3).all())
 
 
