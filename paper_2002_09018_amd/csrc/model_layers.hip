@@ -149,19 +149,28 @@ void use_plan(MmaArgs& q, const MmaPlan& p, int64_t M, int64_t N, int64_t K, int
   q.ld_part = p.ld_part;
 }
 
+// More LDS than a launch may take by default: asked for once per kernel and device.
+template <typename K>
+shampoo_status ask_lds(Handle* h, K k, int bytes, std::atomic<uint64_t>& asked) {
+  const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
+  if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
+    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    asked.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return SHAMPOO_OK;
+}
+
+int64_t groups_of(const MmaArgs& q) { return (int64_t)q.tiles_m * q.tiles_n * q.splits; }
+
 template <typename T, int LA, int LB, typename E>
 shampoo_status mma_launch(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_t s) {
   auto k = mma_kernel<T, LA, LB, E>;
   constexpr int kLds = T::kLdsB + (E::kState ? T::kStateB : 0);
-  // more LDS than a launch may take by default: asked for once per device
   static std::atomic<uint64_t> asked{0};
-  const uint64_t bit = h->device < 64 ? uint64_t(1) << h->device : 0;
-  if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
-    HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
-    asked.fetch_or(bit, std::memory_order_relaxed);
-  }
-  const int64_t groups = (int64_t)q.tiles_m * q.tiles_n * q.splits;
-  return launch(h, cls, s, [&] { hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(T::kThr), kLds, s, q, e); });
+  STATUS_TRY(ask_lds(h, k, kLds, asked));
+  return launch(h, cls, s, [&] {
+    hipLaunchKernelGGL(k, dim3((unsigned)groups_of(q)), dim3(T::kThr), kLds, s, q, e);
+  });
 }
 
 // The product of operands of PA and PB planes; what was cut is left in q.part.
@@ -192,6 +201,33 @@ shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_
   return launch(h, cls, s, [&] {
     hipLaunchKernelGGL(mma_join_kernel<E>, dim3(act_grid(units)), dim3(kThreads), 0, s, q, e);
   });
+}
+
+// dX and the weights' gradient in one launch, and what was cut of them in another.
+template <int LB, int P>
+shampoo_status two_products(Handle* h, int cls, const MmaArgs& x, const OutEpilogue& ex, const MmaArgs& w,
+                            const OutEpilogue& ew, hipStream_t s) {
+  using T = typename Shapes<P, P>::Mid;
+  auto k = mma_two_kernel<T, LB, OutEpilogue>;
+  static std::atomic<uint64_t> asked{0};
+  STATUS_TRY(ask_lds(h, k, T::kLdsB, asked));
+  const int first = (int)groups_of(x);
+  STATUS_TRY(launch(h, cls, s, [&] {
+    hipLaunchKernelGGL(k, dim3((unsigned)(first + groups_of(w))), dim3(T::kThr), T::kLdsB, s, x, ex, w, ew, first);
+  }));
+  if (!x.part || !w.part) {
+    if (x.part) return join(h, cls, x, ex, s);
+    return w.part ? join(h, cls, w, ew, s) : SHAMPOO_OK;
+  }
+  const unsigned nx = act_grid((int64_t)x.M * cdiv64(x.N, 8)), nw = act_grid((int64_t)w.M * cdiv64(w.N, 8));
+  return launch(h, cls, s, [&] {
+    hipLaunchKernelGGL(mma_join_two_kernel<OutEpilogue>, dim3(nx + nw), dim3(kThreads), 0, s, x, ex, w, ew, (int)nx);
+  });
+}
+template <int LB>
+shampoo_status two_products(Handle* h, int cls, int planes, const MmaArgs& x, const OutEpilogue& ex, const MmaArgs& w,
+                            const OutEpilogue& ew, hipStream_t s) {
+  return planes == 1 ? two_products<LB, 1>(h, cls, x, ex, w, ew, s) : two_products<LB, 3>(h, cls, x, ex, w, ew, s);
 }
 
 // A weight gradient X^T D or D^T X of D's terms: three where X has one plane and D's
@@ -384,23 +420,27 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
       const DlogitEpilogue e({targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes);
       STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.z[last].shape, q, e, s)));
       if (q.part) STATUS_TRY(join(h, kCls, q, e, s));
+      const OutEpilogue out(dW ? const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)) : nullptr, ld_dw, nullptr, 0, 0,
+                            (int)dim, (int)dim, g_dtype == SHAMPOO_BF16, beta);
+      const bool two = p.two && dX && dW;
+      MmaArgs qw{};
       if (dX) {
         // a bf16 dX takes the first term alone
+        const MmaPlan& m = two ? p.two_dx : p.dx[last];
         MmaArgs r{};
         add_seg(r, pz, w);
-        use_plan(r, p.dx[last], rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
+        use_plan(r, m, rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
         r.part_add = i > 0;
-        STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, p.dx[last].shape, r, out_x, s)));
+        if (!two) STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, m.shape, r, out_x, s)));
         if (i == 0) qx = r;
       }
       if (dW) {
-        MmaArgs r{};
-        add_seg(r, pz, x);
-        use_plan(r, p.dw[last], n, dim, rows, kLayoutK, kLayoutK, ws + p.at_part);
-        const OutEpilogue out(const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)), ld_dw, nullptr, 0, 0, (int)dim,
-                              (int)dim, g_dtype == SHAMPOO_BF16, beta);
-        STATUS_TRY(weight_product<true>(h, kCls, nx, p.planes, p.dw[last].shape, r, out, s));
+        const MmaPlan& m = two ? p.two_dw : p.dw[last];
+        add_seg(qw, pz, x);
+        use_plan(qw, m, n, dim, rows, kLayoutK, kLayoutK, ws + p.at_part);
+        if (!two) STATUS_TRY(weight_product<true>(h, kCls, nx, p.planes, m.shape, qw, out, s));
       }
+      if (two) return two_products<kLayoutK>(h, kCls, nx, qx, out_x, qw, out, s);
     }
     return dX && qx.part ? join(h, kCls, qx, out_x, s) : SHAMPOO_OK;
   });
@@ -545,22 +585,27 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
       }
     });
     STATUS_TRY(st);
+    const bool two = p.two && dX && dWg;
+    const OutEpilogue out_x(dX, ld_dx, nullptr, 0, 0, (int)dim, (int)dim, dtype == SHAMPOO_BF16, 0.f);
+    const OutEpilogue out_w(dWg, ld_dwg, dWu, ld_dwu, (int)p.ld_d, (int)width, (int)(2 * p.ld_d), g_dtype == SHAMPOO_BF16,
+                            beta);
+    MmaArgs qx{}, qw{};
     if (dX) {
-      MmaArgs q{};
-      add_seg(q, dg, wg);
-      add_seg(q, du, wu);
-      use_plan(q, p.dx, rows, dim, width, kLayoutRow, kLayoutRow, ws + p.at_part);
-      const OutEpilogue out(dX, ld_dx, nullptr, 0, 0, (int)dim, (int)dim, dtype == SHAMPOO_BF16, 0.f);
-      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.dx.shape, q, out, s)));
-      if (q.part) STATUS_TRY(join(h, kCls, q, out, s));
+      const MmaPlan& m = two ? p.two_dx : p.dx;
+      add_seg(qx, dg, wg);
+      add_seg(qx, du, wu);
+      use_plan(qx, m, rows, dim, width, kLayoutRow, kLayoutRow, ws + (two ? p.at_dx : p.at_part));
+      if (!two) {
+        STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, m.shape, qx, out_x, s)));
+        if (qx.part) STATUS_TRY(join(h, kCls, qx, out_x, s));
+      }
     }
     if (!dWg) return SHAMPOO_OK;
-    MmaArgs q{};
-    add_seg(q, x, dg);
-    use_plan(q, p.dw, dim, 2 * p.ld_d, rows, kLayoutK, kLayoutK, ws + p.at_part);
-    const OutEpilogue out(dWg, ld_dwg, dWu, ld_dwu, (int)p.ld_d, (int)width, (int)(2 * p.ld_d), g_dtype == SHAMPOO_BF16,
-                          beta);
-    return weight_product<false>(h, kCls, nx, p.planes, p.dw.shape, q, out, s);
+    const MmaPlan& m = two ? p.two_dw : p.dw;
+    add_seg(qw, x, dg);
+    use_plan(qw, m, dim, 2 * p.ld_d, rows, kLayoutK, kLayoutK, ws + p.at_part);
+    if (two) return two_products<kLayoutRow>(h, kCls, nx, qx, out_x, qw, out_w, s);
+    return weight_product<false>(h, kCls, nx, p.planes, m.shape, qw, out_w, s);
   });
 }
 

@@ -496,11 +496,9 @@ struct UnitEpilogue {
 
 // C, each unit handed to the epilogue E.  ld_part holds whole units.
 template <typename T, int LA, int LB, typename E>
-__global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
-  extern __shared__ __align__(16) char lds_bytes[];
-  lds_char* lds = (lds_char*)lds_bytes;
+__device__ __forceinline__ void mma_body(const MmaArgs& q, const E& e, lds_char* lds, int block, int blocks) {
   const int tiles = q.tiles_m * q.tiles_n;
-  const int l = xcd_remap(blockIdx.x, gridDim.x);
+  const int l = xcd_remap(block, blocks);
   const int split = l / tiles;
   int tm, tn;
   mma_tile(l % tiles, q.tiles_m, q.tiles_n, tm, tn);
@@ -524,13 +522,28 @@ __global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
   mma_units<T>(q, core, lds, state, m0, n0, split, e);
 }
 
+template <typename T, int LA, int LB, typename E>
+__global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
+  extern __shared__ __align__(16) char lds_bytes[];
+  mma_body<T, LA, LB>(q, e, (lds_char*)lds_bytes, blockIdx.x, gridDim.x);
+}
+
+// Two products that hang on nothing of each other in one launch, the first's workgroups
+// before the second's (whose contraction runs along the columns of both operands).
+template <typename T, int LB, typename E>
+__global__ __launch_bounds__(T::kThr, 2) void mma_two_kernel(MmaArgs q, E e, MmaArgs q2, E e2, int first) {
+  extern __shared__ __align__(16) char lds_bytes[];
+  if ((int)blockIdx.x < first) mma_body<T, kLayoutRow, LB>(q, e, (lds_char*)lds_bytes, blockIdx.x, first);
+  else mma_body<T, kLayoutK, kLayoutK>(q2, e2, (lds_char*)lds_bytes, blockIdx.x - first, gridDim.x - first);
+}
+
 // The epilogue of a product whose contraction was cut: parts added in order.  One
 // unit of 8 columns to a thread.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void mma_join_kernel(MmaArgs q, E e) {
+__device__ __forceinline__ void mma_join(const MmaArgs& q, const E& e, int block, int blocks) {
   const int units = (q.N + 7) / 8;
-  const int64_t n = (int64_t)q.M * units, step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += step) {
+  const int64_t n = (int64_t)q.M * units, step = (int64_t)blocks * kThreads;
+  for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < n; i += step) {
     const int row = (int)(i / units), col = (int)(i % units) * 8;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     auto add = [&](float (&w)[8], const float* p) {
@@ -548,6 +561,15 @@ __global__ __launch_bounds__(kThreads) void mma_join_kernel(MmaArgs q, E e) {
     if constexpr (E::kState) st = e.state(row);
     e(row, st, col, x, y);
   }
+}
+template <typename E>
+__global__ __launch_bounds__(kThreads) void mma_join_kernel(MmaArgs q, E e) {
+  mma_join(q, e, blockIdx.x, gridDim.x);
+}
+template <typename E>
+__global__ __launch_bounds__(kThreads) void mma_join_two_kernel(MmaArgs q, E e, MmaArgs q2, E e2, int first) {
+  if ((int)blockIdx.x < first) mma_join(q, e, blockIdx.x, first);
+  else mma_join(q2, e2, blockIdx.x - first, gridDim.x - first);
 }
 
 // x = p0 + p1 + p2 in bf16, each to nearest even: 8 bits apiece, exact from 2^-110 in

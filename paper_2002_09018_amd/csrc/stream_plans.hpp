@@ -17,6 +17,7 @@ struct MmaPlan {
   int64_t tiles_m = 0, tiles_n = 0, seg_stages = 0;
   int64_t ld_part = 0;
   size_t part = 0;  // bytes of the parts
+  double us = 0;    // estimated time
 };
 
 // A tile and what it takes: us of a stage with 1, 2, .. workgroups on a compute unit
@@ -66,27 +67,81 @@ inline double mma_us(const MmaCost& t, int64_t groups, int64_t per) {
   return us;
 }
 
-// The cheapest tile and number of parts (at most most_splits) by estimated time.  Parts cost
-// their way to memory and back (more where the last-level cache does not hold them) and
-// the launch that adds them.  `segs` products of one contraction length are summed.
+// A product in tiles of shape i (cost t) and up to `want` parts; `us` is left out.
+inline MmaPlan mma_cut(int64_t M, int64_t N, int64_t K, const MmaCost& t, int i, int segs, bool pair, int64_t want,
+                       bool always_part) {
+  MmaPlan p;
+  p.shape = i;
+  p.seg_stages = cdiv64(K, t.bk);
+  const int64_t stages = p.seg_stages * segs;
+  p.per_split = (int)cdiv64(stages, want);
+  p.splits = (int)cdiv64(stages, p.per_split);
+  p.tiles_m = cdiv64(M, t.m);
+  p.tiles_n = cdiv64(N, pair ? t.n / 2 : t.n);
+  p.ld_part = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
+  p.part = p.splits > 1 || always_part ? (size_t)(p.splits * M * p.ld_part) * sizeof(float) : 0;
+  return p;
+}
+// What parts cost: their way to memory and back (more where the last-level cache does
+// not hold them) and the launch that adds them.
+inline double parts_us(const MmaPlan& p) {
+  const double mb = 1e-6 * (double)p.part;
+  return p.splits > 1 ? 5 + 0.3 * mb + 0.25 * std::max(0., mb - 256) : 0;
+}
+
+// The cheapest tile and number of parts (at most most_splits) by estimated time.  `segs`
+// products of one contraction length are summed.
 inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, int segs, bool pair, int least_shape,
                         int most_splits, bool always_part) {
   MmaPlan best;
-  double best_us = 0;
-  const int64_t ld = cdiv64(N, 8) * 8 * (pair ? 2 : 1);
   for (int i = least_shape; i <= kShapeBig; ++i) {
     const MmaCost& t = cost[i];
-    const int64_t seg_stages = cdiv64(K, t.bk), stages = seg_stages * segs;
-    const int64_t tm = cdiv64(M, t.m), tn = cdiv64(N, pair ? t.n / 2 : t.n);
+    const int64_t tiles = cdiv64(M, t.m) * cdiv64(N, pair ? t.n / 2 : t.n);
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (want > stages || want > most_splits || (want > 1 && want * tm * tn > 1024)) break;
-      const int64_t per = cdiv64(stages, want), splits = cdiv64(stages, per);
-      const size_t part = splits > 1 || always_part ? (size_t)(splits * M * ld) * sizeof(float) : 0;
-      const double mb = 1e-6 * (double)part;
-      const double us = mma_us(t, tm * tn * splits, per) + (splits > 1 ? 5 + 0.3 * mb + 0.25 * std::max(0., mb - 256) : 0);
-      if (best_us == 0 || us < best_us) {
+      if (want > cdiv64(K, t.bk) * segs || want > most_splits || (want > 1 && want * tiles > 1024)) break;
+      MmaPlan p = mma_cut(M, N, K, t, i, segs, pair, want, always_part);
+      p.us = mma_us(t, tiles * p.splits, p.per_split) + parts_us(p);
+      if (best.us == 0 || p.us < best.us) best = p;
+    }
+  }
+  return best;
+}
+
+// The two products of a gradient, dX (x) and the weights' (w), in one launch of 128 x 128
+// tiles where that is estimated to take less time than theirs one after the other
+// (`on`): each alone often leaves compute units idle, and a launch and a join are saved.
+// Both products have operands of the same number of planes (and so the same waves).
+// Measured, whole calls, two launches and one: 1003 x 333 x 1339 in fp32 70.3 and 58.9
+// us, in bf16 36.0 and 28.0; 2048 x 512 x 1344 in bf16 47.5 and 34.2; a vocabulary of
+// 1000 for 4096 x 1024 in bf16 54.5 and 45.1, where 512 x 1024 x 4096 fills the chip
+// either way and keeps two.
+struct TwoPlan {
+  bool on = false;
+  MmaPlan x, w;
+};
+inline TwoPlan two_plan(const MmaPlan& x, int64_t Mx, int64_t Nx, int64_t Kx, int segs, const MmaPlan& w, int64_t Mw,
+                        int64_t Nw, int64_t Kw, int planes) {
+  TwoPlan best;
+  const MmaCost &tx = mma_cost(planes)[kShapeMid], &tw = weight_cost(planes, planes)[kShapeMid];
+  const double slots = 256. * tx.slots;
+  const int64_t tiles_x = cdiv64(Mx, tx.m) * cdiv64(Nx, tx.n), tiles_w = cdiv64(Mw, tw.m) * cdiv64(Nw, tw.n);
+  if (tiles_x > 1024 || tiles_w > 1024) return best;  // enough for the chip by itself
+  double best_us = x.us + w.us;
+  for (int wx : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    if (wx > cdiv64(Kx, tx.bk) * segs || wx * tiles_x > 1024) break;
+    const MmaPlan px = mma_cut(Mx, Nx, Kx, tx, kShapeMid, segs, false, wx, false);
+    for (int ww : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (ww > cdiv64(Kw, tw.bk) || (ww > 1 && ww * tiles_w > 1024)) break;
+      const MmaPlan pw = mma_cut(Mw, Nw, Kw, tw, kShapeMid, 1, false, ww, false);
+      // workgroups run one after another in the slots, dX's first
+      const double gx = (double)(tiles_x * px.splits), gw = (double)(tiles_w * pw.splits);
+      const int busy = gx + gw <= 256 ? 0 : tx.slots - 1;
+      const double ux = px.per_split * tx.stage[busy] + tx.start, uw = pw.per_split * tw.stage[busy] + tw.start;
+      const double us = std::max({ux, uw, (gx * ux + gw * uw) / slots + (gx + gw > slots ? std::min(ux, uw) / 2 : 0)}) +
+                        std::max(parts_us(px), parts_us(pw)) + 0.5 * std::min(parts_us(px), parts_us(pw));
+      if (us < best_us) {
         best_us = us;
-        best = {i, (int)splits, (int)per, tm, tn, seg_stages, ld, part};
+        best = {true, px, pw};
       }
     }
   }
@@ -177,6 +232,8 @@ struct VocabGradPlan {
   int64_t piece = 0, pieces = 0, ld_dz = 0;
   int planes = 1;  // bf16 terms of the logits' gradient
   MmaPlan z[2], dx[2], dw[2];
+  bool two = false;  // dX and dW in one launch, where both are wanted, cut as follows
+  MmaPlan two_dx, two_dw;
   PackPlan x, w;
   size_t at_x = 0, at_w = 0, at_dz = 0, at_dx = 0, at_part = 0, bytes = 0;
 };
@@ -216,8 +273,14 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
     p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
     part = std::max({part, p.z[i].part, p.dw[i].part});
   }
-  p.at_dx = r.take(p.dx[0].part);
-  p.at_part = r.take(part);
+  if (p.pieces == 1 && p.planes == p.x.planes) {
+    const TwoPlan t = two_plan(p.dx[0], rows, dim, vocab, 1, p.dw[0], vocab, dim, rows, p.planes);
+    p.two = t.on;
+    p.two_dx = t.x;
+    p.two_dw = t.w;
+  }
+  p.at_dx = r.take(std::max(p.dx[0].part, p.two_dx.part));
+  p.at_part = r.take(std::max(part, p.two_dw.part));
   p.bytes = r.at;
   return p;
 }
@@ -246,10 +309,12 @@ inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, boo
 // one product.
 struct FfnGradPlan {
   MmaPlan gu, dx, dw;
+  bool two = false;  // as above
+  MmaPlan two_dx, two_dw;
   PackPlan x, wg, wu;
   int64_t ld_d = 0;
   int planes = 1;
-  size_t at_x = 0, at_wg = 0, at_wu = 0, at_d = 0, at_part = 0, bytes = 0;
+  size_t at_x = 0, at_wg = 0, at_wu = 0, at_d = 0, at_dx = 0, at_part = 0, bytes = 0;
 };
 inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype, bool pack_x,
                                  bool pack_wg, bool pack_wu) {
@@ -266,7 +331,14 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
   p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false);
   p.dw = mma_plan(dim, 2 * p.ld_d, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
-  p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part}));
+  if (p.planes == p.x.planes) {
+    const TwoPlan t = two_plan(p.dx, rows, dim, width, 2, p.dw, dim, 2 * p.ld_d, rows, p.planes);
+    p.two = t.on;
+    p.two_dx = t.x;
+    p.two_dw = t.w;
+  }
+  p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part, p.two_dw.part}));
+  p.at_dx = p.two ? r.take(p.two_dx.part) : p.at_part;
   p.bytes = r.at;
   return p;
 }

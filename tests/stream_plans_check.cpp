@@ -2,8 +2,10 @@
 //   vocab ROWS DIM VOCAB DTYPE PACK | vgrad ROWS DIM VOCAB DTYPE GDTYPE PACK
 //   ffn ROWS DIM WIDTH DTYPE | fgrad ROWS DIM WIDTH DTYPE GDTYPE
 // and prints the shape and the parts of each product (pieces first for vocab and
-// vgrad); every plan, and those of a sweep of sizes, must cover its product once, and
-// its buffers must lie apart.
+// vgrad; of a gradient last whether dX and the weights' gradient may share a launch,
+// and their parts there); every plan, and those of a sweep of sizes, must cover its
+// product once, and its buffers must lie apart.
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <cmath>
@@ -33,6 +35,16 @@ static void product(const MmaPlan& p, ll M, ll N, ll K, const MmaCost* cost, int
   require(p.ld_part % 8 == 0 && p.ld_part >= (pair ? 2 : 1) * N, "rows of parts", M, N, K, p.ld_part);
   require(p.splits == 1 || p.part > 0, "room of parts", M, N, K, p.splits);
   require(p.part == 0 || p.part == (size_t)(p.splits * M * p.ld_part) * 4, "bytes of parts", M, N, K, p.splits);
+}
+
+// Two products of one launch: the same tiles and planes, and numbers that a launch holds.
+static void two(const MmaPlan& x, ll Mx, ll Nx, ll Kx, int segs, const MmaPlan& w, ll Mw, ll Nw, ll Kw, int planes,
+                int dtype) {
+  require(planes == (dtype == SHAMPOO_F32 ? 3 : 1), "planes of two products", Mx, Nx, Kx, planes);
+  require(x.shape == kShapeMid && w.shape == kShapeMid, "tiles of two products", Mx, Nx, Kx, w.shape);
+  product(x, Mx, Nx, Kx, mma_cost(planes), segs, false, kShapeMid);
+  product(w, Mw, Nw, Kw, weight_cost(planes, planes), 1, false, kShapeMid);
+  require(fits(x) && fits(w), "launch of two products", Mx, Nx, Kx, x.splits);
 }
 
 // Buffers in the order they were taken: each begins at or past the end of the one before.
@@ -84,8 +96,12 @@ static VocabGradPlan vgrad(ll rows, ll dim, ll v, int dtype, int g, bool px, boo
   l.put(p.at_x, px ? p.x.bytes : 0, "x");
   l.put(p.at_w, pw ? p.w.bytes : 0, "w");
   l.put(p.at_dz, (size_t)(rows * p.ld_dz * p.planes) * 2, "dz");
-  l.put(p.at_dx, p.dx[0].part, "dX");
-  l.put(p.at_part, std::max(std::max(p.z[0].part, p.z[1].part), std::max(p.dw[0].part, p.dw[1].part)), "parts");
+  l.put(p.at_dx, std::max(p.dx[0].part, p.two_dx.part), "dX");
+  l.put(p.at_part, std::max({p.z[0].part, p.z[1].part, p.dw[0].part, p.dw[1].part, p.two_dw.part}), "parts");
+  if (p.two) {
+    require(p.pieces == 1, "one launch of two products", rows, dim, v, p.pieces);
+    two(p.two_dx, rows, dim, v, 1, p.two_dw, v, dim, rows, p.planes, dtype);
+  }
   require(l.end <= p.bytes, "bytes", rows, dim, v, p.bytes);
   return p;
 }
@@ -113,7 +129,9 @@ static FfnGradPlan fgrad(ll rows, ll dim, ll width, int dtype, int g) {
   l.put(p.at_wg, p.wg.bytes, "wg");
   l.put(p.at_wu, p.wu.bytes, "wu");
   l.put(p.at_d, (size_t)(rows * 2 * p.ld_d * p.planes) * 2, "d");
-  l.put(p.at_part, std::max(p.gu.part, std::max(p.dx.part, p.dw.part)), "parts");
+  l.put(p.at_part, std::max({p.gu.part, p.dx.part, p.dw.part, p.two_dw.part}), "parts");
+  l.put(p.at_dx, p.two_dx.part, "parts of dX");
+  if (p.two) two(p.two_dx, rows, dim, width, 2, p.two_dw, dim, 2 * p.ld_d, rows, p.planes, dtype);
   require(l.end <= p.bytes && p.ld_d >= width && p.ld_d % 64 == 0, "bytes", rows, dim, width, p.bytes);
   return p;
 }
@@ -135,11 +153,13 @@ int main() {
       const VocabGradPlan p = vgrad(a, b, c, d, e, f, f);
       printf("%lld", (ll)p.pieces);
       for (int i = 0; i < 2; ++i) print(p.z[i]), print(p.dx[i]), print(p.dw[i]);
+      printf(" %d %d %d", p.two, p.two_dx.splits, p.two_dw.splits);
     } else if (sscanf(line, "ffn %lld %lld %lld %d", &a, &b, &c, &d) == 4) {
       print(ffn(a, b, c, d).mma);
     } else if (sscanf(line, "fgrad %lld %lld %lld %d %d", &a, &b, &c, &d, &e) == 5) {
       const FfnGradPlan p = fgrad(a, b, c, d, e);
       print(p.gu), print(p.dx), print(p.dw);
+      printf(" %d %d %d", p.two, p.two_dx.splits, p.two_dw.splits);
     } else {
       sscanf(line, "%15s", kind);
       printf("unknown %s", kind);

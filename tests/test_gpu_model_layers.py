@@ -205,7 +205,7 @@ VOCAB_MORE = [(6109, 3490, 72, "bfloat16", "bfloat16", True), (4951, 1163, 408, 
               (2608, 241, 4626, "bfloat16", "float32", True), (843, 1928, 1991, "bfloat16", "float32", True),
               (922, 196, 31249, "bfloat16", "float32", True), (5525, 80, 14027, "float32", "bfloat16", True),
               (130, 3330, 23888, "bfloat16", "float32", True), (4870, 136, 17995, "bfloat16", "bfloat16", False),
-              (6903, 914, 15369, "bfloat16", "float32", True)]
+              (6903, 914, 15369, "bfloat16", "float32", True), (1098, 165, 3544, "bfloat16", "bfloat16", True)]
 
 
 @pytest.mark.parametrize("n,d,v,dtype,g_dtype,copied", VOCAB_MORE)
@@ -213,7 +213,8 @@ def test_vocab_tiles(env, n, d, v, dtype, g_dtype, copied):
     say("vocab tiles", n, d, v, dtype, g_dtype, copied)
     dt, gt, lay = dtype_of(env, dtype), dtype_of(env, g_dtype), (5, 3) if copied else (0, 0)
     check_vocab(env, n, d, v, dt, *lay)
-    check_vocab_grad(env, n, d, v, dt, gt, *lay)
+    for with_x, with_w in ((True, True), (True, False), (False, True)):
+        check_vocab_grad(env, n, d, v, dt, gt, *lay, with_x=with_x, with_w=with_w)
 
 
 def test_vocab_rows_of_their_own(env):
@@ -407,7 +408,7 @@ FFN_MORE = [(1, 1718, 1871, "float32", "float32"), (1, 3508, 1348, "bfloat16", "
             (1441, 2247, 731, "float32", "bfloat16"), (4932, 884, 2504, "bfloat16", "float32"),
             (7880, 75, 269, "float32", "bfloat16"), (688, 3745, 3026, "bfloat16", "float32"),
             (5349, 2491, 844, "bfloat16", "bfloat16"), (992, 723, 2295, "bfloat16", "float32"),
-            (7392, 845, 1327, "bfloat16", "float32")]
+            (7392, 845, 1327, "bfloat16", "float32"), (1154, 103, 436, "bfloat16", "bfloat16")]
 
 
 @pytest.mark.parametrize("n,d,w,dtype,g_dtype", FFN_MORE)
@@ -415,7 +416,8 @@ def test_gated_ffn_tiles(env, n, d, w, dtype, g_dtype):
     say("ffn tiles", n, d, w, dtype, g_dtype)
     dt, gt = dtype_of(env, dtype), dtype_of(env, g_dtype)
     check_ffn(env, n, d, w, dt, "SILU")
-    check_ffn_grad(env, n, d, w, dt, gt, "GELU_TANH", False)
+    for with_x, with_w in ((True, True), (True, False), (False, True)):
+        check_ffn_grad(env, n, d, w, dt, gt, "GELU_TANH", False, with_x=with_x, with_w=with_w)
 
 
 def test_weights_of_different_strides(env):

@@ -49,6 +49,8 @@ def vocab_kernels(ask, sizes):
         for i in (1, 7):
             found |= {("dz", t, 0, b[i], b[i + 1] > 1), ("dX", t, 0, b[i + 2], b[i + 3] > 1),
                       ("dW", t, terms, b[i + 4], b[i + 5] > 1)}
+        if b[13]:
+            found.add(("dX and dW", t, terms, b[14] > 1, b[15] > 1))
     return found
 
 
@@ -58,6 +60,8 @@ def ffn_kernels(ask, sizes):
     for (n, d, w, t, g), b in zip(sizes, ask(["fgrad %d %d %d %d %d" % x for x in sizes])):
         found |= {("pair", t, 0, b[0], b[1] > 1), ("dX", t, 0, b[2], b[3] > 1),
                   ("dW", t, 3 if t == 0 or g == 0 else 1, b[4], b[5] > 1)}
+        if b[6]:
+            found.add(("dX and dW", t, 3 if t == 0 else 1, b[7] > 1, b[8] > 1))
     for (n, d, w, t, _), a in zip(sizes, ask(["ffn %d %d %d %d" % x[:4] for x in sizes])):
         found.add(("pair", t, 0, a[0], a[1] > 1))
     return found
