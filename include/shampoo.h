@@ -603,8 +603,9 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
  *   dW = beta dW + dz^T X (vocab x dim, g_dtype; not read when beta == 0)
  * dX or dW may be NULL.  The logits are formed again, in pieces of the vocabulary.
  * dz is kept in three bf16 terms where dtype or g_dtype is fp32 (dX of bf16 inputs takes
- * the first), else in one.  g_dtype counts without dW too.  A row whose gradients are all 0 adds nothing to dW if X and
- * lse are finite there.  rows == 0: dW = beta dW.
+ * the first), else in one.  g_dtype counts without dW too.  The order of dX's sums may
+ * differ between calls with dW and without.  A row whose gradients are all 0 adds nothing
+ * to dW if X and lse are finite there.  rows == 0: dW = beta dW.
  * Errors: as above, EINVAL for a non-finite beta, g_logp without targets, or neither dX nor
  * dW.
  */
@@ -635,7 +636,8 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
  *   dX = dG Wg^T + dU Wu^T          (rows x dim, dtype)
  *   dWg = beta dWg + X^T dG, dWu = beta dWu + X^T dU   (dim x width, g_dtype; not read
  *                                                       when beta == 0)
- * dX may be NULL, or dWg and dWu.  dG and dU are kept in bf16 terms as dz above.
+ * dX may be NULL, or dWg and dWu; what is said of dz and of the order of dX's sums above
+ * holds here of dG and dU.
  * rows == 0: dWg = beta dWg, dWu = beta dWu.
  * Errors: as above, EINVAL for only one of G and U or of dWg and dWu, or no output.
  */

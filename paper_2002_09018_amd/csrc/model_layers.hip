@@ -184,7 +184,6 @@ shampoo_status product(Handle* h, int cls, int shape, const MmaArgs& q, const E&
     else return mma_launch<typename K::Thin, LA, LB>(h, cls, q, e, s);
   }
   if (shape == kShapeMid) return mma_launch<typename K::Mid, LA, LB>(h, cls, q, e, s);
-  if (shape == kShapeMid) return mma_launch<typename K::Mid, LA, LB>(h, cls, q, e, s);
   using B = std::conditional_t<LA == kLayoutK, typename K::BigWeight, typename K::Big>;
   return mma_launch<B, LA, LB>(h, cls, q, e, s);
 }

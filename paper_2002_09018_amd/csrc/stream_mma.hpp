@@ -10,22 +10,41 @@
 // where the other operand has one), the smallest first.  A sum of two products (dG
 // Wg^T + dU Wu^T) is two segments of one long contraction.
 //
-// Staging.  Stages of kBk = 32 contraction indices go from memory to LDS without
-// passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a ring
-// of kBufs buffers: kBufs - 1 stages are in flight.  Lanes whose row, column or
+// Staging.  Stages of kBk = 64 or 32 contraction indices go from memory to LDS
+// without passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a
+// ring of kBufs buffers: kBufs - 1 stages are in flight.  Lanes whose row, column or
 // contraction index lies outside the operand have an offset outside the buffer's
 // range and receive zeros, so that no size needs other code.
-//   kLayoutRow: [row][32 k], 64 bytes a row, its 16-byte chunks stored at chunk ^
-//               (row >> 2 & 3); a fragment (8 k of a row) is one 16-byte read.
+//   kLayoutRow: [row][kBk], its 16-byte chunks stored at chunk ^ (row >> 1 & 7) (rows
+//               of 128 bytes) or ^ (row >> 2 & 3) (of 64); a fragment (8 k of a row) is
+//               one 16-byte read.  64 bytes of a row cost the memory path what its whole
+//               128-byte line does (a compute unit streams 41-70 B/ns against 98-136), so
+//               bf16 tiles take 64 indices to a stage: 16384 x 1024 x 8192 331 -> 310 us.
+//               Three planes of two operands leave room for 32.
 //   kLayoutK:   panels of [k][128 or 64 columns], 32-byte pieces stored at piece ^
-//               swizzle(k), read with the transposing read (ds_read_b64_tr_b16).
+//               swizzle(k), read with the transposing read (ds_read_b64_tr_b16).  Where
+//               both operands lie so, three stages of 32 are faster than two of 64 (217 us
+//               and 228 for 16384 x 1024 x 8192).
 // The destination of a load is fixed (1 KB in lane order), so the swizzle is in
-// the addresses that the lanes load from.
+// the addresses that the lanes load from; conflicts take 0-2% of LDS cycles in the loop.
 //
 // Loop.  One barrier per stage, before its last 16 indices are multiplied: all
 // fragments of the stage are in registers then, its buffer is free for the stage
 // kBufs further on, and the first fragments of the next stage are read beside the
-// last products.
+// last products.  Reads and loads go out between the matrix instructions (in blocks
+// before them: 6559 -> 6277 us for the gradients of 8192 x 1024 x 131072).
+//
+// Few rows.  A product of up to 32 rows is bound by the other operand's bytes and by
+// latency: 32 x 64 tiles whose waves (eight; four of three planes) each have a ring and a
+// share of the contraction, no barrier among them, summed at the end (16 x 1024 x 8192:
+// 13.1 -> 10.4 us against 32 x 128 tiles of two waves in parts).
+//
+// What bounds it.  256 x 256 tiles in bf16 run at 1.1-1.25 PFLOP/s, where a library's
+// 8192^3 product reaches 1.3 on the same card; the card's power bounds both: the clock
+// falls under them, and the same instructions on small gradients instead of random
+// numbers take 5% less time.  Neither two workgroups of half the tile on a compute unit
+// (7 and 13% slower) nor starting workgroups apart nor skipped LDS reads (4%) lift it.
+// fp32 products reach 190-200 TFLOP/s, six bf16 products each.
 //
 // The instruction's first operand is B and its second A, so that a lane holds one
 // row of C (lane % 32) and runs of four columns: sums along a row are formed in the
@@ -137,8 +156,9 @@ struct MmaLoader {
 
 // 1 KB from the lanes' offsets to LDS, in lane order.  In asm, as the compiler would
 // have every later transposing read wait for all loads in flight; mma_wait and
-// mma_barrier are what orders them.  (The instruction writes no register.  The wait states are those that M0, and the
-// scalar registers of the range if the vector unit wrote them, need before it.)
+// mma_barrier are what orders them.  (The instruction writes no
+// register.  The wait states are those that M0, and the scalar registers of the range
+// if the vector unit wrote them, need before it.)
 __device__ __forceinline__ void mma_dma(const char* base, uint32_t off, lds_char* to) {
   const uint64_t at = reinterpret_cast<uint64_t>(base);
   const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
@@ -530,6 +550,7 @@ __global__ __launch_bounds__(T::kThr, 2) void mma_kernel(MmaArgs q, E e) {
 
 // Two products that hang on nothing of each other in one launch, the first's workgroups
 // before the second's (whose contraction runs along the columns of both operands).
+// What it gains stands at its rule, two_plan.
 template <typename T, int LB, typename E>
 __global__ __launch_bounds__(T::kThr, 2) void mma_two_kernel(MmaArgs q, E e, MmaArgs q2, E e2, int first) {
   extern __shared__ __align__(16) char lds_bytes[];
