@@ -736,6 +736,11 @@ def _room(t, nbytes, dev):
     return (t.dtype is _torch_mod.uint8 and t.numel() >= nbytes and t.is_contiguous() and t.get_device() == dev)
 
 
+def _bytes_on(t, dev):
+    """A contiguous uint8 buffer on dev, or None."""
+    return t is None or (t.dtype is _torch_mod.uint8 and t.is_contiguous() and t.get_device() == dev)
+
+
 def _apart(a, b):
     """Whether two matrices (as from _layout) share no memory: one lies past the
     other, or the rows of each lie between those of the other (column ranges
@@ -1028,10 +1033,13 @@ def _opt(a):
     return (None, 0) if a is None else (a[5], a[2])
 
 
-def _done(handle, rc, written, read):
-    """A call's status.  The library refuses buffers that overlap; which, the tensors tell."""
+def _failed(handle, rc, written, read, workspace, need):
+    """Raises for a call's status.  The library refuses buffers that overlap and a workspace
+    that is too small; which and by how much, the tensors tell."""
     if rc == SHAMPOO_EINVAL:
         _check_all_apart(written, read)
+    if rc == SHAMPOO_ENOMEM:
+        _check_bytes(workspace, need(), "workspace")
     _check(handle, rc)
 
 
@@ -1068,15 +1076,17 @@ def shampoo_vocab_logprobs(handle, X, W, targets, logp, lse, workspace=None, str
         f32, vec = _torch_mod.float32, (rows,)
         ok = (_plain(lse, f32, vec, dev) and _plain(logp, f32, vec, dev) and _on_handle(handle, dev) and
               _plain(targets, _torch_mod.int32, vec, dev) and
-              _room(workspace, _lib.shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dt), dev))
+              _bytes_on(workspace, dev))
     if not ok:
         _refuse_vocab(handle, X, W, targets, lse, (("logp", logp),), workspace,
                       lambda r, d, v: _lib.shampoo_vocab_logprobs_workspace_bytes(r, d, v, _code(X.dtype)),
                       lambda: _need((targets is None) == (logp is None), "targets and logp go together"))
-    _check(handle, _lib.shampoo_vocab_logprobs(handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets),
-                                               _ptr(logp), lse.data_ptr(), _ptr(workspace),
-                                               0 if workspace is None else workspace.numel(),
-                                               _stream_on(stream, dev)))
+    rc = _lib.shampoo_vocab_logprobs(handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets), _ptr(logp),
+                                     lse.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                     _stream_on(stream, dev))
+    if rc:
+        _failed(handle, rc, [], [], workspace,
+                lambda: _lib.shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dt))
 
 
 def _refuse_vocab(handle, X, W, targets, lse, vecs, workspace, room, pairs, more=()):
@@ -1117,7 +1127,7 @@ def shampoo_vocab_logprobs_grad(handle, X, W, targets, lse, dX=None, dW=None, g_
               (dW is None or (dw is not None and dw[0] == vocab and dw[1] == dim and dw[4] == dev)) and
               _plain(lse, f32, vec, dev) and _plain(g_logp, f32, vec, dev) and _plain(g_lse, f32, vec, dev) and
               _plain(targets, _torch_mod.int32, vec, dev) and _on_handle(handle, dev) and
-              _room(workspace, _lib.shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dt, gdt), dev))
+              _bytes_on(workspace, dev))
     if not ok:
         def pairs():
             _need(g_logp is None or targets is not None, "g_logp needs targets")
@@ -1129,11 +1139,13 @@ def shampoo_vocab_logprobs_grad(handle, X, W, targets, lse, dX=None, dW=None, g_
                       lambda r, d, v: _lib.shampoo_vocab_logprobs_grad_workspace_bytes(
                           r, d, v, _code(X.dtype), _code(X.dtype if dW is None else dW.dtype)), pairs,
                       (("dX", dX), ("dW", dW)))
-    _done(handle, _lib.shampoo_vocab_logprobs_grad(
+    rc = _lib.shampoo_vocab_logprobs_grad(
         handle, ptr, w[5], dt, rows, dim, vocab, ld, w[2], _ptr(targets), lse.data_ptr(), _ptr(g_logp), _ptr(g_lse),
         *_opt(dx), _opt(dw)[0], gdt, _opt(dw)[1], beta, _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream_on(stream, dev)),
-        [("dX", dX), ("dW", dW)], [("X", X), ("W", W)])
+        0 if workspace is None else workspace.numel(), _stream_on(stream, dev))
+    if rc:
+        _failed(handle, rc, [("dX", dX), ("dW", dW)], [("X", X), ("W", W)], workspace,
+                lambda: _lib.shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dt, gdt))
 
 
 def shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype):
@@ -1167,16 +1179,18 @@ def shampoo_gated_ffn(handle, X, Wg, Wu, H, act=ACT_SILU, G=None, U=None, worksp
         width = wg[1]
         ok = (_fits(wg, dim, width, x) and _fits(wu, dim, width, x) and _fits(lh, rows, width, x) and
               (G is None or (_fits(lg, rows, width, x) and _fits(lu, rows, width, x))) and _on_handle(handle, dev) and
-              _room(workspace, _lib.shampoo_gated_ffn_workspace_bytes(rows, dim, width, dt), dev))
+              _bytes_on(workspace, dev))
     if not ok:
         _need(H is not None, "H is required")
         _need((G is None) == (U is None), "G and U go together")
         _refuse_ffn(handle, X, Wg, Wu, (("H", H), ("G", G), ("U", U)), (), [("H", H), ("G", G), ("U", U)], [],
                     lambda r, d, w: _lib.shampoo_gated_ffn_workspace_bytes(r, d, w, _code(X.dtype)), workspace)
-    _done(handle, _lib.shampoo_gated_ffn(handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], act,
-                                         lh[5], lh[2], *_opt(lg), *_opt(lu), _ptr(workspace),
-                                         0 if workspace is None else workspace.numel(), _stream_on(stream, dev)),
-          [("H", H), ("G", G), ("U", U)], [("X", X), ("Wg", Wg), ("Wu", Wu)])
+    rc = _lib.shampoo_gated_ffn(handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], act, lh[5], lh[2],
+                                *_opt(lg), *_opt(lu), _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _stream_on(stream, dev))
+    if rc:
+        _failed(handle, rc, [("H", H), ("G", G), ("U", U)], [("X", X), ("Wg", Wg), ("Wu", Wu)], workspace,
+                lambda: _lib.shampoo_gated_ffn_workspace_bytes(rows, dim, width, dt))
 
 
 def shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype):
@@ -1207,7 +1221,7 @@ def shampoo_gated_ffn_grad(handle, X, Wg, Wu, dH, act=ACT_SILU, G=None, U=None, 
               (dX is None or _fits(dx, rows, dim, x)) and
               (dWg is None or (dg is not None and dg[0] == dim and dg[1] == width and dg[4] == dev and
                                _fits(du, dim, width, dg))) and _on_handle(handle, dev) and
-              _room(workspace, _lib.shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dt, gdt), dev))
+              _bytes_on(workspace, dev))
     if not ok:
         _need(dH is not None, "dH is required")
         _need((G is None) == (U is None), "G and U go together")
@@ -1219,11 +1233,14 @@ def shampoo_gated_ffn_grad(handle, X, Wg, Wu, dH, act=ACT_SILU, G=None, U=None, 
                     [("dX", dX), ("dWg", dWg), ("dWu", dWu)], [("dH", dH), ("G", G), ("U", U)],
                     lambda r, d, w: _lib.shampoo_gated_ffn_grad_workspace_bytes(
                         r, d, w, _code(X.dtype), _code(X.dtype if dWg is None else dWg.dtype)), workspace)
-    _done(handle, _lib.shampoo_gated_ffn_grad(
+    rc = _lib.shampoo_gated_ffn_grad(
         handle, ptr, wg[5], wu[5], dt, rows, dim, width, ld, wg[2], wu[2], act, *_opt(lh), *_opt(lg), *_opt(lu),
         *_opt(dx), *_opt(dg), *_opt(du), gdt, beta, _ptr(workspace), 0 if workspace is None else workspace.numel(),
-        _stream_on(stream, dev)),
-        [("dX", dX), ("dWg", dWg), ("dWu", dWu)], [("X", X), ("Wg", Wg), ("Wu", Wu), ("dH", dH), ("G", G), ("U", U)])
+        _stream_on(stream, dev))
+    if rc:
+        _failed(handle, rc, [("dX", dX), ("dWg", dWg), ("dWu", dWu)],
+                [("X", X), ("Wg", Wg), ("Wu", Wu), ("dH", dH), ("G", G), ("U", U)], workspace,
+                lambda: _lib.shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dt, gdt))
 
 
 def shampoo_dropout(handle, X, Y, rate, seed, offset=0, R=None, stream=None):

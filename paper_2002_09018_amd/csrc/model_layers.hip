@@ -299,9 +299,9 @@ extern "C" {
 // ---------------------------------------------------------------- loss
 size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype) {
   if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
-  // (which matrices are copied hangs on strides and addresses: room for either way)
-  const size_t need = vocab_plan(rows, dim, vocab, dtype, true, true).bytes;
-  return dtype == SHAMPOO_F32 ? need : std::max(need, vocab_plan(rows, dim, vocab, dtype, true, false).bytes);
+  const size_t need = vocab_plan(rows, dim, vocab, dtype, true, true).need;
+  if (vocab_alike(dim, vocab, dtype)) return need;
+  return std::max(need, vocab_plan(rows, dim, vocab, dtype, true, false).bytes);
 }
 
 shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W, int dtype, int64_t rows, int64_t dim,
@@ -312,7 +312,10 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     if (rows == 0) return SHAMPOO_OK;
     if (!X || !W || !lse || !logp != !targets)
       return fail(h, SHAMPOO_EINVAL, "X, W or lse, or one of targets and logp is NULL");
-    const size_t need = shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dtype);
+    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
+    const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
+    const size_t need = vocab_alike(dim, vocab, dtype) ? p.need
+                                                       : shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dtype);
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(
         h, {{span(workspace, (int64_t)need), "workspace"}, {span(logp, rows * 4), "logp"}, {span(lse, rows * 4), "lse"}},
@@ -321,8 +324,6 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     constexpr int kCls = SHAMPOO_KCLASS_VOCAB;
-    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
-    const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
     STATUS_TRY(check_tiles(h, {p.mma[0], p.mma[1]}));
     if (rows * cdiv64(p.piece, kStatCols) / (kThreads / 64) >= kMostTiles)
       return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
@@ -361,9 +362,9 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
 size_t shampoo_vocab_logprobs_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype) {
   if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
   if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
-  const size_t need = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, true).bytes;
-  return dtype == SHAMPOO_F32 ? need
-                              : std::max(need, vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, false).bytes);
+  const size_t need = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, true).need;
+  if (vocab_grad_alike(rows, dim, vocab, dtype, grad_planes(dtype, g_dtype))) return need;
+  return std::max(need, vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, true, false).bytes);
 }
 
 shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const void* W, int dtype, int64_t rows,
@@ -384,7 +385,11 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     if (rows == 0) return dW ? scaled(h, kCls, dW, g_dtype, vocab, dim, ld_dw, beta, s) : SHAMPOO_OK;
     if (!X || !W || !lse) return fail(h, SHAMPOO_EINVAL, "X, W or lse is NULL");
     if (g_logp && !targets) return fail(h, SHAMPOO_EINVAL, "g_logp without targets");
-    const size_t need = shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dtype, g_dtype);
+    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
+    const VocabGradPlan p = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, pack_x, pack_w);
+    const size_t need = vocab_grad_alike(rows, dim, vocab, dtype, p.planes)
+                            ? p.need
+                            : shampoo_vocab_logprobs_grad_workspace_bytes(rows, dim, vocab, dtype, g_dtype);
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(h,
                                {{span(workspace, (int64_t)need), "workspace"},
@@ -397,8 +402,6 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
                                 {span(g_logp, rows * 4), "g_logp"},
                                 {span(g_lse, rows * 4), "g_lse"}}));
     char* ws = static_cast<char*>(workspace);
-    const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
-    const VocabGradPlan p = vocab_grad_plan(rows, dim, vocab, dtype, g_dtype, pack_x, pack_w);
     STATUS_TRY(check_tiles(h, {p.z[0], p.z[1], p.dx[0], p.dx[1], p.dw[0], p.dw[1]}));
     Planes16 x, w;
     Packer packer{h, kCls, dtype, s};
@@ -448,7 +451,7 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
 // ---------------------------------------------------------------- feed-forward block
 size_t shampoo_gated_ffn_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype) {
   if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
-  return ffn_plan(rows, dim, width, dtype, true, true, true).bytes;
+  return ffn_plan(rows, dim, width, dtype, true, true, true).need;
 }
 
 shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, const void* Wu, int dtype, int64_t rows,
@@ -463,7 +466,10 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     if (U) STATUS_TRY(check_ld(h, ld_u, width, "ld_u"));
     if (rows == 0) return SHAMPOO_OK;
     if (!X || !Wg || !Wu || !H) return fail(h, SHAMPOO_EINVAL, "X, Wg, Wu or H is NULL");
-    const size_t need = shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype);
+    const bool px = !as_it_lies(X, ld_x, dim, dtype), pg = !as_it_lies(Wg, ld_wg, width, dtype);
+    const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
+    const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
+    const size_t need = p.need;
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(h,
                                {{span(workspace, (int64_t)need), "workspace"},
@@ -477,9 +483,6 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     constexpr int kCls = SHAMPOO_KCLASS_FFN;
-    const bool px = !as_it_lies(X, ld_x, dim, dtype), pg = !as_it_lies(Wg, ld_wg, width, dtype);
-    const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
-    const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
     STATUS_TRY(check_tiles(h, {p.mma}));
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};
@@ -505,7 +508,7 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
 size_t shampoo_gated_ffn_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype) {
   if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
   if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
-  return ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, true, true).bytes;
+  return ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, true, true).need;
 }
 
 shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* Wg, const void* Wu, int dtype,
@@ -537,7 +540,11 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
       return scaled(h, kCls, dWu, g_dtype, dim, width, ld_dwu, beta, s);
     }
     if (!X || !Wg || !Wu || !dH) return fail(h, SHAMPOO_EINVAL, "X, Wg, Wu or dH is NULL");
-    const size_t need = shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype);
+    const bool px = (!G || dWg) && !as_it_lies(X, ld_x, dim, dtype);
+    const bool pg = (!G || dX) && !as_it_lies(Wg, ld_wg, width, dtype);
+    const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
+    const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
+    const size_t need = p.need;
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(h,
                                {{span(workspace, (int64_t)need), "workspace"},
@@ -551,10 +558,6 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
                                 {span(G, rows, width, ld_g, dtype), "G"},
                                 {span(U, rows, width, ld_u, dtype), "U"}}));
     char* ws = static_cast<char*>(workspace);
-    const bool px = (!G || dWg) && !as_it_lies(X, ld_x, dim, dtype);
-    const bool pg = (!G || dX) && !as_it_lies(Wg, ld_wg, width, dtype);
-    const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
-    const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
     STATUS_TRY(check_tiles(h, {p.gu, p.dx, p.dw}));
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};

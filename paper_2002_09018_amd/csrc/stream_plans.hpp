@@ -167,13 +167,20 @@ inline PackPlan pack_plan(int64_t rows, int64_t cols, int dtype) {
   return p;
 }
 
-// Offsets of buffers in a workspace, each aligned to 256 bytes.
+// Offsets of buffers in a workspace, each aligned to 256 bytes; spared: bytes of copies
+// that this call does without, for which a workspace has room all the same (whether a
+// matrix is copied hangs on its address and stride).
 struct Room {
-  size_t at = 0;
+  size_t at = 0, spared = 0;
   size_t take(size_t bytes) {
     const size_t here = at;
     at += (bytes + 255) / 256 * 256;
     return here;
+  }
+  size_t copy(bool made, size_t bytes) {
+    if (made) return take(bytes);
+    spared += (bytes + 255) / 256 * 256;
+    return 0;
   }
 };
 
@@ -196,19 +203,23 @@ struct VocabPlan {
   int64_t piece = 0, pieces = 0, entries = 0;  // entries: statistics of a row
   MmaPlan mma[2];  // of a whole piece and of the last
   PackPlan x, w;
-  size_t at_x = 0, at_w = 0, at_stat = 0, at_target = 0, at_part = 0, bytes = 0;
+  size_t at_x = 0, at_w = 0, at_stat = 0, at_target = 0, at_part = 0, bytes = 0, need = 0;
 };
 inline int64_t vocab_entries(const MmaPlan& p, int64_t n) { return p.part ? cdiv64(n, kStatCols) : p.tiles_n; }
 
+// Whether the table is cut the same way copied or not.
+inline bool vocab_alike(int64_t dim, int64_t vocab, int dtype) {
+  return dtype == SHAMPOO_F32 || vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) == vocab;
+}
 inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, bool pack_x, bool pack_w) {
   VocabPlan p;
   Room r;
   p.x = pack_plan(rows, dim, dtype);
-  if (pack_x) p.at_x = r.take(p.x.bytes);
+  p.at_x = r.copy(pack_x, p.x.bytes);
   p.piece = pack_w ? vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) : vocab;
   p.pieces = cdiv64(vocab, p.piece);
   p.w = pack_plan(p.piece, dim, dtype);
-  if (pack_w) p.at_w = r.take(p.w.bytes);
+  p.at_w = r.copy(pack_w, p.w.bytes);
   const int64_t last = vocab - (p.pieces - 1) * p.piece;
   size_t part = 0;
   for (int i = 0; i < 2; ++i) {
@@ -224,6 +235,7 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
   p.at_target = r.take((size_t)rows * 4);
   p.at_part = r.take(part);
   p.bytes = r.at;
+  p.need = r.at + r.spared;
   return p;
 }
 
@@ -235,7 +247,7 @@ struct VocabGradPlan {
   bool two = false;  // dX and dW in one launch, where both are wanted, cut as follows
   MmaPlan two_dx, two_dw;
   PackPlan x, w;
-  size_t at_x = 0, at_w = 0, at_dz = 0, at_dx = 0, at_part = 0, bytes = 0;
+  size_t at_x = 0, at_w = 0, at_dz = 0, at_dx = 0, at_part = 0, bytes = 0, need = 0;
 };
 
 // An fp32 gradient, of inputs of either type, has three terms of dz: with one it
@@ -243,18 +255,22 @@ struct VocabGradPlan {
 // bf16 gradient of logits, rounded once.
 inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || g_dtype == SHAMPOO_F32 ? 3 : 1; }
 
+inline bool vocab_grad_alike(int64_t rows, int64_t dim, int64_t vocab, int dtype, int planes) {
+  return dtype == SHAMPOO_F32 ||
+         vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) >= vocab_piece(vocab, rows * planes * 2);
+}
 inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype, bool pack_x,
                                      bool pack_w) {
   VocabGradPlan p;
   Room r;
   p.planes = grad_planes(dtype, g_dtype);
   p.x = pack_plan(rows, dim, dtype);
-  if (pack_x) p.at_x = r.take(p.x.bytes);
+  p.at_x = r.copy(pack_x, p.x.bytes);
   p.piece = vocab_piece(vocab, rows * p.planes * 2);
   if (pack_w) p.piece = std::min(p.piece, vocab_piece(vocab, pack_plan(1, dim, dtype).bytes));
   p.pieces = cdiv64(vocab, p.piece);
   p.w = pack_plan(p.piece, dim, dtype);
-  if (pack_w) p.at_w = r.take(p.w.bytes);
+  p.at_w = r.copy(pack_w, p.w.bytes);
   p.ld_dz = cdiv64(p.piece, 64) * 64;
   p.at_dz = r.take((size_t)(rows * p.ld_dz * p.planes) * 2);
   size_t part = 0;
@@ -282,6 +298,7 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
   p.at_dx = r.take(std::max(p.dx[0].part, p.two_dx.part));
   p.at_part = r.take(std::max(part, p.two_dw.part));
   p.bytes = r.at;
+  p.need = r.at + r.spared;
   return p;
 }
 
@@ -289,19 +306,20 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
 struct FfnPlan {
   MmaPlan mma;
   PackPlan x, wg, wu;
-  size_t at_x = 0, at_wg = 0, at_wu = 0, at_part = 0, bytes = 0;
+  size_t at_x = 0, at_wg = 0, at_wu = 0, at_part = 0, bytes = 0, need = 0;
 };
 inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, bool pack_x, bool pack_wg, bool pack_wu) {
   FfnPlan p;
   Room r;
   p.x = pack_plan(rows, dim, dtype);
   p.wg = p.wu = pack_plan(dim, width, dtype);
-  if (pack_x) p.at_x = r.take(p.x.bytes);
-  if (pack_wg) p.at_wg = r.take(p.wg.bytes);
-  if (pack_wu) p.at_wu = r.take(p.wu.bytes);
+  p.at_x = r.copy(pack_x, p.x.bytes);
+  p.at_wg = r.copy(pack_wg, p.wg.bytes);
+  p.at_wu = r.copy(pack_wu, p.wu.bytes);
   p.mma = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
   p.at_part = r.take(p.mma.part);
   p.bytes = r.at;
+  p.need = r.at + r.spared;
   return p;
 }
 
@@ -314,7 +332,7 @@ struct FfnGradPlan {
   PackPlan x, wg, wu;
   int64_t ld_d = 0;
   int planes = 1;
-  size_t at_x = 0, at_wg = 0, at_wu = 0, at_d = 0, at_dx = 0, at_part = 0, bytes = 0;
+  size_t at_x = 0, at_wg = 0, at_wu = 0, at_d = 0, at_dx = 0, at_part = 0, bytes = 0, need = 0;
 };
 inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype, bool pack_x,
                                  bool pack_wg, bool pack_wu) {
@@ -323,9 +341,9 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   p.planes = grad_planes(dtype, g_dtype);
   p.x = pack_plan(rows, dim, dtype);
   p.wg = p.wu = pack_plan(dim, width, dtype);
-  if (pack_x) p.at_x = r.take(p.x.bytes);
-  if (pack_wg) p.at_wg = r.take(p.wg.bytes);
-  if (pack_wu) p.at_wu = r.take(p.wu.bytes);
+  p.at_x = r.copy(pack_x, p.x.bytes);
+  p.at_wg = r.copy(pack_wg, p.wg.bytes);
+  p.at_wu = r.copy(pack_wu, p.wu.bytes);
   p.ld_d = cdiv64(width, 64) * 64;
   p.at_d = r.take((size_t)(rows * 2 * p.ld_d * p.planes) * 2);
   p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
@@ -340,6 +358,7 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   p.at_part = r.take(std::max({p.gu.part, p.dx.part, p.dw.part, p.two_dw.part}));
   p.at_dx = p.two ? r.take(p.two_dx.part) : p.at_part;
   p.bytes = r.at;
+  p.need = r.at + r.spared;
   return p;
 }
 

@@ -57,6 +57,12 @@ struct Layout {
   }
 };
 
+// The room that a call asks for holds its plan, and hangs on sizes alone.
+static void rooms(size_t need, size_t bytes, size_t whole, bool alike, ll a, ll b, ll c) {
+  require(bytes <= whole, "room", a, b, c, bytes);
+  if (alike) require(need == whole, "room of every call", a, b, c, need);
+}
+
 static VocabPlan vocab(ll rows, ll dim, ll v, int dtype, bool px, bool pw) {
   const VocabPlan p = vocab_plan(rows, dim, v, dtype, px, pw);
   const MmaCost* cost = mma_cost(dtype == SHAMPOO_F32 ? 3 : 1);
@@ -72,6 +78,9 @@ static VocabPlan vocab(ll rows, ll dim, ll v, int dtype, bool px, bool pw) {
   l.put(p.at_stat, (size_t)(rows * p.entries) * 8, "statistics");
   l.put(p.at_target, (size_t)rows * 4, "targets");
   l.put(p.at_part, std::max(p.mma[0].part, p.mma[1].part), "parts");
+  const size_t whole = std::max(vocab_plan(rows, dim, v, dtype, true, true).bytes,
+                                dtype == SHAMPOO_F32 ? 0 : vocab_plan(rows, dim, v, dtype, true, false).bytes);
+  if (dtype == SHAMPOO_BF16 || (px && pw)) rooms(p.need, p.bytes, whole, vocab_alike(dim, v, dtype), rows, dim, v);
   require(l.end <= p.bytes, "bytes", rows, dim, v, p.bytes);
   return p;
 }
@@ -98,6 +107,10 @@ static VocabGradPlan vgrad(ll rows, ll dim, ll v, int dtype, int g, bool px, boo
   l.put(p.at_dz, (size_t)(rows * p.ld_dz * p.planes) * 2, "dz");
   l.put(p.at_dx, std::max(p.dx[0].part, p.two_dx.part), "dX");
   l.put(p.at_part, std::max({p.z[0].part, p.z[1].part, p.dw[0].part, p.dw[1].part, p.two_dw.part}), "parts");
+  const size_t whole = std::max(vocab_grad_plan(rows, dim, v, dtype, g, true, true).bytes,
+                                dtype == SHAMPOO_F32 ? 0 : vocab_grad_plan(rows, dim, v, dtype, g, true, false).bytes);
+  if (dtype == SHAMPOO_BF16 || (px && pw))
+    rooms(p.need, p.bytes, whole, vocab_grad_alike(rows, dim, v, dtype, p.planes), rows, dim, v);
   if (p.two) {
     require(p.pieces == 1, "one launch of two products", rows, dim, v, p.pieces);
     two(p.two_dx, rows, dim, v, 1, p.two_dw, v, dim, rows, p.planes, dtype);
@@ -115,6 +128,10 @@ static FfnPlan ffn(ll rows, ll dim, ll width, int dtype) {
   l.put(p.at_wu, p.wu.bytes, "wu");
   l.put(p.at_part, p.mma.part, "parts");
   require(l.end <= p.bytes, "bytes", rows, dim, width, p.bytes);
+  for (int i = 0; i < 8; ++i) {
+    const FfnPlan o = ffn_plan(rows, dim, width, dtype, i & 1, i & 2, i & 4);
+    rooms(o.need, o.bytes, p.bytes, true, rows, dim, width);
+  }
   return p;
 }
 
@@ -131,6 +148,10 @@ static FfnGradPlan fgrad(ll rows, ll dim, ll width, int dtype, int g) {
   l.put(p.at_d, (size_t)(rows * 2 * p.ld_d * p.planes) * 2, "d");
   l.put(p.at_part, std::max({p.gu.part, p.dx.part, p.dw.part, p.two_dw.part}), "parts");
   l.put(p.at_dx, p.two_dx.part, "parts of dX");
+  for (int i = 0; i < 8; ++i) {
+    const FfnGradPlan o = ffn_grad_plan(rows, dim, width, dtype, g, i & 1, i & 2, i & 4);
+    rooms(o.need, o.bytes, p.bytes, true, rows, dim, width);
+  }
   if (p.two) two(p.two_dx, rows, dim, width, 2, p.two_dw, dim, 2 * p.ld_d, rows, p.planes, dtype);
   require(l.end <= p.bytes && p.ld_d >= width && p.ld_d % 64 == 0, "bytes", rows, dim, width, p.bytes);
   return p;
@@ -172,8 +193,8 @@ int main() {
   for (int i = 0; i < 20000; ++i) {
     const ll rows = size(1 << 20), dim = size(1 << 14), v = size(1 << 20);
     const int dt = r() & 1, g = r() & 1;
-    vocab(rows, dim, v, dt, true, r() & 1);
-    vgrad(rows, dim, v, dt, g, true, r() & 1);
+    vocab(rows, dim, v, dt, r() & 1, r() & 1);
+    vgrad(rows, dim, v, dt, g, r() & 1, r() & 1);
     ffn(rows, dim, size(1 << 16), dt);
     fgrad(rows, dim, size(1 << 16), dt, g);
   }
