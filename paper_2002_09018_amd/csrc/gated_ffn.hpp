@@ -4,9 +4,10 @@
 // backward pass where they were not kept.
 //
 // What bounds them.  16 rows of 1024 x 4096 in bf16: 17 MB of weights and latency, 7.1 us
-// (a call 9.1, the host's side).  16384 rows with G and U kept: 296-305 us, 275 GFLOP at
-// 0.9 PFLOP/s and 400 MB of stores that the products of other tiles hide in part (not
-// kept, 65 us less).  Their gradient: the elementwise pass 111 us (671 MB, 6.1 TB/s), dX
+// (a call 8-9, the host's side).  16384 rows with G and U kept: 296-306 us, 275 GFLOP at
+// 0.9 PFLOP/s and 400 MB of stores, which a tile's 16 stages hide in part (without G and
+// U 280; with 64 stages to a tile 1.2 PFLOP/s).  Two workgroups of 128 x 256 on a compute
+// unit take 342 us, and 277 without G and U.  Their gradient: the elementwise pass 111 us (671 MB, 6.1 TB/s), dX
 // 236 and dWg with dWu 241 + 13 (1.15 PFLOP/s); dG and dU in the products' loads instead
 // of a pass would form each of them once per tile that reads it.
 #pragma once
