@@ -569,7 +569,8 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
  * stream reaches its end.  Matrices are row-major with any row stride of at least
  * their columns and any alignment to their element; bf16 ones whose address is a
  * multiple of 16 bytes and whose columns and stride are multiples of 8 are read as
- * they lie, others are copied into the workspace first.  Products of bf16 values
+ * they lie, others are copied into the workspace first (tables and weights of calls of
+ * few rows are not: another kernel, with another order of the sums).  Products of bf16 values
  * are exact; fp32 values are split into three bf16 terms, exactly from 2^-110 in size on
  * (below, what lies under 2^-133 is cut off), of whose nine products the six largest
  * are formed.  Sums are kept in fp32, in a fixed order: results repeat to the bit.  A

@@ -11,7 +11,7 @@ HEADERS = [os.path.join(HERE, "csrc", f) for f in ("kernels.hpp", "tile_mfma.hpp
                                                    "direct_mma.hpp", "small_root.hpp", "embedding.hpp", "handle.hpp",
                                                    "layer_plans.hpp", "logprobs.hpp", "act_checkpoint.hpp",
                                                    "weight_grad.hpp", "layer_host.hpp", "stream_plans.hpp", "stream_mma.hpp",
-                                                   "vocab_loss.hpp", "gated_ffn.hpp", "dropout.hpp")]
+                                                   "vocab_loss.hpp", "gated_ffn.hpp", "dropout.hpp", "few_rows.hpp")]
 HEADERS.append(os.path.join(ROOT, "include", "shampoo.h"))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -9,6 +9,7 @@
 #include <initializer_list>
 
 #include "dropout.hpp"
+#include "few_rows.hpp"
 #include "gated_ffn.hpp"
 #include "layer_host.hpp"
 #include "shampoo.h"
@@ -193,6 +194,25 @@ shampoo_status product(Handle* h, int cls, int planes, int shape, const MmaArgs&
   return planes == 1 ? product<LA, LB, 1, 1>(h, cls, shape, q, e, s) : product<LA, LB, 3, 3>(h, cls, shape, q, e, s);
 }
 
+// A product that reads B (of the type dtype, at any address) where it lies.
+template <typename S, int LB, typename E>
+shampoo_status few_product(Handle* h, int cls, const FewArgs& w, const E& e, hipStream_t s) {
+  auto k = few_kernel<S, LB, E>;
+  constexpr int kLds = FewShape::kLdsB + (E::kState ? FewShape::kStateB : 0);
+  static std::atomic<uint64_t> asked{0};
+  STATUS_TRY(ask_lds(h, k, kLds, asked));
+  return launch(h, cls, s, [&] {
+    hipLaunchKernelGGL(k, dim3((unsigned)groups_of(w.q)), dim3(FewShape::kThr), kLds, s, w, e);
+  });
+}
+template <int LB, typename E>
+shampoo_status few_product(Handle* h, int cls, int dtype, const FewArgs& w, const E& e, hipStream_t s) {
+  return dtype == SHAMPOO_BF16 ? few_product<uint16_t, LB>(h, cls, w, e, s) : few_product<float, LB>(h, cls, w, e, s);
+}
+FewSeg few_seg(const Planes16& a, const void* b, int64_t ldb, const void* b2 = nullptr, int64_t ldb2 = 0) {
+  return {a.p, a.plane, (int)a.ld, b, b2, ldb, ldb2};
+}
+
 // The epilogue over the parts.
 template <typename E>
 shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_t s) {
@@ -300,7 +320,7 @@ extern "C" {
 size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype) {
   if (!sizes_ok(rows, dim, vocab, kMaxVocab, dtype) || rows == 0) return 0;
   const size_t need = vocab_plan(rows, dim, vocab, dtype, true, true).need;
-  if (vocab_alike(dim, vocab, dtype)) return need;
+  if (vocab_alike(rows, dim, vocab, dtype)) return need;
   return std::max(need, vocab_plan(rows, dim, vocab, dtype, true, false).bytes);
 }
 
@@ -314,7 +334,7 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
       return fail(h, SHAMPOO_EINVAL, "X, W or lse, or one of targets and logp is NULL");
     const bool pack_x = !as_it_lies(X, ld_x, dim, dtype), pack_w = !as_it_lies(W, ld_w, dim, dtype);
     const VocabPlan p = vocab_plan(rows, dim, vocab, dtype, pack_x, pack_w);
-    const size_t need = vocab_alike(dim, vocab, dtype) ? p.need
+    const size_t need = vocab_alike(rows, dim, vocab, dtype) ? p.need
                                                        : shampoo_vocab_logprobs_workspace_bytes(rows, dim, vocab, dtype);
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(
@@ -336,13 +356,15 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     for (int64_t i = 0; i < p.pieces; ++i) {
       const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
       const MmaPlan& m = p.mma[i == p.pieces - 1];
-      STATUS_TRY(packer.take(typed(W, v0 * ld_w, dtype), n, dim, ld_w, pack_w, p.w, ws + p.at_w, &w));
+      const char* here = typed(W, v0 * ld_w, dtype);
+      STATUS_TRY(packer.take(here, n, dim, ld_w, pack_w && !p.direct, p.w, ws + p.at_w, &w));
       STATUS_TRY(packer.flush());
       MmaArgs q{};
       add_seg(q, x, w);
       use_plan(q, m, rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
       const LseEpilogue e({targets, (int)vocab, (int)v0}, stat + entry0, p.entries, z_target, (int)n);
-      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, p.x.planes, m.shape, q, e, s)));
+      if (p.direct) STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype, {q, {few_seg(x, here, ld_w)}, (int)dim}, e, s));
+      else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, p.x.planes, m.shape, q, e, s)));
       if (q.part) {
         const int64_t groups = cdiv64(rows * cdiv64(n, kStatCols), kThreads / 64);
         STATUS_TRY(launch(h, kCls, s, [&] {
@@ -414,13 +436,15 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     for (int64_t i = 0; i < p.pieces; ++i) {
       const int64_t v0 = i * p.piece, n = std::min(p.piece, vocab - v0);
       const bool last = i == p.pieces - 1;
-      STATUS_TRY(packer.take(typed(W, v0 * ld_w, dtype), n, dim, ld_w, pack_w, p.w, ws + p.at_w, &w));
+      const char* here = typed(W, v0 * ld_w, dtype);
+      STATUS_TRY(packer.take(here, n, dim, ld_w, pack_w && !p.direct, p.w, ws + p.at_w, &w));
       STATUS_TRY(packer.flush());
       MmaArgs q{};
       add_seg(q, x, w);
       use_plan(q, p.z[last], rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
       const DlogitEpilogue e({targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes);
-      STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.z[last].shape, q, e, s)));
+      if (p.direct) STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype, {q, {few_seg(x, here, ld_w)}, (int)dim}, e, s));
+      else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.z[last].shape, q, e, s)));
       if (q.part) STATUS_TRY(join(h, kCls, q, e, s));
       const OutEpilogue out(dW ? const_cast<char*>(typed(dW, v0 * ld_dw, g_dtype)) : nullptr, ld_dw, nullptr, 0, 0,
                             (int)dim, (int)dim, g_dtype == SHAMPOO_BF16, beta);
@@ -433,7 +457,8 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
         add_seg(r, pz, w);
         use_plan(r, m, rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
         r.part_add = i > 0;
-        if (!two) STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, m.shape, r, out_x, s)));
+        if (p.direct) STATUS_TRY(few_product<kLayoutK>(h, kCls, dtype, {r, {few_seg(pz, here, ld_w)}, (int)n}, out_x, s));
+        else if (!two) STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, m.shape, r, out_x, s)));
         if (i == 0) qx = r;
       }
       if (dW) {
@@ -451,7 +476,8 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
 // ---------------------------------------------------------------- feed-forward block
 size_t shampoo_gated_ffn_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype) {
   if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
-  return ffn_plan(rows, dim, width, dtype, true, true, true).need;
+  const size_t need = ffn_plan(rows, dim, width, dtype, true, true, true).need;
+  return ffn_alike(rows, dim, width, dtype, false) ? need : std::max(need, ffn_plan(rows, dim, width, dtype, true, false, false).bytes);
 }
 
 shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, const void* Wu, int dtype, int64_t rows,
@@ -469,7 +495,7 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     const bool px = !as_it_lies(X, ld_x, dim, dtype), pg = !as_it_lies(Wg, ld_wg, width, dtype);
     const bool pu = !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnPlan p = ffn_plan(rows, dim, width, dtype, px, pg, pu);
-    const size_t need = p.need;
+    const size_t need = ffn_alike(rows, dim, width, dtype, false) ? p.need : shampoo_gated_ffn_workspace_bytes(rows, dim, width, dtype);
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(h,
                                {{span(workspace, (int64_t)need), "workspace"},
@@ -487,8 +513,8 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));
-    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, &wg));
-    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, &wu));
+    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg && !p.direct, p.wg, ws + p.at_wg, &wg));
+    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu && !p.direct, p.wu, ws + p.at_wu, &wu));
     STATUS_TRY(packer.flush());
     MmaArgs q{};
     add_seg(q, x, wg, &wu);
@@ -498,7 +524,9 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
       using S = std::remove_pointer_t<decltype(type)>;
       const GatedEpilogue<S> e(act, (int)width, static_cast<S*>(H), static_cast<S*>(G), static_cast<S*>(U), ld_h, ld_g, ld_u);
       constexpr int kP = sizeof(S) == 2 ? 1 : 3;
-      st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.mma.shape, q, e, s);
+      if (p.direct)
+        st = few_product<S, kLayoutK>(h, kCls, {q, {few_seg(x, Wg, ld_wg, Wu, ld_wu)}, (int)dim}, e, s);
+      else st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.mma.shape, q, e, s);
       if (st == SHAMPOO_OK && q.part) st = join(h, kCls, q, e, s);
     });
     return st;
@@ -508,7 +536,9 @@ shampoo_status shampoo_gated_ffn(void* handle, const void* X, const void* Wg, co
 size_t shampoo_gated_ffn_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t width, int dtype, int g_dtype) {
   if (!sizes_ok(rows, dim, width, kMaxCols / 2, dtype) || rows == 0) return 0;
   if (g_dtype != SHAMPOO_F32 && g_dtype != SHAMPOO_BF16) return 0;
-  return ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, true, true).need;
+  const size_t need = ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, true, true).need;
+  if (ffn_alike(rows, dim, width, dtype, true)) return need;
+  return std::max(need, ffn_grad_plan(rows, dim, width, dtype, g_dtype, true, false, false).bytes);
 }
 
 shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* Wg, const void* Wu, int dtype,
@@ -544,7 +574,9 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     const bool pg = (!G || dX) && !as_it_lies(Wg, ld_wg, width, dtype);
     const bool pu = (!G || dX) && !as_it_lies(Wu, ld_wu, width, dtype);
     const FfnGradPlan p = ffn_grad_plan(rows, dim, width, dtype, g_dtype, px, pg, pu);
-    const size_t need = p.need;
+    const size_t need = ffn_alike(rows, dim, width, dtype, true)
+                            ? p.need
+                            : shampoo_gated_ffn_grad_workspace_bytes(rows, dim, width, dtype, g_dtype);
     STATUS_TRY(check_room(h, workspace, ws_bytes, need));
     STATUS_TRY(check_all_apart(h,
                                {{span(workspace, (int64_t)need), "workspace"},
@@ -562,8 +594,8 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     Planes16 x, wg, wu;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, px, p.x, ws + p.at_x, &x));
-    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg, p.wg, ws + p.at_wg, &wg));
-    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu, p.wu, ws + p.at_wu, &wu));
+    STATUS_TRY(packer.take(Wg, dim, width, ld_wg, pg && !p.direct, p.wg, ws + p.at_wg, &wg));
+    STATUS_TRY(packer.take(Wu, dim, width, ld_wu, pu && !p.direct, p.wu, ws + p.at_wu, &wu));
     STATUS_TRY(packer.flush());
     const int nx = p.x.planes;
     uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.at_d);
@@ -582,7 +614,9 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
         add_seg(q, x, wg, &wu);
         use_plan(q, p.gu, rows, width, dim, kLayoutRow, kLayoutK, ws + p.at_part);
         constexpr int kP = sizeof(S) == 2 ? 1 : 3;
-        st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.gu.shape, q, e, s);
+        if (p.direct)
+          st = few_product<S, kLayoutK>(h, kCls, {q, {few_seg(x, Wg, ld_wg, Wu, ld_wu)}, (int)dim}, e, s);
+        else st = product<kLayoutRow, kLayoutK, kP, kP>(h, kCls, p.gu.shape, q, e, s);
         if (st == SHAMPOO_OK && q.part) st = join(h, kCls, q, e, s);
       }
     });
@@ -598,7 +632,10 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
       add_seg(qx, du, wu);
       use_plan(qx, m, rows, dim, width, kLayoutRow, kLayoutRow, ws + (two ? p.at_dx : p.at_part));
       if (!two) {
-        STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, m.shape, qx, out_x, s)));
+        if (p.direct)
+          STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype,
+                                             {qx, {few_seg(dg, Wg, ld_wg), few_seg(du, Wu, ld_wu)}, (int)width}, out_x, s));
+        else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, m.shape, qx, out_x, s)));
         if (qx.part) STATUS_TRY(join(h, kCls, qx, out_x, s));
       }
     }

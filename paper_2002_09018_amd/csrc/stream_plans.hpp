@@ -2,14 +2,17 @@
 // work: plain host arithmetic on sizes and types.
 #pragma once
 
+#include <cmath>
+
 #include "layer_plans.hpp"
 
 namespace shp {
 
-enum { kShapeSolo = 0, kShapeFew = 1, kShapeMid = 2, kShapeBig = 3 };
+enum { kShapeSolo = 0, kShapeFew = 1, kShapeMid = 2, kShapeBig = 3, kShapeDirect = 4 };
 
 // Shapes of a product: tiles of 32 rows whose waves share the contraction (Solo), of 32
-// rows (Few; small tiles of a weight gradient), of 128 x 128, and larger ones.
+// rows (Few; small tiles of a weight gradient), of 128 x 128, and larger ones; and those of
+// few rows whose other matrix is not copied (Direct, few_rows.hpp).
 
 // How a product is cut: tiles of C, and parts of the contraction.
 struct MmaPlan {
@@ -103,6 +106,44 @@ inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, in
       p.us = mma_us(t, tiles * p.splits, p.per_split) + parts_us(p);
       if (best.us == 0 || p.us < best.us) best = p;
     }
+  }
+  return best;
+}
+
+// Whether a call reads its table or weights (so many elements) where they lie whatever
+// their type and address, once for each 32 rows, instead of copies in planes.  Both
+// measured, copies first: a block of 16 and 64 rows over 1024 x 4096 in fp32 33 and 33 us,
+// 17 and 20, with odd rows in bf16 15 and 20, 10 and 15; its gradients of 14 rows in fp32
+// 75, 57, of 40 rows 57, 58; a loss of 5 and 40 rows over 40960 x 2589 in fp32 330 and 424,
+// 167 and 249, in bf16 122, 105 (71 where rows begin at 16 bytes), but over 4096 x 2589
+// in bf16 25, 30; a loss' gradients of 64 rows over 32768 x 1024 in fp32 233, 242, of 56
+// rows in bf16 48, 81.  (Along rows a lane's 16 bytes are in a line of their own, and
+// bf16 ones mostly across two words.)
+inline bool few_direct(int64_t rows, int64_t weights, int dtype, bool along_rows, bool grad) {
+  const bool odd = dtype == SHAMPOO_BF16 && along_rows;
+  return rows <= (grad || odd ? 32 : 64) && (!odd || weights >= (1 << 24));
+}
+// Its tile; a stage is 64 bytes of a lane's row where the contraction lies along rows.
+inline MmaCost few_tile(int planes, bool along_rows) { return {32, 64, 1, 0, {0}, 4, !along_rows ? 16 : planes == 1 ? 64 : 32}; }
+
+// Such a product: the most of its memory time (of the chip, and of the compute units that
+// have a part) and of its waves' stages, and parts.
+inline MmaPlan few_plan(int64_t M, int64_t N, int64_t K, int planes, bool along_rows, int segs, bool pair,
+                        int most_splits, bool always_part) {
+  const MmaCost t = few_tile(planes, along_rows);
+  const int64_t tiles = cdiv64(M, t.m) * cdiv64(N, pair ? t.n / 2 : t.n);
+  // MB a us of a compute unit: lanes whose 16 bytes lie in lines of their own, at any
+  // address, are served one by one
+  const double each = !along_rows ? 0.04 : planes == 1 ? 0.009 : 0.012;
+  const double mb = 1e-6 * (double)(N * K) * segs * (pair ? 2 : 1) * (planes == 1 ? 2 : 4) * (double)cdiv64(M, t.m);
+  MmaPlan best;
+  for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+    if (want > cdiv64(K, t.bk) * segs || want > most_splits || (want > 1 && want * tiles > 1024)) break;
+    MmaPlan p = mma_cut(M, N, K, t, kShapeDirect, segs, pair, want, always_part);
+    const double groups = (double)(tiles * p.splits), rounds = std::ceil(groups / 256);
+    p.us = std::max(mb / std::min(4.5, each * groups), rounds * 0.6 * (double)cdiv64(p.per_split, 8)) + 4 + rounds +
+           parts_us(p);
+    if (best.us == 0 || p.us < best.us) best = p;
   }
   return best;
 }
@@ -201,6 +242,7 @@ constexpr int kStatCols = 512;  // 8 of a lane
 // The loss: pieces of the vocabulary (one, where the table is read as it lies).
 struct VocabPlan {
   int64_t piece = 0, pieces = 0, entries = 0;  // entries: statistics of a row
+  bool direct = false;                         // the table is read where it lies by few_rows.hpp
   MmaPlan mma[2];  // of a whole piece and of the last
   PackPlan x, w;
   size_t at_x = 0, at_w = 0, at_stat = 0, at_target = 0, at_part = 0, bytes = 0, need = 0;
@@ -208,18 +250,20 @@ struct VocabPlan {
 inline int64_t vocab_entries(const MmaPlan& p, int64_t n) { return p.part ? cdiv64(n, kStatCols) : p.tiles_n; }
 
 // Whether the table is cut the same way copied or not.
-inline bool vocab_alike(int64_t dim, int64_t vocab, int dtype) {
-  return dtype == SHAMPOO_F32 || vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) == vocab;
+inline bool vocab_alike(int64_t rows, int64_t dim, int64_t vocab, int dtype) {
+  return dtype == SHAMPOO_F32 || (!few_direct(rows, vocab * dim, dtype, true, false) && vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) == vocab);
 }
 inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, bool pack_x, bool pack_w) {
   VocabPlan p;
   Room r;
   p.x = pack_plan(rows, dim, dtype);
   p.at_x = r.copy(pack_x, p.x.bytes);
-  p.piece = pack_w ? vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) : vocab;
+  const bool few = few_direct(rows, vocab * dim, dtype, true, false), copy_w = pack_w && !few;
+  p.direct = pack_w && few;
+  p.piece = copy_w ? vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) : vocab;
   p.pieces = cdiv64(vocab, p.piece);
   p.w = pack_plan(p.piece, dim, dtype);
-  p.at_w = r.copy(pack_w, p.w.bytes);
+  if (!few) p.at_w = r.copy(copy_w, p.w.bytes);
   const int64_t last = vocab - (p.pieces - 1) * p.piece;
   size_t part = 0;
   for (int i = 0; i < 2; ++i) {
@@ -227,7 +271,9 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
       p.mma[1] = p.mma[0];
       break;
     }
-    p.mma[i] = mma_plan(rows, i ? last : p.piece, dim, mma_cost(p.x.planes), 1, false, kShapeFew, 64, false);
+    const int64_t n = i ? last : p.piece;
+    p.mma[i] = p.direct ? few_plan(rows, n, dim, p.x.planes, true, 1, false, 64, false)
+                        : mma_plan(rows, n, dim, mma_cost(p.x.planes), 1, false, kShapeFew, 64, false);
     part = std::max(part, p.mma[i].part);
   }
   p.entries = (p.pieces - 1) * vocab_entries(p.mma[0], p.piece) + vocab_entries(p.mma[1], last);
@@ -242,7 +288,8 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
 // Its gradient: the logits of a piece, its share of dX, its rows of dW.
 struct VocabGradPlan {
   int64_t piece = 0, pieces = 0, ld_dz = 0;
-  int planes = 1;  // bf16 terms of the logits' gradient
+  int planes = 1;       // bf16 terms of the logits' gradient
+  bool direct = false;  // as above
   MmaPlan z[2], dx[2], dw[2];
   bool two = false;  // dX and dW in one launch, where both are wanted, cut as follows
   MmaPlan two_dx, two_dw;
@@ -257,7 +304,7 @@ inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || 
 
 inline bool vocab_grad_alike(int64_t rows, int64_t dim, int64_t vocab, int dtype, int planes) {
   return dtype == SHAMPOO_F32 ||
-         vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) >= vocab_piece(vocab, rows * planes * 2);
+         (!few_direct(rows, vocab * dim, dtype, true, true) && vocab_piece(vocab, pack_plan(1, dim, dtype).bytes) >= vocab_piece(vocab, rows * planes * 2));
 }
 inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype, int g_dtype, bool pack_x,
                                      bool pack_w) {
@@ -267,10 +314,12 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
   p.x = pack_plan(rows, dim, dtype);
   p.at_x = r.copy(pack_x, p.x.bytes);
   p.piece = vocab_piece(vocab, rows * p.planes * 2);
-  if (pack_w) p.piece = std::min(p.piece, vocab_piece(vocab, pack_plan(1, dim, dtype).bytes));
+  const bool few = few_direct(rows, vocab * dim, dtype, true, true), copy_w = pack_w && !few;
+  p.direct = pack_w && few;
+  if (copy_w) p.piece = std::min(p.piece, vocab_piece(vocab, pack_plan(1, dim, dtype).bytes));
   p.pieces = cdiv64(vocab, p.piece);
   p.w = pack_plan(p.piece, dim, dtype);
-  p.at_w = r.copy(pack_w, p.w.bytes);
+  if (!few) p.at_w = r.copy(copy_w, p.w.bytes);
   p.ld_dz = cdiv64(p.piece, 64) * 64;
   p.at_dz = r.take((size_t)(rows * p.ld_dz * p.planes) * 2);
   size_t part = 0;
@@ -284,12 +333,18 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
       break;
     }
     const MmaCost* cost = mma_cost(p.x.planes);
-    p.z[i] = mma_plan(rows, n, dim, cost, 1, false, kShapeSolo, 64, false);
-    p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, i ? p.dx[0].splits : 64, p.pieces > 1);
+    const int most = i ? p.dx[0].splits : 64;
+    if (p.direct) {
+      p.z[i] = few_plan(rows, n, dim, p.x.planes, true, 1, false, 64, false);
+      p.dx[i] = few_plan(rows, dim, n, p.x.planes, false, 1, false, most, p.pieces > 1);
+    } else {
+      p.z[i] = mma_plan(rows, n, dim, cost, 1, false, kShapeSolo, 64, false);
+      p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, most, p.pieces > 1);
+    }
     p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
     part = std::max({part, p.z[i].part, p.dw[i].part});
   }
-  if (p.pieces == 1 && p.planes == p.x.planes) {
+  if (!p.direct && p.pieces == 1 && p.planes == p.x.planes) {
     const TwoPlan t = two_plan(p.dx[0], rows, dim, vocab, 1, p.dw[0], vocab, dim, rows, p.planes);
     p.two = t.on;
     p.two_dx = t.x;
@@ -305,18 +360,28 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
 // The feed-forward block.
 struct FfnPlan {
   MmaPlan mma;
+  bool direct = false;  // the weights are read where they lie by few_rows.hpp
   PackPlan x, wg, wu;
   size_t at_x = 0, at_wg = 0, at_wu = 0, at_part = 0, bytes = 0, need = 0;
 };
+// Whether the products are cut the same way for weights copied or not.
+inline bool ffn_alike(int64_t rows, int64_t dim, int64_t width, int dtype, bool grad) {
+  return dtype == SHAMPOO_F32 || !few_direct(rows, 2 * dim * width, dtype, grad, grad);
+}
 inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, bool pack_x, bool pack_wg, bool pack_wu) {
   FfnPlan p;
   Room r;
   p.x = pack_plan(rows, dim, dtype);
   p.wg = p.wu = pack_plan(dim, width, dtype);
+  const bool few = few_direct(rows, 2 * dim * width, dtype, false, false);
+  p.direct = few && (dtype == SHAMPOO_F32 || pack_wg || pack_wu);
   p.at_x = r.copy(pack_x, p.x.bytes);
-  p.at_wg = r.copy(pack_wg, p.wg.bytes);
-  p.at_wu = r.copy(pack_wu, p.wu.bytes);
-  p.mma = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
+  if (!few) {
+    p.at_wg = r.copy(pack_wg, p.wg.bytes);
+    p.at_wu = r.copy(pack_wu, p.wu.bytes);
+  }
+  p.mma = p.direct ? few_plan(rows, width, dim, p.x.planes, false, 1, true, 64, false)
+                   : mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
   p.at_part = r.take(p.mma.part);
   p.bytes = r.at;
   p.need = r.at + r.spared;
@@ -327,7 +392,7 @@ inline FfnPlan ffn_plan(int64_t rows, int64_t dim, int64_t width, int dtype, boo
 // one product.
 struct FfnGradPlan {
   MmaPlan gu, dx, dw;
-  bool two = false;  // as above
+  bool direct = false, two = false;  // as above
   MmaPlan two_dx, two_dw;
   PackPlan x, wg, wu;
   int64_t ld_d = 0;
@@ -341,15 +406,24 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   p.planes = grad_planes(dtype, g_dtype);
   p.x = pack_plan(rows, dim, dtype);
   p.wg = p.wu = pack_plan(dim, width, dtype);
+  const bool few = few_direct(rows, 2 * dim * width, dtype, true, true);
+  p.direct = few && (dtype == SHAMPOO_F32 || pack_wg || pack_wu);
   p.at_x = r.copy(pack_x, p.x.bytes);
-  p.at_wg = r.copy(pack_wg, p.wg.bytes);
-  p.at_wu = r.copy(pack_wu, p.wu.bytes);
+  if (!few) {
+    p.at_wg = r.copy(pack_wg, p.wg.bytes);
+    p.at_wu = r.copy(pack_wu, p.wu.bytes);
+  }
   p.ld_d = cdiv64(width, 64) * 64;
   p.at_d = r.take((size_t)(rows * 2 * p.ld_d * p.planes) * 2);
-  p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
-  p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false);
+  if (p.direct) {
+    p.gu = few_plan(rows, width, dim, p.x.planes, false, 1, true, 64, false);
+    p.dx = few_plan(rows, dim, width, p.x.planes, true, 2, false, 64, false);
+  } else {
+    p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
+    p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false);
+  }
   p.dw = mma_plan(dim, 2 * p.ld_d, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
-  if (p.planes == p.x.planes) {
+  if (!p.direct && p.planes == p.x.planes) {
     const TwoPlan t = two_plan(p.dx, rows, dim, width, 2, p.dw, dim, 2 * p.ld_d, rows, p.planes);
     p.two = t.on;
     p.two_dx = t.x;

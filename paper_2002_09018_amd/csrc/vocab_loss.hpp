@@ -103,6 +103,32 @@ struct LseEpilogue : UnitEpilogue<LseEpilogue> {
       if (m0 + r < q.M) stat[(int64_t)(m0 + r) * ld_stat + tn] = a;
     }
   }
+
+  // The same of a tile of few rows, whose waves hold shares of the contraction: 8 lanes to
+  // a row of 64 columns.
+  template <typename T, typename Core>
+  __device__ __forceinline__ void few(const MmaArgs& q, const Core& core, lds_char* lds, int m0, int n0, int tn) const {
+    mma_rows_out<T>(core.acc[0], lds + (threadIdx.x >> 6) * T::kRingB, threadIdx.x & 63);
+    __syncthreads();
+    const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+    if (r >= T::TM) return;
+    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < T::kSolo; ++w) lds_add8(z, lds + w * T::kRingB + r * T::kPitch + c * 4);
+    const int at = m0 + r < q.M ? t.at(m0 + r) - n0 - c : -1;
+    f32x2p a = {kLowest, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (n0 + c + i >= q.N) z[i] = -INFINITY;
+      else if (i == at) z_target[m0 + r] = z[i];
+      a[0] = fmaxf(a[0], z[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[1] += lse_exp(z[i] - a[0]);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) a = ms_join(a, f32x2p{__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64)});
+    if (c == 0 && m0 + r < q.M) stat[(int64_t)(m0 + r) * ld_stat + tn] = a;
+  }
 };
 
 // (m, s) of kStatCols columns of a row of logits that were formed in parts: a wave

@@ -183,8 +183,8 @@ def test_vocab_grad_options(env, dtype, g_dtype):
 
 
 # sizes whose logits' gradient, or whose packed table, takes several pieces
-PIECES = [(8192, 64, 20000, "bfloat16"), (8192, 64, 6000, "float32"), (3, 4096, 33000, "bfloat16"),
-          (3, 4096, 11000, "float32")]
+PIECES = [(8192, 64, 20000, "bfloat16"), (8192, 64, 6000, "float32"), (70, 4096, 33000, "bfloat16"),
+          (70, 4096, 11000, "float32")]
 
 
 @pytest.mark.parametrize("n,d,v,dtype", PIECES)
@@ -205,7 +205,11 @@ VOCAB_MORE = [(6109, 3490, 72, "bfloat16", "bfloat16", True), (4951, 1163, 408, 
               (2608, 241, 4626, "bfloat16", "float32", True), (843, 1928, 1991, "bfloat16", "float32", True),
               (922, 196, 31249, "bfloat16", "float32", True), (5525, 80, 14027, "float32", "bfloat16", True),
               (130, 3330, 23888, "bfloat16", "float32", True), (4870, 136, 17995, "bfloat16", "bfloat16", False),
-              (6903, 914, 15369, "bfloat16", "float32", True), (1098, 165, 3544, "bfloat16", "bfloat16", True)]
+              (6903, 914, 15369, "bfloat16", "float32", True), (1098, 165, 3544, "bfloat16", "bfloat16", True),
+              (1, 1903, 10, "float32", "bfloat16", True), (65, 359, 9, "float32", "float32", True),
+              (1445, 1406, 18, "float32", "bfloat16", True), (50, 1003, 5001, "bfloat16", "float32", True),
+              (64, 100, 30001, "float32", "float32", True), (9, 439, 39541, "bfloat16", "float32", True),
+              (32, 4099, 4999, "bfloat16", "bfloat16", True)]
 
 
 @pytest.mark.parametrize("n,d,v,dtype,g_dtype,copied", VOCAB_MORE)
@@ -259,11 +263,12 @@ def test_vocab_no_rows(env):
         assert bool((dW == 0).all())
 
 
-def test_vocab_far_offsets(env):
+@pytest.mark.parametrize("d", [4096, 4095])
+def test_vocab_far_offsets(env, d):
     """A table of more than 2^31 elements: rows at its end."""
     import oracle.model_oracle as M
     torch, B, dev, h = env
-    n, d, v = 3, 4096, 524400
+    n, v = 3, 524500
     say("vocab far", n, d, v)
     gen = torch.Generator(device=dev).manual_seed(1)
     W = torch.empty(v, d, device=dev, dtype=torch.bfloat16)
@@ -408,7 +413,12 @@ FFN_MORE = [(1, 1718, 1871, "float32", "float32"), (1, 3508, 1348, "bfloat16", "
             (1441, 2247, 731, "float32", "bfloat16"), (4932, 884, 2504, "bfloat16", "float32"),
             (7880, 75, 269, "float32", "bfloat16"), (688, 3745, 3026, "bfloat16", "float32"),
             (5349, 2491, 844, "bfloat16", "bfloat16"), (992, 723, 2295, "bfloat16", "float32"),
-            (7392, 845, 1327, "bfloat16", "float32"), (1154, 103, 436, "bfloat16", "bfloat16")]
+            (7392, 845, 1327, "bfloat16", "float32"), (1154, 103, 436, "bfloat16", "bfloat16"),
+            (76, 8, 10, "float32", "bfloat16"), (82, 8, 412, "float32", "bfloat16"), (90, 949, 8, "float32", "float32"),
+            (1, 657, 1128, "bfloat16", "bfloat16"), (1, 2940, 392, "bfloat16", "bfloat16"),
+            (68, 87, 2972, "float32", "float32"), (84, 1204, 330, "float32", "bfloat16"),
+            (50, 1337, 1003, "bfloat16", "bfloat16"), (64, 130, 5000, "float32", "float32"),
+            (11, 2243, 4039, "bfloat16", "float32"), (32, 2243, 4039, "bfloat16", "bfloat16")]
 
 
 @pytest.mark.parametrize("n,d,w,dtype,g_dtype", FFN_MORE)
@@ -422,7 +432,9 @@ def test_gated_ffn_tiles(env, n, d, w, dtype, g_dtype):
 
 def test_weights_of_different_strides(env):
     """Wg and Wu in rows of different lengths, and one that is read as it lies beside one
-    that is copied: the bits of the plain call."""
+    that is not: the bits of the plain call.  (Few bf16 rows have two ways through the
+    weights, by whether both lie as the matrix cores take them: bits of its own each, the
+    projections of both within their sums' error and a rounding.)"""
     torch, B, dev, h = env
     for n, d, w in ((3, 64, 136), (40, 72, 1000), (700, 256, 520), (3000, 512, 2056)):
         for dt in (torch.bfloat16, torch.float32):
@@ -440,9 +452,15 @@ def test_weights_of_different_strides(env):
                 B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, B.ACT_SILU, dX=out[3], dWg=out[4], dWu=out[5], workspace=gws)
                 got.append(out)
             torch.cuda.synchronize()
-            for other in got[1:]:
-                for a, b in zip(got[0], other):
-                    assert torch.equal(a, b)
+            two = n <= 64 and dt is torch.bfloat16
+            for i, other in enumerate(got[1:], 1):
+                for a, b in zip(got[2 if two and i > 2 else 0], other):
+                    assert torch.equal(a, b) or (two and i == 2)
+            if two:
+                for a, b, m in ((got[0][1], got[2][1], g), (got[0][2], got[2][2], u)):
+                    # either is the exact sum within e, rounded
+                    e = U * (20 + d ** 0.5) * (X.double().abs() @ m.double().abs())
+                    close(a, b.double(), 2 * e + HALF * (2 * b.double().abs() + 4 * e), "projection")
 
 
 @pytest.mark.parametrize("dtype,g_dtype", [("bfloat16", "bfloat16"), ("float32", "float32")])
