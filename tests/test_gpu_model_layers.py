@@ -725,3 +725,31 @@ def test_two_streams_and_repeats(env):
         got = [b[6], b[5], b[8], b[11], b[12], b[13], b[14]]
         for x, y in zip(got, want):
             assert torch.equal(x, y)
+
+
+def test_a_small_workspace_is_named(env):
+    """The binding leaves the size to the library and says what is missing."""
+    torch, B, dev, h = env
+    n, d, w = 70, 24, 40
+    X, g, u, dH = (normal(env, i, *s) for i, s in ((1, (n, d)), (2, (d, w)), (3, (d, w)), (4, (n, w))))
+    W, t = normal(env, 5, w, d), torch.zeros(n, device=dev, dtype=torch.int32)
+    lse, logp = torch.zeros(n, device=dev), torch.zeros(n, device=dev)
+    H, dX, dW, dg, du = (torch.empty_like(x) for x in (dH, X, W, g, u))
+    f = torch.float32
+    for need, call in (
+            (B.shampoo_vocab_logprobs_workspace_bytes(n, d, w, f),
+             lambda ws: B.shampoo_vocab_logprobs(h, X, W, t, logp, lse, workspace=ws)),
+            (B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, w, f, f),
+             lambda ws: B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX, dW=dW, g_logp=logp, workspace=ws)),
+            (B.shampoo_gated_ffn_workspace_bytes(n, d, w, f), lambda ws: B.shampoo_gated_ffn(h, X, g, u, H, workspace=ws)),
+            (B.shampoo_gated_ffn_grad_workspace_bytes(n, d, w, f, f),
+             lambda ws: B.shampoo_gated_ffn_grad(h, X, g, u, dH, dX=dX, dWg=dg, dWu=du, workspace=ws))):
+        assert need > 0
+        with pytest.raises(ValueError, match="at least"):
+            call(torch.empty(need - 1, device=dev, dtype=torch.uint8))
+        with pytest.raises(ValueError, match="needed"):
+            call(None)
+        with pytest.raises(ValueError, match="uint8"):
+            call(torch.empty(need, device=dev))
+        call(torch.empty(need, device=dev, dtype=torch.uint8))
+    torch.cuda.synchronize()
