@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) inline void lse_join_kernel(int64_t rows,
 // without a target), lse and the target's column.  One term (of bf16 inputs with bf16
 // gradients) rounds each dz once, half a step of 2^-8 of it: what a bf16 tensor of
 // logits' gradients holds, beside the result's own rounding of the same size, so that
-// errors are up to sqrt(2) times those of the result's rounding alone (0.0024 and
+// errors are about sqrt(2) times those of the result's rounding alone (0.0024 and
 // 0.0017 of the norm).  A second term would double both products that read dz.
 struct DlogitEpilogue : UnitEpilogue<DlogitEpilogue> {
   static constexpr bool kState = true;
