@@ -589,7 +589,7 @@ shampoo_status shampoo_act_weight_grad(void* handle, const void* ckpt, int64_t r
  * Errors: EINVAL (NULL pointers, rows outside [0, 2^31), dim outside [1, 2^20],
  * vocab outside [1, 2^30], strides, dtype, a workspace not aligned to 16, outputs or
  * workspace that overlap another buffer), ENOMEM (workspace too small), EUNSUPPORTED
- * (a product of more than 2^22 tiles).
+ * (a product of 2^22 tiles or more).
  */
 size_t shampoo_vocab_logprobs_workspace_bytes(int64_t rows, int64_t dim, int64_t vocab, int dtype);
 shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W, int dtype, int64_t rows, int64_t dim,

@@ -345,8 +345,6 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
     char* ws = static_cast<char*>(workspace);
     constexpr int kCls = SHAMPOO_KCLASS_VOCAB;
     STATUS_TRY(check_tiles(h, {p.mma[0], p.mma[1]}));
-    if (rows * cdiv64(p.piece, kStatCols) / (kThreads / 64) >= kMostTiles)
-      return fail(h, SHAMPOO_EUNSUPPORTED, "%lld rows", (long long)rows);
     Planes16 x, w;
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
@@ -366,9 +364,8 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
       if (p.direct) STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype, {q, {few_seg(x, here, ld_w)}, (int)dim}, e, s));
       else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, p.x.planes, m.shape, q, e, s)));
       if (q.part) {
-        const int64_t groups = cdiv64(rows * cdiv64(n, kStatCols), kThreads / 64);
         STATUS_TRY(launch(h, kCls, s, [&] {
-          hipLaunchKernelGGL(logit_stat_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, q, e);
+          hipLaunchKernelGGL(logit_stat_kernel, dim3((unsigned)stat_groups(rows, n)), dim3(kThreads), 0, s, q, e);
         }));
       }
       entry0 += vocab_entries(m, n);

@@ -238,6 +238,9 @@ inline int64_t vocab_piece(int64_t vocab, int64_t bytes_each) {
 // Columns of a row of logits whose statistics are one entry, where the logits were
 // formed in parts.
 constexpr int kStatCols = 512;  // 8 of a lane
+// Workgroups of the launch that forms them, four waves to one.  Any piece fits: parts are
+// taken for at most 1024 tiles, 2^16 such groups.
+inline int64_t stat_groups(int64_t rows, int64_t n) { return cdiv64(rows * cdiv64(n, kStatCols), 4); }
 
 // The loss: pieces of the vocabulary (one, where the table is read as it lies).
 struct VocabPlan {

@@ -1,0 +1,34 @@
+"""Host check of what a call of the loss from the last activations refuses
+(stream_plans.hpp, compiled for the host): products of 2^22 tiles or more, and nothing
+else, wherever the table lies.  No GPU is used."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CXX = shutil.which("g++") or (HIPCC if os.path.exists(HIPCC) else None)
+
+
+def test_many_logits_are_taken(tmp_path):
+    if CXX is None:
+        pytest.skip("no C++ compiler")
+    exe = str(tmp_path / "stream_limits_check")
+    cmd = [CXX, "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2002_09018_amd", "csrc"),
+           "-I", os.path.join(ROOT, "include"), os.path.join(HERE, "stream_limits_check.cpp"), "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+    sizes = [(65536, 1024, 131072), (32768, 1024, 262144), (16384, 1024, 524288), (16777216, 1024, 512),
+             (32768, 8, 262144), (4200000, 8, 2000)]
+    lines = [(n, d, v, t, c) for n, d, v in sizes for t in (0, 1) for c in (0, 1)]
+    # 256 x 256 tiles: one fewer than 2^22 (2047 2049 of them), and 2^22
+    lines += [(2047 * 256, 64, 2049 * 256, 1, 0), (2048 * 256, 64, 2048 * 256, 1, 0)]
+    r = subprocess.run([exe], input="\n".join(" ".join(map(str, x)) for x in lines) + "\n", capture_output=True,
+                       text=True, timeout=300)
+    out = r.stdout.split("\n")
+    assert r.returncode == 0 and out[len(lines):] == ["ok", ""], r.stdout[-2000:]
+    for x, line in zip(lines, out):
+        assert int(line.split()[0]) == (x != lines[-1]), (x, line)
