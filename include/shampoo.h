@@ -605,8 +605,9 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
  * dX or dW may be NULL.  The logits are formed again, in pieces of the vocabulary.
  * dz is kept in three bf16 terms where dtype or g_dtype is fp32 (dX of bf16 inputs takes
  * the first), else in one.  g_dtype counts without dW too.  The order of dX's sums may
- * differ between calls with dW and without.  A row whose gradients are all 0 adds nothing
- * to dW if X and lse are finite there.  rows == 0: dW = beta dW.
+ * differ between calls with dW and without.  A row whose gradients are all 0 has
+ * dz = 0 whatever W and lse hold, and adds nothing to dW if X is finite there.  rows == 0:
+ * dW = beta dW.
  * Errors: as above, EINVAL for a non-finite beta, g_logp without targets, or neither dX nor
  * dW.
  */

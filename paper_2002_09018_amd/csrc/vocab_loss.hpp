@@ -220,10 +220,14 @@ struct DlogitEpilogue : UnitEpilogue<DlogitEpilogue> {
       for (int i = 0; i < 8; ++i)
         if (i == at) z[i] += g;
     }
-    if (col + 8 > N || l == -INFINITY) {  // columns past the last, and rows of nothing
+    // columns past the last, and rows of nothing: without entries, or without gradients (those
+    // of a padded batch, whose lse may hold anything: exp may be infinite there, and 0 times
+    // it a NaN that the products would carry to other rows)
+    const bool nothing = l == -INFINITY || (c == 0.f && g == 0.f);
+    if (col + 8 > N || nothing) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (col + i >= N || l == -INFINITY) z[i] = 0.f;
+        if (col + i >= N || nothing) z[i] = 0.f;
     }
     uint16_t* d = dz + row * ld + col;
     if (planes == 1) {

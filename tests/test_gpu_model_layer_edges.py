@@ -31,3 +31,55 @@ def test_many_logits(env, n, d, v):
         close(lse[rows], rl, tol, "lse")
         close(logp[rows], rp, 2 * tol + U * rp.abs() * 4, "logp")
         assert bool(torch.isfinite(lse).all()) and bool((logp <= 0).all())
+
+
+# ------------------------------------------------------------------ rows without gradients
+TYPE_PAIRS = [("bfloat16", "bfloat16"), ("bfloat16", "float32"), ("float32", "float32"), ("float32", "bfloat16")]
+# tiles of few rows, middling and large ones, a contraction in parts, tables read as they lie and copied
+ROWS = [(5, 64, 300, 0), (5, 1003, 1001, 3), (40, 72, 1001, 3), (300, 128, 1500, 0), (130, 3330, 700, 5),
+        (1100, 256, 4100, 0)]
+
+
+@pytest.mark.parametrize("dtype,g_dtype", TYPE_PAIRS)
+def test_rows_without_gradients_add_nothing(env, dtype, g_dtype):
+    """Padding rows, whose gradients are 0: whatever their lse holds (zeros where it was
+    never formed, though their logits lie beyond what exp holds), their dX is 0 and the
+    other results are those of the call with their true lse, to the bit.  With no row
+    that has a gradient, dW is 0 whatever the table holds."""
+    torch, B, dev, h = env
+    dt, gt = getattr(torch, dtype), getattr(torch, g_dtype)
+    for n, d, v, pad in ROWS:
+        say("rows without gradients", n, d, v, dtype, g_dtype, pad)
+        x = normal(env, 1, n, d)
+        dead = torch.arange(n, device=dev) % 3 == 0
+        x[dead] *= 64
+        X = Sheet(env, n, d, dt, pad, pad, x).v
+        W = Sheet(env, v, d, dt, pad, pad, normal(env, 2, v, d) * (2.0 / d ** 0.5)).v
+        z = X.double() @ W.double().t().contiguous()
+        assert float(z[dead].amax(1).min()) > 100
+        lse = torch.logsumexp(z, 1).float()
+        t = torch.randint(0, v, (n,), generator=torch.Generator(device=dev).manual_seed(3), device=dev, dtype=torch.int32)
+        g_logp, g_lse = normal(env, 4, n), normal(env, 5, n)
+        t[::6] = -1        # dead rows without a token, whose g_logp counts for nothing
+        g_logp[3::6] = 0   # and with one
+        g_lse[dead] = 0
+        ws = room(env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, v, dt, gt))
+
+        def grads(lse, gl, gs, table=W):
+            dX, dW = torch.full((n, d), 7.0, device=dev, dtype=dt), torch.full((v, d), 7.0, device=dev, dtype=gt)
+            B.shampoo_vocab_logprobs_grad(h, X, table, t, lse, dX=dX, dW=dW, g_logp=gl, g_lse=gs, workspace=ws)
+            torch.cuda.synchronize()
+            return dX, dW
+        want = grads(lse, g_logp, g_lse)
+        assert bool(torch.isfinite(want[0]).all()) and bool(torch.isfinite(want[1]).all())
+        for held in (0.0, -3e38, float("nan"), float("inf"), -float("inf")):
+            other = lse.clone()
+            other[dead] = held
+            got = grads(other, g_logp, g_lse)
+            assert bool((got[0][dead] == 0).all()), held
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), held
+        bad = W.clone()
+        bad[0, 0], bad[-1, 0] = float("nan"), float("inf")
+        none = torch.zeros(n, device=dev)
+        for gl, gs in ((none, none), (none, None), (None, none), (None, None)):
+            assert bool((grads(lse, gl, gs, bad)[1] == 0).all())
