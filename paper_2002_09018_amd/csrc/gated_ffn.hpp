@@ -55,23 +55,24 @@ struct GatedEpilogue : UnitEpilogue<GatedEpilogue<S>> {
   }
 };
 
-// dG = dH o U o act'(G) and dU = dH o act(G), in one or three bf16 terms with zeros up
+// dG = dH o U o act'(G) and dU = dH o act(G), in P = one or three bf16 terms with zeros up
 // to a multiple of 8 columns.  One term (of bf16 inputs with bf16 gradients) rounds each
-// once to bf16, as a tensor of that type between the layers would; fp32 gradients take
-// three, exact.
-template <typename S>
-struct GatedGradEpilogue : UnitEpilogue<GatedGradEpilogue<S>> {
+// once to bf16, as a tensor of that type between the layers would, and takes the
+// activations' short forms, whose errors are 2^-7 of that rounding; fp32 gradients take
+// three, exact, of the activations as exact as fp32 passes have them.
+template <typename S, int P>
+struct GatedGradEpilogue : UnitEpilogue<GatedGradEpilogue<S, P>> {
   static constexpr bool kPair = true;
-  int act, N, planes;
+  int act, N;
   const S* dH;
   int64_t ld_dh;
   uint16_t *dG, *dU;  // M x ld
   int64_t ld, plane;
 
-  GatedGradEpilogue(int a, int n, int np, const S* h, int64_t lh, uint16_t* g, uint16_t* u, int64_t l, int64_t pl)
-      : act(a), N(n), planes(np), dH(h), ld_dh(lh), dG(g), dU(u), ld(l), plane(pl) {}
+  GatedGradEpilogue(int a, int n, const S* h, int64_t lh, uint16_t* g, uint16_t* u, int64_t l, int64_t pl)
+      : act(a), N(n), dH(h), ld_dh(lh), dG(g), dU(u), ld(l), plane(pl) {}
   __device__ __forceinline__ void put(uint16_t* d, const float (&x)[8]) const {
-    if (planes == 1) {
+    if constexpr (P == 1) {
       ActVec<uint16_t> v;
       v.set(x);
       gstore<u32x4u>(d, v.raw[0]);
@@ -90,8 +91,8 @@ struct GatedGradEpilogue : UnitEpilogue<GatedGradEpilogue<S>> {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bool in = col + i < N;
-        const float h = d.at(i), slope = act_slope<kAct, sizeof(S) == 2>(g[i]);
-        const float value = act_value<kAct, sizeof(S) == 2>(g[i]);
+        const float h = d.at(i), slope = act_slope<kAct, P == 1>(g[i]);
+        const float value = act_value<kAct, P == 1>(g[i]);
         g[i] = in ? h * u[i] * slope : 0.f;
         u[i] = in ? h * value : 0.f;
       }
@@ -102,10 +103,10 @@ struct GatedGradEpilogue : UnitEpilogue<GatedGradEpilogue<S>> {
 };
 
 // The same from projections that were kept.
-template <typename S>
+template <typename S, int P>
 __global__ __launch_bounds__(kThreads) void gated_grad_kernel(ActShape h, const S* __restrict__ G, int64_t ld_g,
                                                              const S* __restrict__ U, int64_t ld_u,
-                                                             GatedGradEpilogue<S> e) {
+                                                             GatedGradEpilogue<S, P> e) {
   act_units(h, [&](int64_t row, int unit, bool in) {
     const int n = h.cols - unit * 8;
     if (!in || n <= 0) return;

@@ -262,6 +262,15 @@ shampoo_status weight_product(Handle* h, int cls, int x_planes, int d_planes, in
   return q.part ? join(h, cls, q, e, s) : SHAMPOO_OK;
 }
 
+// Calls f with a null pointer of the type of the inputs and the number of bf16 terms of a
+// gradient between products (grad_planes): fp32 inputs always have three.
+template <typename F>
+void with_terms(int dtype, int terms, F&& f) {
+  if (dtype == SHAMPOO_F32) f((float*)nullptr, std::integral_constant<int, 3>());
+  else if (terms == 3) f((uint16_t*)nullptr, std::integral_constant<int, 3>());
+  else f((uint16_t*)nullptr, std::integral_constant<int, 1>());
+}
+
 shampoo_status scaled(Handle* h, int cls, void* C, int dtype, int64_t rows, int64_t cols, int64_t ld, float beta,
                       hipStream_t s) {
   return launch(h, cls, s, [&] {
@@ -598,13 +607,15 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
     uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.at_d);
     const Planes16 dg{d, 2 * p.ld_d, rows * 2 * p.ld_d}, du{d + p.ld_d, dg.ld, dg.plane};
     shampoo_status st = SHAMPOO_OK;
-    with_type(dtype, [&](auto* type) {
+    with_terms(dtype, p.planes, [&](auto* type, auto terms) {
       using S = std::remove_pointer_t<decltype(type)>;
-      const GatedGradEpilogue<S> e(act, (int)width, p.planes, static_cast<const S*>(dH), ld_dh, d, d + p.ld_d, dg.ld, dg.plane);
+      constexpr int kTerms = decltype(terms)::value;
+      const GatedGradEpilogue<S, kTerms> e(act, (int)width, static_cast<const S*>(dH), ld_dh, d, d + p.ld_d, dg.ld,
+                                           dg.plane);
       if (G) {
         st = unit_launches(h, kCls, rows, width, p.ld_d / 8, s, [&](const ActShape& sh, dim3 grid) {
-          hipLaunchKernelGGL(gated_grad_kernel<S>, grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(G), ld_g,
-                             static_cast<const S*>(U), ld_u, e);
+          hipLaunchKernelGGL((gated_grad_kernel<S, kTerms>), grid, dim3(kThreads), 0, s, sh, static_cast<const S*>(G),
+                             ld_g, static_cast<const S*>(U), ld_u, e);
         });
       } else {
         MmaArgs q{};

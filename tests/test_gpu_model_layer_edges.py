@@ -83,3 +83,54 @@ def test_rows_without_gradients_add_nothing(env, dtype, g_dtype):
         none = torch.zeros(n, device=dev)
         for gl, gs in ((none, none), (none, None), (None, none), (None, None)):
             assert bool((grads(lse, gl, gs, bad)[1] == 0).all())
+
+
+# ------------------------------------------------------------------ fp32 gradients of bf16 inputs
+def tanh_gelu(torch, x):
+    """Value, slope and |w| of gelu's tanh form x p, p = 1 / (1 + e^-w), w = 2 sqrt(2 / pi) (x +
+    0.044715 x^3).  1 + tanh(w / 2) = 2 p, but that sum loses all bits of p below 2^-53, where
+    the library's fp32 still has 24 of them (x = -8: p = 3e-22)."""
+    c = 2 * (2 / torch.pi) ** 0.5
+    w = c * (x + 0.044715 * x ** 3)
+    p, q = torch.sigmoid(w), torch.sigmoid(-w)
+    return x * p, p + x * p * q * c * (1 + 3 * 0.044715 * x * x), w.abs()
+
+
+@pytest.mark.parametrize("keep", [True, False])
+@pytest.mark.parametrize("act", ["RELU", "GELU", "GELU_TANH", "SILU"])
+def test_fp32_block_gradients_are_fp32(env, act, keep):
+    """Rows of X that are unit vectors: G and U are rows of the weights, dWg and dWu are dG
+    and dU, element by element (the other terms of their sums are zeros).  With fp32
+    gradients their errors are those of fp32, of bf16 inputs too: u (16 + x^2) (1 + x^2)
+    relative to 1 for an activation's slope, u (16 + x^2) of its value, and 4 u for the
+    products and the terms' 2^-24.  The value of gelu's tanh form is off by u (16 + 7 |w|):
+    w is two rounded constants and five rounded operations, none of which cancels, and an
+    error dw of it is one of (1 - p) dw <= |dw| relative in p = 1 / (1 + e^-w).  Values below
+    2^-126 and terms below 2^-133 may vanish: 2^-120 of the factors."""
+    import oracle.model_oracle as M
+    torch, B, dev, h = env
+    kind = getattr(B, "ACT_" + act)
+    for n, d, w, pad in ((1, 1, 9, 0), (5, 40, 200, 3), (30, 30, 264, 0), (200, 264, 520, 0), (1100, 1104, 1500, 5)):
+        for dt in (torch.bfloat16, torch.float32):
+            say("fp32 block gradients", n, d, w, dt, act, keep)
+            X = Sheet(env, n, d, dt, pad, pad, torch.eye(n, d, device=dev)).v
+            Wg = Sheet(env, d, w, dt, pad, pad, 2.5 * normal(env, 1, d, w)).v
+            Wu = Sheet(env, d, w, dt, pad, pad, normal(env, 2, d, w)).v
+            dH = Sheet(env, n, w, dt, pad, pad, normal(env, 3, n, w)).v
+            dX = torch.empty(n, d, device=dev, dtype=dt)
+            dWg, dWu = (torch.full((d, w), 7.0, device=dev) for _ in range(2))
+            B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, kind, Wg[:n] if keep else None, Wu[:n] if keep else None, dX, dWg,
+                                     dWu, workspace=room(env, B.shampoo_gated_ffn_grad_workspace_bytes(
+                                         n, d, w, dt, torch.float32)))
+            torch.cuda.synchronize()
+            g, u = Wg[:n].double(), Wu[:n].double()
+            hh, far = dH.double().abs(), g * g
+            a, s = M.act(g, kind), M.slope(g, kind)
+            if act == "GELU_TANH":
+                a, s, far = tanh_gelu(torch, g)
+                far = 7 * far
+            dG, dU = dH.double() * u * s, dH.double() * a
+            least = 2.0 ** -120 * (1 + hh * (1 + u.abs()))
+            close(dWg[:n], dG, hh * u.abs() * U * (16 + g * g) * (1 + g * g) + 4 * U * dG.abs() + least, "dG")
+            close(dWu[:n], dU, hh * U * (16 + far) * a.abs() + 4 * U * dU.abs() + least, "dU")
+            assert bool((dWg[n:] == 0).all()) and bool((dWu[n:] == 0).all())
