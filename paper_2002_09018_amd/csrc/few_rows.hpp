@@ -51,11 +51,13 @@ struct FewStage {
   static constexpr int kBk = 16 * kTogether, kDepth = LB == kLayoutRow ? 2 : sizeof(S) == 2 ? 4 : 2;
 };
 
-// What a lane loads for one stage.
-template <typename S, int LB>
+// What a lane loads for one stage: P planes of B, PA of A (more than B's one of a gradient in
+// terms).
+template <typename S, int LB, int PA_>
 struct FewLoads {
-  static constexpr int P = sizeof(S) == 2 ? 1 : 3, T = FewStage<S, LB>::kTogether;
-  u32x4 a[T][P];
+  static constexpr int P = sizeof(S) == 2 ? 1 : 3, PA = PA_, T = FewStage<S, LB>::kTogether;
+  static_assert(PA >= P, "");
+  u32x4 a[T][PA];
   ActVec<S> row[LB == kLayoutRow ? 2 : 1][T];
   S col[LB == kLayoutRow ? 1 : 2][8];
 
@@ -87,9 +89,9 @@ struct FewCore {
   static constexpr int wm = 0, wn = 0;
 };
 
-template <typename S, int LB, bool PAIR>
+template <typename S, int LB, bool PAIR, int PA>
 __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0, int n0, int split) {
-  using L = FewLoads<S, LB>;
+  using L = FewLoads<S, LB, PA>;
   constexpr int P = L::P, T = L::T, kDepth = FewStage<S, LB>::kDepth, kBk = FewStage<S, LB>::kBk;
   const MmaArgs& q = w.q;
   const int lane = threadIdx.x & 63, half = (lane >> 5) * 8 * T;
@@ -140,7 +142,7 @@ __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0,
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int p = 0; p < P; ++p) l.a[t][p] = *reinterpret_cast<const u32x4*>(pa + p * plane + k0 + t * 8);
+        for (int p = 0; p < PA; ++p) l.a[t][p] = *reinterpret_cast<const u32x4*>(pa + p * plane + k0 + t * 8);
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -158,7 +160,7 @@ __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0,
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
+        for (int p = 0; p < PA; ++p) {
           l.a[t][p] = u32x4{0, 0, 0, 0};
           if (t * 8 < n) l.a[t][p] = *reinterpret_cast<const u32x4*>(pa + p * plane + k0 + t * 8);
         }
@@ -172,13 +174,14 @@ __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0,
     }
   };
 
-  wg_acc small[P == 3 ? 2 : 1];
+  constexpr bool kTwo = PA > 1;  // sums of the small pairs of planes
+  wg_acc small[kTwo ? 2 : 1];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int v = 0; v < 16; ++v) core.acc[0][j][v] = 0.f;
 #pragma unroll
-  for (int j = 0; j < (P == 3 ? 2 : 1); ++j) small[j] = core.acc[0][j];
+  for (int j = 0; j < (kTwo ? 2 : 1); ++j) small[j] = core.acc[0][j];
   L l[kDepth];
 #pragma unroll
   for (int d = 0; d < kDepth; ++d) load(l[d]);
@@ -188,26 +191,28 @@ __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0,
     for (int d = 0; d < kDepth; ++d) {
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        bf16x8 fa[P], fb[2][P];
+        bf16x8 fa[PA], fb[2][P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) fa[p] = __builtin_bit_cast(bf16x8, l[d].a[t][p]);
+        for (int p = 0; p < PA; ++p) fa[p] = __builtin_bit_cast(bf16x8, l[d].a[t][p]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) l[d].planes(j, t, fb[j]);
         // pairs of planes by size, the smallest first and in a sum of their own
 #pragma unroll
-        for (int r = P - 1; r >= 0; --r)
+        for (int r = PA - 1; r >= 0; --r)
 #pragma unroll
-          for (int p = 0; p <= r; ++p)
+          for (int p = 0; p <= r; ++p) {
+            if (r - p >= P) continue;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              wg_acc& c = P == 3 && r > 0 ? small[P == 3 ? j : 0] : core.acc[0][j];
+              wg_acc& c = kTwo && r > 0 ? small[kTwo ? j : 0] : core.acc[0][j];
               c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][r - p], fa[p], c, 0, 0, 0);
             }
+          }
       }
       load(l[d]);
     }
   }
-  if constexpr (P == 3) {
+  if constexpr (kTwo) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -216,7 +221,8 @@ __device__ __forceinline__ void few_run(const FewArgs& w, FewCore& core, int m0,
 }
 
 template <typename S, int LB, typename E>
-__global__ __launch_bounds__(FewShape::kThr, sizeof(S) == 2 && LB == kLayoutK ? 4 : 2) void few_kernel(FewArgs w, E e) {
+__global__ __launch_bounds__(FewShape::kThr, sizeof(S) == 2 && LB == kLayoutK && E::kTerms == 1 ? 4 : 2) void few_kernel(
+    FewArgs w, E e) {
   extern __shared__ __align__(16) char lds_bytes[];
   using T = FewShape;
   lds_char* lds = (lds_char*)lds_bytes;
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(FewShape::kThr, sizeof(S) == 2 && LB == kLayoutK ? 
       *(lds_f32x4*)(state + r * 16) = m0 + r < q.M ? e.state(m0 + r) : f32x4{0.f, 0.f, 0.f, 0.f};
   }
   FewCore core;
-  few_run<S, LB, E::kPair>(w, core, m0, n0, split);
+  few_run<S, LB, E::kPair, sizeof(S) == 4 ? 3 : E::kTerms>(w, core, m0, n0, split);
   if constexpr (E::kWhole) {
     if (!q.part) {
       e.template few<T>(q, core, lds, m0, n0, tn);

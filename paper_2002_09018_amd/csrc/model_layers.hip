@@ -222,6 +222,22 @@ shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_
   });
 }
 
+// dX = D B of a gradient D that is kept in d_planes terms: as many as B has planes, or three
+// beside a B of one, of which kDxTerms count.  What was cut is left in q.part.
+template <int LB>
+shampoo_status dx_product(Handle* h, int cls, int planes, int d_planes, int shape, const MmaArgs& q,
+                          const OutEpilogue& e, hipStream_t s) {
+  if (d_planes == planes) return product<kLayoutRow, LB>(h, cls, planes, shape, q, e, s);
+  return product<kLayoutRow, LB, 1, 1>(h, cls, shape, q, OutTermsEpilogue(e), s);
+}
+template <int LB>
+shampoo_status few_dx_product(Handle* h, int cls, int dtype, int d_planes, const FewArgs& w, const OutEpilogue& e,
+                              hipStream_t s) {
+  if (dtype == SHAMPOO_F32) return few_product<float, LB>(h, cls, w, e, s);
+  return d_planes == 1 ? few_product<uint16_t, LB>(h, cls, w, e, s)
+                       : few_product<uint16_t, LB>(h, cls, w, OutTermsEpilogue(e), s);
+}
+
 // dX and the weights' gradient in one launch, and what was cut of them in another.
 template <int LB, int P>
 shampoo_status two_products(Handle* h, int cls, const MmaArgs& x, const OutEpilogue& ex, const MmaArgs& w,
@@ -457,14 +473,14 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
       const bool two = p.two && dX && dW;
       MmaArgs qw{};
       if (dX) {
-        // a bf16 dX takes the first term alone
         const MmaPlan& m = two ? p.two_dx : p.dx[last];
         MmaArgs r{};
         add_seg(r, pz, w);
         use_plan(r, m, rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
         r.part_add = i > 0;
-        if (p.direct) STATUS_TRY(few_product<kLayoutK>(h, kCls, dtype, {r, {few_seg(pz, here, ld_w)}, (int)n}, out_x, s));
-        else if (!two) STATUS_TRY((product<kLayoutRow, kLayoutK>(h, kCls, nx, m.shape, r, out_x, s)));
+        if (p.direct)
+          STATUS_TRY(few_dx_product<kLayoutK>(h, kCls, dtype, p.planes, {r, {few_seg(pz, here, ld_w)}, (int)n}, out_x, s));
+        else if (!two) STATUS_TRY(dx_product<kLayoutK>(h, kCls, nx, p.planes, m.shape, r, out_x, s));
         if (i == 0) qx = r;
       }
       if (dW) {
@@ -641,9 +657,9 @@ shampoo_status shampoo_gated_ffn_grad(void* handle, const void* X, const void* W
       use_plan(qx, m, rows, dim, width, kLayoutRow, kLayoutRow, ws + (two ? p.at_dx : p.at_part));
       if (!two) {
         if (p.direct)
-          STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype,
-                                             {qx, {few_seg(dg, Wg, ld_wg), few_seg(du, Wu, ld_wu)}, (int)width}, out_x, s));
-        else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, m.shape, qx, out_x, s)));
+          STATUS_TRY(few_dx_product<kLayoutRow>(
+              h, kCls, dtype, p.planes, {qx, {few_seg(dg, Wg, ld_wg), few_seg(du, Wu, ld_wu)}, (int)width}, out_x, s));
+        else STATUS_TRY(dx_product<kLayoutRow>(h, kCls, nx, p.planes, m.shape, qx, out_x, s));
         if (qx.part) STATUS_TRY(join(h, kCls, qx, out_x, s));
       }
     }

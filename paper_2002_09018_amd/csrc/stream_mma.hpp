@@ -8,7 +8,9 @@
 // p2 exactly); a stage holds all planes of both operands, and each 16 contraction
 // indices are multiplied for the pairs of planes that count (six of nine, or three
 // where the other operand has one), the smallest first.  A sum of two products (dG
-// Wg^T + dU Wu^T) is two segments of one long contraction.
+// Wg^T + dU Wu^T) is two segments of one long contraction.  Two terms of A with a B of one
+// plane (dX of bf16 inputs from a gradient in three) are the contraction in two rounds, a
+// term each, the smaller first: tiles and stages stay those of one plane.
 //
 // Staging.  Stages of kBk = 64 or 32 contraction indices go from memory to LDS
 // without passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a
@@ -58,6 +60,7 @@
 #include "act_checkpoint.hpp"
 #include "layer_plans.hpp"
 #include "split_mfma.hpp"
+#include "stream_plans.hpp"
 #include "tile_mfma.hpp"
 #include "weight_grad.hpp"
 
@@ -191,9 +194,11 @@ __device__ __forceinline__ void mma_tile(int t, int tiles_m, int tiles_n, int& t
   tn = in / rows;
 }
 
-// The accumulators of one wave after all stages of its part.
-template <typename T, int LA, int LB, bool PAIR>
+// The accumulators of one wave after all stages of its part, in ROUNDS rounds over the planes
+// of an A that is read as if it had one.
+template <typename T, int LA, int LB, bool PAIR, int ROUNDS = 1>
 struct MmaCore {
+  static_assert(ROUNDS == 1 || T::PA + T::PB == 2, "");
   static constexpr int kWa = T::TM < 128 ? T::TM : 128, kWb = PAIR ? T::TN / 2 : T::TN < 128 ? T::TN : 128;
   wg_acc acc[T::kBm][T::kBn];
   int wm, wn;  // first row of the wave in the tile, and number of its column strip
@@ -238,7 +243,8 @@ struct MmaCore {
     constexpr bool kShared = T::kSolo == 0;
 
     // where the next stage to be loaded lies
-    int seg = first / q.seg_stages, at = first % q.seg_stages, left = stages;
+    int seg = first / q.seg_stages, at = first % q.seg_stages, left = stages * ROUNDS;
+    [[maybe_unused]] int in_round = stages, term = ROUNDS - 1;
     const char *pa, *pb, *pb2;
     int64_t step_a, step_b, step_b2, plane_a, plane_b, plane_b2;  // bytes
     MmaLoader<LA, kWa, T::kBk, T::kLoadsA, T::kWaves> la;
@@ -256,6 +262,7 @@ struct MmaCore {
       pa = reinterpret_cast<const char*>(s.a) + (LA == kLayoutRow ? (int64_t)m0 * s.lda : m0) * 2 + at * step_a;
       pb = reinterpret_cast<const char*>(s.b) + (LB == kLayoutRow ? (int64_t)n0 * s.ldb : n0) * 2 + at * step_b;
       if (PAIR) pb2 = reinterpret_cast<const char*>(s.b2) + (int64_t)n0 * 2 + at * step_b2;
+      if constexpr (ROUNDS > 1) pa += term * plane_a;
       la.template init<false>(m0, q.M, s.lda, wave, lane);
       lb.template init<PAIR>(n0, q.N, s.ldb, wave, lane);
       if (PAIR && s.ldb2 != s.ldb) {
@@ -284,6 +291,16 @@ struct MmaCore {
     };
     auto advance = [&] {
       --left;
+      if constexpr (ROUNDS > 1) {
+        if (--in_round == 0 && left > 0) {  // the next round
+          seg = first / q.seg_stages;
+          at = first % q.seg_stages;
+          in_round = stages;
+          --term;
+          open();
+          return;
+        }
+      }
       if (++at == q.seg_stages && left > 0) {
         ++seg;
         at = 0;
@@ -377,7 +394,7 @@ struct MmaCore {
     for (int k = 0; k < kFrags; ++k) read_one(lds, 0, k);
     issue(lds + (T::kBufs - 1) * T::kStageB);
 #pragma unroll 1
-    for (int s = 0; s < stages; ++s) {
+    for (int s = 0; s < stages * ROUNDS; ++s) {
       lds_char* now = lds + cur;
       cur = cur == (T::kBufs - 1) * T::kStageB ? 0 : cur + T::kStageB;
 #pragma unroll
@@ -503,6 +520,7 @@ __device__ __forceinline__ void mma_units(const MmaArgs& q, const Core& core, ld
 template <typename E>
 struct UnitEpilogue {
   static constexpr bool kPair = false, kWhole = false, kState = false;
+  static constexpr int kTerms = 1;  // planes of A that count, where B has one
   template <int N>
   __device__ __forceinline__ void units(int row, int step, int M, const f32x4 (&st)[N], int col, float (&x)[N][8],
                                         float (&y)[N][8]) const {
@@ -531,7 +549,7 @@ __device__ __forceinline__ void mma_body(const MmaArgs& q, const E& e, lds_char*
         *(lds_f32x4*)(state + r * 16) = m0 + r < q.M ? e.state(m0 + r) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  MmaCore<T, LA, LB, E::kPair> core;
+  MmaCore<T, LA, LB, E::kPair, E::kTerms> core;
   core.run(q, lds, m0, n0, split, states);
   if constexpr (E::kWhole && T::kSolo == 0) {
     if (!q.part) {
@@ -680,6 +698,12 @@ struct OutEpilogue : UnitEpilogue<OutEpilogue> {
     if (bf16) put<uint16_t>(row, col, x);
     else put<float>(row, col, x);
   }
+};
+
+// The same of several of A's terms.
+struct OutTermsEpilogue : OutEpilogue {
+  static constexpr int kTerms = kDxTerms;
+  explicit OutTermsEpilogue(const OutEpilogue& e) : OutEpilogue(e) {}
 };
 
 // C = beta C.

@@ -93,9 +93,9 @@ inline double parts_us(const MmaPlan& p) {
 }
 
 // The cheapest tile and number of parts (at most most_splits) by estimated time.  `segs`
-// products of one contraction length are summed.
+// products of one contraction length are summed, each stage taken in so many rounds.
 inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, int segs, bool pair, int least_shape,
-                        int most_splits, bool always_part) {
+                        int most_splits, bool always_part, int rounds = 1) {
   MmaPlan best;
   for (int i = least_shape; i <= kShapeBig; ++i) {
     const MmaCost& t = cost[i];
@@ -103,7 +103,7 @@ inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, in
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (want > cdiv64(K, t.bk) * segs || want > most_splits || (want > 1 && want * tiles > 1024)) break;
       MmaPlan p = mma_cut(M, N, K, t, i, segs, pair, want, always_part);
-      p.us = mma_us(t, tiles * p.splits, p.per_split) + parts_us(p);
+      p.us = mma_us(t, tiles * p.splits, (int64_t)p.per_split * rounds) + parts_us(p);
       if (best.us == 0 || p.us < best.us) best = p;
     }
   }
@@ -304,6 +304,20 @@ struct VocabGradPlan {
 // would keep 9 bits, with two 17.  A bf16 one takes dz as the framework stores a
 // bf16 gradient of logits, rounded once.
 inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || g_dtype == SHAMPOO_F32 ? 3 : 1; }
+// Terms that dX of bf16 inputs takes of a gradient that is kept in three for an fp32 dW: two
+// are off by 2^-16, 2^-8 of what dX itself is rounded by.  One, measured, was off by as much
+// as that rounding (0.0024 of the norm for 0.0017) and by more than the result where its
+// terms cancel; the third is a third product for nothing that bf16 shows (whole calls
+// with one, two and three: 2048 x 1024 over 32768 712, 830 and 925 us, 16384 rows through
+// 1024 x 4096 1167, 1420 and 1637).
+constexpr int kDxTerms = 2;
+// What its product takes, in rounds of one term: one for each, but of few rows, where the
+// other matrix is in the caches by the second, one (counted twice, more and smaller parts
+// would be cut: 64 x 1024 over 32768 96 and 103 us, 16 and 64 rows through 1024 x 4096 31
+// and 36, 34 and 36; 700 x 768 x 5000, counted once and twice, 98 and 91).
+inline int dx_rounds(int64_t rows, int planes, int terms) {
+  return planes == 1 && terms == 3 && rows > 64 ? kDxTerms : 1;
+}
 
 inline bool vocab_grad_alike(int64_t rows, int64_t dim, int64_t vocab, int dtype, int planes) {
   return dtype == SHAMPOO_F32 ||
@@ -342,7 +356,7 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
       p.dx[i] = few_plan(rows, dim, n, p.x.planes, false, 1, false, most, p.pieces > 1);
     } else {
       p.z[i] = mma_plan(rows, n, dim, cost, 1, false, kShapeSolo, 64, false);
-      p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, most, p.pieces > 1);
+      p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, most, p.pieces > 1, dx_rounds(rows, p.x.planes, p.planes));
     }
     p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
     part = std::max({part, p.z[i].part, p.dw[i].part});
@@ -423,7 +437,8 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
     p.dx = few_plan(rows, dim, width, p.x.planes, true, 2, false, 64, false);
   } else {
     p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
-    p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false);
+    p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false,
+                    dx_rounds(rows, p.x.planes, p.planes));
   }
   p.dw = mma_plan(dim, 2 * p.ld_d, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
   if (!p.direct && p.planes == p.x.planes) {

@@ -4,7 +4,7 @@ inputs, non-finite values.  Tolerances as in test_gpu_model_layers."""
 import pytest
 
 from tests.gpu_util import say
-from tests.test_gpu_model_layers import HALF, U, Sheet, close, env, logprobs, normal, room  # noqa: F401
+from tests.test_gpu_model_layers import HALF, U, Sheet, close, env, logprobs, normal, room, z_error  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -134,3 +134,68 @@ def test_fp32_block_gradients_are_fp32(env, act, keep):
             close(dWg[:n], dG, hh * u.abs() * U * (16 + g * g) * (1 + g * g) + 4 * U * dG.abs() + least, "dG")
             close(dWu[:n], dU, hh * U * (16 + far) * a.abs() + 4 * U * dU.abs() + least, "dU")
             assert bool((dWg[n:] == 0).all()) and bool((dWu[n:] == 0).all())
+
+
+# sizes that reach every tile of dX, whole and in parts and in pieces of the vocabulary
+# (test_stream_limits checks that): rows, dim, vocabulary or width, whether matrices are copied
+VOCAB_TERMS = [(1, 8, 8, 1), (66, 8, 960, 1), (739, 645, 10, 1), (746, 15, 1321, 1), (698, 1434, 175, 1),
+               (7566, 387, 6018, 1), (1374, 10, 1886, 1), (6716, 8, 7080, 1), (3139, 3318, 8, 1), (7614, 1408, 5862, 0),
+               (5404, 170, 4120, 1), (4175, 160, 14388, 1), (5, 3996, 4210, 1)]
+FFN_TERMS = [(1, 8, 8, 1), (68, 10, 481, 1), (831, 611, 8, 0), (341, 68, 936, 1), (1256, 778, 104, 0), (1502, 8, 791, 1),
+             (4474, 2420, 12, 1), (2789, 129, 4045, 1), (1, 3200, 2657, 1), (30, 2243, 40, 1)]
+
+
+@pytest.mark.parametrize("n,d,v,copied", VOCAB_TERMS)
+def test_dx_takes_the_terms_of_dz(env, n, d, v, copied):
+    """bf16 dX beside an fp32 dW: of dz in two terms, each within 2^-8 of what it stands
+    for, so off by 2^-16 of dz, and rounded once, 2^-8 of the result."""
+    import oracle.model_oracle as M
+    torch, B, dev, h = env
+    bf, pad = torch.bfloat16, 5 if copied else 0
+    say("terms of dz", n, d, v, pad)
+    X = Sheet(env, n, d, bf, pad, pad, normal(env, 1, n, d)).v
+    W = Sheet(env, v, d, bf, pad, pad, normal(env, 2, v, d) * (2.0 / d ** 0.5)).v
+    t = torch.randint(-1, v, (n,), generator=torch.Generator(device=dev).manual_seed(3), device=dev, dtype=torch.int32)
+    g_logp, g_lse = normal(env, 4, n), normal(env, 5, n)
+    _, lse, z = M.vocab_logprobs(X, W, t)
+    lse = lse.float()
+    dX, dW = Sheet(env, n, d, bf, pad, pad), torch.empty(v, d, device=dev)
+    B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX.v, dW=dW, g_logp=g_logp, g_lse=g_lse, workspace=room(
+        env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, v, bf, torch.float32)))
+    torch.cuda.synchronize()
+    dz, size = M.vocab_dlogits(z, lse, t, g_logp, g_lse)
+    far = (z_error(X, W) + U * (4 + (z - lse.double().unsqueeze(1)).abs().amax(1))).unsqueeze(1)
+    # two rounds of a sum: its roundings add up like those of twice the length
+    part = (far * size + (2.0 ** -16 + U * (20 + (2 * v) ** 0.5)) * dz.abs()) @ W.double().abs()
+    ref = dz @ W.double()
+    close(dX.v, ref, part + HALF * (ref.abs() + part), "dX")
+    assert dX.intact(torch)
+
+
+@pytest.mark.parametrize("n,d,w,copied", FFN_TERMS)
+def test_dx_takes_the_terms_of_the_block(env, n, d, w, copied):
+    """The same of dG and dU, of projections as kept."""
+    import oracle.model_oracle as M
+    torch, B, dev, h = env
+    bf, pad = torch.bfloat16, 5 if copied else 0
+    X = Sheet(env, n, d, bf, pad, pad, normal(env, 1, n, d)).v
+    Wg, Wu = (Sheet(env, d, w, bf, pad, pad, normal(env, i, d, w) / d ** 0.5).v for i in (2, 3))
+    dH, G, Uo = (Sheet(env, n, w, bf, pad, pad, normal(env, i, n, w)).v for i in (4, 5, 6))
+    for act in ("NONE", "GELU", "SILU"):
+        say("terms of dG and dU", n, d, w, pad, act)
+        kind = getattr(B, "ACT_" + act)
+        dX = Sheet(env, n, d, bf, pad, pad)
+        dWg, dWu = (torch.empty(d, w, device=dev) for _ in range(2))
+        B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, kind, G, Uo, dX.v, dWg, dWu, workspace=room(
+            env, B.shampoo_gated_ffn_grad_workspace_bytes(n, d, w, bf, torch.float32)))
+        torch.cuda.synchronize()
+        g, u, hh = G.double(), Uo.double(), dH.double().abs()
+        dG, dU = M.gated_grad(g, u, dH, kind)
+        f = U * (16 + g * g)
+        q = 2.0 ** -16 + U * (20 + (4 * w) ** 0.5)
+        fg = hh * u.abs() * f * (1 + g * g) + (4 * U + q) * dG.abs()
+        fu = hh * f * M.act(g, kind).abs() + (4 * U + q) * dU.abs()
+        wg, wu = Wg.double().t().contiguous(), Wu.double().t().contiguous()
+        ref, err = dG @ wg + dU @ wu, fg @ wg.abs() + fu @ wu.abs()
+        close(dX.v, ref, err + HALF * (ref.abs() + err), "dX")
+        assert dX.intact(torch)

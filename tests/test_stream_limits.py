@@ -1,11 +1,15 @@
-"""Host check of what a call of the loss from the last activations refuses
-(stream_plans.hpp, compiled for the host): products of 2^22 tiles or more, and nothing
-else, wherever the table lies.  No GPU is used."""
+"""Host checks of the rules in stream_plans.hpp, compiled for the host.  What a call of the
+loss from the last activations refuses: products of 2^22 tiles or more, and nothing else,
+wherever the table lies.  The GPU tests' sizes reach every product that forms dX of bf16
+inputs from a gradient in terms.  No GPU is used."""
 import os
 import shutil
 import subprocess
 
 import pytest
+
+from tests import test_gpu_model_layer_edges as edges
+from tests.test_stream_plans import ask, drawn  # noqa: F401
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -32,3 +36,19 @@ def test_many_logits_are_taken(tmp_path):
     assert r.returncode == 0 and out[len(lines):] == ["ok", ""], r.stdout[-2000:]
     for x, line in zip(lines, out):
         assert int(line.split()[0]) == (x != lines[-1]), (x, line)
+
+
+def dx_kernels(ask, kind, sizes):  # noqa: F811
+    """{(tile, in parts, in pieces of the vocabulary)} of dX, sizes (rows, dim, n, copied)."""
+    at = (3, 9) if kind == "vgrad" else (2,)
+    found = set()
+    for b in ask([f"{kind} %d %d %d 1 0 %d" % x for x in sizes]):
+        found |= {(b[i], b[i + 1] > 1, kind == "vgrad" and b[0] > 1) for i in at}
+    return found
+
+
+@pytest.mark.parametrize("kind,tested,top", [("vgrad", edges.VOCAB_TERMS, 40000), ("fgrad", edges.FFN_TERMS, 8192)])
+def test_sizes_reach_every_dx_of_terms(ask, kind, tested, top):  # noqa: F811
+    tested = [x for x in tested if x[3] or (x[1] if kind == "vgrad" else x[2]) % 8 == 0]
+    some = [x[:3] + (x[5],) for x in drawn(9, 20000, top)]
+    assert not dx_kernels(ask, kind, some) - dx_kernels(ask, kind, tested)
