@@ -199,3 +199,146 @@ def test_dx_takes_the_terms_of_the_block(env, n, d, w, copied):
         ref, err = dG @ wg + dU @ wu, fg @ wg.abs() + fu @ wu.abs()
         close(dX.v, ref, err + HALF * (ref.abs() + err), "dX")
         assert dX.intact(torch)
+
+
+# ------------------------------------------------------------------ non-finite values, ends of the range
+# tiles of few rows (as it lies, and through registers), small, middling and large tiles, contraction in parts
+FFN_ROWS = [(3, 64, 136, 0), (5, 100, 200, 3), (40, 72, 1000, 8), (300, 128, 520, 3), (100, 3001, 64, 1), (2100, 264, 2056, 0)]
+
+
+def same_but(torch, a, b, rows, cols, what):
+    """a equals b to the bit outside the given rows and columns (None: none), where it is not finite."""
+    on = torch.zeros(a.shape, dtype=torch.bool, device=a.device)
+    if rows is not None:
+        on[rows] = True
+    if cols is not None:
+        on[:, cols] = True
+    assert not bool(torch.isfinite(a[on]).any()), what
+    assert torch.equal(a[~on], b[~on]), what
+
+
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("dtype,g_dtype", TYPE_PAIRS)
+def test_non_finite_values_in_the_block(env, dtype, g_dtype, bad):
+    """A NaN or an infinity reaches what its products reach, and nothing else: one in row r
+    of X row r of the projections; one in column c of Wg column c of G and H; one in dH[r, c]
+    row r of dX and column c of dWg and dWu."""
+    torch, B, dev, h = env
+    dt, gt, bad = getattr(torch, dtype), getattr(torch, g_dtype), float(bad)
+    for n, d, w, pad in FFN_ROWS:
+        say("non-finite block", n, d, w, dtype, g_dtype, bad, pad)
+        r, c, k = n // 2, w // 3, d // 2
+        X = Sheet(env, n, d, dt, pad, pad, normal(env, 1, n, d) + 3).v
+        Wg, Wu = (Sheet(env, d, w, dt, pad, pad, normal(env, i, d, w) / d ** 0.5).v for i in (2, 3))
+        dH = Sheet(env, n, w, dt, pad, pad, normal(env, 4, n, w)).v
+        fw = room(env, B.shampoo_gated_ffn_workspace_bytes(n, d, w, dt))
+        gw = room(env, B.shampoo_gated_ffn_grad_workspace_bytes(n, d, w, dt, gt))
+
+        def forward():
+            out = [torch.empty(n, w, device=dev, dtype=dt) for _ in range(3)]
+            B.shampoo_gated_ffn(h, X, Wg, Wu, out[0], B.ACT_NONE, out[1], out[2], workspace=fw)
+            torch.cuda.synchronize()
+            return out
+
+        def grads(keep):
+            out = [torch.empty(n, d, device=dev, dtype=dt)] + [torch.empty(d, w, device=dev, dtype=gt) for _ in range(2)]
+            B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, B.ACT_SILU, keep and keep[1], keep and keep[2], *out, workspace=gw)
+            torch.cuda.synchronize()
+            return out
+        want = forward()
+        for keep in (want, None):
+            ref, old = grads(keep), dH[r, c].clone()
+            dH[r, c] = bad
+            got = grads(keep)
+            dH[r, c] = old
+            same_but(torch, got[0], ref[0], [r], None, "dX")
+            same_but(torch, got[1], ref[1], None, [c], "dWg")
+            same_but(torch, got[2], ref[2], None, [c], "dWu")
+        old = X[r, k].clone()
+        X[r, k] = bad
+        for a, b, what in zip(forward(), want, ("H", "G", "U")):
+            same_but(torch, a, b, [r], None, what)
+        X[r, k] = old
+        Wg[k, c] = bad
+        got = forward()
+        same_but(torch, got[0], want[0], None, [c], "H")
+        same_but(torch, got[1], want[1], None, [c], "G")
+        assert torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("dtype,g_dtype", TYPE_PAIRS)
+def test_non_finite_values_in_the_gradient_of_the_loss(env, dtype, g_dtype):
+    """A NaN or an infinity in g_logp[r] reaches row r of dX, and dW; one in X[r, k], of a row
+    without gradients, column k of dW; the rest is as it was, to the bit."""
+    torch, B, dev, h = env
+    dt, gt = getattr(torch, dtype), getattr(torch, g_dtype)
+    for n, d, v, pad in ROWS:
+        say("non-finite loss gradient", n, d, v, dtype, g_dtype, pad)
+        r, k = n // 2, d // 2
+        X = Sheet(env, n, d, dt, pad, pad, normal(env, 1, n, d)).v
+        W = Sheet(env, v, d, dt, pad, pad, normal(env, 2, v, d) * (2.0 / d ** 0.5)).v
+        t = torch.randint(0, v, (n,), generator=torch.Generator(device=dev).manual_seed(3), device=dev, dtype=torch.int32)
+        _, lse = logprobs(env, X, W, t)
+        g = normal(env, 4, n)
+        ws = room(env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, v, dt, gt))
+
+        def grads():
+            dX, dW = torch.empty(n, d, device=dev, dtype=dt), torch.empty(v, d, device=dev, dtype=gt)
+            B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX, dW=dW, g_logp=g, workspace=ws)
+            torch.cuda.synchronize()
+            return dX, dW
+        g[r] = 0
+        want = grads()
+        old = X[r, k].clone()
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            X[r, k] = bad
+            got = grads()
+            assert torch.equal(got[0], want[0]) and bool((got[0][r] == 0).all())
+            same_but(torch, got[1], want[1], None, [k], "dW")
+            X[r, k] = old
+            g[r] = bad
+            got = grads()
+            same_but(torch, got[0], want[0], [r], None, "dX")
+            assert not bool(torch.isfinite(got[1]).any())
+            g[r] = 0
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_ends_of_the_range(env, dtype):
+    """Products of small values with large ones.  bf16 values are exact down to the smallest,
+    2^-133; fp32 ones have three terms that end there, so a value x is off by 2^-134 at most,
+    beside the products' own errors, and is exact from 2^-110 on.  The largest values below
+    2^128 - 2^119 stay finite, those from there on become infinite in fp32."""
+    torch, B, dev, h = env
+    dt = getattr(torch, dtype)
+    for n, d, w, pad in FFN_ROWS:
+        for small in (-90, -104, -112, -120, -126, -130):
+            say("ends of the range", n, d, w, dtype, small, pad)
+            x = normal(env, 1, n, d) * 2.0 ** 8
+            X = Sheet(env, n, d, dt, pad, pad, torch.ldexp(x, torch.tensor(small - 8, device=dev))).v
+            Wg, Wu = (Sheet(env, d, w, dt, pad, pad, normal(env, i, d, w) * 2.0 ** 100).v for i in (2, 3))
+            H, G, Uo = (torch.empty(n, w, device=dev, dtype=dt) for _ in range(3))
+            ws = room(env, B.shampoo_gated_ffn_workspace_bytes(n, d, w, dt))
+            B.shampoo_gated_ffn(h, X, Wg, Wu, H, B.ACT_NONE, G, Uo, workspace=ws)
+            torch.cuda.synchronize()
+            for got, m in ((G, Wg), (Uo, Wu)):
+                ref, size = X.double() @ m.double(), X.double().abs() @ m.double().abs()
+                cut = 0.0 if dt is torch.bfloat16 else 2.0 ** -134 * m.double().abs().sum(0, keepdim=True)
+                err = U * (20 + d ** 0.5) * size + cut
+                close(got, ref, err + (HALF if dt is torch.bfloat16 else U) * (ref.abs() + err), "projection")
+        X = Sheet(env, n, d, dt, pad, pad, torch.zeros(n, d, device=dev)).v
+        largest = torch.tensor(2.0 ** 128 - 2.0 ** 120 if dt is torch.bfloat16 else 2.0 ** 128 - 2.0 ** 119 - 2.0 ** 104,
+                               dtype=torch.float64, device=dev).to(dt)
+        X[0, 0], X[n - 1, d - 1] = largest, -largest
+        g, u = Wg.double() * 2.0 ** -140, Wu.double() * 2.0 ** -140
+        Wg.copy_(g), Wu.copy_(u)
+        B.shampoo_gated_ffn(h, X, Wg, Wu, H, B.ACT_NONE, G, Uo, workspace=ws)
+        torch.cuda.synchronize()
+        for got, m in ((G, Wg), (Uo, Wu)):
+            ref = X.double() @ m.double()
+            close(got, ref, (HALF + 40 * U) * ref.abs(), "projection of the largest")
+        if dt is torch.float32:
+            X[0, 0] = torch.tensor(2.0 ** 128 - 2.0 ** 119, dtype=torch.float64).float()
+            B.shampoo_gated_ffn(h, X, Wg, Wu, H, B.ACT_NONE, G, Uo, workspace=ws)
+            torch.cuda.synchronize()
+            assert not bool(torch.isfinite(G[0]).any()) and bool(torch.isfinite(G[1:]).all())
