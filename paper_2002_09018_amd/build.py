@@ -20,8 +20,6 @@ def command(out=LIB, extra=()):
     return [HIPCC, "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
             # packed-fp32 VALU ops are kept out of the device code
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            # the loads to LDS set M0, which the compiler uses for nothing else in this code
-            "-Wno-inline-asm",
             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
             *extra, *SOURCES, "-o", out]
 

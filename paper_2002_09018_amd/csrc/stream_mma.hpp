@@ -161,7 +161,10 @@ struct MmaLoader {
 // have every later transposing read wait for all loads in flight; mma_wait and
 // mma_barrier are what orders them.  (The instruction writes no
 // register.  The wait states are those that M0, and the scalar registers of the range
-// if the vector unit wrote them, need before it.)
+// if the vector unit wrote them, need before it.  M0 is a reserved register, which the compiler
+// warns of; it uses it for nothing else in this code.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void mma_dma(const char* base, uint32_t off, lds_char* to) {
   const uint64_t at = reinterpret_cast<uint64_t>(base);
   const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
@@ -169,6 +172,7 @@ __device__ __forceinline__ void mma_dma(const char* base, uint32_t off, lds_char
                ::"s"((uint32_t)(uintptr_t)to), "v"(off), "s"(rsrc)
                : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 template <int N>
 __device__ __forceinline__ void mma_wait() {
