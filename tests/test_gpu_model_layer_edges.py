@@ -342,3 +342,67 @@ def test_ends_of_the_range(env, dtype):
             B.shampoo_gated_ffn(h, X, Wg, Wu, H, B.ACT_NONE, G, Uo, workspace=ws)
             torch.cuda.synchronize()
             assert not bool(torch.isfinite(G[0]).any()) and bool(torch.isfinite(G[1:]).all())
+
+
+# ------------------------------------------------------------------ other calls that the header allows
+@pytest.mark.parametrize("dtype,g_dtype", TYPE_PAIRS)
+def test_gradient_of_lse_alone(env, dtype, g_dtype):
+    """Without targets: the bits of the call whose targets are all outside the vocabulary."""
+    torch, B, dev, h = env
+    dt, gt = getattr(torch, dtype), getattr(torch, g_dtype)
+    for n, d, v, pad in ROWS:
+        say("gradient of lse", n, d, v, dtype, g_dtype, pad)
+        X = Sheet(env, n, d, dt, pad, pad, normal(env, 1, n, d)).v
+        W = Sheet(env, v, d, dt, pad, pad, normal(env, 2, v, d) * (2.0 / d ** 0.5)).v
+        _, lse = logprobs(env, X, W, None)
+        g = normal(env, 3, n)
+        ws = room(env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, v, dt, gt))
+        out = []
+        for t in (None, torch.full((n,), -1, device=dev, dtype=torch.int32), torch.full((n,), v, device=dev, dtype=torch.int32)):
+            dX, dW = torch.empty(n, d, device=dev, dtype=dt), torch.empty(v, d, device=dev, dtype=gt)
+            B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX, dW=dW, g_lse=g, workspace=ws)
+            out.append((dX, dW))
+        torch.cuda.synchronize()
+        for dX, dW in out[1:]:
+            assert torch.equal(dX, out[0][0]) and torch.equal(dW, out[0][1])
+        p = torch.softmax(X.double() @ W.double().t().contiguous(), 1) * g.double().unsqueeze(1)
+        err = float((out[0][0].double() - p @ W.double()).norm() / (p @ W.double()).norm())
+        # two roundings, each of at most half a step
+        assert err <= (2 * HALF if dt is torch.bfloat16 else 1e-5), err
+
+
+def test_rows_far_apart(env):
+    """Rows 2^21 elements apart and more: the bits of the same matrices side by side (of few
+    rows in bf16, whose weights lie another way then, of the copied ones)."""
+    torch, B, dev, h = env
+    d, w, gap = 40, 72, 2 ** 21 + 8
+    for n in (3, 90):
+        for dt in (torch.bfloat16, torch.float32):
+            say("rows far apart", n, dt)
+
+            def far(rows, cols, x):
+                s = torch.empty(rows, gap, device=dev, dtype=dt)[:, :cols]
+                s.copy_(x)
+                return s
+
+            def near(rows, cols, x):
+                return Sheet(env, rows, cols, dt, 3, 1, x).v
+            out = []
+            for place in (near, far):
+                X, W = place(n, d, normal(env, 1, n, d)), place(w, d, normal(env, 2, w, d))
+                Wg, Wu, dH = (place(a, w, normal(env, i, a, w)) for i, a in ((3, d), (4, d), (5, n)))
+                t = torch.arange(n, device=dev, dtype=torch.int32) % w
+                logp, lse = logprobs(env, X, W, t)
+                dX, dW = place(n, d, 0 * X), place(w, d, 0 * W)
+                B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX, dW=dW, g_logp=normal(env, 6, n), workspace=room(
+                    env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, w, dt, dt)))
+                H, dY = place(n, w, 0 * dH), place(n, d, 0 * X)
+                dg, du = place(d, w, 0 * Wg), place(d, w, 0 * Wu)
+                B.shampoo_gated_ffn(h, X, Wg, Wu, H, workspace=room(
+                    env, B.shampoo_gated_ffn_workspace_bytes(n, d, w, dt)))
+                B.shampoo_gated_ffn_grad(h, X, Wg, Wu, dH, dX=dY, dWg=dg, dWu=du, workspace=room(
+                    env, B.shampoo_gated_ffn_grad_workspace_bytes(n, d, w, dt, dt)))
+                torch.cuda.synchronize()
+                out.append([x.clone() for x in (logp, lse, dX, dW, H, dY, dg, du)])
+            for a, b in zip(*out):
+                assert torch.equal(a, b)
