@@ -41,11 +41,15 @@
 // share of the contraction, no barrier among them, summed at the end (16 x 1024 x 8192:
 // 13.1 -> 10.4 us against 32 x 128 tiles of two waves in parts).
 //
-// What bounds it.  256 x 256 tiles in bf16 run at 1.1-1.25 PFLOP/s, where a library's
-// 8192^3 product reaches 1.3 on the same card; the card's power bounds both: the clock
-// falls under them, and the same instructions on small gradients instead of random
-// numbers take 5% less time.  Neither two workgroups of half the tile on a compute unit
-// (7 and 13% slower) nor starting workgroups apart nor skipped LDS reads (4%) lift it.
+// What bounds it.  256 x 256 tiles in bf16 run at 1.15-1.24 PFLOP/s, where a library's
+// 8192^3 product reaches 1.3 on the same card: the clock falls under both, and the same
+// instructions on small gradients instead of random numbers take 5% less time.  With an
+// epilogue that stores more than the tile (the logits' gradient, the block with its projections)
+// they run at 0.91-0.94: one workgroup to a compute unit has nothing of its next tile in flight
+// while a tile leaves, 55-70 us of each launch of 275 GFLOP (294-301 us, the plain products
+// 221-238).  Neither two workgroups of half the tile on a compute unit (7 and 13% slower)
+// nor starting workgroups apart nor skipped LDS reads (4%) lift it; loads of the next tile
+// ahead of this one's stores were not tried.
 // fp32 products reach 190-200 TFLOP/s, six bf16 products each.
 //
 // The instruction's first operand is B and its second A, so that a lane holds one
