@@ -604,7 +604,8 @@ shampoo_status shampoo_vocab_logprobs(void* handle, const void* X, const void* W
  *   dW = beta dW + dz^T X (vocab x dim, g_dtype; not read when beta == 0)
  * dX or dW may be NULL.  The logits are formed again, in pieces of the vocabulary.
  * dz is kept in three bf16 terms (24 bits) where dtype or g_dtype is fp32 (a bf16 dX
- * takes two of them, 16 bits), else in one (8 bits, as a stored bf16 gradient of logits).
+ * takes two of them, 16 bits), else of up to 32 rows in two, of more in one (8 bits, as a
+ * stored bf16 gradient of logits).
  * g_dtype counts without dW too.  The order of dX's sums may differ between calls with dW
  * and without.  A row whose gradients are all 0 has dz = 0 whatever W and lse hold, and
  * adds nothing to dW if X is finite there.  rows == 0: dW = beta dW.

@@ -40,6 +40,17 @@ struct Shapes<1, 1> {
   using BigWeight = MmaShape<256, 256, 128, 64, 3>;
 };
 
+// ... of two and one, whose large tiles take rounds of one.
+template <>
+struct Shapes<kDxTerms, 1> {
+  using Solo = MmaShape<32, 64, 32, 64, 2, kDxTerms, 1, 8>;
+  using Few = MmaShape<32, 128, 32, 64, 3, kDxTerms, 1>;
+  using Thin = MmaShape<64, 64, 32, 32, 2, kDxTerms, 1>;
+  using Mid = Shapes<1, 1>::Mid;
+  using Big = Shapes<1, 1>::Big;
+  using BigWeight = Shapes<1, 1>::BigWeight;
+};
+
 // A buffer of a call and what to call it.
 struct Named {
   Span s;
@@ -228,7 +239,7 @@ template <int LB>
 shampoo_status dx_product(Handle* h, int cls, int planes, int d_planes, int shape, const MmaArgs& q,
                           const OutEpilogue& e, hipStream_t s) {
   if (d_planes == planes) return product<kLayoutRow, LB>(h, cls, planes, shape, q, e, s);
-  return product<kLayoutRow, LB, 1, 1>(h, cls, shape, q, OutTermsEpilogue(e), s);
+  return product<kLayoutRow, LB, kDxTerms, 1>(h, cls, shape, q, OutTermsEpilogue(e), s);
 }
 template <int LB>
 shampoo_status few_dx_product(Handle* h, int cls, int dtype, int d_planes, const FewArgs& w, const OutEpilogue& e,
@@ -239,11 +250,11 @@ shampoo_status few_dx_product(Handle* h, int cls, int dtype, int d_planes, const
 }
 
 // dX and the weights' gradient in one launch, and what was cut of them in another.
-template <int LB, int P>
-shampoo_status two_products(Handle* h, int cls, const MmaArgs& x, const OutEpilogue& ex, const MmaArgs& w,
-                            const OutEpilogue& ew, hipStream_t s) {
+template <int LB, int P, typename E>
+shampoo_status two_products(Handle* h, int cls, const MmaArgs& x, const E& ex, const MmaArgs& w, const E& ew,
+                            hipStream_t s) {
   using T = typename Shapes<P, P>::Mid;
-  auto k = mma_two_kernel<T, LB, OutEpilogue>;
+  auto k = mma_two_kernel<T, LB, E>;
   static std::atomic<uint64_t> asked{0};
   STATUS_TRY(ask_lds(h, k, T::kLdsB, asked));
   const int first = (int)groups_of(x);
@@ -251,12 +262,13 @@ shampoo_status two_products(Handle* h, int cls, const MmaArgs& x, const OutEpilo
     hipLaunchKernelGGL(k, dim3((unsigned)(first + groups_of(w))), dim3(T::kThr), T::kLdsB, s, x, ex, w, ew, first);
   }));
   if (!x.part || !w.part) {
-    if (x.part) return join(h, cls, x, ex, s);
-    return w.part ? join(h, cls, w, ew, s) : SHAMPOO_OK;
+    if (x.part) return join<OutEpilogue>(h, cls, x, ex, s);
+    return w.part ? join<OutEpilogue>(h, cls, w, ew, s) : SHAMPOO_OK;
   }
   const unsigned nx = act_grid((int64_t)x.M * cdiv64(x.N, 8)), nw = act_grid((int64_t)w.M * cdiv64(w.N, 8));
   return launch(h, cls, s, [&] {
-    hipLaunchKernelGGL(mma_join_two_kernel<OutEpilogue>, dim3(nx + nw), dim3(kThreads), 0, s, x, ex, w, ew, (int)nx);
+    hipLaunchKernelGGL(mma_join_two_kernel<OutEpilogue>, dim3(nx + nw), dim3(kThreads), 0, s, x,
+                       static_cast<const OutEpilogue&>(ex), w, static_cast<const OutEpilogue&>(ew), (int)nx);
   });
 }
 template <int LB>
@@ -273,6 +285,7 @@ shampoo_status weight_product(Handle* h, int cls, int x_planes, int d_planes, in
   constexpr int K = kLayoutK;
   shampoo_status st;
   if (x_planes == d_planes) st = product<K, K>(h, cls, x_planes, shape, q, e, s);
+  else if (D_FIRST && d_planes == kDxTerms) st = product<K, K, kDxTerms, 1>(h, cls, shape, q, OutTermsEpilogue(e), s);
   else st = product<K, K, D_FIRST ? 3 : 1, D_FIRST ? 1 : 3>(h, cls, shape, q, e, s);
   STATUS_TRY(st);
   return q.part ? join(h, cls, q, e, s) : SHAMPOO_OK;
@@ -451,7 +464,7 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
     Packer packer{h, kCls, dtype, s};
     STATUS_TRY(packer.take(X, rows, dim, ld_x, pack_x, p.x, ws + p.at_x, &x));
     uint16_t* dz = reinterpret_cast<uint16_t*>(ws + p.at_dz);
-    const Planes16 pz{dz, p.ld_dz, rows * p.ld_dz};
+    const Planes16 pz{dz, p.ld_dz, p.second ? (int64_t)(p.at_second - p.at_dz) / 2 : rows * p.ld_dz};
     const int nx = p.x.planes;
     MmaArgs qx{};
     const OutEpilogue out_x(dX, ld_dx, nullptr, 0, 0, (int)dim, (int)dim, dtype == SHAMPOO_BF16, 0.f);
@@ -464,7 +477,7 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
       MmaArgs q{};
       add_seg(q, x, w);
       use_plan(q, p.z[last], rows, n, dim, kLayoutRow, kLayoutRow, ws + p.at_part);
-      const DlogitEpilogue e({targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.planes);
+      const DlogitEpilogue e({targets, (int)vocab, (int)v0}, lse, g_logp, g_lse, dz, p.ld_dz, pz.plane, (int)n, p.terms());
       if (p.direct) STATUS_TRY(few_product<kLayoutRow>(h, kCls, dtype, {q, {few_seg(x, here, ld_w)}, (int)dim}, e, s));
       else STATUS_TRY((product<kLayoutRow, kLayoutRow>(h, kCls, nx, p.z[last].shape, q, e, s)));
       if (q.part) STATUS_TRY(join(h, kCls, q, e, s));
@@ -479,16 +492,18 @@ shampoo_status shampoo_vocab_logprobs_grad(void* handle, const void* X, const vo
         use_plan(r, m, rows, dim, n, kLayoutRow, kLayoutK, ws + p.at_dx);
         r.part_add = i > 0;
         if (p.direct)
-          STATUS_TRY(few_dx_product<kLayoutK>(h, kCls, dtype, p.planes, {r, {few_seg(pz, here, ld_w)}, (int)n}, out_x, s));
-        else if (!two) STATUS_TRY(dx_product<kLayoutK>(h, kCls, nx, p.planes, m.shape, r, out_x, s));
+          STATUS_TRY(few_dx_product<kLayoutK>(h, kCls, dtype, p.terms(), {r, {few_seg(pz, here, ld_w)}, (int)n}, out_x, s));
+        else if (!two) STATUS_TRY(dx_product<kLayoutK>(h, kCls, nx, p.terms(), m.shape, r, out_x, s));
         if (i == 0) qx = r;
       }
       if (dW) {
         const MmaPlan& m = two ? p.two_dw : p.dw[last];
         add_seg(qw, pz, x);
         use_plan(qw, m, n, dim, rows, kLayoutK, kLayoutK, ws + p.at_part);
-        if (!two) STATUS_TRY(weight_product<true>(h, kCls, nx, p.planes, m.shape, qw, out, s));
+        if (!two) STATUS_TRY(weight_product<true>(h, kCls, nx, p.terms(), m.shape, qw, out, s));
       }
+      if (two && p.second)
+        return two_products<kLayoutK, 1>(h, kCls, qx, OutTermsEpilogue(out_x), qw, OutTermsEpilogue(out), s);
       if (two) return two_products<kLayoutK>(h, kCls, nx, qx, out_x, qw, out, s);
     }
     return dX && qx.part ? join(h, kCls, qx, out_x, s) : SHAMPOO_OK;

@@ -9,8 +9,10 @@
 // indices are multiplied for the pairs of planes that count (six of nine, or three
 // where the other operand has one), the smallest first.  A sum of two products (dG
 // Wg^T + dU Wu^T) is two segments of one long contraction.  Two terms of A with a B of one
-// plane (dX of bf16 inputs from a gradient in three) are the contraction in two rounds, a
-// term each, the smaller first: tiles and stages stay those of one plane.
+// plane (a gradient's, before bf16 matrices) go beside each other through small tiles, which
+// the bytes of B bound, and through larger ones in two rounds of the contraction, the
+// smaller first: a stage of both would leave one workgroup to a compute unit (128 x 128: 1021
+// x 333 x 50001 400 -> 412 us, 48 to 128 rows 5-8% less).
 //
 // Staging.  Stages of kBk = 64 or 32 contraction indices go from memory to LDS
 // without passing registers (buffer_load ... lds, 1 KB a wave and instruction), into a
@@ -362,7 +364,7 @@ struct MmaCore {
     // The products of a step, pairs of planes by size, the smallest first.  beside(n)
     // puts what else the wave issues behind product n: a product keeps the matrix unit
     // busy for 32 cycles, in which a few other instructions go out.
-    constexpr int kPairs = T::PA + T::PB == 2 ? 1 : T::PA + T::PB == 4 ? 3 : 6;
+    constexpr int kPairs = T::PA + T::PB < 6 ? T::PA + T::PB - 1 : 6;
     constexpr int kProducts = kPairs * T::kBm * T::kBn;
     auto multiply = [&](int step, auto&& beside) {
       int n = 0;
@@ -557,7 +559,7 @@ __device__ __forceinline__ void mma_body(const MmaArgs& q, const E& e, lds_char*
         *(lds_f32x4*)(state + r * 16) = m0 + r < q.M ? e.state(m0 + r) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  MmaCore<T, LA, LB, E::kPair, E::kTerms> core;
+  MmaCore<T, LA, LB, E::kPair, T::PA == 1 ? E::kTerms : 1> core;
   core.run(q, lds, m0, n0, split, states);
   if constexpr (E::kWhole && T::kSolo == 0) {
     if (!q.part) {

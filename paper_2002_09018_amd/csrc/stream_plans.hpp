@@ -63,10 +63,10 @@ inline const MmaCost* weight_cost(int x_planes, int d_planes) {
 }
 
 // Time of `groups` workgroups of `per` stages: full rounds of the chip, then the rest.
-inline double mma_us(const MmaCost& t, int64_t groups, int64_t per) {
+inline double mma_us(const MmaCost& t, int64_t groups, double per) {
   const int64_t full = 256 * t.slots, rest = groups % full;
-  double us = (double)(groups / full) * ((double)per * t.stage[t.slots - 1] + t.start);
-  if (rest) us += (double)per * (rest <= 128 ? t.alone : t.stage[(rest - 1) / 256]) + t.start;
+  double us = (double)(groups / full) * (per * t.stage[t.slots - 1] + t.start);
+  if (rest) us += per * (rest <= 128 ? t.alone : t.stage[(rest - 1) / 256]) + t.start;
   return us;
 }
 
@@ -93,7 +93,10 @@ inline double parts_us(const MmaPlan& p) {
 }
 
 // The cheapest tile and number of parts (at most most_splits) by estimated time.  `segs`
-// products of one contraction length are summed, each stage taken in so many rounds.
+// products of one contraction length are summed.  rounds: terms of A beside a B of one plane;
+// tiles of 128 rows and more take every stage once for each, 32 x 128 ones take half again as
+// long for a second (1, 1.5 and 2 times as long measured: 700 x 768 x 5000 113, 88 and 91 us,
+// 64 x 1024 over 32768 92, 90 and 103), and 32 x 64 ones are bound by B.
 inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, int segs, bool pair, int least_shape,
                         int most_splits, bool always_part, int rounds = 1) {
   MmaPlan best;
@@ -103,7 +106,8 @@ inline MmaPlan mma_plan(int64_t M, int64_t N, int64_t K, const MmaCost* cost, in
     for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (want > cdiv64(K, t.bk) * segs || want > most_splits || (want > 1 && want * tiles > 1024)) break;
       MmaPlan p = mma_cut(M, N, K, t, i, segs, pair, want, always_part);
-      p.us = mma_us(t, tiles * p.splits, (int64_t)p.per_split * rounds) + parts_us(p);
+      const double each = i >= kShapeMid ? rounds : i == kShapeFew ? 0.5 + 0.5 * rounds : 1;
+      p.us = mma_us(t, tiles * p.splits, each * p.per_split) + parts_us(p);
       if (best.us == 0 || p.us < best.us) best = p;
     }
   }
@@ -151,7 +155,9 @@ inline MmaPlan few_plan(int64_t M, int64_t N, int64_t K, int planes, bool along_
 // The two products of a gradient, dX (x) and the weights' (w), in one launch of 128 x 128
 // tiles where that is estimated to take less time than theirs one after the other
 // (`on`): each alone often leaves compute units idle, and a launch and a join are saved.
-// Both products have operands of the same number of planes (and so the same waves).
+// Both products have operands of the same number of planes (and so the same waves); a
+// second term of a gradient of few rows is not counted (8 and 30 rows x 2048 over 2000 22
+// and 25 us, 24 and 28 if it is).
 // Measured, whole calls, two launches and one: 1003 x 333 x 1339 in fp32 70.3 and 58.9
 // us, in bf16 36.0 and 28.0; 2048 x 512 x 1344 in bf16 47.5 and 34.2; a vocabulary of
 // 1000 for 4096 x 1024 in bf16 54.5 and 45.1, where 512 x 1024 x 4096 fills the chip
@@ -292,12 +298,14 @@ inline VocabPlan vocab_plan(int64_t rows, int64_t dim, int64_t vocab, int dtype,
 struct VocabGradPlan {
   int64_t piece = 0, pieces = 0, ld_dz = 0;
   int planes = 1;       // bf16 terms of the logits' gradient
+  bool second = false;  // another one, where `planes` is one
   bool direct = false;  // as above
   MmaPlan z[2], dx[2], dw[2];
   bool two = false;  // dX and dW in one launch, where both are wanted, cut as follows
   MmaPlan two_dx, two_dw;
   PackPlan x, w;
-  size_t at_x = 0, at_w = 0, at_dz = 0, at_dx = 0, at_part = 0, bytes = 0, need = 0;
+  size_t at_x = 0, at_w = 0, at_dz = 0, at_second = 0, at_dx = 0, at_part = 0, bytes = 0, need = 0;
+  int terms() const { return second ? 2 : planes; }
 };
 
 // An fp32 gradient, of inputs of either type, has three terms of dz: with one it
@@ -311,13 +319,17 @@ inline int grad_planes(int dtype, int g_dtype) { return dtype == SHAMPOO_F32 || 
 // with one, two and three: 2048 x 1024 over 32768 712, 830 and 925 us, 16384 rows through
 // 1024 x 4096 1167, 1420 and 1637).
 constexpr int kDxTerms = 2;
-// What its product takes, in rounds of one term: one for each, but of few rows, where the
-// other matrix is in the caches by the second, one (counted twice, more and smaller parts
-// would be cut: 64 x 1024 over 32768 96 and 103 us, 16 and 64 rows through 1024 x 4096 31
-// and 36, 34 and 36; 700 x 768 x 5000, counted once and twice, 98 and 91).
-inline int dx_rounds(int64_t rows, int planes, int terms) {
-  return planes == 1 && terms == 3 && rows > 64 ? kDxTerms : 1;
-}
+// Rounds of its product: one for each of them (in small tiles both go beside one read of the
+// other matrix).
+inline int dx_rounds(int planes, int terms) { return planes == 1 && terms > 1 ? kDxTerms : 1; }
+
+// Up to so many rows dz has two terms also where inputs and gradients are bf16, for dX and
+// dW: the entries of few tokens hold most of its norm, and the roundings of one term do not
+// average out there (results off by up to 2.8 times their own rounding).  Such calls are
+// bound by the table or by launches: 1, 16 and 32 rows x 1024 over 32768 55, 57 and 60 us with one
+// term, 58, 56 and 63 with two, 8 rows x 512 over 5000 16 and 19; 64, 128 and 512 rows x 1024
+// over 32768 65, 73 and 127, with two 78, 93 and 202.
+constexpr int kSecondRows = 32;
 
 inline bool vocab_grad_alike(int64_t rows, int64_t dim, int64_t vocab, int dtype, int planes) {
   return dtype == SHAMPOO_F32 ||
@@ -339,6 +351,8 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
   if (!few) p.at_w = r.copy(copy_w, p.w.bytes);
   p.ld_dz = cdiv64(p.piece, 64) * 64;
   p.at_dz = r.take((size_t)(rows * p.ld_dz * p.planes) * 2);
+  p.second = p.planes == 1 && rows <= kSecondRows;  // (in a buffer of its own)
+  if (p.second) p.at_second = r.take((size_t)(rows * p.ld_dz) * 2);
   size_t part = 0;
   const int64_t last = vocab - (p.pieces - 1) * p.piece;
   for (int i = 0; i < 2; ++i) {
@@ -356,9 +370,9 @@ inline VocabGradPlan vocab_grad_plan(int64_t rows, int64_t dim, int64_t vocab, i
       p.dx[i] = few_plan(rows, dim, n, p.x.planes, false, 1, false, most, p.pieces > 1);
     } else {
       p.z[i] = mma_plan(rows, n, dim, cost, 1, false, kShapeSolo, 64, false);
-      p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, most, p.pieces > 1, dx_rounds(rows, p.x.planes, p.planes));
+      p.dx[i] = mma_plan(rows, dim, n, cost, 1, false, kShapeSolo, most, p.pieces > 1, dx_rounds(p.x.planes, p.terms()));
     }
-    p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
+    p.dw[i] = mma_plan(n, dim, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false, p.second ? 2 : 1);
     part = std::max({part, p.z[i].part, p.dw[i].part});
   }
   if (!p.direct && p.pieces == 1 && p.planes == p.x.planes) {
@@ -438,7 +452,7 @@ inline FfnGradPlan ffn_grad_plan(int64_t rows, int64_t dim, int64_t width, int d
   } else {
     p.gu = mma_plan(rows, width, dim, mma_cost(p.x.planes), 1, true, kShapeSolo, 64, false);
     p.dx = mma_plan(rows, dim, width, mma_cost(p.x.planes), 2, false, kShapeSolo, 64, false,
-                    dx_rounds(rows, p.x.planes, p.planes));
+                    dx_rounds(p.x.planes, p.planes));
   }
   p.dw = mma_plan(dim, 2 * p.ld_d, rows, weight_cost(p.x.planes, p.planes), 1, false, kShapeFew, 64, false);
   if (!p.direct && p.planes == p.x.planes) {

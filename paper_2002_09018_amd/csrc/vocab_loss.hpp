@@ -187,15 +187,16 @@ __global__ __launch_bounds__(kThreads) inline void lse_join_kernel(int64_t rows,
   }
 }
 
-// The gradient of the logits, in one or three bf16 terms.  A row's state: c, g (0
+// The gradient of the logits, in one, two or three bf16 terms.  A row's state: c, g (0
 // without a target), lse and the target's column.  One term (of bf16 inputs with bf16
 // gradients) rounds each dz once, half a step of 2^-8 of it: what a bf16 tensor of
 // logits' gradients holds, beside the result's own rounding of the same size.  Of many rows
 // errors are about sqrt(2) times those of the result's rounding alone (0.0024 and 0.0017 of
-// the norm); of few, where a few entries hold most of the norm, their roundings do not
-// average out: up to 0.0043 (of 40 random calls each, 1 row up to 2.8 times, 16 rows 2.0, 64
-// rows 1.7, 512 rows 1.6).  A second term would double both products that read dz (8192 x
-// 1024 over 131072 6.2 -> about 10 ms): a caller who wants it takes dW in fp32.
+// the norm).  Where a few entries hold most of the norm their roundings do not average out
+// (of 40 random calls each, 1 row up to 2.8 times, 16 rows 2.0, 64 rows 1.7, 512 rows 1.6):
+// calls of up to kSecondRows rows have two terms, off by 2^-16.  Of more rows a second term
+// would double both products that read dz (8192 x 1024 over 131072 6.2 -> about 10 ms): a
+// caller who wants it takes dW in fp32.
 struct DlogitEpilogue : UnitEpilogue<DlogitEpilogue> {
   static constexpr bool kState = true;
   VocabTargets t;
@@ -241,7 +242,8 @@ struct DlogitEpilogue : UnitEpilogue<DlogitEpilogue> {
       u32x4u p[3];
       planes_of(z, p);
 #pragma unroll
-      for (int s = 0; s < 3; ++s) gstore<u32x4u>(d + s * plane, p[s]);
+      for (int s = 0; s < 3; ++s)
+        if (s < planes) gstore<u32x4u>(d + s * plane, p[s]);
     }
   }
 };

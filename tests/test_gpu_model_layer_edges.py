@@ -140,9 +140,12 @@ def test_fp32_block_gradients_are_fp32(env, act, keep):
 # (test_stream_limits checks that): rows, dim, vocabulary or width, whether matrices are copied
 VOCAB_TERMS = [(1, 8, 8, 1), (66, 8, 960, 1), (739, 645, 10, 1), (746, 15, 1321, 1), (698, 1434, 175, 1),
                (7566, 387, 6018, 1), (1374, 10, 1886, 1), (6716, 8, 7080, 1), (3139, 3318, 8, 1), (7614, 1408, 5862, 0),
-               (5404, 170, 4120, 1), (4175, 160, 14388, 1), (5, 3996, 4210, 1)]
+               (5404, 170, 4120, 1), (4175, 160, 14388, 1), (5, 3996, 4210, 1), (1, 12, 1831, 1), (2582, 8, 20755, 1),
+               (1, 1441, 2188, 1), (33, 4002, 35019, 1), (2418, 1725, 8, 1), (4205, 9, 3514, 1), (5016, 9, 9385, 1),
+               (6673, 131, 5552, 1)]
 FFN_TERMS = [(1, 8, 8, 1), (68, 10, 481, 1), (831, 611, 8, 0), (341, 68, 936, 1), (1256, 778, 104, 0), (1502, 8, 791, 1),
-             (4474, 2420, 12, 1), (2789, 129, 4045, 1), (1, 3200, 2657, 1), (30, 2243, 40, 1)]
+             (4474, 2420, 12, 1), (2789, 129, 4045, 1), (1, 3200, 2657, 1), (30, 2243, 40, 1), (2, 8, 897, 1),
+             (1, 1379, 1240, 1), (2058, 1925, 12, 1), (1390, 8, 3522, 1)]
 
 
 @pytest.mark.parametrize("n,d,v,copied", VOCAB_TERMS)
@@ -170,6 +173,45 @@ def test_dx_takes_the_terms_of_dz(env, n, d, v, copied):
     ref = dz @ W.double()
     close(dX.v, ref, part + HALF * (ref.abs() + part), "dX")
     assert dX.intact(torch)
+
+
+# the same for dX and dW of up to 32 rows, together and each alone, and with a table read where it lies
+FEW_TERMS = [(4, 8, 449, 0), (8, 68, 32989, 1), (1, 129, 45455, 1), (2, 8, 5122, 0), (1, 646, 14172, 1), (1, 270, 62204, 1),
+             (1, 8, 8, 0), (3, 8, 973, 0), (32, 1024, 5000, 0), (31, 333, 1027, 1)]
+
+
+@pytest.mark.parametrize("n,d,v,copied", FEW_TERMS)
+def test_few_rows_take_two_terms(env, n, d, v, copied):
+    """bf16 gradients of up to 32 rows of bf16: dz in two terms, off by 2^-16, and one rounding
+    of each result."""
+    import oracle.model_oracle as M
+    torch, B, dev, h = env
+    bf, pad = torch.bfloat16, 5 if copied else 0
+    say("two terms of few rows", n, d, v, pad)
+    X = Sheet(env, n, d, bf, pad, pad, normal(env, 1, n, d)).v
+    W = Sheet(env, v, d, bf, pad, pad, normal(env, 2, v, d) * (2.0 / d ** 0.5)).v
+    t = torch.randint(0, v, (n,), generator=torch.Generator(device=dev).manual_seed(3), device=dev, dtype=torch.int32)
+    g_logp, g_lse = normal(env, 4, n), 0.1 * normal(env, 5, n)
+    _, lse, z = M.vocab_logprobs(X, W, t)
+    lse = lse.float()
+    dz, size = M.vocab_dlogits(z, lse, t, g_logp, g_lse)
+    far = (z_error(X, W) + U * (4 + (z - lse.double().unsqueeze(1)).abs().amax(1))).unsqueeze(1) * size
+    ws = room(env, B.shampoo_vocab_logprobs_grad_workspace_bytes(n, d, v, bf, bf))
+    for with_x, with_w in ((True, True), (True, False), (False, True)):
+        dX, dW = Sheet(env, n, d, bf, pad, pad), Sheet(env, v, d, bf, pad, pad)
+        B.shampoo_vocab_logprobs_grad(h, X, W, t, lse, dX=dX.v if with_x else None, dW=dW.v if with_w else None,
+                                      g_logp=g_logp, g_lse=g_lse, workspace=ws)
+        torch.cuda.synchronize()
+        if with_x:
+            part = (far + (2.0 ** -16 + U * (20 + (2 * v) ** 0.5)) * dz.abs()) @ W.double().abs()
+            ref = dz @ W.double()
+            close(dX.v, ref, part + HALF * (ref.abs() + part), "dX")
+            assert dX.intact(torch)
+        if with_w:
+            part = (far + (2.0 ** -16 + U * (20 + (2 * n) ** 0.5)) * dz.abs()).t().contiguous() @ X.double().abs()
+            ref = dz.t().contiguous() @ X.double()
+            close(dW.v, ref, part + HALF * (ref.abs() + part), "dW")
+            assert dW.intact(torch)
 
 
 @pytest.mark.parametrize("n,d,w,copied", FFN_TERMS)

@@ -2,7 +2,9 @@
 loss from the last activations refuses: products of 2^22 tiles or more, and nothing else,
 wherever the table lies.  The GPU tests' sizes reach every product that forms dX of bf16
 inputs from a gradient in terms.  No GPU is used."""
+import math
 import os
+import random
 import shutil
 import subprocess
 
@@ -52,3 +54,19 @@ def test_sizes_reach_every_dx_of_terms(ask, kind, tested, top):  # noqa: F811
     tested = [x for x in tested if x[3] or (x[1] if kind == "vgrad" else x[2]) % 8 == 0]
     some = [x[:3] + (x[5],) for x in drawn(9, 20000, top)]
     assert not dx_kernels(ask, kind, some) - dx_kernels(ask, kind, tested)
+
+
+def test_sizes_reach_every_product_of_few_rows(ask):  # noqa: F811
+    """bf16 gradients of up to 32 rows, whose dz has two terms."""
+    def kernels(sizes):
+        found = set()
+        for x, b in zip(sizes, ask(["vgrad %d %d %d 1 1 %d" % x for x in sizes])):
+            found |= {("dX", b[3], b[4] > 1), ("dW", b[5], b[6] > 1)}
+            if b[13]:
+                found.add(("dX and dW", b[14] > 1, b[15] > 1))
+        return found
+    r = random.Random(5)
+    some = [tuple(int(math.exp(r.uniform(math.log(lo), math.log(hi)))) for lo, hi in ((1, 33), (8, 4096), (8, 200000)))
+            for _ in range(20000)]
+    some = [x + (1 if x[1] % 8 else r.randint(0, 1),) for x in some]
+    assert not kernels(some) - kernels(edges.FEW_TERMS)
