@@ -233,7 +233,7 @@ shampoo_status join(Handle* h, int cls, const MmaArgs& q, const E& e, hipStream_
   });
 }
 
-// dX = D B of a gradient D that is kept in d_planes terms: as many as B has planes, or three
+// dX = D B of a gradient D that is kept in d_planes terms: as many as B has planes, or more
 // beside a B of one, of which kDxTerms count.  What was cut is left in q.part.
 template <int LB>
 shampoo_status dx_product(Handle* h, int cls, int planes, int d_planes, int shape, const MmaArgs& q,
